@@ -22,6 +22,7 @@ CALLS_PATH = os.path.join(_HERE, "_calls.so")
 HGNN_OK, HGNN_EINVAL, HGNN_EUNSUPPORTED, HGNN_ENOMEM, HGNN_EHIP = range(5)
 HGNN_SUM, HGNN_MEAN = 0, 1
 HGNN_SDDMM_DOT, HGNN_SDDMM_GAT_SCORE = 0, 1
+HGNN_F16, HGNN_F32 = 0, 1
 
 EXPORTS = (
     "hgnn_status_str", "hgnn_last_error", "hgnn_csr_validate", "hgnn_transpose", "hgnn_coo_to_csr", "hgnn_plan_create",
@@ -34,7 +35,8 @@ EXPORTS = (
     "hgnn_plan_vector_halves", "hgnn_spmm_workspace", "hgnn_plan_add_slices", "hgnn_plan_num_slices", "hgnn_edge_colsum", "hgnn_spmm_static", "hgnn_spmm_static_limit", "hgnn_gat_forward_fused", "hgnn_gat_alpha", "hgnn_gat_backward_fused",
     "hgnn_edge_to_transposed", "hgnn_scale_rows", "hgnn_linear", "hgnn_linear_padded", "hgnn_linear_wgrad", "hgnn_linear_wgrad_workspace",
     "hgnn_gat_feature_grad", "hgnn_gat_feature_grad_workspace", "hgnn_gat_forward_fused_save",
-    "hgnn_gat_backward_fused_saved",
+    "hgnn_gat_backward_fused_saved", "hgnn_embedding", "hgnn_embedding_grad", "hgnn_embedding_grad_workspace", "hgnn_logprob", "hgnn_logprob_workspace",
+    "hgnn_logprob_grad", "hgnn_grad_norm", "hgnn_grad_norm_workspace", "hgnn_grad_clip",
 )
 
 HGNN_EDGE_SEGMENTS, HGNN_EDGE_SEGMENTS_ATOMIC, HGNN_VERTEX_GROUPS, HGNN_VERTEX_GROUPS_HALF2 = 0, 1, 2, 3
@@ -56,6 +58,11 @@ class _CsrStruct(ctypes.Structure):
     _fields_ = [("nrows", ctypes.c_int32), ("ncols", ctypes.c_int32), ("nnz", ctypes.c_int64),
                 ("rowptr", ctypes.c_void_p), ("col", ctypes.c_void_p), ("row", ctypes.c_void_p),
                 ("eid", ctypes.c_void_p)]
+
+
+class _GradStruct(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("type", ctypes.c_int), ("out_type", ctypes.c_int)]
 
 
 _lib = None
@@ -144,6 +151,20 @@ def load() -> ctypes.CDLL:
     lib.hgnn_gat_feature_grad_workspace.restype = ctypes.c_size_t
     lib.hgnn_gat_feature_grad.argtypes = [i64, i32, i32, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
                                           ctypes.c_size_t, vp]
+    ct = ctypes.c_int
+    lib.hgnn_embedding.argtypes = [i64, i32, vp, i32, ct, vp, i64, f32, vp, i64, vp]
+    lib.hgnn_embedding_grad_workspace.argtypes = [i64, i32, i32]
+    lib.hgnn_embedding_grad_workspace.restype = ctypes.c_size_t
+    lib.hgnn_embedding_grad.argtypes = [i64, i32, vp, i32, vp, i64, f32, i32, ct, vp, i64, vp, ctypes.c_size_t, vp]
+    lib.hgnn_logprob_workspace.argtypes = [i64, i32, i32]
+    lib.hgnn_logprob_workspace.restype = ctypes.c_size_t
+    lib.hgnn_logprob.argtypes = [i64, i32, ct, vp, i64, vp, vp, vp, vp, i32, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.hgnn_logprob_grad.argtypes = [i64, i32, ct, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    grads = ctypes.POINTER(_GradStruct)
+    lib.hgnn_grad_norm_workspace.argtypes = []
+    lib.hgnn_grad_norm_workspace.restype = ctypes.c_size_t
+    lib.hgnn_grad_norm.argtypes = [i32, grads, f32, vp, vp, ctypes.c_size_t, vp]
+    lib.hgnn_grad_clip.argtypes = [i32, grads, f32, f32, vp, vp, ctypes.c_size_t, vp]
     for name in EXPORTS:
         getattr(lib, name)  # every declared entry point must be exported
     _calls = _load_calls(lib)
@@ -599,3 +620,177 @@ def hgnn_plan_add_slices(p: Plan, g: Csr, slice_cols: int = 0, stream=None) -> N
 
 def hgnn_plan_num_slices(p: Plan) -> int:
     return load().hgnn_plan_num_slices(p.handle)
+
+
+# ---- the two ends of a training step and its guard: what the C side cannot see of a tensor (its shape, its device) is checked here
+_TYPES = {torch.float16: HGNN_F16, torch.float32: HGNN_F32}
+
+
+def _type(t: torch.Tensor) -> int:
+    if t.dtype not in _TYPES:
+        raise TypeError(f"expected float16 or float32, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    here = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else None
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise TypeError("hgnn expects CUDA (HIP) tensors")
+        if t is not None and t.device.index != here:
+            raise ValueError(f"a tensor of device {t.device.index} while device {here} is the current one")
+
+
+def _dense(name: str, t: Optional[torch.Tensor], dtype, *shape: int) -> Optional[int]:
+    """Address of a contiguous tensor of that type and shape."""
+    if t is None:
+        return None
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {list(shape)}, got {list(t.shape)} with strides {list(t.stride())}")
+    return _ptr(t, dtype)
+
+
+def _rows(name: str, t: torch.Tensor, rows: int, cols: int):
+    """-> (address, pitch) of rows x cols elements with unit stride along the columns."""
+    if t.dim() != 2 or tuple(t.shape) != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a tensor of {rows} x {cols} with unit stride along its rows, got {list(t.shape)} with strides {list(t.stride())}")
+    return _ptr(t), t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+
+def _room(workspace: Optional[torch.Tensor]):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def _two(name: str, t: torch.Tensor):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got {list(t.shape)}")
+    return t.shape[0], t.shape[1]
+
+
+def hgnn_embedding(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0, stream=None) -> None:
+    """out[i] = scale * table[ids[i]]: int32 ids, a table of fp16 or fp32 rows, out fp16; an id that is no row of the table gives zeros."""
+    if _calls is not None and _done(_calls.embedding(ids, table, out, scale, stream)):
+        return
+    _here(ids, table, out)
+    V, F = _two("table", table)
+    n = ids.numel()
+    T, ldt = _rows("table", table, V, F)
+    o, ldo = _rows("out", out, n, F)
+    _ptr(out, torch.float16)
+    _check(load().hgnn_embedding(n, F, _dense("ids", ids, torch.int32, n), V, _type(table), T, ldt, scale, o, ldo, _stream(stream)))
+
+
+def hgnn_embedding_grad_workspace(n: int, F: int, V: int) -> int:
+    return load().hgnn_embedding_grad_workspace(n, F, V)
+
+
+def hgnn_embedding_grad(ids: torch.Tensor, dY: torch.Tensor, dT: torch.Tensor, workspace: Optional[torch.Tensor], scale: float = 1.0,
+                        accumulate: bool = False, stream=None) -> None:
+    """dT (fp16 or fp32, one row for each of the table) = scale * the sums of the rows of dY with the same id, or that much more (accumulate);
+    workspace: device tensor of hgnn_embedding_grad_workspace(n, F, V) bytes."""
+    if _calls is not None and _done(_calls.embedding_grad(ids, dY, dT, workspace, scale, accumulate, stream)):
+        return
+    _here(ids, dY, dT, workspace)
+    V, F = _two("dT", dT)
+    n = ids.numel()
+    y, ldy = _rows("dY", dY, n, F)
+    T, ldt = _rows("dT", dT, V, F)
+    _ptr(dY, torch.float16)
+    ws, bytes = _room(workspace)
+    _check(load().hgnn_embedding_grad(n, F, _dense("ids", ids, torch.int32, n), V, y, ldy, scale, 1 if accumulate else 0, _type(dT), T, ldt, ws, bytes,
+                                      _stream(stream)))
+
+
+def hgnn_logprob_workspace(n: int, C: int, k: int = 0) -> int:
+    return load().hgnn_logprob_workspace(n, C, k)
+
+
+def hgnn_logprob(logits: torch.Tensor, labels: Optional[torch.Tensor], logprob: Optional[torch.Tensor], stats: Optional[torch.Tensor] = None,
+                 entropy: Optional[torch.Tensor] = None, top_logprob: Optional[torch.Tensor] = None, top_class: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Of every row of logits (fp16 or fp32): the log probability of its label (int32, another number than a class's is none), stats [n][2] for
+    hgnn_logprob_grad, the entropy, and the k best classes with their log probabilities [n][k]; workspace: hgnn_logprob_workspace(n, C, k) bytes."""
+    if _calls is not None and _done(_calls.logprob(logits, labels, logprob, stats, entropy, top_logprob, top_class, workspace, stream)):
+        return
+    _here(logits, labels, logprob, stats, entropy, top_logprob, top_class, workspace)
+    n, C = _two("logits", logits)
+    k = 0 if top_class is None else _two("top_class", top_class)[1]
+    x, ld = _rows("logits", logits, n, C)
+    ws, bytes = _room(workspace)
+    single = torch.float32
+    if (top_class is None) != (top_logprob is None):
+        raise ValueError("top_logprob and top_class go together")
+    _check(load().hgnn_logprob(n, C, _type(logits), x, ld, _dense("labels", labels, torch.int32, n), _dense("logprob", logprob, single, n),
+                               _dense("stats", stats, single, n, 2), _dense("entropy", entropy, single, n), k,
+                               _dense("top_logprob", top_logprob, single, n, k), _dense("top_class", top_class, torch.int32, n, k), ws, bytes, _stream(stream)))
+
+
+def hgnn_logprob_grad(logits: torch.Tensor, labels: Optional[torch.Tensor], stats: torch.Tensor, dlogprob: Optional[torch.Tensor],
+                      dlogits: torch.Tensor, entropy: Optional[torch.Tensor] = None, dentropy: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dlogits (of the logits' type, or the logits themselves) from the gradients of the log probabilities and, with dentropy, of the entropies."""
+    if _calls is not None and _done(_calls.logprob_grad(logits, labels, stats, dlogprob, dlogits, entropy, dentropy, stream)):
+        return
+    _here(logits, labels, stats, dlogprob, dlogits, entropy, dentropy)
+    n, C = _two("logits", logits)
+    x, ld = _rows("logits", logits, n, C)
+    d, ldd = _rows("dlogits", dlogits, n, C)
+    _ptr(dlogits, logits.dtype)
+    single = torch.float32
+    _check(load().hgnn_logprob_grad(n, C, _type(logits), x, ld, _dense("labels", labels, torch.int32, n), _dense("stats", stats, single, n, 2),
+                                    _dense("dlogprob", dlogprob, single, n), _dense("entropy", entropy, single, n),
+                                    _dense("dentropy", dentropy, single, n), d, ldd, _stream(stream)))
+
+
+def hgnn_grad_norm_workspace() -> int:
+    return load().hgnn_grad_norm_workspace()
+
+
+def _extent(name: str, t: torch.Tensor):
+    """-> (rows, cols, pitch): one row of a tensor without gaps, the rows of a matrix with a pitch."""
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
+        return t.shape[0], t.shape[1], t.stride(0)
+    raise ValueError(f"{name} must be contiguous, or a matrix with unit stride along its rows, got {list(t.shape)} with strides {list(t.stride())}")
+
+
+def _grads(grads, outs=None):
+    if outs is not None and len(outs) != len(grads):
+        raise ValueError("grads and outs must have the same length")
+    a = (_GradStruct * max(len(grads), 1))()
+    for i, t in enumerate(grads):
+        o = t if outs is None else outs[i]
+        _here(t, o)
+        if o.shape != t.shape:
+            raise ValueError(f"outs[{i}] must have the shape {list(t.shape)}, got {list(o.shape)}")
+        rows, cols, ld = _extent(f"grads[{i}]", t)
+        orows, ocols, ldo = _extent(f"outs[{i}]", o)
+        if rows != orows:  # one of the two has gaps: both as matrices
+            (rows, cols), ld, ldo = t.shape, t.stride(0), o.stride(0)
+        a[i] = _GradStruct(_ptr(t), _ptr(o), rows, cols, ld, ldo, _type(t), _type(o))
+    return a
+
+
+def hgnn_grad_norm(grads, norm: torch.Tensor, workspace: torch.Tensor, inv_scale: float = 1.0, stream=None) -> None:
+    """norm (fp32 [1]) = inv_scale * the 2-norm of all elements of a list of fp16 and fp32 tensors; workspace: hgnn_grad_norm_workspace() bytes."""
+    if _calls is not None and _done(_calls.grad_norm(grads, norm, workspace, inv_scale, stream)):
+        return
+    a = _grads(grads)
+    _here(norm, workspace)
+    ws, bytes = _room(workspace)
+    _check(load().hgnn_grad_norm(len(grads), a, inv_scale, _dense("norm", norm, torch.float32, 1), ws, bytes, _stream(stream)))
+
+
+def hgnn_grad_clip(grads, max_norm: float, norm: torch.Tensor, workspace: torch.Tensor, outs=None, inv_scale: float = 1.0, stream=None) -> None:
+    """hgnn_grad_norm, and then all gradients times inv_scale * min(1, max_norm / norm), in place or into outs (fp16 or fp32 tensors of the same
+    shapes); zeros where the norm is not finite."""
+    if _calls is not None and _done(_calls.grad_clip(grads, max_norm, norm, workspace, outs, inv_scale, stream)):
+        return
+    a = _grads(grads, outs)
+    _here(norm, workspace)
+    ws, bytes = _room(workspace)
+    _check(load().hgnn_grad_clip(len(grads), a, inv_scale, max_norm, _dense("norm", norm, torch.float32, 1), ws, bytes, _stream(stream)))

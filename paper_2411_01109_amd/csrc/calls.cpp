@@ -16,6 +16,7 @@
 #include <exception>
 #include <new>
 #include <optional>
+#include <vector>
 
 #include "hgnn.h"
 
@@ -36,6 +37,8 @@ struct Table {  // a vertex-level tensor: rows of a pitch, unit stride along the
 // Reads arguments; ok turns false with the first that is not plain.
 struct Reader {
   bool ok = true;
+  int device = -1;  // of the tensors; kMixed: of several
+  static constexpr int kMixed = -2;
 
   const at::Tensor* tensor(PyObject* o) {
     if (!THPVariable_CheckExact(o)) {  // (a parameter is plain, another subclass is not)
@@ -47,6 +50,8 @@ struct Reader {
       ok = false;
       return nullptr;
     }
+    const int d = t.device().index();
+    device = device == -1 || device == d ? d : kMixed;
     return &t;
   }
   void* data(PyObject* o, at::ScalarType type) {
@@ -73,6 +78,89 @@ struct Reader {
       return r;
     }
     r.ld = t.stride(0), r.rows = t.size(0), r.cols = t.size(1);
+    return r;
+  }
+  // for the calls that check what a tensor is behind its address: rows of unit stride and a pitch, of either type
+  hgnn_type type_of(PyObject* o) {
+    const at::ScalarType t = ok ? THPVariable_Unpack(o).scalar_type() : at::kHalf;
+    if (t != at::kHalf && t != at::kFloat) ok = false;
+    return t == at::kFloat ? HGNN_F32 : HGNN_F16;
+  }
+  Table rows(PyObject* o) {
+    Table r;
+    const at::Tensor* const t = tensor(o);
+    if (!t) return r;
+    if (t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1)) {
+      ok = false;
+      return r;
+    }
+    r.p = t->data_ptr(), r.rows = t->size(0), r.cols = t->size(1);
+    r.ld = r.rows > 1 || t->stride(0) > r.cols ? t->stride(0) : r.cols;
+    return r;
+  }
+  Table rows(PyObject* o, int64_t n, int64_t cols) {
+    const Table r = rows(o);
+    if (r.rows != n || r.cols != cols) ok = false;
+    return r;
+  }
+  // a contiguous tensor of n elements, n x cols where cols > 0; None is allowed
+  void* dense(PyObject* o, at::ScalarType type, int64_t n, int64_t cols = 0) {
+    if (o == Py_None) return nullptr;
+    void* const p = data(o, type);
+    if (!ok) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_contiguous() || t.dim() != (cols > 0 ? 2 : 1) || t.size(0) != n || (cols > 0 && t.size(1) != cols)) ok = false;
+    return p;
+  }
+  int64_t columns(PyObject* o) {  // of a matrix, 0 of None
+    if (o == Py_None) return 0;
+    const at::Tensor* const t = tensor(o);
+    if (t && (t->dim() != 2 || t->size(1) == 0)) ok = false;
+    return ok ? t->size(1) : 0;
+  }
+  int32_t count(int64_t n) {
+    if (n > INT_MAX) ok = false;
+    return int32_t(n);
+  }
+  void* room(PyObject* o, size_t* bytes) {
+    *bytes = 0;
+    if (o == Py_None) return nullptr;
+    void* const p = workspace(o, bytes);
+    if (ok && !THPVariable_Unpack(o).is_contiguous()) ok = false;
+    return p;
+  }
+  void* stream_here(PyObject* o) {  // and all tensors are the current device's
+    PyObject* const here = ok ? PyObject_CallNoArgs(g_current_device) : nullptr;
+    if (!here || PyLong_AsLong(here) != device) ok = false;
+    Py_XDECREF(here);
+    return stream(o);
+  }
+  // a list or tuple of tensors, another of where they go, or None
+  std::vector<hgnn_grad> gradients(PyObject* o, PyObject* outs) {
+    std::vector<hgnn_grad> r;
+    const auto listed = [](PyObject* x) { return PyList_CheckExact(x) || PyTuple_CheckExact(x); };
+    if (!listed(o) || (outs != Py_None && !listed(outs)) || (outs != Py_None && PySequence_Fast_GET_SIZE(outs) != PySequence_Fast_GET_SIZE(o))) {
+      ok = false;
+      return r;
+    }
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+    r.resize(size_t(n));
+    for (Py_ssize_t i = 0; i < n && ok; ++i) {
+      PyObject *const a = PySequence_Fast_GET_ITEM(o, i), *const b = outs == Py_None ? a : PySequence_Fast_GET_ITEM(outs, i);
+      const at::Tensor *const t = tensor(a), *const u = ok ? tensor(b) : nullptr;
+      if (!ok) break;
+      hgnn_grad& g = r[size_t(i)];
+      g.grad = t->data_ptr(), g.out = u->data_ptr(), g.type = type_of(a), g.out_type = type_of(b);
+      if (t->sizes() != u->sizes()) {
+        ok = false;
+      } else if (t->is_contiguous() && u->is_contiguous()) {
+        g.rows = 1, g.cols = g.ld = g.ld_out = t->numel();
+      } else if (t->dim() == 2 && t->stride(1) == 1 && u->stride(1) == 1 && t->stride(0) >= t->size(1) && u->stride(0) >= t->size(1)) {
+        g.rows = t->size(0), g.cols = t->size(1), g.ld = t->stride(0), g.ld_out = u->stride(0);
+      } else {
+        ok = false;
+      }
+    }
     return r;
   }
   Table table_or_null(PyObject* o) { return o == Py_None ? Table() : table(o); }
@@ -193,7 +281,7 @@ PyObject* run(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F&& f) {
 #define HGNN_ENTRIES(X)                                                                                                          \
   X(linear) X(linear_padded) X(linear_wgrad) X(spmm) X(spmm_discretized) X(spmm_discretized_fused) X(sddmm) X(edge_softmax)       \
   X(edge_softmax_bwd) X(edge_rowsum) X(edge_colsum) X(gat_forward_fused) X(gat_forward_fused_save) X(gat_backward_fused_saved) \
-  X(gat_feature_grad)
+  X(gat_feature_grad) X(embedding) X(embedding_grad) X(logprob) X(logprob_grad) X(grad_norm) X(grad_clip)
 #define HGNN_ENTRY(name) decltype(&hgnn_##name) f_##name = nullptr;
 HGNN_ENTRIES(HGNN_ENTRY)
 
@@ -380,6 +468,89 @@ HGNN_CALL(gat_feature_grad, 13) {
   return [=] { return f_gat_feature_grad(dV.rows, H, D, dV.half(), dV.ld, d_el, d_er, al, ar, h.half(), h.ld, dh.half(), dh.ld, da_l, da_r, ws, bytes, s); };
 } HGNN_END
 
+HGNN_CALL(embedding, 5) {
+  const Table T = r.rows(a[1]);
+  const hgnn_type type = r.type_of(a[1]);
+  const Table out = r.rows(a[2]);
+  const auto* const ids = static_cast<const int32_t*>(r.dense(a[0], at::kInt, out.rows));
+  if (!ids || out.cols != T.cols || r.type_of(a[2]) != HGNN_F16) r.ok = false;
+  const float scale = r.real(a[3]);
+  const int32_t F = r.count(T.cols), V = r.count(T.rows);
+  void* const s = r.stream_here(a[4]);
+  return [=] { return f_embedding(out.rows, F, ids, V, type, T.p, T.ld, scale, out.half(), out.ld, s); };
+} HGNN_END
+
+HGNN_CALL(embedding_grad, 7) {
+  const Table T = r.rows(a[2]);
+  const hgnn_type type = r.type_of(a[2]);
+  const Table dY = r.rows(a[1]);
+  const auto* const ids = static_cast<const int32_t*>(r.dense(a[0], at::kInt, dY.rows));
+  if (!ids || dY.cols != T.cols || r.type_of(a[1]) != HGNN_F16) r.ok = false;
+  size_t bytes;
+  void* const ws = r.room(a[3], &bytes);
+  const float scale = r.real(a[4]);
+  const bool add = r.truth(a[5]);
+  const int32_t F = r.count(T.cols), V = r.count(T.rows);
+  void* const s = r.stream_here(a[6]);
+  return [=] { return f_embedding_grad(dY.rows, F, ids, V, dY.half(), dY.ld, scale, add, type, T.p, T.ld, ws, bytes, s); };
+} HGNN_END
+
+HGNN_CALL(logprob, 9) {
+  const Table x = r.rows(a[0]);
+  const hgnn_type type = r.type_of(a[0]);
+  const auto* const labels = static_cast<const int32_t*>(r.dense(a[1], at::kInt, x.rows));
+  auto* const logprob = static_cast<float*>(r.dense(a[2], at::kFloat, x.rows));
+  auto* const stats = static_cast<float*>(r.dense(a[3], at::kFloat, x.rows, 2));
+  auto* const entropy = static_cast<float*>(r.dense(a[4], at::kFloat, x.rows));
+  const int64_t k = r.columns(a[6]);
+  if ((a[5] == Py_None) != (a[6] == Py_None)) r.ok = false;
+  auto* const top = static_cast<float*>(r.dense(a[5], at::kFloat, x.rows, k));
+  auto* const top_class = static_cast<int32_t*>(r.dense(a[6], at::kInt, x.rows, k));
+  size_t bytes;
+  void* const ws = r.room(a[7], &bytes);
+  const int32_t C = r.count(x.cols), K = r.count(k);
+  void* const s = r.stream_here(a[8]);
+  return [=] { return f_logprob(x.rows, C, type, x.p, x.ld, labels, logprob, stats, entropy, K, top, top_class, ws, bytes, s); };
+} HGNN_END
+
+HGNN_CALL(logprob_grad, 8) {
+  const Table x = r.rows(a[0]);
+  const hgnn_type type = r.type_of(a[0]);
+  const auto* const labels = static_cast<const int32_t*>(r.dense(a[1], at::kInt, x.rows));
+  const auto* const stats = static_cast<const float*>(r.dense(a[2], at::kFloat, x.rows, 2));
+  const auto* const g = static_cast<const float*>(r.dense(a[3], at::kFloat, x.rows));
+  const Table dx = r.rows(a[4], x.rows, x.cols);
+  if (r.type_of(a[4]) != type) r.ok = false;
+  const auto* const entropy = static_cast<const float*>(r.dense(a[5], at::kFloat, x.rows));
+  const auto* const h = static_cast<const float*>(r.dense(a[6], at::kFloat, x.rows));
+  const int32_t C = r.count(x.cols);
+  void* const s = r.stream_here(a[7]);
+  return [=] { return f_logprob_grad(x.rows, C, type, x.p, x.ld, labels, stats, g, entropy, h, dx.p, dx.ld, s); };
+} HGNN_END
+
+HGNN_CALL(grad_norm, 5) {
+  const std::vector<hgnn_grad> g = r.gradients(a[0], Py_None);
+  auto* const norm = static_cast<float*>(r.dense(a[1], at::kFloat, 1));
+  size_t bytes;
+  void* const ws = r.room(a[2], &bytes);
+  const float inv_scale = r.real(a[3]);
+  const int32_t n = r.count(int64_t(g.size()));
+  void* const s = r.stream_here(a[4]);
+  return [=] { return f_grad_norm(n, g.data(), inv_scale, norm, ws, bytes, s); };
+} HGNN_END
+
+HGNN_CALL(grad_clip, 7) {
+  const std::vector<hgnn_grad> g = r.gradients(a[0], a[4]);
+  const float max_norm = r.real(a[1]);
+  auto* const norm = static_cast<float*>(r.dense(a[2], at::kFloat, 1));
+  size_t bytes;
+  void* const ws = r.room(a[3], &bytes);
+  const float inv_scale = r.real(a[5]);
+  const int32_t n = r.count(int64_t(g.size()));
+  void* const s = r.stream_here(a[6]);
+  return [=] { return f_grad_clip(n, g.data(), inv_scale, max_norm, norm, ws, bytes, s); };
+} HGNN_END
+
 // bind({entry point: address}, raw stream of a device, current device)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 3 || !PyDict_Check(a[0])) {
@@ -406,7 +577,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {HGNN_METHOD(bind), HGNN_METHOD(linear), HGNN_METHOD(linear_wgrad), HGNN_METHOD(spmm), HGNN_METHOD(spmm_discretized),
                          HGNN_METHOD(spmm_discretized_fused), HGNN_METHOD(sddmm), HGNN_METHOD(edge_softmax), HGNN_METHOD(edge_softmax_bwd),
                          HGNN_METHOD(edge_rowsum), HGNN_METHOD(edge_colsum), HGNN_METHOD(gat_forward_fused), HGNN_METHOD(gat_forward_fused_save),
-                         HGNN_METHOD(gat_backward_fused_saved), HGNN_METHOD(gat_feature_grad), {nullptr, nullptr, 0, nullptr}};
+                         HGNN_METHOD(gat_backward_fused_saved), HGNN_METHOD(gat_feature_grad), HGNN_METHOD(embedding), HGNN_METHOD(embedding_grad),
+                         HGNN_METHOD(logprob), HGNN_METHOD(logprob_grad), HGNN_METHOD(grad_norm), HGNN_METHOD(grad_clip), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
