@@ -1,4 +1,6 @@
 // Rows of a learned vertex table by id, and the gradient of the table: what stands before the first layer of a graph without vertex features.
+#include <algorithm>
+
 #include "common.h"
 #include "rows.h"
 #include "sort.h"
@@ -35,10 +37,11 @@ __global__ __launch_bounds__(kBlock) void embedding_kernel(LookupArgs a) {
 }
 
 // ---- the gradient -------------------------------------------------------------------------------------------
-// dT[v] = scale * sum of dY[i] over the i with ids[i] = v.  The positions are sorted by id (stable, so the rows of an id keep their order), the sorted list is cut
-// into shares of T positions, and L lanes walk a share: a run of equal ids that begins and ends inside it is stored at once; what a share holds of a run that
-// it shares with its neighbours is left as a partial sum in fp32, `head` of a run that began earlier, `tail` of one that goes on, and a second pass adds the
-// partial sums of a run in order.  No atomics: the same bits on every run.  Rows without a position are zeros, which the workgroups behind those of the shares write.
+// dT[v] = scale * sum of dY[i] over the i with ids[i] = v.  The positions are sorted by id (stable, so the rows of an id keep their order).  L lanes walk a share of
+// the sorted list, kShare positions, a workgroup so many consecutive ones as it has groups of L.  A run of equal ids inside a share is stored at once.  What
+// shares hold of a run in common goes to LDS, `head` of a run that began before the share, `tail` of one that goes on behind it, and is added in order by the share where the run
+// begins; what workgroups hold in common goes to memory in the same two forms, and a second pass adds it.  No atomics: the same bits on every run.  Rows without a position
+// are zeros, which workgroups behind those of the shares write.
 
 // words: (id, position), an id that is none counts as V
 struct IdWords {
@@ -62,19 +65,20 @@ struct IdWords {
 
 struct TableGradArgs {
   const uint64_t* words;  // sorted
-  int64_t n, shares;
-  int pos_bits, T, F, V;
+  int64_t n;
+  int pos_bits, F, V;
   const half_t* dY;
   int64_t ldy;
   float scale;
   void* dT;
   int64_t lddt;
-  float* part;  // [shares][2][pitch]: head and tail
+  float* part;  // [blocks][2][pitch]: head and tail of a workgroup
   int pitch;
-  int64_t share_blocks;
+  int64_t blocks;  // workgroups of shares
   __device__ __forceinline__ int id(int64_t k) const { return int(words[k] >> pos_bits); }
+  __device__ __forceinline__ int id_of(uint64_t w) const { return int(w >> pos_bits); }
   __device__ __forceinline__ int64_t pos(uint64_t w) const { return int64_t(w & ((uint64_t(1) << pos_bits) - 1)); }
-  __device__ __forceinline__ float* partial(int64_t share, int tail) const { return part + (2 * share + tail) * pitch; }
+  __device__ __forceinline__ float* partial(int64_t block, int tail) const { return part + (2 * block + tail) * pitch; }
 };
 
 template <class T, bool ADD>
@@ -89,78 +93,186 @@ __device__ __forceinline__ void add_row(const TableGradArgs& a, int id, int f, P
   }
   store_piece(p, a.F - f, x);
 }
+__device__ __forceinline__ void add_to(Piece& x, const Piece& y) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x.v[j] += y.v[j];
+}
+
+// by a whole wave, 64 places looked at in each step: how many of the n sorted words have an id below `id`
+__device__ __forceinline__ int64_t wave_words_below(const TableGradArgs& a, int64_t id) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int64_t lo = 0, hi = a.n;  // the answer is in [lo, hi]
+  while (lo < hi) {
+    const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+    const int held = __popcll(__ballot(at < hi && a.id(at) < id));  // the first lanes
+    if (held == 0) {
+      hi = lo;
+    } else {
+      const int64_t last = lo + (held - 1) * step;
+      hi = last + step < hi ? last + step : hi;
+      lo = last + 1;
+    }
+  }
+  return lo;
+}
 
 constexpr int kZeroRows = kWave;  // table rows of a wave that writes zeros
 
-template <class T, bool ADD, int L>
-__global__ __launch_bounds__(kBlock) void table_grad_kernel(TableGradArgs a) {
-  if (int64_t(blockIdx.x) >= a.share_blocks) {  // zeros
-    const int lane = threadIdx.x & (kWave - 1);
-    const int64_t r0 = ((int64_t(blockIdx.x) - a.share_blocks) * kWavesPerBlock + threadIdx.x / kWave) * kZeroRows, r = r0 + lane;
-    if (r0 >= a.V) return;
-    int64_t lo = 0, hi = a.n;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) >> 1;
-      if (a.id(mid) < r) lo = mid + 1;
-      else hi = mid;
-    }
-    const uint64_t there = __ballot(r >= a.V || (lo < a.n && a.id(lo) == r));
-    const int pieces = (a.F + 7) / 8;
-    for (int k = 0; k < kZeroRows; ++k) {
-      if (there >> k & 1) continue;
-      T* const p = static_cast<T*>(a.dT) + (r0 + k) * a.lddt;
-      for (int f = lane; f < pieces; f += kWave) store_piece(p + 8 * f, a.F - 8 * f, Piece{});
-    }
-    return;
+// zeros in those of 64 rows that no position has
+template <class T, int L>
+__device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0) {
+  if (r0 >= a.V) return;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t r = r0 + lane;
+  int64_t lo = wave_words_below(a, r0), hi = wave_words_below(a, r0 + kZeroRows);
+  const int64_t end = hi;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (a.id(mid) < r) lo = mid + 1;
+    else hi = mid;
   }
-  const int64_t share = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / L;
-  if (share >= a.shares) return;
-  const int64_t first = share * a.T, end = first + a.T < a.n ? first + a.T : a.n;
-  const int before = first > 0 ? a.id(first - 1) : -1, after = end < a.n ? a.id(end) : -1;
-  for (int f = 8 * (threadIdx.x % L); f < a.F; f += 8 * L) {
-    int cur = -1;
-    bool head = false;
-    Piece sum{};
-    auto done = [&](bool tail) {
-      if (cur < 0 || cur >= a.V) return;
-      if (head || tail) store_piece(a.partial(share, head ? 0 : 1) + f, sum);
-      else add_row<T, ADD>(a, cur, f, sum);
-    };
-    for (int64_t k = first; k < end; ++k) {
-      const uint64_t w = a.words[k];
-      const int id = int(w >> a.pos_bits);
-      if (id != cur) {
-        done(false);
-        cur = id;
-        head = k == first && id == before;
-        sum = Piece{};
-      }
-      if (id >= a.V) break;  // the rest are ids that are none
-      const Piece x = load_piece(a.dY + a.pos(w) * a.ldy + f, a.F - f, 0.f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum.v[j] += x.v[j];
-    }
-    done(cur == after);
+  const uint64_t there = __ballot(r >= a.V || (lo < end && a.id(lo) == r));
+  for (int k = lane / L; k < kZeroRows; k += kWave / L) {
+    if (there >> k & 1) continue;
+    T* const p = static_cast<T*>(a.dT) + (r0 + k) * a.lddt;
+    for (int f = 8 * (lane % L); f < a.F; f += 8 * L) store_piece(p + f, a.F - f, Piece{});
   }
 }
 
-// The runs that several shares hold, by the share where a run begins.
+constexpr int kShare = 16;  // positions of a share
+constexpr int kAhead = 8;   // rows of a share that are fetched together
+
+template <class T, bool ADD, int L>
+__global__ __launch_bounds__(kBlock) void table_grad_kernel(TableGradArgs a) {
+  constexpr int G = kBlock / L;  // shares of a workgroup
+  if (int64_t(blockIdx.x) >= a.blocks) {
+    if (blockIdx.y == 0) write_zeros<T, L>(a, ((int64_t(blockIdx.x) - a.blocks) * kWavesPerBlock + threadIdx.x / kWave) * kZeroRows);
+    return;
+  }
+  __shared__ __align__(16) float s_part[2][kBlock * 8];  // head and tail of the shares
+  __shared__ int s_id[G];                                // of the run that begins in a share and goes on, -1: none; and
+  __shared__ int s_through[G];                           // whether a run that began before the share goes on behind it
+  const int g = threadIdx.x / L, l = threadIdx.x % L, f = 8 * (int(blockIdx.y) * L + l);
+  const int64_t begin = int64_t(blockIdx.x) * (G * kShare), stop = begin + G * kShare < a.n ? begin + G * kShare : a.n;
+  const int64_t first = begin + g * kShare < stop ? begin + g * kShare : stop, end = first + kShare < stop ? first + kShare : stop;
+  const int before = first > 0 && first < end ? a.id(first - 1) : -1, after = end < a.n && first < end ? a.id(end) : -1;
+  const bool mine = f < a.F;
+  int cur = -1, tail_id = -1;
+  bool head = false;
+  Piece sum{};
+  auto done = [&](bool goes_on) {  // with the run of cur
+    if (cur < 0 || cur >= a.V) return;
+    if (head || goes_on) {
+      float* const s = s_part[head ? 0 : 1] + threadIdx.x * 8;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = sum.v[j];
+      if (!head) tail_id = cur;
+    } else if (mine) {
+      add_row<T, ADD>(a, cur, f, sum);
+    }
+  };
+  for (int64_t k = first; k < end; k += kAhead) {
+    uint64_t w[kAhead];
+    half8_t x[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) w[i] = a.words[k + i < end ? k + i : end - 1];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      x[i] = half8_t{};
+      if (mine) x[i] = load_halves(a.dY + a.pos(w[i]) * a.ldy + f, a.F - f);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (k + i >= end) break;
+      const int id = a.id_of(w[i]);
+      if (id != cur) {
+        done(false);
+        cur = id;
+        head = k + i == first && id == before;
+        sum = Piece{};
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum.v[j] += float(x[i][j]);
+    }
+  }
+  const bool goes_on = cur >= 0 && cur == after;
+  done(goes_on);
+  if (l == 0) s_id[g] = tail_id, s_through[g] = head && goes_on;
+  __syncthreads();
+  // the chain of a run: from the share where it begins, or the workgroup's first, through shares that hold nothing else, to the share where it ends
+  auto chain = [&](Piece x, int last_through, bool* whole) {  // the heads of the shares behind g
+    int i = g + 1;
+    bool open = last_through;
+    while (open && i < G && begin + i * kShare < stop) {
+      const float* const s = s_part[0] + (i * L + l) * 8;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x.v[j] += s[j];
+      open = s_through[i];
+      ++i;
+    }
+    *whole = open;  // beyond the workgroup
+    return x;
+  };
+  auto of_lds = [&](int tail) {
+    Piece x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x.v[j] = s_part[tail][threadIdx.x * 8 + j];
+    return x;
+  };
+  bool open;
+  if (tail_id >= 0) {
+    const Piece x = chain(of_lds(1), true, &open);
+    if (mine) {
+      if (open) store_piece(a.partial(blockIdx.x, 1) + f, x);
+      else add_row<T, ADD>(a, tail_id, f, x);
+    }
+  }
+  if (g == 0 && before >= 0 && before < a.V && a.id(first) == before) {
+    const Piece x = chain(of_lds(0), s_through[0], &open);
+    if (mine) store_piece(a.partial(blockIdx.x, 0) + f, x);
+  }
+}
+
+// The runs that several workgroups hold, by a workgroup for each one where a run may begin: its tail and the heads of those behind it, every group of L lanes
+// a part of them.
 template <class T, bool ADD, int L>
 __global__ __launch_bounds__(kBlock) void table_grad_join_kernel(TableGradArgs a) {
-  const int64_t share = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / L;
-  if (share >= a.shares - 1) return;
-  const int64_t first = share * a.T, end = first + a.T;
+  constexpr int G = kBlock / L;
+  constexpr int64_t kPer = int64_t(G) * kShare;
+  __shared__ __align__(16) float s_part[kBlock * 8];
+  const int64_t b = blockIdx.x, begin = b * kPer, end = begin + kPer;
   const int id = a.id(end);
-  if (id >= a.V || a.id(end - 1) != id || (first > 0 && a.id(first - 1) == id && a.id(first) == id)) return;
-  for (int f = 8 * (threadIdx.x % L); f < a.F; f += 8 * L) {
-    Piece sum = load_piece(a.partial(share, 1) + f);
-    for (int64_t s = share + 1; s < a.shares && a.id(s * a.T) == id; ++s) {
-      const Piece x = load_piece(a.partial(s, 0) + f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum.v[j] += x.v[j];
+  if (id >= a.V || a.id(end - 1) != id || (begin > 0 && a.id(begin - 1) == id)) return;
+  // workgroups behind this one that begin inside the run: all waves look for the last of them
+  int64_t lo = 1, hi = a.blocks - b;  // first one (counted from here) that does not, in [lo, hi]
+  while (lo < hi) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+    const int held = __popcll(__ballot(at < hi && a.id((b + at) * kPer) == id));
+    if (held == 0) {
+      hi = lo;
+    } else {
+      const int64_t last = lo + (held - 1) * step;
+      hi = last + step < hi ? last + step : hi;
+      lo = last + 1;
     }
-    add_row<T, ADD>(a, id, f, sum);
   }
+  const int g = threadIdx.x / L, l = threadIdx.x % L, f = 8 * (int(blockIdx.y) * L + l);
+  if (f < a.F) {
+    Piece sum{};
+    if (g == 0) sum = load_piece(a.partial(b, 1) + f);
+#pragma unroll 4
+    for (int64_t i = 1 + g; i < lo; i += G) add_to(sum, load_piece(a.partial(b + i, 0) + f));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s_part[threadIdx.x * 8 + j] = sum.v[j];
+  }
+  __syncthreads();
+  if (g > 0 || f >= a.F) return;
+  Piece sum{};
+  for (int i = 0; i < G && i < lo; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum.v[j] += s_part[(i * L + l) * 8 + j];
+  add_row<T, ADD>(a, id, f, sum);
 }
 
 static int bits_of(int64_t values) {  // that tell so many values apart
@@ -169,14 +281,12 @@ static int bits_of(int64_t values) {  // that tell so many values apart
   return b;
 }
 
-constexpr int kShare = 16;
-
 struct TableGradSpace {
   uint64_t *buf0, *buf1;
   void* scratch;
   float* part;
-  int64_t shares;
-  int T, pitch;
+  int64_t blocks;
+  int pitch;
   size_t bytes;
 };
 static TableGradSpace table_grad_space(void* base, int64_t n, int32_t F) {
@@ -187,13 +297,13 @@ static TableGradSpace table_grad_space(void* base, int64_t n, int32_t F) {
     at += (bytes + 255) / 256 * 256;
     return q;
   };
-  p.T = kShare;
-  p.shares = ceil_div(n, p.T);
+  const int groups = kBlock / std::min(kWave, pow2_at_least((F + 7) / 8));
+  p.blocks = ceil_div(n, int64_t(groups) * kShare);
   p.pitch = (F + 7) / 8 * 8;
   p.buf0 = reinterpret_cast<uint64_t*>(take(8 * size_t(n)));
   p.buf1 = reinterpret_cast<uint64_t*>(take(8 * size_t(n)));
   p.scratch = take(n > 0 ? sort_scratch_bytes(n) : 0);
-  p.part = reinterpret_cast<float*>(take(2 * size_t(p.shares) * size_t(p.pitch) * sizeof(float)));
+  p.part = reinterpret_cast<float*>(take(p.blocks > 1 ? 2 * size_t(p.blocks) * size_t(p.pitch) * sizeof(float) : 0));
   p.bytes = size_t(at - static_cast<char*>(base));
   return p;
 }
@@ -216,17 +326,14 @@ static hgnn_status table_grad(const TableGradArgs& a, hipStream_t s) {
   hgnn_status st = HGNN_OK;
   with_lanes(a.F, [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
-    TableGradArgs b = a;
-    b.share_blocks = ceil_div(a.shares * L, kBlock);
     const int64_t zeros = ADD ? 0 : ceil_div(a.V, int64_t(kZeroRows) * kWavesPerBlock);
+    const unsigned fy = unsigned(ceil_div(a.F, 8 * L));  // 1 up to 512 features
     auto go = [&]() -> hgnn_status {
-      HGNN_REQUIRE(b.share_blocks + zeros <= 0x7fffffff, HGNN_EUNSUPPORTED, "hgnn_embedding_grad: grid too large");
-      if (b.share_blocks + zeros > 0) {
-        table_grad_kernel<T, ADD, L><<<dim3(unsigned(b.share_blocks + zeros)), kBlock, 0, s>>>(b);
-        HGNN_LAUNCH_CHECK("table_grad_kernel");
-      }
-      if (a.shares > 1) {
-        table_grad_join_kernel<T, ADD, L><<<dim3(unsigned(b.share_blocks)), kBlock, 0, s>>>(b);
+      HGNN_REQUIRE(a.blocks + zeros <= 0x7fffffff, HGNN_EUNSUPPORTED, "hgnn_embedding_grad: grid too large");
+      table_grad_kernel<T, ADD, L><<<dim3(unsigned(a.blocks + zeros), fy), kBlock, 0, s>>>(a);
+      HGNN_LAUNCH_CHECK("table_grad_kernel");
+      if (a.blocks > 1) {
+        table_grad_join_kernel<T, ADD, L><<<dim3(unsigned(a.blocks - 1), fy), kBlock, 0, s>>>(a);
         HGNN_LAUNCH_CHECK("table_grad_join_kernel");
       }
       return HGNN_OK;
@@ -296,7 +403,7 @@ hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_
   hipStream_t s = static_cast<hipStream_t>(stream);
   const TableGradSpace w = table_grad_space(workspace, n, F);
   TableGradArgs a{};
-  a.n = n, a.shares = w.shares, a.T = w.T, a.F = F, a.V = V;
+  a.n = n, a.blocks = w.blocks, a.F = F, a.V = V;
   a.pos_bits = bits_of(n);
   a.dY = reinterpret_cast<const half_t*>(dY), a.ldy = ldy, a.scale = scale;
   a.dT = dT, a.lddt = lddt, a.part = w.part, a.pitch = w.pitch;

@@ -26,6 +26,15 @@ __device__ __forceinline__ Piece load_piece(const float* p) {
   const float4_t a = *reinterpret_cast<const float4_any_t*>(p), b = *reinterpret_cast<const float4_any_t*>(p + 4);
   return Piece{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
+// as it is in memory, the elements behind the first `left` as zeros
+__device__ __forceinline__ half8_t load_halves(const half_t* p, int left) {
+  if (left >= 8) return *reinterpret_cast<const half8_any_t*>(p);
+  half8_t h = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < left) h[i] = p[i];
+  return h;
+}
 // the first `left` elements, the others as `none`
 template <class T>
 __device__ __forceinline__ Piece load_piece(const T* p, int left, float none) {
