@@ -7,32 +7,44 @@
 
 namespace hgnn {
 
+constexpr int kLookups = 4;                     // rows that L lanes take together, of many
+constexpr int64_t kFewLookups = int64_t(1) << 20;  // lanes of all rows up to which they take one
+
 struct LookupArgs {
   int64_t n;
   int F, V;
   const int* ids;
   const void* table;
-  int64_t ldt;
+  int64_t ldt, inside;  // elements from the table's first to its last
   float scale;
   half_t* out;
   int64_t ldo;
 };
 
-// out[i] = scale * T[ids[i]]: L lanes take a row in pieces of eight.  Bound by memory.
-template <class T, int L>
+// out[i] = scale * T[ids[i]]: L lanes take N rows in pieces of eight, whose reads go out together.  Bound by memory.
+template <class T, int L, int N>
 __global__ __launch_bounds__(kBlock) void embedding_kernel(LookupArgs a) {
-  const int64_t i = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / L;
-  if (i >= a.n) return;
-  const int id = a.ids[i];
-  const bool real = uint32_t(id) < uint32_t(a.V);
-  const T* const row = static_cast<const T*>(a.table) + int64_t(real ? id : 0) * a.ldt;
-  half_t* const out = a.out + i * a.ldo;
-  for (int f = 8 * (threadIdx.x % L); f < a.F; f += 8 * L) {
-    Piece x{};
-    if (real) x = load_piece(row + f, a.F - f, 0.f);
+  constexpr int G = kBlock / L;
+  const int64_t i0 = int64_t(blockIdx.x) * (G * N) + threadIdx.x / L;
+  int id[N];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x.v[j] *= a.scale;
-    store_piece(out + f, a.F - f, x);
+  for (int u = 0; u < N; ++u) id[u] = i0 + u * G < a.n ? a.ids[i0 + u * G] : -1;
+  for (int f = 8 * (threadIdx.x % L); f < a.F; f += 8 * L) {
+    RawPiece<T> x[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      x[u].v = 0;
+      const int64_t at = int64_t(id[u]) * a.ldt + f;
+      if (uint32_t(id[u]) < uint32_t(a.V)) x[u] = load_raw(static_cast<const T*>(a.table) + at, a.F - f, a.inside - at);
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      if (i0 + u * G >= a.n) break;
+      Piece y = floats(x[u]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y.v[j] *= a.scale;
+      store_piece(a.out + (i0 + u * G) * a.ldo + f, a.F - f, y);
+    }
   }
 }
 
@@ -63,39 +75,61 @@ struct IdWords {
   __device__ __forceinline__ uint64_t count(const SortPass&, int64_t k) const { return word(ids[k], k); }
 };
 
+enum { kPastZeros = 1, kPastAll = 2 };
 struct TableGradArgs {
   const uint64_t* words;  // sorted
   int64_t n;
   int pos_bits, F, V;
   const half_t* dY;
-  int64_t ldy;
+  int64_t ldy, inside;  // elements from the first of dY to its last
   float scale;
   void* dT;
   int64_t lddt;
   float* part;  // [blocks][2][pitch]: head and tail of a workgroup
   int pitch;
   int64_t blocks;  // workgroups of shares
+  int past;  // the caches: zeros, or all rows
   __device__ __forceinline__ int id(int64_t k) const { return int(words[k] >> pos_bits); }
   __device__ __forceinline__ int id_of(uint64_t w) const { return int(w >> pos_bits); }
   __device__ __forceinline__ int64_t pos(uint64_t w) const { return int64_t(w & ((uint64_t(1) << pos_bits) - 1)); }
   __device__ __forceinline__ float* partial(int64_t block, int tail) const { return part + (2 * block + tail) * pitch; }
 };
 
-template <class T, bool ADD>
-__device__ __forceinline__ void add_row(const TableGradArgs& a, int id, int f, Piece x) {
-  T* const p = static_cast<T*>(a.dT) + int64_t(id) * a.lddt + f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x.v[j] *= a.scale;
-  if (ADD) {
-    const Piece y = load_piece(p, a.F - f, 0.f);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x.v[j] += y.v[j];
-  }
-  store_piece(p, a.F - f, x);
+// A lane's eight features of a row: four at f and four at f + 4 L, so that the 16 bytes that lanes store lie beside each other
+struct Quads {
+  float4_t lo, hi;
+  __device__ __forceinline__ void add(const Quads& y) { lo += y.lo, hi += y.hi; }
+};
+template <int L>
+__device__ __forceinline__ Quads load_quads(const float* p, int f, int F) {  // of a row that is padded to whole quads
+  Quads r{};
+  if (f < F) r.lo = *reinterpret_cast<const float4_t*>(p + f);
+  if (f + 4 * L < F) r.hi = *reinterpret_cast<const float4_t*>(p + f + 4 * L);
+  return r;
 }
-__device__ __forceinline__ void add_to(Piece& x, const Piece& y) {
+template <int L>
+__device__ __forceinline__ void store_quads(float* p, int f, int F, const Quads& x) {
+  if (f < F) *reinterpret_cast<float4_t*>(p + f) = x.lo;
+  if (f + 4 * L < F) *reinterpret_cast<float4_t*>(p + f + 4 * L) = x.hi;
+}
+template <class T, bool ADD>
+__device__ __forceinline__ void add_quad(const TableGradArgs& a, T* p, int left, float4_t v) {
+  if (left <= 0) return;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x.v[j] += y.v[j];
+  for (int j = 0; j < 4; ++j) v[j] *= a.scale;
+  if (ADD) {
+    const auto y = load_quad(p, left, left);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] += float(y[j]);
+  }
+  if (a.past == kPastAll) store_quad<T, true>(p, left, v);
+  else store_quad(p, left, v);
+}
+template <class T, bool ADD, int L>
+__device__ __forceinline__ void add_row(const TableGradArgs& a, int id, int f, const Quads& x) {
+  T* const p = static_cast<T*>(a.dT) + int64_t(id) * a.lddt + f;
+  add_quad<T, ADD>(a, p, a.F - f, x.lo);
+  add_quad<T, ADD>(a, p + 4 * L, a.F - f - 4 * L, x.hi);
 }
 
 // by a whole wave, 64 places looked at in each step: how many of the n sorted words have an id below `id`
@@ -135,52 +169,54 @@ __device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0) 
   for (int k = lane / L; k < kZeroRows; k += kWave / L) {
     if (there >> k & 1) continue;
     T* const p = static_cast<T*>(a.dT) + (r0 + k) * a.lddt;
-    for (int f = 8 * (lane % L); f < a.F; f += 8 * L) store_piece(p + f, a.F - f, Piece{});
+    for (int f = 4 * (lane % L); f < a.F; f += 4 * L)
+      if (a.past != 0) store_quad<T, true>(p + f, a.F - f, float4_t{});
+      else store_quad(p + f, a.F - f, float4_t{});
   }
 }
 
-constexpr int kShare = 16;  // positions of a share
-constexpr int kAhead = 8;   // rows of a share that are fetched together
+constexpr int kShare = 8;  // positions of a share
+constexpr int kAhead = 4;  // rows of a share that are fetched together
 
 template <class T, bool ADD, int L>
-__global__ __launch_bounds__(kBlock) void table_grad_kernel(TableGradArgs a) {
+__global__ __launch_bounds__(kBlock, 6) void table_grad_kernel(TableGradArgs a) {
   constexpr int G = kBlock / L;  // shares of a workgroup
   if (int64_t(blockIdx.x) >= a.blocks) {
     if (blockIdx.y == 0) write_zeros<T, L>(a, ((int64_t(blockIdx.x) - a.blocks) * kWavesPerBlock + threadIdx.x / kWave) * kZeroRows);
     return;
   }
-  __shared__ __align__(16) float s_part[2][kBlock * 8];  // head and tail of the shares
-  __shared__ int s_id[G];                                // of the run that begins in a share and goes on, -1: none; and
-  __shared__ int s_through[G];                           // whether a run that began before the share goes on behind it
-  const int g = threadIdx.x / L, l = threadIdx.x % L, f = 8 * (int(blockIdx.y) * L + l);
-  const int64_t begin = int64_t(blockIdx.x) * (G * kShare), stop = begin + G * kShare < a.n ? begin + G * kShare : a.n;
+  const int64_t block = blockIdx.x;
+  __shared__ Quads s_part[2][kBlock];  // head and tail of the shares
+  __shared__ int s_through[G];         // whether a run that began before the share goes on behind it
+  const int g = threadIdx.x / L, l = threadIdx.x % L, f = 8 * L * int(blockIdx.y) + 4 * l;
+  const int64_t begin = block * (G * kShare), stop = begin + G * kShare < a.n ? begin + G * kShare : a.n;
   const int64_t first = begin + g * kShare < stop ? begin + g * kShare : stop, end = first + kShare < stop ? first + kShare : stop;
   const int before = first > 0 && first < end ? a.id(first - 1) : -1, after = end < a.n && first < end ? a.id(end) : -1;
-  const bool mine = f < a.F;
   int cur = -1, tail_id = -1;
   bool head = false;
-  Piece sum{};
-  auto done = [&](bool goes_on) {  // with the run of cur
+  Quads sum{};
+  auto done = [&](bool goes_on) __attribute__((always_inline)) {  // with the run of cur
     if (cur < 0 || cur >= a.V) return;
     if (head || goes_on) {
-      float* const s = s_part[head ? 0 : 1] + threadIdx.x * 8;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = sum.v[j];
+      s_part[head ? 0 : 1][threadIdx.x] = sum;
       if (!head) tail_id = cur;
-    } else if (mine) {
-      add_row<T, ADD>(a, cur, f, sum);
+    } else {
+      add_row<T, ADD, L>(a, cur, f, sum);
     }
   };
   for (int64_t k = first; k < end; k += kAhead) {
     uint64_t w[kAhead];
-    half8_t x[kAhead];
+    half4_t x[kAhead][2];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) w[i] = a.words[k + i < end ? k + i : end - 1];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      x[i] = half8_t{};
-      if (mine) x[i] = load_halves(a.dY + a.pos(w[i]) * a.ldy + f, a.F - f);
-    }
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int64_t at = a.pos(w[i]) * a.ldy + f + 4 * L * q;
+        x[i][q] = 0;
+        if (f + 4 * L * q < a.F) x[i][q] = load_quad(a.dY + at, a.F - f - 4 * L * q, a.inside - at);
+      }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (k + i >= end) break;
@@ -189,48 +225,33 @@ __global__ __launch_bounds__(kBlock) void table_grad_kernel(TableGradArgs a) {
         done(false);
         cur = id;
         head = k + i == first && id == before;
-        sum = Piece{};
+        sum = Quads{};
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum.v[j] += float(x[i][j]);
+      for (int j = 0; j < 4; ++j) sum.lo[j] += float(x[i][0][j]), sum.hi[j] += float(x[i][1][j]);
     }
   }
   const bool goes_on = cur >= 0 && cur == after;
   done(goes_on);
-  if (l == 0) s_id[g] = tail_id, s_through[g] = head && goes_on;
+  if (l == 0) s_through[g] = head && goes_on;
   __syncthreads();
   // the chain of a run: from the share where it begins, or the workgroup's first, through shares that hold nothing else, to the share where it ends
-  auto chain = [&](Piece x, int last_through, bool* whole) {  // the heads of the shares behind g
-    int i = g + 1;
-    bool open = last_through;
-    while (open && i < G && begin + i * kShare < stop) {
-      const float* const s = s_part[0] + (i * L + l) * 8;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x.v[j] += s[j];
+  auto chain = [&](Quads x, bool open, bool* beyond) __attribute__((always_inline)) {  // and the heads of the shares behind g
+    for (int i = g + 1; open && i < G && begin + i * kShare < stop; ++i) {
+      x.add(s_part[0][i * L + l]);
       open = s_through[i];
-      ++i;
     }
-    *whole = open;  // beyond the workgroup
-    return x;
-  };
-  auto of_lds = [&](int tail) {
-    Piece x;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x.v[j] = s_part[tail][threadIdx.x * 8 + j];
+    *beyond = open;  // the workgroup
     return x;
   };
   bool open;
   if (tail_id >= 0) {
-    const Piece x = chain(of_lds(1), true, &open);
-    if (mine) {
-      if (open) store_piece(a.partial(blockIdx.x, 1) + f, x);
-      else add_row<T, ADD>(a, tail_id, f, x);
-    }
+    const Quads x = chain(s_part[1][threadIdx.x], true, &open);
+    if (open) store_quads<L>(a.partial(block, 1), f, a.F, x);
+    else add_row<T, ADD, L>(a, tail_id, f, x);
   }
-  if (g == 0 && before >= 0 && before < a.V && a.id(first) == before) {
-    const Piece x = chain(of_lds(0), s_through[0], &open);
-    if (mine) store_piece(a.partial(blockIdx.x, 0) + f, x);
-  }
+  if (g == 0 && before >= 0 && before < a.V && a.id(first) == before)
+    store_quads<L>(a.partial(block, 0), f, a.F, chain(s_part[0][threadIdx.x], s_through[0], &open));
 }
 
 // The runs that several workgroups hold, by a workgroup for each one where a run may begin: its tail and the heads of those behind it, every group of L lanes
@@ -239,7 +260,7 @@ template <class T, bool ADD, int L>
 __global__ __launch_bounds__(kBlock) void table_grad_join_kernel(TableGradArgs a) {
   constexpr int G = kBlock / L;
   constexpr int64_t kPer = int64_t(G) * kShare;
-  __shared__ __align__(16) float s_part[kBlock * 8];
+  __shared__ Quads s_part[kBlock];
   const int64_t b = blockIdx.x, begin = b * kPer, end = begin + kPer;
   const int id = a.id(end);
   if (id >= a.V || a.id(end - 1) != id || (begin > 0 && a.id(begin - 1) == id)) return;
@@ -257,22 +278,17 @@ __global__ __launch_bounds__(kBlock) void table_grad_join_kernel(TableGradArgs a
       lo = last + 1;
     }
   }
-  const int g = threadIdx.x / L, l = threadIdx.x % L, f = 8 * (int(blockIdx.y) * L + l);
-  if (f < a.F) {
-    Piece sum{};
-    if (g == 0) sum = load_piece(a.partial(b, 1) + f);
+  const int g = threadIdx.x / L, l = threadIdx.x % L, f = 8 * L * int(blockIdx.y) + 4 * l;
+  Quads sum{};
+  if (g == 0) sum = load_quads<L>(a.partial(b, 1), f, a.F);
 #pragma unroll 4
-    for (int64_t i = 1 + g; i < lo; i += G) add_to(sum, load_piece(a.partial(b + i, 0) + f));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s_part[threadIdx.x * 8 + j] = sum.v[j];
-  }
+  for (int64_t i = 1 + g; i < lo; i += G) sum.add(load_quads<L>(a.partial(b + i, 0), f, a.F));
+  s_part[threadIdx.x] = sum;
   __syncthreads();
-  if (g > 0 || f >= a.F) return;
-  Piece sum{};
-  for (int i = 0; i < G && i < lo; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum.v[j] += s_part[(i * L + l) * 8 + j];
-  add_row<T, ADD>(a, id, f, sum);
+  if (g > 0) return;
+  sum = Quads{};
+  for (int i = 0; i < G && i < lo; ++i) sum.add(s_part[i * L + l]);
+  add_row<T, ADD, L>(a, id, f, sum);
 }
 
 static int bits_of(int64_t values) {  // that tell so many values apart
@@ -361,16 +377,20 @@ hgnn_status hgnn_embedding(int64_t n, int32_t F, const int32_t* ids, int32_t V, 
   HGNN_REQUIRE(ids && out && (table || V == 0), HGNN_EINVAL, "%s: NULL argument", who);
   HGNN_REQUIRE(aligned_to_type(ids, HGNN_F32) && aligned_to_type(table, table_type) && aligned_to_type(out, HGNN_F16), HGNN_EINVAL,
                "%s: an array that is not aligned to its type", who);
-  const LookupArgs a{n, F, V, ids, table, ldt, scale, reinterpret_cast<half_t*>(out), ldo};
+  const LookupArgs a{n, F, V, ids, table, ldt, extent_of(V, F, ldt), scale, reinterpret_cast<half_t*>(out), ldo};
   hgnn_status st = HGNN_OK;
   with_lanes(F, [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
     auto go = [&]() -> hgnn_status {
-      HGNN_REQUIRE(n <= int64_t(0x7fffffff) * kBlock / L, HGNN_EUNSUPPORTED, "%s: grid too large", who);
-      const dim3 grid{unsigned(ceil_div(n * L, kBlock))};
+      const bool many = n * L >= kFewLookups;
+      const int64_t blocks = ceil_div(n, int64_t(kBlock / L) * (many ? kLookups : 1));
+      HGNN_REQUIRE(blocks <= 0x7fffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
+      const dim3 grid{unsigned(blocks)};
       hipStream_t s = static_cast<hipStream_t>(stream);
-      if (table_type == HGNN_F16) embedding_kernel<half_t, L><<<grid, kBlock, 0, s>>>(a);
-      else embedding_kernel<float, L><<<grid, kBlock, 0, s>>>(a);
+      if (table_type == HGNN_F16 && many) embedding_kernel<half_t, L, kLookups><<<grid, kBlock, 0, s>>>(a);
+      else if (table_type == HGNN_F16) embedding_kernel<half_t, L, 1><<<grid, kBlock, 0, s>>>(a);
+      else if (many) embedding_kernel<float, L, kLookups><<<grid, kBlock, 0, s>>>(a);
+      else embedding_kernel<float, L, 1><<<grid, kBlock, 0, s>>>(a);
       HGNN_LAUNCH_CHECK("embedding_kernel");
       return HGNN_OK;
     };
@@ -405,7 +425,13 @@ hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_
   TableGradArgs a{};
   a.n = n, a.blocks = w.blocks, a.F = F, a.V = V;
   a.pos_bits = bits_of(n);
-  a.dY = reinterpret_cast<const half_t*>(dY), a.ldy = ldy, a.scale = scale;
+
+  // Rows of whole 128-byte lines are written past the caches: they are not read again before the caches have lost them.  us, through the caches / zeros past them / all rows past
+  // them, 64 M elements of gradients into 200 M (rows of 8 features 1 M into 3 M): rows of 128 bytes (32 x fp32) 191 / 182 / 183, 256 (64 x fp32) 265 / 236 / 229, 512 233 / 227 / 215,
+  // 512 (256 x fp16) 162 / 153 / 143; but parts of lines cost more, rows of 32 bytes 127 / 136 / 198, of 168 bytes 312 / 343 / 371.
+  const size_t row_bytes = size_t(F) * (grad_type == HGNN_F16 ? 2 : 4), pitch_bytes = size_t(lddt) * (grad_type == HGNN_F16 ? 2 : 4);
+  a.past = row_bytes % 128 == 0 && pitch_bytes % 128 == 0 && (reinterpret_cast<uintptr_t>(dT) & 127u) == 0 ? (row_bytes >= 256 ? kPastAll : kPastZeros) : 0;
+  a.dY = reinterpret_cast<const half_t*>(dY), a.ldy = ldy, a.inside = extent_of(n, F, ldy), a.scale = scale;
   a.dT = dT, a.lddt = lddt, a.part = w.part, a.pitch = w.pitch;
   if (n > 0) {
     a.words = sort_words(IdWords{ids, V, a.pos_bits}, n, a.pos_bits, a.pos_bits + bits_of(int64_t(V) + 1), w.buf0, w.buf1, w.scratch, s);
