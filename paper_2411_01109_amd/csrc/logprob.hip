@@ -3,62 +3,149 @@
 // lose the small differences of large scores to its rounding.
 #include <math.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "common.h"
 #include "rows.h"
 
 namespace hgnn {
 
 constexpr float kLow = -INFINITY;
-constexpr int kMostTop = 32;   // alternatives at most: a lane of a wave each
+constexpr int kMostTop = 32;     // alternatives at most: a lane of a wave each
 constexpr int kMostSplits = 64;  // workgroups of a row at most: a lane of a wave each
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// What a set of classes holds: the maximum, sum of exp(x - max), sum of exp(x - max) (x - max).  An empty one, or one of -inf alone, is (kNone, 0, 0): a maximum that is
-// finite takes no part in inf - inf.
-constexpr float kNone = -3.4028235e38f;
+// What a set of classes holds: the maximum m, s = sum 2^y and t = sum 2^y y, y = (x - m) log2(e).  An empty one, or one of -inf alone, has s = 0 and a maximum below all
+// others, which is finite, so that it takes no part in inf - inf.
+// fp16: y = fma(x, log2(e), -c) in one instruction, with the conversion; c, the rounded m log2(e), is the same for all classes, so its error goes in and out with it (shift_of).
+// fp32, whose products with log2(e) may overflow: a difference and a product.
+template <class T>
 struct Mass {
-  float m = kNone, s = 0.f, t = 0.f;
+  static constexpr bool kHalf = sizeof(T) == 2;
+  static constexpr float kNone = kHalf ? -1e5f : -3.4028235e38f;
+  float m, s, t;
+  static __device__ __forceinline__ Mass none() { return Mass{kNone, 0.f, 0.f}; }
+  static __device__ __forceinline__ float offset(float m) {
+#pragma clang fp contract(off)  // rounded here, whatever it is added to: it has to be the same everywhere
+    return kHalf ? m * kLog2e : m;
+  }
+  static __device__ __forceinline__ float y(float x, float offset) { return kHalf ? fmaf(x, kLog2e, -offset) : (x - offset) * kLog2e; }
+  // from the maximum m to the maximum to, in y
+  static __device__ __forceinline__ float step(float m, float to) { return kHalf ? offset(m) - offset(to) : (m - to) * kLog2e; }
+  // what y lacks of (x - m) log2(e)
+  static __device__ __forceinline__ float shift(float m) { return kHalf ? -fmaf(m, kLog2e, -offset(m)) : 0.f; }
 };
+__device__ __forceinline__ float exp2_of(float y) { return __builtin_amdgcn_exp2f(y); }
+// (-inf comes with a factor of zero, whose product would be no number)
+__device__ __forceinline__ float bounded(float y) { return fmaxf(y, -1e4f); }
 
-__device__ __forceinline__ Mass joined(const Mass& a, const Mass& b) {
-  Mass r;
+template <class T>
+__device__ __forceinline__ Mass<T> joined(const Mass<T>& a, const Mass<T>& b) {
+  Mass<T> r;
   r.m = fmaxf(a.m, b.m);
-  const float da = a.m - r.m, db = b.m - r.m, fa = __expf(da), fb = __expf(db);
+  const float da = Mass<T>::step(a.m, r.m), db = Mass<T>::step(b.m, r.m), fa = exp2_of(da), fb = exp2_of(db);
   r.s = fa * a.s + fb * b.s;
-  // (a difference beyond the range comes with a factor of zero, whose product would be no number)
-  r.t = fa * (a.t + fmaxf(da, -1e4f) * a.s) + fb * (b.t + fmaxf(db, -1e4f) * b.s);
+  r.t = fa * (a.t + bounded(da) * a.s) + fb * (b.t + bounded(db) * b.s);
   return r;
 }
 
-__device__ __forceinline__ float piece_max(const Piece& x) {
-  return fmaxf(fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3])), fmaxf(fmaxf(x.v[4], x.v[5]), fmaxf(x.v[6], x.v[7])));
+// ---- over L lanes, L a power of two: pairs of lanes by data-parallel primitives (common.h), beyond a row of 16 by swaps
+enum class Over { kSum, kMax, kMin };
+template <Over OP>
+__device__ __forceinline__ float both(float a, float b) {
+  return OP == Over::kSum ? a + b : fmaxf(a, b);
+}
+template <Over OP>
+__device__ __forceinline__ int both(int a, int b) {
+  return OP == Over::kSum ? a + b : (OP == Over::kMax ? max(a, b) : min(a, b));
+}
+template <int CTRL, class V>
+__device__ __forceinline__ V paired(V v) {
+  int w;
+  __builtin_memcpy(&w, &v, 4);
+  w = __builtin_amdgcn_update_dpp(0, w, CTRL, 0xf, 0xf, false);
+  __builtin_memcpy(&v, &w, 4);
+  return v;
+}
+template <int L, Over OP, class V>
+__device__ __forceinline__ V lanes_all(V v) {
+  if (L >= 2) v = both<OP>(v, paired<0xB1>(v));
+  if (L >= 4) v = both<OP>(v, paired<0x4E>(v));
+  if (L >= 8) v = both<OP>(v, paired<0x141>(v));
+  if (L >= 16) v = both<OP>(v, paired<0x140>(v));
+  typedef unsigned uint2_t __attribute__((ext_vector_type(2)));
+  auto halves = [](uint2_t r) {
+    V a, b;
+    const unsigned p = r[0], q = r[1];
+    __builtin_memcpy(&a, &p, 4);
+    __builtin_memcpy(&b, &q, 4);
+    return both<OP>(a, b);
+  };
+  unsigned w;
+  if (L >= 32) {
+    __builtin_memcpy(&w, &v, 4);
+    v = halves(__builtin_amdgcn_permlane16_swap(w, w, false, false));
+  }
+  if (L >= 64) {
+    __builtin_memcpy(&w, &v, 4);
+    v = halves(__builtin_amdgcn_permlane32_swap(w, w, false, false));
+  }
+  return v;
+}
+template <int L, class T>
+__device__ __forceinline__ Mass<T> lanes_mass(const Mass<T>& a) {
+  Mass<T> r;
+  r.m = lanes_all<L, Over::kMax>(a.m);
+  const float d = Mass<T>::step(a.m, r.m), f = exp2_of(d);
+  r.s = lanes_all<L, Over::kSum>(f * a.s);
+  r.t = lanes_all<L, Over::kSum>(f * (a.t + bounded(d) * a.s));
+  return r;
+}
+
+template <class T>
+__device__ __forceinline__ float piece_max(const RawPiece<T>& x) {
+  if constexpr (sizeof(T) == 2) {
+    const half4_t a = __builtin_elementwise_max(half4_t{x.v[0], x.v[1], x.v[2], x.v[3]}, half4_t{x.v[4], x.v[5], x.v[6], x.v[7]});
+    const half2_t b = __builtin_elementwise_max(half2_t{a[0], a[1]}, half2_t{a[2], a[3]});
+    return fmaxf(float(b[0]), float(b[1]));
+  } else {
+    return fmaxf(fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3])), fmaxf(fmaxf(x.v[4], x.v[5]), fmaxf(x.v[6], x.v[7])));
+  }
+}
+// a row's piece at class c; -inf behind the row's end
+template <class T>
+__device__ __forceinline__ RawPiece<T> load_classes(const T* row, int c, int C, int64_t inside) {
+  RawPiece<T> r;
+  r.v = T(kLow);
+  if (c >= C) return r;
+  const RawPiece<T> x = load_raw(row + c, C - c, inside - c);
+  if (c + 8 <= C) return x;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r.v[j] = c + j < C ? x.v[j] : T(kLow);
+  return r;
 }
 
 // adds pieces to a lane's mass; a class that is masked by -inf adds nothing
-template <int N>
-__device__ __forceinline__ void add_pieces(Mass& a, const Piece (&x)[N], const float (&top)[N]) {
+template <bool ENTROPY, class T, int N>
+__device__ __forceinline__ void add_pieces(Mass<T>& a, const RawPiece<T> (&x)[N], const float (&top)[N]) {
   float m = a.m;
 #pragma unroll
   for (int i = 0; i < N; ++i) m = fmaxf(m, top[i]);
+  const float offset = Mass<T>::offset(m);
   float s = 0.f, t = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float d = x[i].v[j] - m, e = __expf(d);
+      const float y = Mass<T>::y(float(x[i].v[j]), offset), e = exp2_of(y);
       s += e;
-      t = fmaf(e, fmaxf(d, -1e4f), t);
+      if (ENTROPY) t = fmaf(e, bounded(y), t);
     }
-  const float d = a.m - m, f = __expf(d);
-  a.t = fmaf(f, a.t + fmaxf(d, -1e4f) * a.s, t);
+  const float d = Mass<T>::step(a.m, m), f = exp2_of(d);
+  if (ENTROPY) a.t = fmaf(f, a.t + bounded(d) * a.s, t);
   a.s = fmaf(f, a.s, s);
   a.m = m;
-}
-
-template <int L>
-__device__ __forceinline__ Mass lanes_mass(Mass a) {
-#pragma unroll
-  for (int d = 1; d < L; d <<= 1) a = joined(a, Mass{__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
-  return a;
 }
 
 // What is kept of a row: its maximum and the logarithm of the sum.  A row of -inf alone is (-inf, 0); one with +inf or NaN is no number.
@@ -66,47 +153,59 @@ struct RowStats {
   float m, l;
   __device__ __forceinline__ float log_p(float x) const { return m == kLow ? kLow : (x - m) - l; }
 };
-__device__ __forceinline__ RowStats stats_of(const Mass& a) {
+template <class T>
+__device__ __forceinline__ RowStats stats_of(const Mass<T>& a) {
   if (a.s == 0.f) return RowStats{kLow, 0.f};
   if (!(a.s > 0.f)) return RowStats{NAN, NAN};
-  return RowStats{a.m, logf(a.s)};
+  return RowStats{a.m, fmaf(Mass<T>::shift(a.m), kLn2, logf(a.s))};
 }
-__device__ __forceinline__ float entropy_of(const Mass& a) { return a.s == 0.f ? 0.f : logf(a.s) - a.t / a.s; }
+template <class T>
+__device__ __forceinline__ float entropy_of(const Mass<T>& a) {
+  return a.s == 0.f ? 0.f : logf(a.s) - kLn2 * (a.t / a.s);
+}
 
 // ---- the best k of a wave: lane j holds the j-th best (x > -inf), falling, classes rising among equals
 struct Best {
   float v = kLow;
   int c = -1;
 };
-
-// Takes those of a wave's classes c0 + 8 lane + j (j < 8, scores x, -inf where there is none) that are among the best k.  They are taken in falling order, so no more than
-// k are, and a wave comes by its classes in rising order, so among equals the first one stays ahead.
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+__device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+// v, c into the list of a wave
+__device__ __forceinline__ void insert(Best& best, float v, int c) {
+  const int lane = threadIdx.x & (kWave - 1), rank = __popcll(__ballot(best.v >= v));
+  const float pv = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(best.v), 0x138, 0xf, 0xf, false));  // of the lane before: wave_shr:1
+  const int pc = __builtin_amdgcn_update_dpp(0, best.c, 0x138, 0xf, 0xf, false);
+  if (lane > rank) best.v = pv, best.c = pc;
+  if (lane == rank) best.v = v, best.c = c;
 }
-__device__ __forceinline__ void take_best(Best& best, float& least, int k, Piece& x, float top, int c0) {
+
+// Takes those of a wave's classes c0 + 512 i + 8 lane + j (i < N, j < 8, scores x, -inf where there is none) that are among the best k.  They are taken in falling order,
+// equal ones by their class, so no more than k are; a wave comes by its classes in rising order, so among equals the first one stays ahead.
+template <class T, int N>
+__device__ __forceinline__ void take_best(Best& best, float& least, int k, RawPiece<T> (&x)[N], float (&top)[N], int c0) {
   const int lane = threadIdx.x & (kWave - 1);
-  while (__ballot(top > least)) {
-    const float v = wave_max(top);
-    const int from = __builtin_ctzll(__ballot(top == v));
-    int j = 0;
+  for (;;) {
+    float t = top[0];
 #pragma unroll
-    for (int i = 7; i >= 0; --i) j = x.v[i] == v ? i : j;
-    const int c = __shfl(c0 + 8 * lane + j, from);
-    if (lane == from) {
+    for (int i = 1; i < N; ++i) t = fmaxf(t, top[i]);
+    if (!__ballot(t > least)) return;
+    const float v = lanes_all<kWave, Over::kMax>(t);
+    bool out = false;  // the same on all lanes
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i == j) x.v[i] = kLow;
-      top = piece_max(x);
+    for (int i = 0; i < N; ++i) {
+      const uint64_t there = out ? 0 : __ballot(top[i] == v);
+      if (!there) continue;
+      out = true;
+      const int from = __builtin_ctzll(there);
+      int j = 8;
+#pragma unroll
+      for (int q = 7; q >= 0; --q) j = float(x[i].v[q]) == v ? q : j;
+      insert(best, v, c0 + 8 * kWave * i + 8 * from + __builtin_amdgcn_readlane(j, from));
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[i].v[q] = lane == from && q == j ? T(kLow) : x[i].v[q];
+      top[i] = piece_max(x[i]);
     }
-    const int rank = __popcll(__ballot(best.v >= v));
-    const float pv = __shfl_up(best.v, 1);
-    const int pc = __shfl_up(best.c, 1);
-    if (lane > rank) best.v = pv, best.c = pc;
-    if (lane == rank) best.v = v, best.c = c;
-    least = __shfl(best.v, k - 1);
+    least = lane_value(best.v, k - 1);
   }
 }
 
@@ -114,35 +213,34 @@ struct ScoreArgs {
   int64_t n;
   int C, k;
   const void* logits;
-  int64_t ld;
+  int64_t ld, inside;  // inside: elements from the first of the logits to the last
   const int* labels;
   float *logprob, *stats, *entropy, *top;
   int* top_class;
   // several workgroups to a row: what each of them has found
   int splits;
-  int64_t span;      // classes of a wave
+  int span;          // classes of a part
   float* part;       // [n][splits][3]
   float* part_top;   // [n][splits][k]
   int* part_class;
 };
 
-// The outputs of a row but for the alternatives, by one lane.
+// The outputs of a row but for the alternatives, by one lane; at: the score of its label.
 template <class T>
-__device__ __forceinline__ void store_row(const ScoreArgs& a, int64_t row, const Mass& mass) {
+__device__ __forceinline__ void store_row(const ScoreArgs& a, int64_t row, const Mass<T>& mass, int y, float at) {
   const RowStats st = stats_of(mass);
   if (a.stats) a.stats[2 * row] = st.m, a.stats[2 * row + 1] = st.l;
   if (a.entropy) a.entropy[row] = entropy_of(mass);
-  if (a.logprob) {
-    const int y = a.labels[row];
-    float v = 0.f;
-    if (uint32_t(y) < uint32_t(a.C)) v = st.log_p(float(static_cast<const T*>(a.logits)[row * a.ld + y]));
-    a.logprob[row] = v;
-  }
+  if (a.logprob) a.logprob[row] = uint32_t(y) < uint32_t(a.C) ? st.log_p(at) : 0.f;
+}
+template <class T>
+__device__ __forceinline__ float score_at(const ScoreArgs& a, int64_t row, int y) {
+  return uint32_t(y) < uint32_t(a.C) ? float(static_cast<const T*>(a.logits)[row * a.ld + y]) : 0.f;
 }
 
 // The alternatives of a row, by a wave.  Where fewer than k scores are above -inf, the first of the other classes fill up.
 template <class T>
-__device__ __forceinline__ void store_best(const ScoreArgs& a, int64_t row, const Mass& mass, Best best) {
+__device__ __forceinline__ void store_best(const ScoreArgs& a, int64_t row, const Mass<T>& mass, const Best& best) {
   const int lane = threadIdx.x & (kWave - 1);
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   int held = __popcll(__ballot(lane < a.k && best.c >= 0));
@@ -162,7 +260,7 @@ __device__ __forceinline__ void store_best(const ScoreArgs& a, int64_t row, cons
   }
 }
 
-// lists of falling scores, one for each lane (p: its next entry, n entries in all, class -1: an empty one), become one; among equals a lower lane's come first
+// lists of falling scores, one for each lane (n entries, class -1: an empty one), become one; among equals the lowest class comes first
 template <class Entry>
 __device__ __forceinline__ Best merge_lists(int k, int n, Entry&& entry) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -170,12 +268,14 @@ __device__ __forceinline__ Best merge_lists(int k, int n, Entry&& entry) {
   int p = 0;
   if (n > 0) mine = entry(0);
   for (int r = 0; r < k; ++r) {
-    const float v = wave_max(mine.c >= 0 ? mine.v : kLow);
+    const float v = lanes_all<kWave, Over::kMax>(mine.v);
     const uint64_t have = __ballot(mine.c >= 0 && mine.v == v);
     if (!have) break;
-    const int from = __builtin_ctzll(have), c = __shfl(mine.c, from);
+    int c;
+    if (have & (have - 1)) c = lanes_all<kWave, Over::kMin>(mine.c >= 0 && mine.v == v ? mine.c : 0x7fffffff);
+    else c = __builtin_amdgcn_readlane(mine.c, __builtin_ctzll(have));
     if (lane == r) out.v = v, out.c = c;
-    if (lane == from) {
+    if (mine.c == c) {
       ++p;
       mine = Best{};
       if (p < n) mine = entry(p);
@@ -184,106 +284,129 @@ __device__ __forceinline__ Best merge_lists(int k, int n, Entry&& entry) {
   return out;
 }
 
-// Rows of up to 512 classes: L lanes hold a row, a piece each.
-template <class T, int L>
+// Rows of up to 512 classes: L lanes hold a row, N pieces each.  What a row costs beside its classes (reductions, logarithm, stores) is a wave's for all of its 64 / L rows at once: 262 144 rows
+// of 512, 64 lanes with a piece / 16 with four, 78 / 51 us.
+template <class T, int L, int N, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(kBlock) void logprob_group_kernel(ScoreArgs a) {
-  const int64_t row = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / L;
+  const int64_t i = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / L, row = i < a.n ? i : a.n - 1;
   const int l = threadIdx.x % L;
-  const bool real = row < a.n;
-  const T* const x = static_cast<const T*>(a.logits) + (real ? row : a.n - 1) * a.ld;
-  Piece p[1];
+  const bool writes = i < a.n && l == 0;
+  const int y = a.labels ? a.labels[row] : -1;
+  RawPiece<T> p[N];
+  float top[N], m = Mass<T>::kNone, at = kLow;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) p[0].v[j] = kLow;
-  if (8 * l < a.C) p[0] = load_piece(x + 8 * l, a.C - 8 * l, kLow);
-  float top[1] = {piece_max(p[0])};
-  Mass mass;
-  add_pieces(mass, p, top);
-  mass = lanes_mass<L>(mass);
-  if (real && l == 0) store_row<T>(a, row, mass);
+  for (int q = 0; q < N; ++q) p[q] = load_classes(static_cast<const T*>(a.logits) + row * a.ld, 8 * (q * L + l), a.C, a.inside - row * a.ld);
+#pragma unroll
+  for (int q = 0; q < N; ++q) {
+    top[q] = piece_max(p[q]);
+    m = fmaxf(m, top[q]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) at = y == 8 * (q * L + l) + j ? float(p[q].v[j]) : at;
+  }
+  Mass<T> mass{lanes_all<L, Over::kMax>(m), 0.f, 0.f};
+  at = lanes_all<L, Over::kMax>(at);
+  add_pieces<ENTROPY>(mass, p, top);
+  mass.s = lanes_all<L, Over::kSum>(mass.s);
+  if (ENTROPY) mass.t = lanes_all<L, Over::kSum>(mass.t);
+  if (writes) store_row(a, row, mass, y, at);
+  if (!TOP) return;
   const RowStats st = stats_of(mass);
+  static_assert(!TOP || N == 1, "a piece each");
   float t = top[0];
   // of equal scores the lowest class; those that are not above -inf, in their order, once the others are out
   uint32_t left = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) left |= uint32_t(8 * l + j < a.C) << j;
-  for (int r = 0; r < a.k; ++r) {
-    float v = t;
-#pragma unroll
-    for (int d = 1; d < L; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
+  for (int k = 0; k < a.k; ++k) {
+    const float v = lanes_all<L, Over::kMax>(t);
     const bool fill = !(v > kLow);
     int c = 0x7fffffff;
 #pragma unroll
     for (int j = 7; j >= 0; --j)
-      if ((left >> j & 1) && (fill ? !(p[0].v[j] > kLow) : p[0].v[j] == v)) c = 8 * l + j;
-#pragma unroll
-    for (int d = 1; d < L; d <<= 1) c = min(c, __shfl_xor(c, d));
+      if ((left >> j & 1) && (fill ? !(float(p[0].v[j]) > kLow) : float(p[0].v[j]) == v)) c = 8 * l + j;
+    c = lanes_all<L, Over::kMin>(c);
     if (c / 8 == l) {
       left &= ~(1u << (c % 8));
       t = kLow;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (left >> j & 1) t = fmaxf(t, p[0].v[j]);
+        if (left >> j & 1) t = fmaxf(t, float(p[0].v[j]));
     }
-    if (real && l == 0) {
-      a.top[row * a.k + r] = mass.s == mass.s ? st.log_p(v) : NAN;
-      a.top_class[row * a.k + r] = c;
+    if (writes) {
+      a.top[row * a.k + k] = mass.s == mass.s ? st.log_p(v) : NAN;
+      a.top_class[row * a.k + k] = c;
     }
   }
 }
 
-// A workgroup to a row, or to one of `splits` parts of it; every wave takes a stretch of classes, so that what it finds has a place among the others'.
-constexpr int kPieces = 4;  // of a lane in flight
+// Longer rows: W waves take one, or one of its `splits` parts, W = 4 a workgroup, W = 1 a wave by itself.  The waves take 4 KB in turn, the next ones on their way.
 template <class T>
+constexpr int kPieces = sizeof(T) == 2 ? 4 : 2;  // 64 bytes
+template <class T>
+constexpr int kStep = 8 * kWave * kPieces<T>;  // classes that a wave takes at a time
+template <class T, int W, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(kBlock) void logprob_row_kernel(ScoreArgs a) {
-  __shared__ float s_mass[kWavesPerBlock][3], s_top[kWavesPerBlock][kMostTop];
-  __shared__ int s_class[kWavesPerBlock][kMostTop];
+  constexpr int N = kPieces<T>;
+  __shared__ float s_mass[kWavesPerBlock][3], s_top[TOP ? kWavesPerBlock : 1][kMostTop];
+  __shared__ int s_class[TOP ? kWavesPerBlock : 1][kMostTop];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int64_t row = blockIdx.x / a.splits;
-  const int split = blockIdx.x % a.splits;
+  const int64_t unit = W == 1 ? int64_t(blockIdx.x) * kWavesPerBlock + wave : int64_t(blockIdx.x);
+  if (W == 1 && unit >= a.n) return;
+  const int64_t row = W == 1 ? unit : int64_t(blockIdx.x / unsigned(a.splits));
+  const int split = W == 1 ? 0 : int(blockIdx.x % unsigned(a.splits));
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
-  const int64_t first = (int64_t(split) * kWavesPerBlock + wave) * a.span;
-  const int c0 = int(first < a.C ? first : a.C), c1 = int(first + a.span < a.C ? first + a.span : a.C);
-  Mass mass;
+  const int64_t inside = a.inside - row * a.ld, first = W == 1 ? 0 : int64_t(split) * a.span;
+  const int c1 = int(first + a.span < a.C ? first + a.span : a.C), c0 = int(first < a.C ? first : a.C) + (W == 1 ? 0 : wave * kStep<T>);
+  const int y = a.labels ? a.labels[row] : -1;
+  Mass<T> mass = Mass<T>::none();
   Best best;
   float least = kLow;
-  for (int c = c0; c < c1; c += 8 * kWave * kPieces) {
-    Piece p[kPieces];
-    float top[kPieces];
+  RawPiece<T> next[N];
+  auto fetch = [&](int c) __attribute__((always_inline)) {
+    if (c + kStep<T> <= c1) {
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int at = c + 8 * (i * kWave + lane);
+      for (int i = 0; i < N; ++i) next[i] = load_raw(x + c + 8 * (i * kWave + lane));
+    } else if (c < c1) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) p[i].v[j] = kLow;
-      if (at < c1) p[i] = load_piece(x + at, c1 - at, kLow);
+      for (int i = 0; i < N; ++i) next[i] = load_classes(x, c + 8 * (i * kWave + lane), c1, inside);
     }
+  };
+  fetch(c0);
+  for (int c = c0; c < c1; c += W * kStep<T>) {
+    RawPiece<T> p[N];
+    float top[N];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) top[i] = piece_max(p[i]);
-    add_pieces(mass, p, top);
-    if (a.k > 0)
+    for (int i = 0; i < N; ++i) p[i] = next[i];
+    fetch(c + W * kStep<T>);
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) take_best(best, least, a.k, p[i], top[i], c + 8 * i * kWave);
+    for (int i = 0; i < N; ++i) top[i] = piece_max(p[i]);
+    add_pieces<ENTROPY>(mass, p, top);
+    if (TOP) take_best(best, least, a.k, p, top, c);
   }
   mass = lanes_mass<kWave>(mass);
-  if (lane == 0) s_mass[wave][0] = mass.m, s_mass[wave][1] = mass.s, s_mass[wave][2] = mass.t;
-  if (lane < a.k) s_top[wave][lane] = best.v, s_class[wave][lane] = best.c;
-  __syncthreads();
-  if (wave > 0) return;
-  mass = Mass{s_mass[0][0], s_mass[0][1], s_mass[0][2]};
-  for (int w = 1; w < kWavesPerBlock; ++w) mass = joined(mass, Mass{s_mass[w][0], s_mass[w][1], s_mass[w][2]});
-  if (a.k > 0) best = merge_lists(a.k, lane < kWavesPerBlock ? a.k : 0, [&](int p) { return Best{s_top[lane][p], s_class[lane][p]}; });
-  if (a.splits == 1) {
-    if (lane == 0) store_row<T>(a, row, mass);
-    if (a.k > 0) store_best<T>(a, row, mass, best);
-    return;
+  if (W > 1) {
+    if (lane == 0) s_mass[wave][0] = mass.m, s_mass[wave][1] = mass.s, s_mass[wave][2] = mass.t;
+    if (TOP && lane < a.k) s_top[wave][lane] = best.v, s_class[wave][lane] = best.c;
+    __syncthreads();
+    if (wave > 0) return;
+    mass = Mass<T>::none();
+    if (lane < W) mass = Mass<T>{s_mass[lane][0], s_mass[lane][1], s_mass[lane][2]};
+    mass = lanes_mass<kWave>(mass);
+    if (TOP) best = merge_lists(a.k, lane < W ? a.k : 0, [&](int p) { return Best{s_top[lane][p], s_class[lane][p]}; });
+    if (a.splits > 1) {
+      if (lane == 0) {
+        float* const q = a.part + 3 * (row * a.splits + split);
+        q[0] = mass.m, q[1] = mass.s, q[2] = mass.t;
+      }
+      if (TOP && lane < a.k) {
+        a.part_top[(row * a.splits + split) * a.k + lane] = best.v;
+        a.part_class[(row * a.splits + split) * a.k + lane] = best.c;
+      }
+      return;
+    }
   }
-  if (lane == 0) {
-    float* const q = a.part + 3 * (row * a.splits + split);
-    q[0] = mass.m, q[1] = mass.s, q[2] = mass.t;
-  }
-  if (lane < a.k) {
-    a.part_top[(row * a.splits + split) * a.k + lane] = best.v;
-    a.part_class[(row * a.splits + split) * a.k + lane] = best.c;
-  }
+  if (lane == 0) store_row(a, row, mass, y, score_at<T>(a, row, y));
+  if (TOP) store_best(a, row, mass, best);
 }
 
 // the parts of a row, by a wave
@@ -291,17 +414,19 @@ template <class T>
 __global__ __launch_bounds__(kWave) void logprob_join_kernel(ScoreArgs a) {
   const int lane = threadIdx.x;
   const int64_t row = blockIdx.x;
-  Mass mass;
+  const int y = a.labels ? a.labels[row] : -1;
+  const float score = score_at<T>(a, row, y);
+  Mass<T> mass = Mass<T>::none();
   if (lane < a.splits) {
     const float* const q = a.part + 3 * (row * a.splits + lane);
-    mass = Mass{q[0], q[1], q[2]};
+    mass = Mass<T>{q[0], q[1], q[2]};
   }
   mass = lanes_mass<kWave>(mass);
-  if (lane == 0) store_row<T>(a, row, mass);
+  if (lane == 0) store_row(a, row, mass, y, score);
   if (a.k == 0) return;
   const int64_t at = (row * a.splits + lane) * a.k;
   const Best best = merge_lists(a.k, lane < a.splits ? a.k : 0, [&](int p) { return Best{a.part_top[at + p], a.part_class[at + p]}; });
-  store_best<T>(a, row, mass, best);
+  store_best(a, row, mass, best);
 }
 
 // ---- the gradient: dx_c = g (1[c = y] - p_c) - h p_c (log p_c + entropy), p_c = exp((x_c - m) - L)
@@ -309,81 +434,120 @@ struct ScoreGradArgs {
   int64_t n;
   int C, chunks;
   const void* logits;
-  int64_t ld;
+  int64_t ld, inside;
   const int* labels;
   const float *stats, *dlogprob, *entropy, *dentropy;
   void* dlogits;
   int64_t ldd;
 };
 
-// L lanes take a row, or 64 of them one of its chunks, a piece or kPieces each.  A lane reads what it overwrites: the logits may be the output.
-template <class T, int L, int N>
+// L lanes take a row (or its only chunk, ONE), or 64 of them one of its chunks, N pieces each.  A lane reads what it overwrites: the logits may be the output.  With e = 2^y (Mass) p is e times
+// a factor of the row, and a class's gradient e times a line in y.
+template <class T, int L, int N, bool ENTROPY, bool ONE>
 __global__ __launch_bounds__(kBlock) void logprob_grad_kernel(ScoreGradArgs a) {
   const int64_t unit = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / L;
-  const int64_t row = N == 1 ? unit : unit / a.chunks;
+  const int64_t row = ONE ? unit : int64_t(uint32_t(unit) / uint32_t(a.chunks));
   if (row >= a.n) return;
-  const int l = threadIdx.x % L, c0 = N == 1 ? 0 : int(unit % a.chunks) * (8 * L * N);
+  const int l = threadIdx.x % L, c0 = ONE ? 0 : int(uint32_t(unit) - uint32_t(row) * uint32_t(a.chunks)) * (8 * L * N);
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   T* const dx = static_cast<T*>(a.dlogits) + row * a.ldd;
-  Piece p[N];
+  const int64_t inside = a.inside - row * a.ld;
+  RawPiece<T> p[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int at = c0 + 8 * (i * L + l);
-    if (at < a.C) p[i] = load_piece(x + at, a.C - at, kLow);
-  }
+  for (int i = 0; i < N; ++i) p[i] = load_classes(x, c0 + 8 * (i * L + l), a.C, inside);
   const int y = a.labels ? a.labels[row] : -1;
-  const bool real = uint32_t(y) < uint32_t(a.C);
-  const float m = a.stats[2 * row], s = a.stats[2 * row + 1], g = real ? a.dlogprob[row] : 0.f;
-  const float h = a.dentropy ? a.dentropy[row] : 0.f, e = a.dentropy ? a.entropy[row] : 0.f;
+  const float m = a.stats[2 * row], ls = a.stats[2 * row + 1];
   const bool none = m == kLow;  // a row of -inf alone
+  const float g = uint32_t(y) < uint32_t(a.C) && !none ? a.dlogprob[row] : 0.f;
+  const float offset = none ? 0.f : Mass<T>::offset(m), shift = none ? 0.f : kLn2 * Mass<T>::shift(m);
+  const float r = none ? 0.f : expf(shift - ls);  // p = r e, log p = ln2 y + shift - ls
+  float slope = 0.f, at0 = -g * r;
+  if (ENTROPY) {
+    const float h = a.dentropy[row] * r;
+    slope = -h * kLn2;
+    at0 -= h * (a.entropy[row] + shift - ls);
+  }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int at = c0 + 8 * (i * L + l);
     if (at >= a.C) continue;
+    Piece out;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float lp = none ? kLow : (p[i].v[j] - m) - s, q = __expf(lp);
-      float v = g * ((at + j == y && !none ? 1.f : 0.f) - q);
-      v -= h * (q * (fmaxf(lp, -1e4f) + e));
-      p[i].v[j] = v;
+      const float z = Mass<T>::y(float(p[i].v[j]), offset), e = exp2_of(z), v = e * (ENTROPY ? fmaf(bounded(z), slope, at0) : at0);
+      out.v[j] = at + j == y ? v + g : v;
     }
-    store_piece(dx + at, a.C - at, p[i]);
+    store_piece(dx + at, a.C - at, out);
   }
 }
 
 constexpr int kGroupClasses = 8 * kWave;  // most classes that the lanes of a wave hold at once
-// Workgroups of a row: as many as fill the chip, of no less than a piece chunk for every wave
+static int group_lanes(int C, int pieces) { return std::min(kWave, pow2_at_least(int(ceil_div(C, 8 * pieces)))); }
+// Pieces of a lane, more than one where rows fill the chip all the same.  us, 1 / 2 / 4: 233 000 rows of 41 (fp16) 10.2 / 8.4 / 8.8, their gradient 11.5 / 11.2 / 13.3; 262 144 of 512 78 / 57 / 51,
+// gradient 97 / 94 / 94; 100 000 of 200 18 / 12.8 / 13.6; fp32, 100 000 of 512 - / 34.8 / 36.8, gradient - / 77.7 / 81.9.
+static int row_pieces(int64_t n, int C, bool wide) {
+  if (C <= 8 || C > kGroupClasses || n * group_lanes(C, 1) < int64_t(1) << 20) return 1;
+  return wide && C > 256 ? 4 : 2;
+}
+template <class Call>
+static void with_pieces(int pieces, Call&& call) {
+  if (pieces == 1) call(std::integral_constant<int, 1>());
+  else if (pieces == 2) call(std::integral_constant<int, 2>());
+  else call(std::integral_constant<int, 4>());
+}
+constexpr int kWaveClasses = 4096;        // up to so many, a row is a wave's where there are rows enough
+static bool by_waves(int64_t n, int C) { return C <= kWaveClasses && n >= 4096; }
+// Workgroups of a row: as many as fill the chip, of no less than a piece for every lane
 static int splits_of(int64_t n, int C) {
-  const int64_t most = ceil_div(C, int64_t(8) * kWave * kPieces * kWavesPerBlock);
-  const int64_t want = ceil_div(1024, n);
-  int64_t s = most < want ? most : want;
+  if (C <= kGroupClasses || by_waves(n, C)) return 1;
+  const int64_t most = ceil_div(C, int64_t(8) * kWave * kWavesPerBlock), want = ceil_div(1024, n), s = most < want ? most : want;
   return int(s < 1 ? 1 : (s > kMostSplits ? kMostSplits : s));
 }
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
+template <class Call>
+static void with_flags(bool x, bool y, Call&& call) {
+  const std::true_type yes;
+  const std::false_type no;
+  if (x) y ? call(yes, yes) : call(yes, no);
+  else y ? call(no, yes) : call(no, no);
+}
+template <class Call>
+static void with_group(int lanes, Call&& call) {
+  switch (lanes) {
+    case 1: return call(std::integral_constant<int, 1>());
+    case 2: return call(std::integral_constant<int, 2>());
+    case 4: return call(std::integral_constant<int, 4>());
+    case 8: return call(std::integral_constant<int, 8>());
+    case 16: return call(std::integral_constant<int, 16>());
+    case 32: return call(std::integral_constant<int, 32>());
+    default: return call(std::integral_constant<int, 64>());
+  }
+}
+
 template <class T>
 static hgnn_status logprob(ScoreArgs& a, hipStream_t s) {
-  if (a.C <= kGroupClasses) {
-    const int L = pow2_at_least((a.C + 7) / 8);
-    const int64_t blocks = ceil_div(a.n * L, kBlock);
-    HGNN_REQUIRE(blocks <= 0x7fffffff, HGNN_EUNSUPPORTED, "hgnn_logprob: grid too large");
-    const dim3 grid{unsigned(blocks)};
-    switch (L) {
-      case 1: logprob_group_kernel<T, 1><<<grid, kBlock, 0, s>>>(a); break;
-      case 2: logprob_group_kernel<T, 2><<<grid, kBlock, 0, s>>>(a); break;
-      case 4: logprob_group_kernel<T, 4><<<grid, kBlock, 0, s>>>(a); break;
-      case 8: logprob_group_kernel<T, 8><<<grid, kBlock, 0, s>>>(a); break;
-      case 16: logprob_group_kernel<T, 16><<<grid, kBlock, 0, s>>>(a); break;
-      case 32: logprob_group_kernel<T, 32><<<grid, kBlock, 0, s>>>(a); break;
-      default: logprob_group_kernel<T, 64><<<grid, kBlock, 0, s>>>(a); break;
+  const char* who = "hgnn_logprob";
+  const bool group = a.C <= kGroupClasses, waves = by_waves(a.n, a.C);
+  const int N = a.k > 0 ? 1 : row_pieces(a.n, a.C, sizeof(T) == 2), L = group_lanes(a.C, N);
+  const int64_t blocks = group ? ceil_div(a.n * L, kBlock) : (waves ? ceil_div(a.n, kWavesPerBlock) : a.n * a.splits);
+  HGNN_REQUIRE(a.n <= (int64_t(1) << 40) && blocks <= 0x7fffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
+  const dim3 grid{unsigned(blocks)};
+  a.span = waves ? a.C : int(ceil_div(ceil_div(a.C, a.splits), 8) * 8);
+  with_flags(a.entropy != nullptr, a.k > 0, [&](auto entropy, auto top) {
+    constexpr bool E = decltype(entropy)::value, K = decltype(top)::value;
+    if (group) {
+      with_group(L, [&](auto width) {
+        constexpr int W = decltype(width)::value;
+        with_pieces(N, [&](auto pieces) { logprob_group_kernel<T, W, K ? 1 : decltype(pieces)::value, E, K><<<grid, kBlock, 0, s>>>(a); });
+      });
+    } else if (waves) {
+      logprob_row_kernel<T, 1, E, K><<<grid, kBlock, 0, s>>>(a);
+    } else {
+      logprob_row_kernel<T, kWavesPerBlock, E, K><<<grid, kBlock, 0, s>>>(a);
     }
-    HGNN_LAUNCH_CHECK("logprob_group_kernel");
-    return HGNN_OK;
-  }
-  HGNN_REQUIRE(a.n * a.splits <= 0x7fffffff, HGNN_EUNSUPPORTED, "hgnn_logprob: grid too large");
-  a.span = ceil_div(ceil_div(a.C, int64_t(a.splits) * kWavesPerBlock), 8) * 8;
-  logprob_row_kernel<T><<<dim3(unsigned(a.n * a.splits)), kBlock, 0, s>>>(a);
-  HGNN_LAUNCH_CHECK("logprob_row_kernel");
+  });
+  HGNN_LAUNCH_CHECK("logprob_group_kernel or logprob_row_kernel");
   if (a.splits > 1) {
     logprob_join_kernel<T><<<dim3(unsigned(a.n)), kWave, 0, s>>>(a);
     HGNN_LAUNCH_CHECK("logprob_join_kernel");
@@ -394,24 +558,17 @@ static hgnn_status logprob(ScoreArgs& a, hipStream_t s) {
 template <class T>
 static hgnn_status logprob_grad(ScoreGradArgs& a, hipStream_t s) {
   const bool group = a.C <= kGroupClasses;
-  const int L = group ? pow2_at_least((a.C + 7) / 8) : kWave;
-  a.chunks = group ? 1 : int(ceil_div(a.C, int64_t(8) * kWave * kPieces));
-  const int64_t blocks = ceil_div(a.n * a.chunks * L, kBlock);
-  HGNN_REQUIRE(blocks <= 0x7fffffff, HGNN_EUNSUPPORTED, "hgnn_logprob_grad: grid too large");
-  const dim3 grid{unsigned(blocks)};
-  if (!group) {
-    logprob_grad_kernel<T, kWave, kPieces><<<grid, kBlock, 0, s>>>(a);
-  } else {
-    switch (L) {
-      case 1: logprob_grad_kernel<T, 1, 1><<<grid, kBlock, 0, s>>>(a); break;
-      case 2: logprob_grad_kernel<T, 2, 1><<<grid, kBlock, 0, s>>>(a); break;
-      case 4: logprob_grad_kernel<T, 4, 1><<<grid, kBlock, 0, s>>>(a); break;
-      case 8: logprob_grad_kernel<T, 8, 1><<<grid, kBlock, 0, s>>>(a); break;
-      case 16: logprob_grad_kernel<T, 16, 1><<<grid, kBlock, 0, s>>>(a); break;
-      case 32: logprob_grad_kernel<T, 32, 1><<<grid, kBlock, 0, s>>>(a); break;
-      default: logprob_grad_kernel<T, 64, 1><<<grid, kBlock, 0, s>>>(a); break;
-    }
-  }
+  const int N = row_pieces(a.n, a.C, false), L = group ? group_lanes(a.C, N) : kWave;
+  a.chunks = group ? 1 : int(ceil_div(a.C, int64_t(8) * kWave * kPieces<T>));
+  HGNN_REQUIRE(a.n <= (int64_t(1) << 40) && ceil_div(a.n * a.chunks * L, kBlock) <= 0x7fffffff && (group || a.n * a.chunks <= 0xffffffff), HGNN_EUNSUPPORTED,
+               "hgnn_logprob_grad: grid too large");
+  const dim3 grid{unsigned(ceil_div(a.n * a.chunks * L, kBlock))};
+  with_flags(a.dentropy != nullptr, N == 2, [&](auto entropy, auto two) {
+    constexpr bool E = decltype(entropy)::value;
+    constexpr int P = decltype(two)::value ? 2 : 1;
+    if (!group) logprob_grad_kernel<T, kWave, kPieces<T>, E, false><<<grid, kBlock, 0, s>>>(a);
+    else with_group(L, [&](auto lanes) { logprob_grad_kernel<T, decltype(lanes)::value, P, E, true><<<grid, kBlock, 0, s>>>(a); });
+  });
   HGNN_LAUNCH_CHECK("logprob_grad_kernel");
   return HGNN_OK;
 }
@@ -468,7 +625,7 @@ hgnn_status hgnn_logprob(int64_t n, int32_t C, hgnn_type type, const void* logit
                    aligned_to_type(entropy, HGNN_F32) && aligned_to_type(top_logprob, HGNN_F32) && aligned_to_type(top_class, HGNN_F32) &&
                    (w.bytes == 0 || aligned_to_type(workspace, HGNN_F32)),
                HGNN_EINVAL, "%s: an array that is not aligned to its type", who);
-  ScoreArgs a{n, C, k, logits, ld, labels, logprob_out, stats, entropy, top_logprob, top_class, splits_of(n, C), 0, w.part, w.part_top, w.part_class};
+  ScoreArgs a{n, C, k, logits, ld, extent_of(n, C, ld), labels, logprob_out, stats, entropy, top_logprob, top_class, splits_of(n, C), 0, w.part, w.part_top, w.part_class};
   hipStream_t s = static_cast<hipStream_t>(stream);
   return type == HGNN_F16 ? logprob<half_t>(a, s) : logprob<float>(a, s);
 }
@@ -489,7 +646,7 @@ hgnn_status hgnn_logprob_grad(int64_t n, int32_t C, hgnn_type type, const void* 
   HGNN_REQUIRE(aligned_to_type(logits, type) && aligned_to_type(dlogits, type) && aligned_to_type(labels, HGNN_F32) && aligned_to_type(stats, HGNN_F32) &&
                    aligned_to_type(dlogprob, HGNN_F32) && aligned_to_type(entropy, HGNN_F32) && aligned_to_type(dentropy, HGNN_F32),
                HGNN_EINVAL, "%s: an array that is not aligned to its type", who);
-  ScoreGradArgs a{n, C, 1, logits, ld, labels, stats, dlogprob, entropy, dentropy, dlogits, ldd};
+  ScoreGradArgs a{n, C, 1, logits, ld, extent_of(n, C, ld), labels, stats, dlogprob, entropy, dentropy, dlogits, ldd};
   hipStream_t s = static_cast<hipStream_t>(stream);
   return type == HGNN_F16 ? logprob_grad<half_t>(a, s) : logprob_grad<float>(a, s);
 }
