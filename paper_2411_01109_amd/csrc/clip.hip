@@ -54,20 +54,6 @@ __device__ __forceinline__ const ClipTensor& tensor_of(const ClipArgs& a, int c)
 
 // The elements of chunk c of a tensor, row by row in pieces of V, several of a lane's fetched together: use(row, column, columns left, piece).  V: 16 bytes of the wider of what
 // is read and written, so that the lanes' 16 bytes lie beside each other.
-template <class I, int V>
-struct Part;
-template <class I>
-struct Part<I, 8> {
-  typename Vec<I>::eight v;
-  static __device__ __forceinline__ Part load(const I* p) { return Part{load_raw(p).v}; }
-  static __device__ __forceinline__ Part load(const I* p, int left) { return Part{load_raw(p, left, left).v}; }
-};
-template <class I>
-struct Part<I, 4> {
-  typename Vec<I>::four v;
-  static __device__ __forceinline__ Part load(const I* p) { return Part{*reinterpret_cast<const typename Vec<I>::four*>(p)}; }
-  static __device__ __forceinline__ Part load(const I* p, int left) { return Part{load_quad(p, left, left)}; }
-};
 template <class I, int V, class Use>
 __device__ __forceinline__ void walk_chunk(const ClipArgs& a, const ClipTensor& t, int c, Use&& use) {
   constexpr int kAhead = kClipAhead * 8 / V, kTurn = V * kBlock;
@@ -84,7 +70,7 @@ __device__ __forceinline__ void walk_chunk(const ClipArgs& a, const ClipTensor& 
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) use(0, p + i * kTurn, V, x[i]);
     }
-    for (; p < c1; p += kTurn) use(0, p, int(c1 - p), P::load(g + p, int(c1 - p)));
+    for (; p < c1; p += kTurn) use(0, p, int(c1 - p), P::load(g + p, int(c1 - p), c1 - p));
     return;
   }
   // a band of rows; rows that are longer than a chunk alone
@@ -94,7 +80,7 @@ __device__ __forceinline__ void walk_chunk(const ClipArgs& a, const ClipTensor& 
     const uint32_t r = nr == 1 ? 0 : q / per;
     const int64_t row = r0 + int(r), col = int64_t(V) * (q - r * per);
     const int left = int(t.cols - col < V ? t.cols - col : V);
-    use(row, col, left, P::load(g + row * t.ld() + col, left));
+    use(row, col, left, P::load(g + row * t.ld() + col, left, left));
   }
 }
 
@@ -153,8 +139,7 @@ __device__ __forceinline__ void clip_chunk(const ClipArgs& a, const ClipTensor& 
     float y[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) y[j] = factor == 0.f ? 0.f : float(x.v[j]) * factor;
-    if constexpr (V == 8) store_piece(o, left, Piece{{y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]}});
-    else store_quad<O, PAST>(o, left, float4_t{y[0], y[1], y[2], y[3]});
+    Part<O, V>::template store<PAST>(o, left, y);
   });
 }
 

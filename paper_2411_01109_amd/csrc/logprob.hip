@@ -441,20 +441,24 @@ struct ScoreGradArgs {
   int64_t ldd;
 };
 
-// L lanes take a row (or its only chunk, ONE), or 64 of them one of its chunks, N pieces each.  A lane reads what it overwrites: the logits may be the output.  With e = 2^y (Mass) p is e times
-// a factor of the row, and a class's gradient e times a line in y.
-template <class T, int L, int N, bool ENTROPY, bool ONE>
+// L lanes take a row (ONE), or 64 of them one of its chunks, N parts of V each.  A lane reads what it overwrites: the logits may be the output.  With e = 2^y (Mass) p is e times a
+// factor of the row, and a class's gradient e times a line in y.
+template <class T, int L, int N, int V, bool ENTROPY, bool ONE, bool PAST>
 __global__ __launch_bounds__(kBlock) void logprob_grad_kernel(ScoreGradArgs a) {
   const int64_t unit = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / L;
   const int64_t row = ONE ? unit : int64_t(uint32_t(unit) / uint32_t(a.chunks));
   if (row >= a.n) return;
-  const int l = threadIdx.x % L, c0 = ONE ? 0 : int(uint32_t(unit) - uint32_t(row) * uint32_t(a.chunks)) * (8 * L * N);
+  const int l = threadIdx.x % L, c0 = ONE ? 0 : int(uint32_t(unit) - uint32_t(row) * uint32_t(a.chunks)) * (V * L * N);
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   T* const dx = static_cast<T*>(a.dlogits) + row * a.ldd;
   const int64_t inside = a.inside - row * a.ld;
-  RawPiece<T> p[N];
+  typedef Part<T, V> P;
+  P p[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) p[i] = load_classes(x, c0 + 8 * (i * L + l), a.C, inside);
+  for (int i = 0; i < N; ++i) {
+    const int at = c0 + V * (i * L + l);
+    if (at < a.C) p[i] = P::load(x + at, a.C - at, inside - at);
+  }
   const int y = a.labels ? a.labels[row] : -1;
   const float m = a.stats[2 * row], ls = a.stats[2 * row + 1];
   const bool none = m == kLow;  // a row of -inf alone
@@ -469,15 +473,15 @@ __global__ __launch_bounds__(kBlock) void logprob_grad_kernel(ScoreGradArgs a) {
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int at = c0 + 8 * (i * L + l);
+    const int at = c0 + V * (i * L + l);
     if (at >= a.C) continue;
-    Piece out;
+    float out[V];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < V; ++j) {
       const float z = Mass<T>::y(float(p[i].v[j]), offset), e = exp2_of(z), v = e * (ENTROPY ? fmaf(bounded(z), slope, at0) : at0);
-      out.v[j] = at + j == y ? v + g : v;
+      out[j] = at + j == y ? v + g : v;
     }
-    store_piece(dx + at, a.C - at, out);
+    P::template store<PAST>(dx + at, a.C - at, out);
   }
 }
 
@@ -559,15 +563,18 @@ template <class T>
 static hgnn_status logprob_grad(ScoreGradArgs& a, hipStream_t s) {
   const bool group = a.C <= kGroupClasses;
   const int N = row_pieces(a.n, a.C, false), L = group ? group_lanes(a.C, N) : kWave;
-  a.chunks = group ? 1 : int(ceil_div(a.C, int64_t(8) * kWave * kPieces<T>));
+  constexpr int V = 16 / int(sizeof(T)), W = 4;  // of long rows: 16 bytes, four of them
+  a.chunks = group ? 1 : int(ceil_div(a.C, V * kWave * W));
+  // Long rows that the caches would have lost before they are read are written past them.  us, the log probabilities and this, through / past: 4096 rows of 50 021 (fp16) 257 / 232,
+  // 1024 68.5 / 59; rows of 41 and 100 classes, whose ends share lines, 19 / 28, 159 / 214.
+  const bool past = a.n * double(a.C) * sizeof(T) >= double(1 << 27);
   HGNN_REQUIRE(a.n <= (int64_t(1) << 40) && ceil_div(a.n * a.chunks * L, kBlock) <= 0x7fffffff && (group || a.n * a.chunks <= 0xffffffff), HGNN_EUNSUPPORTED,
                "hgnn_logprob_grad: grid too large");
   const dim3 grid{unsigned(ceil_div(a.n * a.chunks * L, kBlock))};
-  with_flags(a.dentropy != nullptr, N == 2, [&](auto entropy, auto two) {
-    constexpr bool E = decltype(entropy)::value;
-    constexpr int P = decltype(two)::value ? 2 : 1;
-    if (!group) logprob_grad_kernel<T, kWave, kPieces<T>, E, false><<<grid, kBlock, 0, s>>>(a);
-    else with_group(L, [&](auto lanes) { logprob_grad_kernel<T, decltype(lanes)::value, P, E, true><<<grid, kBlock, 0, s>>>(a); });
+  with_flags(a.dentropy != nullptr, group ? N == 2 : past, [&](auto entropy, auto flag) {
+    constexpr bool E = decltype(entropy)::value, F = decltype(flag)::value;
+    if (!group) logprob_grad_kernel<T, kWave, W, V, E, false, F><<<grid, kBlock, 0, s>>>(a);
+    else with_group(L, [&](auto lanes) { logprob_grad_kernel<T, decltype(lanes)::value, F ? 2 : 1, 8, E, true, false><<<grid, kBlock, 0, s>>>(a); });
   });
   HGNN_LAUNCH_CHECK("logprob_grad_kernel");
   return HGNN_OK;

@@ -170,6 +170,38 @@ __device__ __forceinline__ void store_quad(T* p, int left, float4_t x) {
   if (left & 1) p[left - 1] = T(left & 2 ? x2 : x0);
 }
 
+// ---- V elements of a tensor as they are in memory, eight or four
+template <class T, int V>
+struct Part;
+template <class T>
+struct Part<T, 8> {
+  typename Vec<T>::eight v;
+  static __device__ __forceinline__ Part load(const T* p) { return Part{load_raw(p).v}; }
+  static __device__ __forceinline__ Part load(const T* p, int left, int64_t inside) { return Part{load_raw(p, left, inside).v}; }
+  template <bool PAST>
+  static __device__ __forceinline__ void store(T* p, int left, const float (&x)[8]) {
+    const Piece y{{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}};
+    if constexpr (PAST && sizeof(T) == 2) {
+      if (left >= 8) {
+        half8_any_t h;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = half_t(x[i]);
+        __builtin_nontemporal_store(h, reinterpret_cast<half8_any_t*>(p));
+        return;
+      }
+    }
+    store_piece(p, left, y);
+  }
+};
+template <class T>
+struct Part<T, 4> {
+  typename Vec<T>::four v;
+  static __device__ __forceinline__ Part load(const T* p) { return Part{*reinterpret_cast<const typename Vec<T>::four*>(p)}; }
+  static __device__ __forceinline__ Part load(const T* p, int left, int64_t inside) { return Part{load_quad(p, left, inside)}; }
+  template <bool PAST>
+  static __device__ __forceinline__ void store(T* p, int left, const float (&x)[4]) { store_quad<T, PAST>(p, left, float4_t{x[0], x[1], x[2], x[3]}); }
+};
+
 inline bool known_type(hgnn_type t) { return t == HGNN_F16 || t == HGNN_F32; }
 inline bool aligned_to_type(const void* p, hgnn_type t) { return (reinterpret_cast<uintptr_t>(p) & (t == HGNN_F32 ? 3u : 1u)) == 0; }
 // elements from a tensor's first to its last: what a row's last piece may be read from
