@@ -132,40 +132,71 @@ __device__ __forceinline__ void add_row(const TableGradArgs& a, int id, int f, c
   add_quad<T, ADD>(a, p + 4 * L, a.F - f - 4 * L, x.hi);
 }
 
-// by a whole wave, 64 places looked at in each step: how many of the n sorted words have an id below `id`
-__device__ __forceinline__ int64_t wave_words_below(const TableGradArgs& a, int64_t id) {
+// by a whole wave, 64 places looked at in each step: how many of the n sorted words have an id below id[0], and below id[1]
+__device__ __forceinline__ void wave_words_below(const TableGradArgs& a, const int64_t (&id)[2], int64_t (&below)[2]) {
   const int lane = threadIdx.x & (kWave - 1);
-  int64_t lo = 0, hi = a.n;  // the answer is in [lo, hi]
-  while (lo < hi) {
-    const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
-    const int held = __popcll(__ballot(at < hi && a.id(at) < id));  // the first lanes
-    if (held == 0) {
-      hi = lo;
-    } else {
-      const int64_t last = lo + (held - 1) * step;
-      hi = last + step < hi ? last + step : hi;
-      lo = last + 1;
+  int64_t lo[2] = {0, 0}, hi[2] = {a.n, a.n};  // the answers are in [lo, hi]
+  while (lo[0] < hi[0] || lo[1] < hi[1]) {
+    int64_t step[2];
+    bool holds[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      step[i] = (hi[i] - lo[i] + kWave - 1) / kWave;
+      const int64_t at = lo[i] + lane * step[i];
+      holds[i] = at < hi[i] && a.id(at < hi[i] ? at : 0) < id[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (lo[i] >= hi[i]) continue;
+      const int held = __popcll(__ballot(holds[i]));  // the first lanes
+      if (held == 0) {
+        hi[i] = lo[i];
+      } else {
+        const int64_t last = lo[i] + (held - 1) * step[i];
+        hi[i] = last + step[i] < hi[i] ? last + step[i] : hi[i];
+        lo[i] = last + 1;
+      }
     }
   }
-  return lo;
+  below[0] = lo[0], below[1] = lo[1];
 }
 
 constexpr int kZeroRows = kWave;  // table rows of a wave that writes zeros
+constexpr int kMarked = 4;        // times 64 positions in those rows up to which each marks its row
 
-// zeros in those of 64 rows that no position has
+// zeros in those of 64 rows that no position has; s_there: 64 words of the wave's own
 template <class T, int L>
-__device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0) {
+__device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, int* s_there) {
   if (r0 >= a.V) return;
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t r = r0 + lane;
-  int64_t lo = wave_words_below(a, r0), hi = wave_words_below(a, r0 + kZeroRows);
-  const int64_t end = hi;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (a.id(mid) < r) lo = mid + 1;
-    else hi = mid;
+  const int64_t r = r0 + lane, ids[2] = {r0, r0 + kZeroRows};
+  int64_t range[2] = {0, 0};
+  if (a.n > 0) wave_words_below(a, ids, range);
+  bool mine = r >= a.V;
+  if (range[1] - range[0] <= kMarked * kWave) {
+    int id[kMarked];
+#pragma unroll
+    for (int i = 0; i < kMarked; ++i) {
+      const int64_t at = range[0] + i * kWave + lane;
+      id[i] = at < range[1] ? a.id(at) - int(r0) : -1;
+    }
+    s_there[lane] = 0;
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < kMarked; ++i)
+      if (id[i] >= 0) s_there[id[i]] = 1;
+    wave_sync();
+    mine = mine || s_there[lane] != 0;
+  } else {
+    int64_t lo = range[0], hi = range[1];
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) >> 1;
+      if (a.id(mid) < r) lo = mid + 1;
+      else hi = mid;
+    }
+    mine = mine || (lo < range[1] && a.id(lo) == r);
   }
-  const uint64_t there = __ballot(r >= a.V || (lo < end && a.id(lo) == r));
+  const uint64_t there = __ballot(mine);
   for (int k = lane / L; k < kZeroRows; k += kWave / L) {
     if (there >> k & 1) continue;
     T* const p = static_cast<T*>(a.dT) + (r0 + k) * a.lddt;
@@ -181,12 +212,13 @@ constexpr int kAhead = 4;  // rows of a share that are fetched together
 template <class T, bool ADD, int L>
 __global__ __launch_bounds__(kBlock, 6) void table_grad_kernel(TableGradArgs a) {
   constexpr int G = kBlock / L;  // shares of a workgroup
+  __shared__ Quads s_part[2][kBlock];  // head and tail of the shares
   if (int64_t(blockIdx.x) >= a.blocks) {
-    if (blockIdx.y == 0) write_zeros<T, L>(a, ((int64_t(blockIdx.x) - a.blocks) * kWavesPerBlock + threadIdx.x / kWave) * kZeroRows);
+    const int wave = threadIdx.x / kWave;
+    if (blockIdx.y == 0) write_zeros<T, L>(a, ((int64_t(blockIdx.x) - a.blocks) * kWavesPerBlock + wave) * kZeroRows, reinterpret_cast<int*>(s_part) + wave * kZeroRows);
     return;
   }
   const int64_t block = blockIdx.x;
-  __shared__ Quads s_part[2][kBlock];  // head and tail of the shares
   __shared__ int s_through[G];         // whether a run that began before the share goes on behind it
   const int g = threadIdx.x / L, l = threadIdx.x % L, f = 8 * L * int(blockIdx.y) + 4 * l;
   const int64_t begin = block * (G * kShare), stop = begin + G * kShare < a.n ? begin + G * kShare : a.n;

@@ -459,10 +459,12 @@ __global__ __launch_bounds__(kBlock) void logprob_grad_kernel(ScoreGradArgs a) {
     const int at = c0 + V * (i * L + l);
     if (at < a.C) p[i] = P::load(x + at, a.C - at, inside - at);
   }
-  const int y = a.labels ? a.labels[row] : -1;
+  int y = -1;
+  float g = 0.f;
+  if (a.labels) y = a.labels[row], g = a.dlogprob[row];
   const float m = a.stats[2 * row], ls = a.stats[2 * row + 1];
   const bool none = m == kLow;  // a row of -inf alone
-  const float g = uint32_t(y) < uint32_t(a.C) && !none ? a.dlogprob[row] : 0.f;
+  g = uint32_t(y) < uint32_t(a.C) && !none ? g : 0.f;
   const float offset = none ? 0.f : Mass<T>::offset(m), shift = none ? 0.f : kLn2 * Mass<T>::shift(m);
   const float r = none ? 0.f : expf(shift - ls);  // p = r e, log p = ln2 y + shift - ls
   float slope = 0.f, at0 = -g * r;
@@ -490,9 +492,12 @@ static int group_lanes(int C, int pieces) { return std::min(kWave, pow2_at_least
 // Pieces of a lane, more than one where rows fill the chip all the same.  us, 1 / 2 / 4: 233 000 rows of 41 (fp16) 10.2 / 8.4 / 8.8, their gradient 11.5 / 11.2 / 13.3; 262 144 of 512 78 / 57 / 51,
 // gradient 97 / 94 / 94; 100 000 of 200 18 / 12.8 / 13.6; fp32, 100 000 of 512 - / 34.8 / 36.8, gradient - / 77.7 / 81.9.
 static int row_pieces(int64_t n, int C, bool wide) {
-  if (C <= 8 || C > kGroupClasses || n * group_lanes(C, 1) < int64_t(1) << 20) return 1;
+  if (C > kGroupClasses) return C <= 2 * kGroupClasses ? 2 : 4;
+  if (C <= 8 || n * group_lanes(C, 1) < int64_t(1) << 20) return 1;
   return wide && C > 256 ? 4 : 2;
 }
+// What a group of lanes holds: up to 512 classes, 2048 without alternatives (200 000 rows of 520 and their gradient, by waves / groups: 203 / 191 us, of 600 189 / 172).
+static bool by_groups(int C, int k) { return C <= (k > 0 ? 1 : 4) * kGroupClasses; }
 template <class Call>
 static void with_pieces(int pieces, Call&& call) {
   if (pieces == 1) call(std::integral_constant<int, 1>());
@@ -502,8 +507,8 @@ static void with_pieces(int pieces, Call&& call) {
 constexpr int kWaveClasses = 4096;        // up to so many, a row is a wave's where there are rows enough
 static bool by_waves(int64_t n, int C) { return C <= kWaveClasses && n >= 4096; }
 // Workgroups of a row: as many as fill the chip, of no less than a piece for every lane
-static int splits_of(int64_t n, int C) {
-  if (C <= kGroupClasses || by_waves(n, C)) return 1;
+static int splits_of(int64_t n, int C, int k) {
+  if (by_groups(C, k) || by_waves(n, C)) return 1;
   const int64_t most = ceil_div(C, int64_t(8) * kWave * kWavesPerBlock), want = ceil_div(1024, n), s = most < want ? most : want;
   return int(s < 1 ? 1 : (s > kMostSplits ? kMostSplits : s));
 }
@@ -532,7 +537,7 @@ static void with_group(int lanes, Call&& call) {
 template <class T>
 static hgnn_status logprob(ScoreArgs& a, hipStream_t s) {
   const char* who = "hgnn_logprob";
-  const bool group = a.C <= kGroupClasses, waves = by_waves(a.n, a.C);
+  const bool group = by_groups(a.C, a.k), waves = by_waves(a.n, a.C);
   const int N = a.k > 0 ? 1 : row_pieces(a.n, a.C, sizeof(T) == 2), L = group_lanes(a.C, N);
   const int64_t blocks = group ? ceil_div(a.n * L, kBlock) : (waves ? ceil_div(a.n, kWavesPerBlock) : a.n * a.splits);
   HGNN_REQUIRE(a.n <= (int64_t(1) << 40) && blocks <= 0x7fffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
@@ -562,7 +567,7 @@ static hgnn_status logprob(ScoreArgs& a, hipStream_t s) {
 template <class T>
 static hgnn_status logprob_grad(ScoreGradArgs& a, hipStream_t s) {
   const bool group = a.C <= kGroupClasses;
-  const int N = row_pieces(a.n, a.C, false), L = group ? group_lanes(a.C, N) : kWave;
+  const int N = group ? row_pieces(a.n, a.C, false) : 1, L = group ? group_lanes(a.C, N) : kWave;
   constexpr int V = 16 / int(sizeof(T)), W = 4;  // of long rows: 16 bytes, four of them
   a.chunks = group ? 1 : int(ceil_div(a.C, V * kWave * W));
   // Long rows that the caches would have lost before they are read are written past them.  us, the log probabilities and this, through / past: 4096 rows of 50 021 (fp16) 257 / 232,
@@ -587,8 +592,8 @@ struct ScoreSpace {
 };
 static ScoreSpace score_space(void* base, int64_t n, int C, int k) {
   ScoreSpace p{};
-  if (n <= 0 || C <= kGroupClasses) return p;
-  const int splits = splits_of(n, C);
+  if (n <= 0) return p;
+  const int splits = splits_of(n, C, k);
   if (splits == 1) return p;
   const size_t each = size_t(n) * size_t(splits);
   char* const at = static_cast<char*>(base);
@@ -632,7 +637,7 @@ hgnn_status hgnn_logprob(int64_t n, int32_t C, hgnn_type type, const void* logit
                    aligned_to_type(entropy, HGNN_F32) && aligned_to_type(top_logprob, HGNN_F32) && aligned_to_type(top_class, HGNN_F32) &&
                    (w.bytes == 0 || aligned_to_type(workspace, HGNN_F32)),
                HGNN_EINVAL, "%s: an array that is not aligned to its type", who);
-  ScoreArgs a{n, C, k, logits, ld, extent_of(n, C, ld), labels, logprob_out, stats, entropy, top_logprob, top_class, splits_of(n, C), 0, w.part, w.part_top, w.part_class};
+  ScoreArgs a{n, C, k, logits, ld, extent_of(n, C, ld), labels, logprob_out, stats, entropy, top_logprob, top_class, splits_of(n, C, k), 0, w.part, w.part_top, w.part_class};
   hipStream_t s = static_cast<hipStream_t>(stream);
   return type == HGNN_F16 ? logprob<half_t>(a, s) : logprob<float>(a, s);
 }
