@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kBlock) void embedding_kernel(LookupArgs a) {
 
 // ---- the gradient -------------------------------------------------------------------------------------------
 // dT[v] = scale * sum of dY[i] over the i with ids[i] = v.  The positions are sorted by id (stable, so the rows of an id keep their order).  L lanes walk a share of
-// the sorted list, kShare positions, a workgroup so many consecutive ones as it has groups of L.  A run of equal ids inside a share is stored at once.  What
+// the sorted list, 8 or 16 positions, a workgroup so many consecutive ones as it has groups of L.  A run of equal ids inside a share is stored at once.  What
 // shares hold of a run in common goes to LDS, `head` of a run that began before the share, `tail` of one that goes on behind it, and is added in order by the share where the run
 // begins; what workgroups hold in common goes to memory in the same two forms, and a second pass adds it.  No atomics: the same bits on every run.  Rows without a position
 // are zeros, which workgroups behind those of the shares write.
@@ -88,6 +88,7 @@ struct TableGradArgs {
   float* part;  // [blocks][2][pitch]: head and tail of a workgroup
   int pitch;
   int64_t blocks;  // workgroups of shares
+  int share;
   int past;  // the caches: zeros, or all rows
   __device__ __forceinline__ int id(int64_t k) const { return int(words[k] >> pos_bits); }
   __device__ __forceinline__ int id_of(uint64_t w) const { return int(w >> pos_bits); }
@@ -206,7 +207,9 @@ __device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, 
   }
 }
 
-constexpr int kShare = 8;  // positions of a share
+// Positions of a share: many positions leave more shares than the chip holds at once, and shares of some hundred workgroups' runs to be joined.  us, 8 / 16: 1024 of 64 into 4096 rows 15.2 / 18.5, 30 000 of 64 into
+// 233 000 36 / 39, 200 000 of 128 into 233 000 59 / 57, 1 000 003 of 128 (power law) into 2.4 M 339 / 336, into 10 000 113 / 103, into 100 97 / 86.
+static int share_of(int64_t n) { return n < int64_t(1) << 19 ? 8 : 16; }
 constexpr int kAhead = 4;  // rows of a share that are fetched together
 
 template <class T, bool ADD, int L>
@@ -221,8 +224,8 @@ __global__ __launch_bounds__(kBlock, 6) void table_grad_kernel(TableGradArgs a) 
   const int64_t block = blockIdx.x;
   __shared__ int s_through[G];         // whether a run that began before the share goes on behind it
   const int g = threadIdx.x / L, l = threadIdx.x % L, f = 8 * L * int(blockIdx.y) + 4 * l;
-  const int64_t begin = block * (G * kShare), stop = begin + G * kShare < a.n ? begin + G * kShare : a.n;
-  const int64_t first = begin + g * kShare < stop ? begin + g * kShare : stop, end = first + kShare < stop ? first + kShare : stop;
+  const int64_t begin = block * (G * a.share), stop = begin + G * a.share < a.n ? begin + G * a.share : a.n;
+  const int64_t first = begin + g * a.share < stop ? begin + g * a.share : stop, end = first + a.share < stop ? first + a.share : stop;
   const int before = first > 0 && first < end ? a.id(first - 1) : -1, after = end < a.n && first < end ? a.id(end) : -1;
   int cur = -1, tail_id = -1;
   bool head = false;
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(kBlock, 6) void table_grad_kernel(TableGradArgs a) 
   __syncthreads();
   // the chain of a run: from the share where it begins, or the workgroup's first, through shares that hold nothing else, to the share where it ends
   auto chain = [&](Quads x, bool open, bool* beyond) __attribute__((always_inline)) {  // and the heads of the shares behind g
-    for (int i = g + 1; open && i < G && begin + i * kShare < stop; ++i) {
+    for (int i = g + 1; open && i < G && begin + i * a.share < stop; ++i) {
       x.add(s_part[0][i * L + l]);
       open = s_through[i];
     }
@@ -291,9 +294,8 @@ __global__ __launch_bounds__(kBlock, 6) void table_grad_kernel(TableGradArgs a) 
 template <class T, bool ADD, int L>
 __global__ __launch_bounds__(kBlock) void table_grad_join_kernel(TableGradArgs a) {
   constexpr int G = kBlock / L;
-  constexpr int64_t kPer = int64_t(G) * kShare;
   __shared__ Quads s_part[kBlock];
-  const int64_t b = blockIdx.x, begin = b * kPer, end = begin + kPer;
+  const int64_t per = int64_t(G) * a.share, b = blockIdx.x, begin = b * per, end = begin + per;
   const int id = a.id(end);
   if (id >= a.V || a.id(end - 1) != id || (begin > 0 && a.id(begin - 1) == id)) return;
   // workgroups behind this one that begin inside the run: all waves look for the last of them
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(kBlock) void table_grad_join_kernel(TableGradArgs a
   while (lo < hi) {
     const int lane = threadIdx.x & (kWave - 1);
     const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
-    const int held = __popcll(__ballot(at < hi && a.id((b + at) * kPer) == id));
+    const int held = __popcll(__ballot(at < hi && a.id((b + at) * per) == id));
     if (held == 0) {
       hi = lo;
     } else {
@@ -346,7 +348,7 @@ static TableGradSpace table_grad_space(void* base, int64_t n, int32_t F) {
     return q;
   };
   const int groups = kBlock / std::min(kWave, pow2_at_least((F + 7) / 8));
-  p.blocks = ceil_div(n, int64_t(groups) * kShare);
+  p.blocks = ceil_div(n, int64_t(groups) * share_of(n));
   p.pitch = (F + 7) / 8 * 8;
   p.buf0 = reinterpret_cast<uint64_t*>(take(8 * size_t(n)));
   p.buf1 = reinterpret_cast<uint64_t*>(take(8 * size_t(n)));
@@ -455,7 +457,7 @@ hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_
   hipStream_t s = static_cast<hipStream_t>(stream);
   const TableGradSpace w = table_grad_space(workspace, n, F);
   TableGradArgs a{};
-  a.n = n, a.blocks = w.blocks, a.F = F, a.V = V;
+  a.n = n, a.blocks = w.blocks, a.share = share_of(n), a.F = F, a.V = V;
   a.pos_bits = bits_of(n);
 
   // Rows of whole 128-byte lines are written past the caches: they are not read again before the caches have lost them.  us, through the caches / zeros past them / all rows past
