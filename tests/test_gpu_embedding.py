@@ -158,6 +158,14 @@ def test_table_gradient_of_runs_that_end_at_shares(hgnn, dev):
         check_grad(hgnn, dev, ids[order], dY, lengths.size, 40, torch.float32, 1.0, False, 40, 40, label="runs")
 
 
+@pytest.mark.parametrize("kind", ["uniform", "hubs", "one"])
+def test_table_gradient_of_many_positions(hgnn, dev, kind):
+    """Longer shares, and a run over more workgroups than one has groups of lanes."""
+    rng = np.random.default_rng(6)
+    n, V, F = 2 ** 19 + 77, 3001, 12
+    check_grad(hgnn, dev, ids_of(n, V, kind, rng), rng.standard_normal((n, F)).astype(np.float16), V, F, torch.float32, 1.0, False, 16, 12, label=kind)
+
+
 def test_table_gradient_without_positions(hgnn, dev):
     T = torch.full((70, 9), FILL, device=dev)
     none = torch.empty((0,), dtype=torch.int32, device=dev)
