@@ -170,42 +170,138 @@ struct Best {
   int c = -1;
 };
 __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
-// v, c into the list of a wave
-__device__ __forceinline__ void insert(Best& best, float v, int c) {
-  const int lane = threadIdx.x & (kWave - 1), rank = __popcll(__ballot(best.v >= v));
-  const float pv = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(best.v), 0x138, 0xf, 0xf, false));  // of the lane before: wave_shr:1
-  const int pc = __builtin_amdgcn_update_dpp(0, best.c, 0x138, 0xf, 0xf, false);
-  if (lane > rank) best.v = pv, best.c = pc;
-  if (lane == rank) best.v = v, best.c = c;
+// a piece whose scores are taken apart here and not ahead of the loop, where all pieces' would fill the registers
+template <class T>
+__device__ __forceinline__ RawPiece<T> held_back(const RawPiece<T>& x) {
+  constexpr int kWords = int(sizeof(x) / 4);
+  int w[kWords];
+  __builtin_memcpy(w, &x, sizeof(x));
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
+  RawPiece<T> r;
+  __builtin_memcpy(&r, w, sizeof(r));
+  return r;
 }
 
-// Takes those of a wave's classes c0 + 512 i + 8 lane + j (i < N, j < 8, scores x, -inf where there is none) that are among the best k.  They are taken in falling order,
-// equal ones by their class, so no more than k are; a wave comes by its classes in rising order, so among equals the first one stays ahead.
-template <class T, int N>
-__device__ __forceinline__ void take_best(Best& best, float& least, int k, RawPiece<T> (&x)[N], float (&top)[N], int c0) {
+// Lists are made of what lanes hold without rounds that wait for one another: who is ahead of whom is counted for all at once.
+struct Candidates {  // of a wave, in shared memory, in any order
+  float v[kWave];
+  int c[kWave];
+  int n;
+};
+__device__ __forceinline__ void add_candidate(Candidates& s, float v, int c) {
+  const int at = atomicAdd(&s.n, 1);
+  if (at < kWave) s.v[at] = v, s.c[at] = c;
+}
+// no more than the k-th largest of the lanes' values: the k-th of the best of every four lanes, or of all lanes' (-inf where fewer than k are above it)
+__device__ __forceinline__ float kth_of_lanes(float v, int k) {
+  int ahead = 0;
+  if (k <= 6) {
+    v = fmaxf(v, paired<0xB1>(v));
+    v = fmaxf(v, paired<0x4E>(v));
+#pragma unroll
+    for (int i = 0; i < kWave; i += 4) ahead += lane_value(v, i) > v ? 1 : 0;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kWave; ++i) ahead += lane_value(v, i) > v ? 1 : 0;
+  }
+  return -lanes_all<kWave, Over::kMax>(ahead < k ? -v : kLow);
+}
+// the next lower number of a type (of one that is above -inf)
+__device__ __forceinline__ float lower(float x) {
+  const int b = __float_as_int(x + 0.f);  // no -0
+  return __int_as_float(b > 0 ? b - 1 : (b == 0 ? int(0x80000001u) : b + 1));
+}
+__device__ __forceinline__ half_t lower(half_t x) {
+  uint16_t b;
+  x = x + half_t(0);
+  __builtin_memcpy(&b, &x, 2);
+  b = uint16_t(b == 0 ? 0x8001 : (b & 0x8000 ? b + 1 : b - 1));
+  __builtin_memcpy(&x, &b, 2);
+  return x;
+}
+// a number that rises with the score and falls with the class (no two are the same)
+__device__ __forceinline__ uint64_t place_of(float v, int c) {
+  const uint32_t b = uint32_t(__float_as_int(v + 0.f));
+  return uint64_t(b ^ (b >> 31 ? 0xffffffffu : 0x80000000u)) << 32 | uint32_t(~c);
+}
+// the candidates of the first `count` lanes, falling, classes rising among equals (no two have the same class)
+__device__ __forceinline__ Best sorted(float v, int c, int count, Candidates& s) {
   const int lane = threadIdx.x & (kWave - 1);
-  for (;;) {
-    float t = top[0];
+  const uint64_t mine = place_of(v, c);
+  int ahead = 0;
+  for (int i = 0; i < count; ++i) {
+    const uint32_t hi = uint32_t(__builtin_amdgcn_readlane(int(mine >> 32), i)), lo = uint32_t(__builtin_amdgcn_readlane(int(mine), i));
+    ahead += (uint64_t(hi) << 32 | lo) > mine ? 1 : 0;
+  }
+  if (lane < count) s.v[ahead] = v, s.c[ahead] = c;
+  wave_sync();
+  Best r;
+  if (lane < count) r.v = s.v[lane], r.c = s.c[lane];
+  wave_sync();
+  return r;
+}
+__device__ __forceinline__ Best sorted(Candidates& s) {  // at most 64
+  const int lane = threadIdx.x & (kWave - 1);
+  wave_sync();
+  const int count = __builtin_amdgcn_readfirstlane(s.n);
+  const float v = lane < count ? s.v[lane] : kLow;
+  const int c = lane < count ? s.c[lane] : -1;
+  wave_sync();
+  return sorted(v, c, count, s);
+}
+
+// Takes those of a wave's classes c0 + 512 i + 8 lane + j (i < N, j < 8, scores x, -inf where there is none) that are among the best k; `least`, the k-th so far.  A wave comes by its
+// classes in rising order, so a score that equals the k-th is behind it.  What is better becomes candidates, of many no more than what is as good as the k-th of the lanes' best.  Where
+// there are too many all the same (equal scores), pieces are gone through in their order.
+template <class T, int N>
+__device__ __forceinline__ void take_best(Best& best, float& least, int k, const RawPiece<T> (&x)[N], const float (&top)[N], int c0, Candidates& s) {
+  const int lane = threadIdx.x & (kWave - 1);
+  float t = top[0];
 #pragma unroll
-    for (int i = 1; i < N; ++i) t = fmaxf(t, top[i]);
-    if (!__ballot(t > least)) return;
-    const float v = lanes_all<kWave, Over::kMax>(t);
-    bool out = false;  // the same on all lanes
+  for (int i = 1; i < N; ++i) t = fmaxf(t, top[i]);
+  const uint64_t better = __ballot(t > least);
+  if (!better) return;
+  float bound = kLow;
+  if (__popcll(better) > k) bound = kth_of_lanes(t > least ? t : kLow, k);
+  if (lane == 0) s.n = 0;
+  wave_sync();
+  if (lane < k && best.c >= 0) add_candidate(s, best.v, best.c);
+  const T above = bound > least ? lower(T(bound)) : T(least);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint64_t there = out ? 0 : __ballot(top[i] == v);
-      if (!there) continue;
-      out = true;
-      const int from = __builtin_ctzll(there);
-      int j = 8;
+  for (int i = 0; i < N; ++i) {
+    if (!(top[i] > float(above))) continue;
+    const RawPiece<T> p = held_back(x[i]);
 #pragma unroll
-      for (int q = 7; q >= 0; --q) j = float(x[i].v[q]) == v ? q : j;
-      insert(best, v, c0 + 8 * kWave * i + 8 * from + __builtin_amdgcn_readlane(j, from));
-#pragma unroll
-      for (int q = 0; q < 8; ++q) x[i].v[q] = lane == from && q == j ? T(kLow) : x[i].v[q];
-      top[i] = piece_max(x[i]);
-    }
+    for (int j = 0; j < 8; ++j)
+      if (p.v[j] > above) add_candidate(s, float(p.v[j]), c0 + 8 * kWave * i + 8 * lane + j);
+  }
+  wave_sync();
+  if (__builtin_amdgcn_readfirstlane(s.n) <= kWave) {
+    best = sorted(s);
     least = lane_value(best.v, k - 1);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    uint64_t left = __ballot(top[i] > least);
+    while (left) {
+      const int from = __builtin_ctzll(left);
+      const RawPiece<T> p = held_back(x[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float v = lane_value(float(p.v[j]), from);
+        if (!(v > least)) continue;  // (the same on all lanes)
+        const int at = __popcll(__ballot(best.v >= v)), c = c0 + 8 * kWave * i + 8 * from + j;
+        const float pv = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(best.v), 0x138, 0xf, 0xf, false));  // of the lane before: wave_shr:1
+        const int pc = __builtin_amdgcn_update_dpp(0, best.c, 0x138, 0xf, 0xf, false);
+        if (lane > at) best.v = pv, best.c = pc;
+        if (lane == at) best.v = v, best.c = c;
+        least = lane_value(best.v, k - 1);
+      }
+      left &= left - 1;
+      left &= __ballot(top[i] > least);
+    }
   }
 }
 
@@ -349,6 +445,7 @@ __global__ __launch_bounds__(kBlock) void logprob_row_kernel(ScoreArgs a) {
   constexpr int N = kPieces<T>;
   __shared__ float s_mass[kWavesPerBlock][3], s_top[TOP ? kWavesPerBlock : 1][kMostTop];
   __shared__ int s_class[TOP ? kWavesPerBlock : 1][kMostTop];
+  __shared__ Candidates s_found[TOP ? kWavesPerBlock : 1];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int64_t unit = W == 1 ? int64_t(blockIdx.x) * kWavesPerBlock + wave : int64_t(blockIdx.x);
   if (W == 1 && unit >= a.n) return;
@@ -381,7 +478,7 @@ __global__ __launch_bounds__(kBlock) void logprob_row_kernel(ScoreArgs a) {
 #pragma unroll
     for (int i = 0; i < N; ++i) top[i] = piece_max(p[i]);
     add_pieces<ENTROPY>(mass, p, top);
-    if (TOP) take_best(best, least, a.k, p, top, c);
+    if (TOP) take_best(best, least, a.k, p, top, c, s_found[wave]);
   }
   mass = lanes_mass<kWave>(mass);
   if (W > 1) {
@@ -392,7 +489,15 @@ __global__ __launch_bounds__(kBlock) void logprob_row_kernel(ScoreArgs a) {
     mass = Mass<T>::none();
     if (lane < W) mass = Mass<T>{s_mass[lane][0], s_mass[lane][1], s_mass[lane][2]};
     mass = lanes_mass<kWave>(mass);
-    if (TOP) best = merge_lists(a.k, lane < W ? a.k : 0, [&](int p) { return Best{s_top[lane][p], s_class[lane][p]}; });
+    if (TOP && W * a.k <= kWave) {
+      const int w = lane / a.k, p = lane - w * a.k;
+      Best mine{kLow, 0x7fffffff - lane};  // (none; each in a place of its own)
+      if (w < W && s_class[w][p] >= 0) mine = Best{s_top[w][p], s_class[w][p]};
+      best = sorted(mine.v, mine.c, W * a.k, s_found[0]);
+      if (best.v == kLow) best.c = -1;
+    } else if (TOP) {
+      best = merge_lists(a.k, lane < W ? a.k : 0, [&](int p) { return Best{s_top[lane][p], s_class[lane][p]}; });
+    }
     if (a.splits > 1) {
       if (lane == 0) {
         float* const q = a.part + 3 * (row * a.splits + split);
@@ -425,7 +530,24 @@ __global__ __launch_bounds__(kWave) void logprob_join_kernel(ScoreArgs a) {
   if (lane == 0) store_row(a, row, mass, y, score);
   if (a.k == 0) return;
   const int64_t at = (row * a.splits + lane) * a.k;
-  const Best best = merge_lists(a.k, lane < a.splits ? a.k : 0, [&](int p) { return Best{a.part_top[at + p], a.part_class[at + p]}; });
+  const auto entry = [&](int p) { return Best{a.part_top[at + p], a.part_class[at + p]}; };
+  // what is as good as the k-th of the parts' best, or, of many equal scores, one by one
+  __shared__ Candidates s_found;
+  Best next;
+  if (lane < a.splits) next = entry(0);
+  const float bound = kth_of_lanes(next.v, a.k);
+  if (lane == 0) s_found.n = 0;
+  wave_sync();
+  for (int p = 0; p < a.k; ++p) {
+    const Best mine = next;
+    next = Best{};
+    if (lane < a.splits && p + 1 < a.k) next = entry(p + 1);
+    const bool here = mine.c >= 0 && mine.v >= bound;
+    if (!__ballot(here)) break;
+    if (here) add_candidate(s_found, mine.v, mine.c);
+  }
+  wave_sync();
+  const Best best = s_found.n <= kWave ? sorted(s_found) : merge_lists(a.k, lane < a.splits ? a.k : 0, entry);
   store_best(a, row, mass, best);
 }
 
