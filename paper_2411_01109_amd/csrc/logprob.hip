@@ -435,6 +435,91 @@ __global__ __launch_bounds__(kBlock) void logprob_group_kernel(ScoreArgs a) {
   }
 }
 
+// Alternatives of few classes, many rows: a lane takes a row by itself, with no reduction across lanes.  The 64 rows of a wave come in whole pieces through LDS (rows of P pieces and a pad
+// word, so that lanes that read their own rows meet on no bank).  us, lanes in groups / a lane a row, best five of 233 000 rows of 41: 41.7 / 19.8; without alternatives 8.8 / 8.3 and the
+// gradient, which would go back that way, 9.9 / 12.5: not kept.
+template <class T, int P>
+struct LaneRows {
+  static constexpr int kPitch = 8 * P + 4 / int(sizeof(T));  // elements
+  T x[kWave][kPitch];
+  // pieces f, f + 64, ... of the wave's rows, neighbours to neighbouring lanes: f(row, piece)
+  template <class F>
+  static __device__ __forceinline__ void each(F&& f) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int at = i * kWave + int(threadIdx.x & (kWave - 1));
+      f(i, at / P, at % P);
+    }
+  }
+  __device__ __forceinline__ void fetch(const T* logits, int64_t ld, int64_t row0, int64_t n, int C, int64_t inside) {
+    RawPiece<T> p[P];
+    each([&](int i, int r, int q) __attribute__((always_inline)) {
+      const int64_t row = row0 + r < n ? row0 + r : n - 1;
+      p[i] = load_classes(logits + row * ld, 8 * q, C, inside - row * ld);
+    });
+    each([&](int i, int r, int q) __attribute__((always_inline)) { put(r, q, p[i]); });
+    wave_sync();
+  }
+  __device__ __forceinline__ void put(int r, int q, const RawPiece<T>& p) {
+    constexpr int kWords = int(sizeof(RawPiece<T>) / 4);
+    int w[kWords];
+    __builtin_memcpy(w, &p, sizeof(w));
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) reinterpret_cast<int*>(&x[r][8 * q])[j] = w[j];
+  }
+  __device__ __forceinline__ RawPiece<T> piece(int r, int q) const {
+    constexpr int kWords = int(sizeof(RawPiece<T>) / 4);
+    int w[kWords];
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) w[j] = reinterpret_cast<const int*>(&x[r][8 * q])[j];
+    RawPiece<T> p;
+    __builtin_memcpy(&p, w, sizeof(w));
+    return p;
+  }
+};
+template <class T, int P, bool ENTROPY>
+__global__ __launch_bounds__(kBlock) void logprob_lane_kernel(ScoreArgs a) {
+  __shared__ __align__(16) LaneRows<T, P> s_rows[kWavesPerBlock];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int64_t row0 = (int64_t(blockIdx.x) * kWavesPerBlock + wave) * kWave, row = row0 + lane;
+  if (row0 >= a.n) return;
+  const int y = a.labels && row < a.n ? a.labels[row] : -1;
+  LaneRows<T, P>& s = s_rows[wave];
+  s.fetch(static_cast<const T*>(a.logits), a.ld, row0, a.n, a.C, a.inside);
+  RawPiece<T> p[P];
+  float top[P];
+  Mass<T> mass = Mass<T>::none();
+#pragma unroll
+  for (int q = 0; q < P; ++q) {
+    p[q] = s.piece(lane, q);
+    top[q] = piece_max(p[q]);
+    mass.m = fmaxf(mass.m, top[q]);
+  }
+  add_pieces<ENTROPY>(mass, p, top);
+  if (row >= a.n) return;
+  store_row(a, row, mass, y, float(s.x[lane][uint32_t(y) < uint32_t(a.C) ? y : 0]));
+  // the best one that is left, k times; those that are not above -inf, in their order, once the others are out
+  const RowStats st = stats_of(mass);
+  uint64_t left = a.C == 64 ? ~uint64_t(0) : (uint64_t(1) << a.C) - 1;
+  for (int k = 0; k < a.k; ++k) {
+    float v = kLow;
+    int c = -1;
+#pragma unroll
+    for (int q = 0; q < P; ++q)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float e = float(p[q].v[j]);
+        const bool better = e > v && (left >> (8 * q + j) & 1);
+        v = better ? e : v;
+        c = better ? 8 * q + j : c;
+      }
+    if (c < 0) c = __builtin_ctzll(left);
+    left &= ~(uint64_t(1) << c);
+    a.top[row * a.k + k] = mass.s == mass.s ? st.log_p(v) : NAN;
+    a.top_class[row * a.k + k] = c;
+  }
+}
+
 // Longer rows: W waves take one, or one of its `splits` parts, W = 4 a workgroup, W = 1 a wave by itself.  The waves take 4 KB in turn, the next ones on their way.
 template <class T>
 constexpr int kPieces = sizeof(T) == 2 ? 4 : 2;  // 64 bytes
@@ -563,8 +648,36 @@ struct ScoreGradArgs {
   int64_t ldd;
 };
 
-// L lanes take a row (ONE), or 64 of them one of its chunks, N parts of V each.  A lane reads what it overwrites: the logits may be the output.  With e = 2^y (Mass) p is e times a
-// factor of the row, and a class's gradient e times a line in y.
+// With e = 2^y (Mass) p is e times a factor of the row, and a class's gradient e times a line in y.
+template <class T>
+struct RowGrad {
+  int y;
+  float g, offset, slope, at0;
+  template <bool ENTROPY>
+  __device__ __forceinline__ float grad(float x, int c) const {
+    const float z = Mass<T>::y(x, offset), e = exp2_of(z), v = e * (ENTROPY ? fmaf(bounded(z), slope, at0) : at0);
+    return c == y ? v + g : v;
+  }
+};
+template <class T, bool ENTROPY>
+__device__ __forceinline__ RowGrad<T> row_grad(const ScoreGradArgs& a, int64_t row) {
+  RowGrad<T> r{-1, 0.f, 0.f, 0.f, 0.f};
+  if (a.labels) r.y = a.labels[row], r.g = a.dlogprob[row];
+  const float m = a.stats[2 * row], ls = a.stats[2 * row + 1];
+  const bool none = m == kLow;  // a row of -inf alone
+  r.g = uint32_t(r.y) < uint32_t(a.C) && !none ? r.g : 0.f;
+  r.offset = none ? 0.f : Mass<T>::offset(m);
+  const float shift = none ? 0.f : kLn2 * Mass<T>::shift(m), p = none ? 0.f : expf(shift - ls);  // p is this times e, log p = ln2 y + shift - ls
+  r.at0 = -r.g * p;
+  if (ENTROPY) {
+    const float h = a.dentropy[row] * p;
+    r.slope = -h * kLn2;
+    r.at0 -= h * (a.entropy[row] + shift - ls);
+  }
+  return r;
+}
+
+// L lanes take a row (ONE), or 64 of them one of its chunks, N parts of V each.  A lane reads what it overwrites: the logits may be the output.
 template <class T, int L, int N, int V, bool ENTROPY, bool ONE, bool PAST>
 __global__ __launch_bounds__(kBlock) void logprob_grad_kernel(ScoreGradArgs a) {
   const int64_t unit = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / L;
@@ -581,30 +694,14 @@ __global__ __launch_bounds__(kBlock) void logprob_grad_kernel(ScoreGradArgs a) {
     const int at = c0 + V * (i * L + l);
     if (at < a.C) p[i] = P::load(x + at, a.C - at, inside - at);
   }
-  int y = -1;
-  float g = 0.f;
-  if (a.labels) y = a.labels[row], g = a.dlogprob[row];
-  const float m = a.stats[2 * row], ls = a.stats[2 * row + 1];
-  const bool none = m == kLow;  // a row of -inf alone
-  g = uint32_t(y) < uint32_t(a.C) && !none ? g : 0.f;
-  const float offset = none ? 0.f : Mass<T>::offset(m), shift = none ? 0.f : kLn2 * Mass<T>::shift(m);
-  const float r = none ? 0.f : expf(shift - ls);  // p = r e, log p = ln2 y + shift - ls
-  float slope = 0.f, at0 = -g * r;
-  if (ENTROPY) {
-    const float h = a.dentropy[row] * r;
-    slope = -h * kLn2;
-    at0 -= h * (a.entropy[row] + shift - ls);
-  }
+  const RowGrad<T> of = row_grad<T, ENTROPY>(a, row);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int at = c0 + V * (i * L + l);
     if (at >= a.C) continue;
     float out[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float z = Mass<T>::y(float(p[i].v[j]), offset), e = exp2_of(z), v = e * (ENTROPY ? fmaf(bounded(z), slope, at0) : at0);
-      out[j] = at + j == y ? v + g : v;
-    }
+    for (int j = 0; j < V; ++j) out[j] = of.template grad<ENTROPY>(float(p[i].v[j]), at + j);
     P::template store<PAST>(dx + at, a.C - at, out);
   }
 }
@@ -643,6 +740,22 @@ static void with_flags(bool x, bool y, Call&& call) {
   if (x) y ? call(yes, yes) : call(yes, no);
   else y ? call(no, yes) : call(no, no);
 }
+// a lane to a row, for its alternatives, where a row has more than one piece and the rows fill the chip
+constexpr int kLaneClasses = 64;
+constexpr int64_t kLaneRows = 65536;
+static bool by_lanes(int64_t n, int C, int k) { return k > 0 && C > 8 && C <= kLaneClasses && n >= kLaneRows; }
+template <class Call>
+static void with_lane_pieces(int C, Call&& call) {
+  switch ((C + 7) / 8) {
+    case 2: return call(std::integral_constant<int, 2>());
+    case 3: return call(std::integral_constant<int, 3>());
+    case 4: return call(std::integral_constant<int, 4>());
+    case 5: return call(std::integral_constant<int, 5>());
+    case 6: return call(std::integral_constant<int, 6>());
+    case 7: return call(std::integral_constant<int, 7>());
+    default: return call(std::integral_constant<int, 8>());
+  }
+}
 template <class Call>
 static void with_group(int lanes, Call&& call) {
   switch (lanes) {
@@ -661,13 +774,16 @@ static hgnn_status logprob(ScoreArgs& a, hipStream_t s) {
   const char* who = "hgnn_logprob";
   const bool group = by_groups(a.C, a.k), waves = by_waves(a.n, a.C);
   const int N = a.k > 0 ? 1 : row_pieces(a.n, a.C, sizeof(T) == 2), L = group_lanes(a.C, N);
-  const int64_t blocks = group ? ceil_div(a.n * L, kBlock) : (waves ? ceil_div(a.n, kWavesPerBlock) : a.n * a.splits);
+  const bool lanes = by_lanes(a.n, a.C, a.k);
+  const int64_t blocks = lanes ? ceil_div(a.n, kBlock) : group ? ceil_div(a.n * L, kBlock) : (waves ? ceil_div(a.n, kWavesPerBlock) : a.n * a.splits);
   HGNN_REQUIRE(a.n <= (int64_t(1) << 40) && blocks <= 0x7fffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
   const dim3 grid{unsigned(blocks)};
   a.span = waves ? a.C : int(ceil_div(ceil_div(a.C, a.splits), 8) * 8);
   with_flags(a.entropy != nullptr, a.k > 0, [&](auto entropy, auto top) {
     constexpr bool E = decltype(entropy)::value, K = decltype(top)::value;
-    if (group) {
+    if (lanes) {
+      with_lane_pieces(a.C, [&](auto pieces) { logprob_lane_kernel<T, decltype(pieces)::value, E><<<grid, kBlock, 0, s>>>(a); });
+    } else if (group) {
       with_group(L, [&](auto width) {
         constexpr int W = decltype(width)::value;
         with_pieces(N, [&](auto pieces) { logprob_group_kernel<T, W, K ? 1 : decltype(pieces)::value, E, K><<<grid, kBlock, 0, s>>>(a); });
@@ -678,7 +794,7 @@ static hgnn_status logprob(ScoreArgs& a, hipStream_t s) {
       logprob_row_kernel<T, kWavesPerBlock, E, K><<<grid, kBlock, 0, s>>>(a);
     }
   });
-  HGNN_LAUNCH_CHECK("logprob_group_kernel or logprob_row_kernel");
+  HGNN_LAUNCH_CHECK("logprob_lane_kernel, logprob_group_kernel or logprob_row_kernel");
   if (a.splits > 1) {
     logprob_join_kernel<T><<<dim3(unsigned(a.n)), kWave, 0, s>>>(a);
     HGNN_LAUNCH_CHECK("logprob_join_kernel");

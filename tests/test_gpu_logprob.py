@@ -153,6 +153,39 @@ def test_shapes(hgnn, dev, n, C, pitch, offset, k, dtype):
         check_grad(hgnn, dev, x, labels, pitch, offset, t, y, out, r, with_entropy, rng)
 
 
+ROWS = [(65536, 9, 9, 0, 9), (66001, 41, 48, 0, 5), (70000, 16, 17, 1, 2), (65800, 64, 64, 0, 20), (80001, 57, 59, 3, 0), (68000, 24, 24, 0, 1), (70000, 47, 47, 0, 8), (66000, 33, 40, 0, 32)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("n,C,pitch,offset,k", ROWS)
+def test_many_rows_of_few_classes(hgnn, dev, n, C, pitch, offset, k, dtype):
+    """With rows among them that the mask leaves empty or nearly so, whose scores are equal, and that hold no numbers."""
+    print(f"logprob n={n} C={C} pitch={pitch} k={k} {dtype}", flush=True)
+    rng = np.random.default_rng(n + C + k)
+    x = (rng.standard_normal((n, C)) * 2).astype(NP[dtype])
+    x[5], x[64 * 7 + 63], x[n - 1] = -np.inf, -np.inf, 1.0
+    x[9], x[9, C - 1] = -np.inf, 3.0
+    x[100:200] = np.round(x[100:200])
+    x[300:400][rng.random((100, C)) < 0.7] = -np.inf
+    x[500] = np.finfo(NP[dtype]).min
+    labels = rng.integers(0, C, n).astype(np.int32)
+    labels[rng.random(n) < 0.2] = -1
+    labels[:4] = C, -2 ** 31, 2 ** 31 - 1, C - 1
+    for with_entropy in (False, True):
+        t, y, out, r = check(hgnn, dev, x, labels, k, pitch, offset)
+        check_grad(hgnn, dev, x, labels, pitch, offset, t, y, out, r, with_entropy, rng)
+    x[77, C // 2] = np.nan
+    x[78, 0] = np.inf
+    t, y, out = run(hgnn, dev, x, labels, k, pitch, offset)
+    for name in ("logprob", "stats", "entropy") + (("top_logprob",) if k else ()):
+        v = down(out[name]).reshape(n, -1)
+        bad = np.isnan(v).any(1)
+        assert bad[77] == (name != "logprob" or 0 <= labels[77] < C) and np.all(np.isnan(v[bad])) and not bad[[76, 79, 80]].any(), name
+    if k:
+        c = down(out["top_class"])
+        assert np.all((c >= 0) & (c < C)) and all(len(set(c[i])) == k for i in (77, 78, 5, 9))
+
+
 @pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
 @pytest.mark.parametrize("C", [6, 41, 300, 700, 5000, 70001])
 def test_masks_and_far_values(hgnn, dev, C, dtype):
