@@ -195,16 +195,11 @@ static hgnn_status check_outputs(const char* who, int32_t count, const hgnn_grad
   return HGNN_OK;
 }
 
-static double elements_of(int32_t count, const hgnn_grad* g) {
-  double n = 0;
-  for (int i = 0; i < count; ++i) n += double(g[i].rows) * double(g[i].cols);
-  return n;
-}
-
 // launches f(arguments, workgroups) over the tensors, as many at a time as the arguments hold
 template <class Launch>
 static hgnn_status over_tensors(const char* who, int32_t count, const hgnn_grad* g, bool clip, ClipArgs& a, Launch&& f) {
-  const double total = elements_of(count, g);
+  double total = 0;
+  for (int i = 0; i < count; ++i) total += double(g[i].rows) * double(g[i].cols);
   a.chunk = kClipChunk * int(std::min<double>(kClipMost / kClipChunk, std::ceil(std::max(total, 1.) / (double(kClipParts) * kClipChunk))));
   int i = 0;
   while (i < count) {
@@ -297,9 +292,10 @@ hgnn_status hgnn_grad_clip(int32_t count, const hgnn_grad* grads, float inv_scal
     HGNN_LAUNCH_CHECK("grad_norm_kernel");
     return HGNN_OK;
   }
-  // Many outputs are written past the caches, which would have lost them before they are read.  us, fp32 to fp32, through / past: 307 M elements 677 / 647, 60 M 146 / 116,
-  // 30 M 74 / 58.5, 3 M 12.7 / 12.8; fp16 to fp32, 307 M 471 / 424.
-  const bool past = elements_of(count, grads) >= double(1 << 24);
+  // Large outputs are written past the caches.  us, fp32 to fp32, through / past: 307 M elements 677 / 647, 60 M 146 / 116; fp16 to fp32, 307 M 471 / 424.
+  double bytes = 0;
+  for (int i = 0; i < count; ++i) bytes += double(grads[i].rows) * double(grads[i].cols) * ((grads[i].out ? grads[i].out_type : grads[i].type) == HGNN_F32 ? 4 : 2);
+  const bool past = bytes >= kPastBytes;
   return over_tensors(who, count, grads, true, a, [&](unsigned blocks) -> hgnn_status {
     if (past) grad_clip_kernel<true><<<dim3(blocks), kBlock, 0, s>>>(a);
     else grad_clip_kernel<false><<<dim3(blocks), kBlock, 0, s>>>(a);

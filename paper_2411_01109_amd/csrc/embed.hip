@@ -22,7 +22,7 @@ struct LookupArgs {
 };
 
 // out[i] = scale * T[ids[i]]: L lanes take N rows in pieces of eight, whose reads go out together.  Bound by memory.
-template <class T, int L, int N>
+template <class T, int L, int N, bool PAST>
 __global__ __launch_bounds__(kBlock) void embedding_kernel(LookupArgs a) {
   constexpr int G = kBlock / L;
   const int64_t i0 = int64_t(blockIdx.x) * (G * N) + threadIdx.x / L;
@@ -40,10 +40,10 @@ __global__ __launch_bounds__(kBlock) void embedding_kernel(LookupArgs a) {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       if (i0 + u * G >= a.n) break;
-      Piece y = floats(x[u]);
+      float y[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y.v[j] *= a.scale;
-      store_piece(a.out + (i0 + u * G) * a.ldo + f, a.F - f, y);
+      for (int j = 0; j < 8; ++j) y[j] = float(x[u].v[j]) * a.scale;
+      Part<half_t, 8>::template store<PAST>(a.out + (i0 + u * G) * a.ldo + f, a.F - f, y);
     }
   }
 }
@@ -416,15 +416,19 @@ hgnn_status hgnn_embedding(int64_t n, int32_t F, const int32_t* ids, int32_t V, 
   with_lanes(F, [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
     auto go = [&]() -> hgnn_status {
-      const bool many = n * L >= kFewLookups;
+      const bool many = n * L >= kFewLookups, past = double(n) * F * sizeof(half_t) >= kPastBytes;
       const int64_t blocks = ceil_div(n, int64_t(kBlock / L) * (many ? kLookups : 1));
       HGNN_REQUIRE(blocks <= 0x7fffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
       const dim3 grid{unsigned(blocks)};
       hipStream_t s = static_cast<hipStream_t>(stream);
-      if (table_type == HGNN_F16 && many) embedding_kernel<half_t, L, kLookups><<<grid, kBlock, 0, s>>>(a);
-      else if (table_type == HGNN_F16) embedding_kernel<half_t, L, 1><<<grid, kBlock, 0, s>>>(a);
-      else if (many) embedding_kernel<float, L, kLookups><<<grid, kBlock, 0, s>>>(a);
-      else embedding_kernel<float, L, 1><<<grid, kBlock, 0, s>>>(a);
+      auto launch = [&](auto type) {
+        typedef decltype(type) T;
+        if (many && past) embedding_kernel<T, L, kLookups, true><<<grid, kBlock, 0, s>>>(a);
+        else if (many) embedding_kernel<T, L, kLookups, false><<<grid, kBlock, 0, s>>>(a);
+        else embedding_kernel<T, L, 1, false><<<grid, kBlock, 0, s>>>(a);
+      };
+      if (table_type == HGNN_F16) launch(half_t());
+      else launch(float());
       HGNN_LAUNCH_CHECK("embedding_kernel");
       return HGNN_OK;
     };
@@ -460,11 +464,11 @@ hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_
   a.n = n, a.blocks = w.blocks, a.share = share_of(n), a.F = F, a.V = V;
   a.pos_bits = bits_of(n);
 
-  // Rows of whole 128-byte lines are written past the caches: they are not read again before the caches have lost them.  us, through the caches / zeros past them / all rows past
+  // Large tables (kPastBytes) whose rows are whole 128-byte lines are written past the caches.  us, through the caches / zeros past them / all rows past
   // them, 64 M elements of gradients into 200 M (rows of 8 features 1 M into 3 M): rows of 128 bytes (32 x fp32) 191 / 182 / 183, 256 (64 x fp32) 265 / 236 / 229, 512 233 / 227 / 215,
   // 512 (256 x fp16) 162 / 153 / 143; but parts of lines cost more, rows of 32 bytes 127 / 136 / 198, of 168 bytes 312 / 343 / 371.
   const size_t row_bytes = size_t(F) * (grad_type == HGNN_F16 ? 2 : 4), pitch_bytes = size_t(lddt) * (grad_type == HGNN_F16 ? 2 : 4);
-  a.past = row_bytes % 128 == 0 && pitch_bytes % 128 == 0 && (reinterpret_cast<uintptr_t>(dT) & 127u) == 0 ? (row_bytes >= 256 ? kPastAll : kPastZeros) : 0;
+  a.past = double(V) * pitch_bytes >= kPastBytes && row_bytes % 128 == 0 && pitch_bytes % 128 == 0 && (reinterpret_cast<uintptr_t>(dT) & 127u) == 0 ? (row_bytes >= 256 ? kPastAll : kPastZeros) : 0;
   a.dY = reinterpret_cast<const half_t*>(dY), a.ldy = ldy, a.inside = extent_of(n, F, ldy), a.scale = scale;
   a.dT = dT, a.lddt = lddt, a.part = w.part, a.pitch = w.pitch;
   if (n > 0) {

@@ -808,9 +808,9 @@ static hgnn_status logprob_grad(ScoreGradArgs& a, hipStream_t s) {
   const int N = group ? row_pieces(a.n, a.C, false) : 1, L = group ? group_lanes(a.C, N) : kWave;
   constexpr int V = 16 / int(sizeof(T)), W = 4;  // of long rows: 16 bytes, four of them
   a.chunks = group ? 1 : int(ceil_div(a.C, V * kWave * W));
-  // Long rows that the caches would have lost before they are read are written past them.  us, the log probabilities and this, through / past: 4096 rows of 50 021 (fp16) 257 / 232,
+  // Long rows of large outputs are written past the caches.  us, the log probabilities and this, through / past: 4096 rows of 50 021 (fp16) 257 / 232,
   // 1024 68.5 / 59; rows of 41 and 100 classes, whose ends share lines, 19 / 28, 159 / 214.
-  const bool past = a.n * double(a.C) * sizeof(T) >= double(1 << 27);
+  const bool past = a.n * double(a.C) * sizeof(T) >= kPastBytes;
   HGNN_REQUIRE(a.n <= (int64_t(1) << 40) && ceil_div(a.n * a.chunks * L, kBlock) <= 0x7fffffff && (group || a.n * a.chunks <= 0xffffffff), HGNN_EUNSUPPORTED,
                "hgnn_logprob_grad: grid too large");
   const dim3 grid{unsigned(ceil_div(a.n * a.chunks * L, kBlock))};

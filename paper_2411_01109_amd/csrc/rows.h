@@ -202,6 +202,10 @@ struct Part<T, 4> {
   static __device__ __forceinline__ void store(T* p, int left, const float (&x)[4]) { store_quad<T, PAST>(p, left, float4_t{x[0], x[1], x[2], x[3]}); }
 };
 
+// Outputs of so many bytes are written past the caches: the last-level cache (256 MiB) would have lost most of them before they are read.  us, rows of 128 by id and then a reader of them, through / past: 61 MB
+// 35 / 38, 122 MB 62 / 66, 244 MB 126 / 121 (the rows alone: 20 / 16, 41 / 31, 81 / 58).
+constexpr double kPastBytes = 192. * (1 << 20);
+
 inline bool known_type(hgnn_type t) { return t == HGNN_F16 || t == HGNN_F32; }
 inline bool aligned_to_type(const void* p, hgnn_type t) { return (reinterpret_cast<uintptr_t>(p) & (t == HGNN_F32 ? 3u : 1u)) == 0; }
 // elements from a tensor's first to its last: what a row's last piece may be read from
