@@ -165,6 +165,12 @@ __device__ __forceinline__ void wave_words_below(const TableGradArgs& a, const i
 constexpr int kZeroRows = kWave;  // table rows of a wave that writes zeros
 constexpr int kMarked = 4;        // times 64 positions in those rows up to which each marks its row
 
+// whether the 128-byte line of `at` lies in the row from..to
+__device__ __forceinline__ bool in_whole_line(const char* at, const char* from, const char* to) {
+  const char* const line = at - (reinterpret_cast<uintptr_t>(at) & 127u);
+  return line >= from && line + 128 <= to;
+}
+
 // zeros in those of 64 rows that no position has; s_there: 64 words of the wave's own
 template <class T, int L>
 __device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, int* s_there) {
@@ -201,8 +207,10 @@ __device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, 
   for (int k = lane / L; k < kZeroRows; k += kWave / L) {
     if (there >> k & 1) continue;
     T* const p = static_cast<T*>(a.dT) + (r0 + k) * a.lddt;
+    const char* const from = reinterpret_cast<const char*>(p);
+    const char* const to = reinterpret_cast<const char*>(p + a.F);
     for (int f = 4 * (lane % L); f < a.F; f += 4 * L)
-      if (a.past != 0) store_quad<T, true>(p + f, a.F - f, float4_t{});
+      if (const char* const at = reinterpret_cast<const char*>(p + f); a.past != 0 && in_whole_line(at, from, to)) store_quad<T, true>(p + f, a.F - f, float4_t{});
       else store_quad(p + f, a.F - f, float4_t{});
   }
 }
@@ -467,8 +475,12 @@ hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_
   // Large tables (kPastBytes) whose rows are whole 128-byte lines are written past the caches.  us, through the caches / zeros past them / all rows past
   // them, 64 M elements of gradients into 200 M (rows of 8 features 1 M into 3 M): rows of 128 bytes (32 x fp32) 191 / 182 / 183, 256 (64 x fp32) 265 / 236 / 229, 512 233 / 227 / 215,
   // 512 (256 x fp16) 162 / 153 / 143; but parts of lines cost more, rows of 32 bytes 127 / 136 / 198, of 168 bytes 312 / 343 / 371.
+  // Of rows with gaps, whose parts of lines cost more either way, zeros in the whole lines alone: 16 positions into 400 MB of fp32, rows of 64 of a pitch of 72 159 / 169, 80 of 88 154 / 119, 100 of 104 149 / 110, 200 of 208
+  // 134 / 87, 333 of 336 127 / 91, 1000 of 1008 107 / 93 (all of the row past them: 100 of 104 174, 200 of 208 136); without gaps, where the caches join the parts, 100 91 / 122, 333 92 / 129.
   const size_t row_bytes = size_t(F) * (grad_type == HGNN_F16 ? 2 : 4), pitch_bytes = size_t(lddt) * (grad_type == HGNN_F16 ? 2 : 4);
-  a.past = double(V) * pitch_bytes >= kPastBytes && row_bytes % 128 == 0 && pitch_bytes % 128 == 0 && (reinterpret_cast<uintptr_t>(dT) & 127u) == 0 ? (row_bytes >= 256 ? kPastAll : kPastZeros) : 0;
+  const bool lines = row_bytes % 128 == 0 && pitch_bytes % 128 == 0 && (reinterpret_cast<uintptr_t>(dT) & 127u) == 0;
+  const bool gaps = pitch_bytes > row_bytes && row_bytes >= 288;
+  a.past = double(V) * pitch_bytes < kPastBytes ? 0 : lines && row_bytes >= 256 ? kPastAll : lines || gaps ? kPastZeros : 0;
   a.dY = reinterpret_cast<const half_t*>(dY), a.ldy = ldy, a.inside = extent_of(n, F, ldy), a.scale = scale;
   a.dT = dT, a.lddt = lddt, a.part = w.part, a.pitch = w.pitch;
   if (n > 0) {

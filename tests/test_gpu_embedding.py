@@ -189,6 +189,28 @@ def test_table_gradient_far_rows(hgnn, dev):
     assert int(torch.count_nonzero(T)) == 0
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("F,ldt,offset", [(100, 104, 0), (333, 333, 0), (256, 256, 0), (161, 200, 3), (1000, 1008, 0)])
+def test_table_gradient_of_large_tables(hgnn, dev, F, ldt, offset, dtype):
+    """Tables too large for the last-level cache: rows and zeros in whole lines and in parts of lines, what lies between the rows as it was, NaN at positions without an id."""
+    size = 2 if dtype == torch.float16 else 4
+    V = (2 ** 28 + 2 ** 20) // (ldt * size)
+    buf = torch.full((V * ldt + offset,), FILL, dtype=dtype, device=dev)
+    T = torch.as_strided(buf, (V, F), (ldt, 1), offset)
+    ids = torch.tensor([5, V - 1, -1, 5, V, 64, 63, 5, V // 2], dtype=torch.int32, device=dev)
+    dY = torch.arange(1, 10, device=dev).half()[:, None].repeat(1, F)
+    dY[2] = dY[4] = float("nan")
+    ws = torch.empty(hgnn.hgnn_embedding_grad_workspace(9, F, V), dtype=torch.uint8, device=dev)
+    hgnn.hgnn_embedding_grad(ids, dY, T, ws)
+    for v, want in ((5, 1 + 4 + 8), (V - 1, 2), (64, 6), (63, 7), (V // 2, 9)):
+        assert bool((T[v] == want).all()), v
+        T[v] = 0
+    assert int(torch.count_nonzero(T)) == 0
+    if ldt > F:  # the rows are counted out, the rest is as it was
+        T.fill_(FILL)
+        assert bool((buf == FILL).all())
+
+
 def test_gradient_is_the_lookups(hgnn, dev):
     """<lookup(T), dY> moves with T as the gradient says: the lookup is linear in T, so differences are exact up to the roundings of both sides."""
     rng = np.random.default_rng(3)
