@@ -380,6 +380,68 @@ __device__ __forceinline__ Best merge_lists(int k, int n, Entry&& entry) {
   return out;
 }
 
+// ---- the best k of a row that a group of lanes holds, a piece each: every lane puts its eight in order once, then the row's best is the best of the lanes' first, k times.  us, with rounds that looked
+// for score and class among all that is left / this: 212 828 rows of 247 (fp16) best five 137 / 82, twenty 461 / 135; 19 rows of 16, all sixteen 14 / 4.3
+// A score and its class.  NaN counts as -inf, and what is behind the row's end comes after both.
+template <class T>
+struct Place;
+template <>
+struct Place<half_t> {  // in one number, that rises with the score and falls with the class (less than 2^16)
+  int key;
+  Place() = default;
+  __device__ __forceinline__ Place(half_t x, int c, bool there) {
+    x = (x > half_t(kLow) ? x : half_t(kLow)) + half_t(0);  // no -0
+    int16_t b;
+    __builtin_memcpy(&b, &x, 2);
+    key = there ? int(uint32_t(b >= 0 ? b : b ^ 0x7fff) << 16) | (0xffff - c) : int(0x80000000u);
+  }
+  static __device__ __forceinline__ void order(Place (&e)[8]) {
+    constexpr int kPairs[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6}, {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
+#pragma unroll
+    for (int q = 0; q < 19; ++q) {
+      const int x = e[kPairs[q][0]].key, y = e[kPairs[q][1]].key;
+      e[kPairs[q][0]].key = max(x, y);
+      e[kPairs[q][1]].key = min(x, y);
+    }
+  }
+  template <int L>
+  __device__ __forceinline__ bool best_of_lanes() const { return lanes_all<L, Over::kMax>(key) == key; }
+  __device__ __forceinline__ float score() const {
+    const int16_t s = int16_t(key >> 16), b = s >= 0 ? s : s ^ 0x7fff;
+    half_t x;
+    __builtin_memcpy(&x, &b, 2);
+    return float(x);
+  }
+  __device__ __forceinline__ int cls() const { return 0xffff - (key & 0xffff); }
+};
+template <>
+struct Place<float> {
+  float v;
+  int c;  // -1: none
+  Place() = default;
+  __device__ __forceinline__ Place(float x, int cls, bool there) : v(there && x > kLow ? x : kLow), c(there ? cls : -1) {}
+  static __device__ __forceinline__ void order(Place (&e)[8]) {  // neighbours only, so that equal ones stay in the order of their classes
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+#pragma unroll
+      for (int j = q & 1; j + 1 < 8; j += 2) {
+        const Place x = e[j], y = e[j + 1];
+        const bool swap = y.v > x.v;
+        e[j] = swap ? y : x;
+        e[j + 1] = swap ? x : y;
+      }
+  }
+  template <int L>
+  __device__ __forceinline__ bool best_of_lanes() const {  // of equal ones the first lane's, whose classes are lower
+    const int lane = threadIdx.x & (kWave - 1);
+    const float m = lanes_all<L, Over::kMax>(v);
+    const uint64_t those = __ballot(c >= 0 && v == m) >> (lane & ~(L - 1));
+    return __builtin_ctzll(those) == (lane & (L - 1));
+  }
+  __device__ __forceinline__ float score() const { return v; }
+  __device__ __forceinline__ int cls() const { return c; }
+};
+
 // Rows of up to 512 classes: L lanes hold a row, N pieces each.  What a row costs beside its classes (reductions, logarithm, stores) is a wave's for all of its 64 / L rows at once: 262 144 rows
 // of 512, 64 lanes with a piece / 16 with four, 78 / 51 us.
 template <class T, int L, int N, bool ENTROPY, bool TOP>
@@ -406,38 +468,37 @@ __global__ __launch_bounds__(kBlock) void logprob_group_kernel(ScoreArgs a) {
   if (ENTROPY) mass.t = lanes_all<L, Over::kSum>(mass.t);
   if (writes) store_row(a, row, mass, y, at);
   if (!TOP) return;
-  const RowStats st = stats_of(mass);
   static_assert(!TOP || N == 1, "a piece each");
-  float t = top[0];
-  // of equal scores the lowest class; those that are not above -inf, in their order, once the others are out
-  uint32_t left = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) left |= uint32_t(8 * l + j < a.C) << j;
+  constexpr int kRows = kWave / L, kMost = 8 * L < kMostTop ? 8 * L : kMostTop;
+  __shared__ Place<T> s_best[TOP ? kWavesPerBlock : 1][TOP ? kRows * kMost : 1];
+  __shared__ RowStats s_stats[TOP ? kWavesPerBlock : 1][TOP ? kRows : 1];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, r = lane / L;
+  Place<T> e[8] = {{p[0].v[0], 8 * l, 8 * l < a.C},         {p[0].v[1], 8 * l + 1, 8 * l + 1 < a.C}, {p[0].v[2], 8 * l + 2, 8 * l + 2 < a.C}, {p[0].v[3], 8 * l + 3, 8 * l + 3 < a.C},
+                   {p[0].v[4], 8 * l + 4, 8 * l + 4 < a.C}, {p[0].v[5], 8 * l + 5, 8 * l + 5 < a.C}, {p[0].v[6], 8 * l + 6, 8 * l + 6 < a.C}, {p[0].v[7], 8 * l + 7, 8 * l + 7 < a.C}};
+  Place<T>::order(e);
+  const Place<T> none(T(0), 0, false);
   for (int k = 0; k < a.k; ++k) {
-    const float v = lanes_all<L, Over::kMax>(t);
-    const bool fill = !(v > kLow);
-    int c = 0x7fffffff;
+    if (!e[0].template best_of_lanes<L>()) continue;
+    s_best[wave][r * a.k + k] = e[0];
 #pragma unroll
-    for (int j = 7; j >= 0; --j)
-      if ((left >> j & 1) && (fill ? !(float(p[0].v[j]) > kLow) : float(p[0].v[j]) == v)) c = 8 * l + j;
-    c = lanes_all<L, Over::kMin>(c);
-    if (c / 8 == l) {
-      left &= ~(1u << (c % 8));
-      t = kLow;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (left >> j & 1) t = fmaxf(t, float(p[0].v[j]));
-    }
-    if (writes) {
-      a.top[row * a.k + k] = mass.s == mass.s ? st.log_p(v) : NAN;
-      a.top_class[row * a.k + k] = c;
-    }
+    for (int j = 0; j + 1 < 8; ++j) e[j] = e[j + 1];
+    e[7] = none;
+  }
+  if (l == 0) s_stats[wave][r] = stats_of(mass);
+  wave_sync();
+  // the wave's rows lie one behind the other
+  const int64_t row0 = i - r;
+  const int count = int(a.n - row0 < kRows ? a.n - row0 : kRows) * a.k;
+  for (int q = lane; q < count; q += kWave) {
+    const Place<T> best = s_best[wave][q];
+    a.top[row0 * a.k + q] = s_stats[wave][uint32_t(q) / uint32_t(a.k)].log_p(best.score());
+    a.top_class[row0 * a.k + q] = best.cls();
   }
 }
 
-// Alternatives of few classes, many rows: a lane takes a row by itself, with no reduction across lanes.  The 64 rows of a wave come in whole pieces through LDS (rows of P pieces and a pad
-// word, so that lanes that read their own rows meet on no bank).  us, lanes in groups / a lane a row, best five of 233 000 rows of 41: 41.7 / 19.8; without alternatives 8.8 / 8.3 and the
-// gradient, which would go back that way, 9.9 / 12.5: not kept.
+// Few alternatives of few classes, many rows: a lane takes a row by itself, with no reduction across lanes.  The 64 rows of a wave come in whole pieces through LDS (rows of P pieces and a pad
+// word, so that lanes that read their own rows meet on no bank).  us, lanes in groups / a lane a row, 233 000 rows of 41 (fp16): the best one 18.5 / 11.2, five 22 / 18.3, eight 26.2 / 25.5, twenty
+// 34 / 76; of 16 five 9.5 / 8.8, eight 11 / 15; without alternatives 8.8 / 8.3 and the gradient, which would go back that way, 9.9 / 12.5: not kept.
 template <class T, int P>
 struct LaneRows {
   static constexpr int kPitch = 8 * P + 4 / int(sizeof(T));  // elements
@@ -741,9 +802,9 @@ static void with_flags(bool x, bool y, Call&& call) {
   else y ? call(no, yes) : call(no, no);
 }
 // a lane to a row, for its alternatives, where a row has more than one piece and the rows fill the chip
-constexpr int kLaneClasses = 64;
+constexpr int kLaneClasses = 64, kLaneTop = 5;
 constexpr int64_t kLaneRows = 65536;
-static bool by_lanes(int64_t n, int C, int k) { return k > 0 && C > 8 && C <= kLaneClasses && n >= kLaneRows; }
+static bool by_lanes(int64_t n, int C, int k) { return k > 0 && k <= kLaneTop && C > 8 && C <= kLaneClasses && n >= kLaneRows; }
 template <class Call>
 static void with_lane_pieces(int C, Call&& call) {
   switch ((C + 7) / 8) {

@@ -187,6 +187,32 @@ def test_many_rows_of_few_classes(hgnn, dev, n, C, pitch, offset, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("C", [1, 2, 7, 8, 9, 16, 17, 33, 64, 65, 128, 129, 247, 511, 512])
+def test_all_alternatives(hgnn, dev, C, dtype):
+    """As many alternatives as there may be, of rows that lanes share: equal scores, both zeros, few above -inf, the last rows of a wave; NaN takes places, but no two the same."""
+    rng = np.random.default_rng(C)
+    n, k = 75, min(C, 32)
+    x = rng.standard_normal((n, C)).astype(NP[dtype])
+    x[3:20] = np.round(x[3:20])
+    x[20:30] = np.where(rng.random((10, C)) < 0.5, NP[dtype](-0.0), NP[dtype](0.0))
+    x[30:50][rng.random((20, C)) < 0.8] = -np.inf
+    x[50], x[51] = -np.inf, np.finfo(NP[dtype]).min
+    x[52] = np.arange(C)
+    x[53] = -np.arange(C)
+    labels = rng.integers(0, C, n).astype(np.int32)
+    for m in sorted({1, (k + 1) // 2, k}):
+        check(hgnn, dev, x, labels, m, C)
+    x[60:70][rng.random((10, C)) < 0.3] = np.nan
+    x[60:70, C // 2] = np.nan
+    t, y, out = run(hgnn, dev, x, labels, k, C)
+    c, v = down(out["top_class"]), down(out["top_logprob"])
+    assert np.all((c >= 0) & (c < C)) and all(len(set(row)) == k for row in c)
+    assert np.all(np.isnan(v[60:70])) and not np.isnan(np.delete(v, range(60, 70), 0)).any()
+    keep = np.delete(np.arange(n), range(60, 70))
+    assert np.array_equal(c[keep], alternatives(x[keep], k))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
 @pytest.mark.parametrize("C", [6, 41, 300, 700, 5000, 70001])
 def test_masks_and_far_values(hgnn, dev, C, dtype):
     """Rows where the mask (-inf, or the type's lowest value) leaves little or nothing, equal scores, scores at the ends of the type, very sure ones."""
