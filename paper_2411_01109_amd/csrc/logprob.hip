@@ -187,11 +187,14 @@ __device__ __forceinline__ RawPiece<T> held_back(const RawPiece<T>& x) {
 struct Candidates {  // of a wave, in shared memory, in any order
   float v[kWave];
   int c[kWave];
-  int n;
 };
-__device__ __forceinline__ void add_candidate(Candidates& s, float v, int c) {
-  const int at = atomicAdd(&s.n, 1);
-  if (at < kWave) s.v[at] = v, s.c[at] = c;
+// adds those of the lanes that have one; n: how many there are, of which those behind the 64th are lost
+__device__ __forceinline__ void add_candidates(Candidates& s, int& n, bool one, float v, int c) {
+  const uint64_t ones = __ballot(one);
+  if (!ones) return;
+  const int at = n + int(__builtin_amdgcn_mbcnt_hi(uint32_t(ones >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(ones), 0)));
+  if (one && at < kWave) s.v[at] = v, s.c[at] = c;
+  n += __popcll(ones);
 }
 // no more than the k-th largest of the lanes' values: the k-th of the best of every four lanes, or of all lanes' (-inf where fewer than k are above it)
 __device__ __forceinline__ float kth_of_lanes(float v, int k) {
@@ -241,10 +244,9 @@ __device__ __forceinline__ Best sorted(float v, int c, int count, Candidates& s)
   wave_sync();
   return r;
 }
-__device__ __forceinline__ Best sorted(Candidates& s) {  // at most 64
+__device__ __forceinline__ Best sorted(Candidates& s, int count) {  // at most 64
   const int lane = threadIdx.x & (kWave - 1);
   wave_sync();
-  const int count = __builtin_amdgcn_readfirstlane(s.n);
   const float v = lane < count ? s.v[lane] : kLow;
   const int c = lane < count ? s.c[lane] : -1;
   wave_sync();
@@ -264,21 +266,18 @@ __device__ __forceinline__ void take_best(Best& best, float& least, int k, const
   if (!better) return;
   float bound = kLow;
   if (__popcll(better) > k) bound = kth_of_lanes(t > least ? t : kLow, k);
-  if (lane == 0) s.n = 0;
-  wave_sync();
-  if (lane < k && best.c >= 0) add_candidate(s, best.v, best.c);
+  int n = 0;
+  add_candidates(s, n, lane < k && best.c >= 0, best.v, best.c);
   const T above = bound > least ? lower(T(bound)) : T(least);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    if (!(top[i] > float(above))) continue;
+    if (!__ballot(top[i] > float(above))) continue;
     const RawPiece<T> p = held_back(x[i]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (p.v[j] > above) add_candidate(s, float(p.v[j]), c0 + 8 * kWave * i + 8 * lane + j);
+    for (int j = 0; j < 8; ++j) add_candidates(s, n, p.v[j] > above, float(p.v[j]), c0 + 8 * kWave * i + 8 * lane + j);
   }
-  wave_sync();
-  if (__builtin_amdgcn_readfirstlane(s.n) <= kWave) {
-    best = sorted(s);
+  if (n <= kWave) {
+    best = sorted(s, n);
     least = lane_value(best.v, k - 1);
     return;
   }
@@ -354,6 +353,34 @@ __device__ __forceinline__ void store_best(const ScoreArgs& a, int64_t row, cons
     a.top[row * a.k + lane] = stats_of(mass).log_p(best.v);
     a.top_class[row * a.k + lane] = best.c;
   }
+}
+
+// W lists of k, in shared memory, become one, by a wave: an entry's place is the number of those before it, in its own list and, found by halving, in the others
+template <int W>
+__device__ __forceinline__ Best joined_lists(const float (&v)[W][kMostTop], const int (&c)[W][kMostTop], int k, Candidates& s) {
+  const int lane = threadIdx.x & (kWave - 1);
+  s.v[lane] = kLow, s.c[lane] = -1;
+  wave_sync();
+  for (int q = lane; q < W * k; q += kWave) {
+    const int w = q / k, p = q - w * k;
+    if (c[w][p] < 0) continue;
+    const uint64_t mine = place_of(v[w][p], c[w][p]);
+    int lo[W - 1] = {}, at = p;
+    for (int step = kMostTop / 2; step > 0; step >>= 1)
+#pragma unroll
+      for (int o = 0; o < W - 1; ++o) {
+        const int u = o < w ? o : o + 1, x = lo[o] + step - 1;
+        if (x < k && place_of(v[u][x], c[u][x]) > mine) lo[o] += step;
+      }
+#pragma unroll
+    for (int o = 0; o < W - 1; ++o) {
+      const int u = o < w ? o : o + 1;
+      at += lo[o] + (lo[o] < k && place_of(v[u][lo[o]], c[u][lo[o]]) > mine ? 1 : 0);
+    }
+    if (at < k) s.v[at] = v[w][p], s.c[at] = c[w][p];
+  }
+  wave_sync();
+  return Best{s.v[lane], s.c[lane]};
 }
 
 // lists of falling scores, one for each lane (n entries, class -1: an empty one), become one; among equals the lowest class comes first
@@ -635,15 +662,7 @@ __global__ __launch_bounds__(kBlock) void logprob_row_kernel(ScoreArgs a) {
     mass = Mass<T>::none();
     if (lane < W) mass = Mass<T>{s_mass[lane][0], s_mass[lane][1], s_mass[lane][2]};
     mass = lanes_mass<kWave>(mass);
-    if (TOP && W * a.k <= kWave) {
-      const int w = lane / a.k, p = lane - w * a.k;
-      Best mine{kLow, 0x7fffffff - lane};  // (none; each in a place of its own)
-      if (w < W && s_class[w][p] >= 0) mine = Best{s_top[w][p], s_class[w][p]};
-      best = sorted(mine.v, mine.c, W * a.k, s_found[0]);
-      if (best.v == kLow) best.c = -1;
-    } else if (TOP) {
-      best = merge_lists(a.k, lane < W ? a.k : 0, [&](int p) { return Best{s_top[lane][p], s_class[lane][p]}; });
-    }
+    if constexpr (TOP && W > 1) best = joined_lists<W>(s_top, s_class, a.k, s_found[0]);
     if (a.splits > 1) {
       if (lane == 0) {
         float* const q = a.part + 3 * (row * a.splits + split);
@@ -679,21 +698,25 @@ __global__ __launch_bounds__(kWave) void logprob_join_kernel(ScoreArgs a) {
   const auto entry = [&](int p) { return Best{a.part_top[at + p], a.part_class[at + p]}; };
   // what is as good as the k-th of the parts' best, or, of many equal scores, one by one
   __shared__ Candidates s_found;
-  Best next;
-  if (lane < a.splits) next = entry(0);
-  const float bound = kth_of_lanes(next.v, a.k);
-  if (lane == 0) s_found.n = 0;
-  wave_sync();
-  for (int p = 0; p < a.k; ++p) {
-    const Best mine = next;
-    next = Best{};
-    if (lane < a.splits && p + 1 < a.k) next = entry(p + 1);
-    const bool here = mine.c >= 0 && mine.v >= bound;
-    if (!__ballot(here)) break;
-    if (here) add_candidate(s_found, mine.v, mine.c);
+  int n = 0;
+  if (a.splits * a.k <= kWave) {
+    Best mine;
+    if (lane < a.splits * a.k) mine = Best{a.part_top[row * a.splits * a.k + lane], a.part_class[row * a.splits * a.k + lane]};
+    add_candidates(s_found, n, mine.c >= 0, mine.v, mine.c);
+  } else {
+    Best next;
+    if (lane < a.splits) next = entry(0);
+    const float bound = kth_of_lanes(next.v, a.k);
+    for (int p = 0; p < a.k; ++p) {
+      const Best mine = next;
+      next = Best{};
+      if (lane < a.splits && p + 1 < a.k) next = entry(p + 1);
+      const bool here = mine.c >= 0 && mine.v >= bound;
+      if (!__ballot(here)) break;
+      add_candidates(s_found, n, here, mine.v, mine.c);
+    }
   }
-  wave_sync();
-  const Best best = s_found.n <= kWave ? sorted(s_found) : merge_lists(a.k, lane < a.splits ? a.k : 0, entry);
+  const Best best = n <= kWave ? sorted(s_found, n) : merge_lists(a.k, lane < a.splits ? a.k : 0, entry);
   store_best(a, row, mass, best);
 }
 

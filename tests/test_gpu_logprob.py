@@ -187,9 +187,9 @@ def test_many_rows_of_few_classes(hgnn, dev, n, C, pitch, offset, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
-@pytest.mark.parametrize("C", [1, 2, 7, 8, 9, 16, 17, 33, 64, 65, 128, 129, 247, 511, 512])
+@pytest.mark.parametrize("C", [1, 2, 7, 8, 9, 16, 17, 33, 64, 65, 128, 129, 247, 511, 512, 513, 2049, 3200, 20011])
 def test_all_alternatives(hgnn, dev, C, dtype):
-    """As many alternatives as there may be, of rows that lanes share: equal scores, both zeros, few above -inf, the last rows of a wave; NaN takes places, but no two the same."""
+    """As many alternatives as there may be, of rows that lanes share, of one for a wave or more: equal scores, both zeros, few above -inf, the last rows of a wave; NaN takes places, but no two the same."""
     rng = np.random.default_rng(C)
     n, k = 75, min(C, 32)
     x = rng.standard_normal((n, C)).astype(NP[dtype])
