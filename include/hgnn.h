@@ -535,7 +535,8 @@ hgnn_status hgnn_edge_colsum(const hgnn_csr* g, const hgnn_plan* p, int32_t H, c
  * What stands before the first layer (rows of a learned vertex table by id), behind the last one (log probabilities of
  * the vertices' labels) and between the gradients and the optimizer (their norm, unscaling and clipping).  These calls take
  * rows of any width and pitch: a tensor has to be aligned to its elements' type alone, nothing between or behind
- * its rows is read or written, and an output may overlap no other argument where nothing else is said. */
+ * its rows is written, nothing behind the last one read (what lies between rows may be, and never reaches a result), and an output may
+ * overlap no other argument where nothing else is said. */
 
 /* out[i, f] = fp16(scale * table[ids[i], f]) for i < n, f < F: rows of a table [V][ldt] of fp16 or fp32 by id.  An id outside [0, V) is padding: its
  * row is zeros.  out is [n][ldo].  F <= 65536 (HGNN_EUNSUPPORTED beyond). */
@@ -561,7 +562,7 @@ hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_
  *   top_logprob, top_class [n][k]: the k classes of the largest scores, falling, among equal scores the lowest class first (0 <= k <= 32, k <= C)
  * all fp32, the classes int32.  A class whose score is -inf is masked out: its probability is 0, and as an alternative it comes last.  A row of -inf
  * alone has the log probability -inf everywhere, the entropy 0 and the stats (-inf, 0).  A row that holds +inf or NaN is NaN everywhere (its
- * alternatives are some k different classes).  workspace is device memory of at least hgnn_logprob_workspace(n, C, k) bytes (4-byte aligned; 0: none is
+ * alternatives are some k different classes).  What a launch does not hold is refused with HGNN_EUNSUPPORTED: more than 2^30 classes, 2^34 scores or so.  workspace is device memory of at least hgnn_logprob_workspace(n, C, k) bytes (4-byte aligned; 0: none is
  * needed), owned by the caller and overwritten. */
 size_t hgnn_logprob_workspace(int64_t n, int32_t C, int32_t k);
 hgnn_status hgnn_logprob(int64_t n, int32_t C, hgnn_type type, const void* logits, int64_t ld, const int32_t* labels, float* logprob,
@@ -571,7 +572,7 @@ hgnn_status hgnn_logprob(int64_t n, int32_t C, hgnn_type type, const void* logit
 /* The gradient of the logits given those of logprob (g = dlogprob, [n]) and, unless dentropy is NULL, of the entropy (h = dentropy, [n]):
  *   dlogits[i,c] = g_i (1[c = labels[i]] - p[i,c]) - h_i p[i,c] (log p[i,c] + entropy[i])            [n][ldd], the type of the logits
  * with the stats and the entropy that hgnn_logprob gave.  A row without a label has g = 0; labels and dlogprob may both be NULL.  Masked classes and rows of
- * -inf alone have the gradient 0.  dlogits may be the logits themselves (with the same pitch). */
+ * -inf alone have the gradient 0.  Sizes as for hgnn_logprob.  dlogits may be the logits themselves (with the same pitch). */
 hgnn_status hgnn_logprob_grad(int64_t n, int32_t C, hgnn_type type, const void* logits, int64_t ld, const int32_t* labels,
                               const float* stats, const float* dlogprob, const float* entropy, const float* dentropy, void* dlogits,
                               int64_t ldd, void* stream);

@@ -4,7 +4,8 @@
 
 #include <algorithm>
 #include <cmath>
-#include <vector>
+#include <memory>
+#include <new>
 
 #include "common.h"
 #include "rows.h"
@@ -186,12 +187,14 @@ static hgnn_status check_grads(const char* who, int32_t count, const hgnn_grad* 
 }
 
 static hgnn_status check_outputs(const char* who, int32_t count, const hgnn_grad* g) {
-  std::vector<const void*> outs;
-  outs.reserve(size_t(count));
+  if (count < 2) return HGNN_OK;
+  const std::unique_ptr<const void*[]> outs(new (std::nothrow) const void*[size_t(count)]);
+  HGNN_REQUIRE(outs != nullptr, HGNN_ENOMEM, "%s: host allocation failed", who);
+  const void** end = outs.get();
   for (int i = 0; i < count; ++i)
-    if (g[i].rows > 0 && g[i].cols > 0) outs.push_back(g[i].out ? g[i].out : g[i].grad);
-  std::sort(outs.begin(), outs.end());
-  HGNN_REQUIRE(std::adjacent_find(outs.begin(), outs.end()) == outs.end(), HGNN_EINVAL, "%s: the same output twice", who);
+    if (g[i].rows > 0 && g[i].cols > 0) *end++ = g[i].out ? g[i].out : g[i].grad;
+  std::sort(outs.get(), end);
+  HGNN_REQUIRE(std::adjacent_find(outs.get(), end) == end, HGNN_EINVAL, "%s: the same output twice", who);
   return HGNN_OK;
 }
 

@@ -387,7 +387,7 @@ static hgnn_status table_grad(const TableGradArgs& a, hipStream_t s) {
     const int64_t zeros = ADD ? 0 : ceil_div(a.V, int64_t(kZeroRows) * kWavesPerBlock);
     const unsigned fy = unsigned(ceil_div(a.F, 8 * L));  // 1 up to 512 features
     auto go = [&]() -> hgnn_status {
-      HGNN_REQUIRE(a.blocks + zeros <= 0x7fffffff, HGNN_EUNSUPPORTED, "hgnn_embedding_grad: grid too large");
+      HGNN_REQUIRE(a.blocks + zeros <= kMostBlocks, HGNN_EUNSUPPORTED, "hgnn_embedding_grad: grid too large");
       table_grad_kernel<T, ADD, L><<<dim3(unsigned(a.blocks + zeros), fy), kBlock, 0, s>>>(a);
       HGNN_LAUNCH_CHECK("table_grad_kernel");
       if (a.blocks > 1) {
@@ -414,7 +414,7 @@ hgnn_status hgnn_embedding(int64_t n, int32_t F, const int32_t* ids, int32_t V, 
   HGNN_REQUIRE(n >= 0 && F > 0 && V >= 0, HGNN_EINVAL, "%s: n = %lld, F = %d, V = %d", who, static_cast<long long>(n), F, V);
   HGNN_REQUIRE(known_type(table_type), HGNN_EINVAL, "%s: unknown type %d", who, int(table_type));
   HGNN_REQUIRE(ldt >= F && ldo >= F, HGNN_EINVAL, "%s: leading dimension smaller than F", who);
-  HGNN_REQUIRE(F <= 65536, HGNN_EUNSUPPORTED, "%s: F = %d above 65536", who, F);
+  HGNN_REQUIRE(F <= 65536 && n <= (int64_t(1) << 40), HGNN_EUNSUPPORTED, "%s: F = %d above 65536, or n = %lld above 2^40", who, F, static_cast<long long>(n));
   if (n == 0) return HGNN_OK;
   HGNN_REQUIRE(ids && out && (table || V == 0), HGNN_EINVAL, "%s: NULL argument", who);
   HGNN_REQUIRE(aligned_to_type(ids, HGNN_F32) && aligned_to_type(table, table_type) && aligned_to_type(out, HGNN_F16), HGNN_EINVAL,
@@ -426,7 +426,7 @@ hgnn_status hgnn_embedding(int64_t n, int32_t F, const int32_t* ids, int32_t V, 
     auto go = [&]() -> hgnn_status {
       const bool many = n * L >= kFewLookups, past = double(n) * F * sizeof(half_t) >= kPastBytes;
       const int64_t blocks = ceil_div(n, int64_t(kBlock / L) * (many ? kLookups : 1));
-      HGNN_REQUIRE(blocks <= 0x7fffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
+      HGNN_REQUIRE(blocks <= kMostBlocks, HGNN_EUNSUPPORTED, "%s: grid too large", who);
       const dim3 grid{unsigned(blocks)};
       hipStream_t s = static_cast<hipStream_t>(stream);
       auto launch = [&](auto type) {

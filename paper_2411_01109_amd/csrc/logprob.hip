@@ -860,7 +860,7 @@ static hgnn_status logprob(ScoreArgs& a, hipStream_t s) {
   const int N = a.k > 0 ? 1 : row_pieces(a.n, a.C, sizeof(T) == 2), L = group_lanes(a.C, N);
   const bool lanes = by_lanes(a.n, a.C, a.k);
   const int64_t blocks = lanes ? ceil_div(a.n, kBlock) : group ? ceil_div(a.n * L, kBlock) : (waves ? ceil_div(a.n, kWavesPerBlock) : a.n * a.splits);
-  HGNN_REQUIRE(a.n <= (int64_t(1) << 40) && blocks <= 0x7fffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
+  HGNN_REQUIRE(blocks <= kMostBlocks, HGNN_EUNSUPPORTED, "%s: grid too large", who);
   const dim3 grid{unsigned(blocks)};
   a.span = waves ? a.C : int(ceil_div(ceil_div(a.C, a.splits), 8) * 8);
   with_flags(a.entropy != nullptr, a.k > 0, [&](auto entropy, auto top) {
@@ -895,8 +895,7 @@ static hgnn_status logprob_grad(ScoreGradArgs& a, hipStream_t s) {
   // Long rows of large outputs are written past the caches.  us, the log probabilities and this, through / past: 4096 rows of 50 021 (fp16) 257 / 232,
   // 1024 68.5 / 59; rows of 41 and 100 classes, whose ends share lines, 19 / 28, 159 / 214.
   const bool past = a.n * double(a.C) * sizeof(T) >= kPastBytes;
-  HGNN_REQUIRE(a.n <= (int64_t(1) << 40) && ceil_div(a.n * a.chunks * L, kBlock) <= 0x7fffffff && (group || a.n * a.chunks <= 0xffffffff), HGNN_EUNSUPPORTED,
-               "hgnn_logprob_grad: grid too large");
+  HGNN_REQUIRE(double(a.n) * a.chunks * L <= double(kMostBlocks) * kBlock, HGNN_EUNSUPPORTED, "hgnn_logprob_grad: grid too large");
   const dim3 grid{unsigned(ceil_div(a.n * a.chunks * L, kBlock))};
   with_flags(a.dentropy != nullptr, group ? N == 2 : past, [&](auto entropy, auto flag) {
     constexpr bool E = decltype(entropy)::value, F = decltype(flag)::value;
@@ -948,7 +947,7 @@ hgnn_status hgnn_logprob(int64_t n, int32_t C, hgnn_type type, const void* logit
   HGNN_REQUIRE(ld >= C, HGNN_EINVAL, "%s: leading dimension smaller than C", who);
   HGNN_REQUIRE(k >= 0 && k <= C, HGNN_EINVAL, "%s: %d alternatives of %d classes", who, k, C);
   HGNN_REQUIRE(k <= kMostTop, HGNN_EUNSUPPORTED, "%s: more than %d alternatives", who, kMostTop);
-  HGNN_REQUIRE(C <= (1 << 30), HGNN_EUNSUPPORTED, "%s: C = %d above 2^30", who, C);
+  HGNN_REQUIRE(C <= (1 << 30) && n <= (int64_t(1) << 40), HGNN_EUNSUPPORTED, "%s: C = %d above 2^30, or n = %lld above 2^40", who, C, static_cast<long long>(n));
   if (n == 0) return HGNN_OK;
   HGNN_REQUIRE(logits && (k == 0 || (top_logprob && top_class)), HGNN_EINVAL, "%s: NULL argument", who);
   HGNN_REQUIRE((labels == nullptr) == (logprob_out == nullptr), HGNN_EINVAL, "%s: labels and logprob go together", who);
@@ -971,7 +970,7 @@ hgnn_status hgnn_logprob_grad(int64_t n, int32_t C, hgnn_type type, const void* 
   HGNN_REQUIRE(n >= 0 && C > 0, HGNN_EINVAL, "%s: n = %lld, C = %d", who, static_cast<long long>(n), C);
   HGNN_REQUIRE(known_type(type), HGNN_EINVAL, "%s: unknown type %d", who, int(type));
   HGNN_REQUIRE(ld >= C && ldd >= C, HGNN_EINVAL, "%s: leading dimension smaller than C", who);
-  HGNN_REQUIRE(C <= (1 << 30), HGNN_EUNSUPPORTED, "%s: C = %d above 2^30", who, C);
+  HGNN_REQUIRE(C <= (1 << 30) && n <= (int64_t(1) << 40), HGNN_EUNSUPPORTED, "%s: C = %d above 2^30, or n = %lld above 2^40", who, C, static_cast<long long>(n));
   HGNN_REQUIRE((labels == nullptr) == (dlogprob == nullptr), HGNN_EINVAL, "%s: labels and dlogprob go together", who);
   HGNN_REQUIRE((dentropy == nullptr) || entropy, HGNN_EINVAL, "%s: dentropy without the entropy", who);
   if (n == 0) return HGNN_OK;

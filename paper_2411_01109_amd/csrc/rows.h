@@ -206,6 +206,9 @@ struct Part<T, 4> {
 // 35 / 38, 122 MB 62 / 66, 244 MB 126 / 121 (the rows alone: 20 / 16, 41 / 31, 81 / 58).
 constexpr double kPastBytes = 192. * (1 << 20);
 
+// what a launch holds: fewer than 2^32 lanes
+constexpr int64_t kMostBlocks = 0xffffffffll / kBlock;
+
 inline bool known_type(hgnn_type t) { return t == HGNN_F16 || t == HGNN_F32; }
 inline bool aligned_to_type(const void* p, hgnn_type t) { return (reinterpret_cast<uintptr_t>(p) & (t == HGNN_F32 ? 3u : 1u)) == 0; }
 // elements from a tensor's first to its last: what a row's last piece may be read from

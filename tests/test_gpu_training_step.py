@@ -1,5 +1,7 @@
 """A training step from learned vertex features to clipped gradients: lookup, GCN layer, projection to class scores, loss, every gradient, clipping.  Every stage is held to its
 definition in 64 bits on the values that the stage before it has left; the whole of it is captured, replayed and run beside other work."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -282,3 +284,28 @@ def test_refusals_of_the_binding(hgnn, dev, what):
         REFUSED[what](hgnn, s)
     torch.cuda.synchronize()
     assert same(s.outputs(), before)
+
+
+def test_tensors_of_another_device(hgnn, dev, monkeypatch):
+    """Tensors of a device that is not the current one are refused by both routes (the streams and launches would be the current one's): nothing has changed."""
+    b = hgnn.binding
+    s = Step(hgnn, dev, seed=7)
+    before = s.outputs()
+    calls = [lambda: hgnn.hgnn_embedding(s.ids, s.table, s.x), lambda: hgnn.hgnn_embedding_grad(s.ids, s.dx, s.dT, s.ws_t),
+             lambda: hgnn.hgnn_logprob(s.logits, s.labels, s.logprob, stats=s.stats), lambda: hgnn.hgnn_logprob_grad(s.logits, s.labels, s.stats, s.dlogprob, s.dlogits),
+             lambda: hgnn.hgnn_grad_norm([s.dT], s.norm, s.ws_n), lambda: hgnn.hgnn_grad_clip([s.dT], 1.0, s.norm, s.ws_n)]
+    native, addresses = b._calls, {n: ctypes.cast(getattr(hgnn.load(), n), ctypes.c_void_p).value for n in hgnn.EXPORTS}
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    native.bind(addresses, b._raw_stream, lambda: 1)
+    try:
+        for call in calls:
+            with pytest.raises(ValueError, match="device 0 while device 1"):
+                call()
+    finally:
+        native.bind(addresses, b._raw_stream, b._current_device)
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert same(s.outputs(), before)
+    for call in calls:
+        call()
+    torch.cuda.synchronize()

@@ -23,6 +23,8 @@ def test_lookup_refuses(lib, hgnn):
         assert call(**bad) == EINVAL, bad
         assert b"hgnn_embedding" in lib.hgnn_last_error()
     assert call(F=65537, ldt=70000, ldo=70000) == EUNSUP
+    for many in (dict(n=(1 << 40) + 1), dict(n=1 << 38), dict(n=1 << 62)):
+        assert call(**many) == EUNSUP, many
     assert call(n=0, ids=None, table=None, out=None) == 0  # nothing to do
 
 
@@ -59,6 +61,8 @@ def test_logprob_refuses(lib, hgnn):
         assert b"hgnn_logprob" in lib.hgnn_last_error()
     assert call(k=33) == EUNSUP and call(c=(1 << 30) + 1, ld=1 << 31) == EUNSUP
     assert call(n=0, x=None, tv=None, tc=None) == 0
+    for many in (dict(n=(1 << 40) + 1), dict(n=1 << 33, c=500, ld=500), dict(n=1 << 28, c=4000, ld=4000), dict(n=1 << 62)):
+        assert call(**many) == EUNSUP, many
     assert hgnn.hgnn_logprob_workspace(0, 100, 0) == 0 and hgnn.hgnn_logprob_workspace(1000, 41, 5) == 0
 
 
@@ -72,6 +76,8 @@ def test_logprob_gradient_refuses(lib, hgnn):
         assert call(**bad) == EINVAL, bad
         assert b"hgnn_logprob_grad" in lib.hgnn_last_error()
     assert call(n=0, x=None, st=None, dx=None) == 0
+    for many in (dict(n=(1 << 40) + 1), dict(n=1 << 40, c=1 << 30, ld=1 << 30, ldd=1 << 30), dict(n=1 << 33, c=500, ld=500, ldd=500), dict(n=1 << 62)):
+        assert call(**many) == hgnn.HGNN_EUNSUPPORTED, many
 
 
 def test_clip_refuses(lib, hgnn):
