@@ -539,7 +539,7 @@ hgnn_status hgnn_edge_colsum(const hgnn_csr* g, const hgnn_plan* p, int32_t H, c
  * overlap no other argument where nothing else is said. */
 
 /* out[i, f] = fp16(scale * table[ids[i], f]) for i < n, f < F: rows of a table [V][ldt] of fp16 or fp32 by id.  An id outside [0, V) is padding: its
- * row is zeros.  out is [n][ldo].  F <= 65536 (HGNN_EUNSUPPORTED beyond). */
+ * row is zeros, whatever the scale.  out is [n][ldo].  F <= 65536 (HGNN_EUNSUPPORTED beyond). */
 hgnn_status hgnn_embedding(int64_t n, int32_t F, const int32_t* ids, int32_t V, hgnn_type table_type, const void* table,
                            int64_t ldt, float scale, hgnn_half* out, int64_t ldo, void* stream);
 
@@ -571,8 +571,8 @@ hgnn_status hgnn_logprob(int64_t n, int32_t C, hgnn_type type, const void* logit
 
 /* The gradient of the logits given those of logprob (g = dlogprob, [n]) and, unless dentropy is NULL, of the entropy (h = dentropy, [n]):
  *   dlogits[i,c] = g_i (1[c = labels[i]] - p[i,c]) - h_i p[i,c] (log p[i,c] + entropy[i])            [n][ldd], the type of the logits
- * with the stats and the entropy that hgnn_logprob gave.  A row without a label has g = 0; labels and dlogprob may both be NULL.  Masked classes and rows of
- * -inf alone have the gradient 0.  Sizes as for hgnn_logprob.  dlogits may be the logits themselves (with the same pitch). */
+ * with the stats and the entropy that hgnn_logprob gave.  A row without a label has g = 0; labels and dlogprob may both be NULL.  The gradient of a masked
+ * class is 0 (g_i if it is the label), and of a row of -inf alone 0 whatever g_i and h_i are.  Sizes as for hgnn_logprob.  dlogits may be the logits themselves (with the same pitch). */
 hgnn_status hgnn_logprob_grad(int64_t n, int32_t C, hgnn_type type, const void* logits, int64_t ld, const int32_t* labels,
                               const float* stats, const float* dlogprob, const float* entropy, const float* dentropy, void* dlogits,
                               int64_t ldd, void* stream);

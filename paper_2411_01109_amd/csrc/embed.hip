@@ -40,9 +40,10 @@ __global__ __launch_bounds__(kBlock) void embedding_kernel(LookupArgs a) {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       if (i0 + u * G >= a.n) break;
+      const float scale = uint32_t(id[u]) < uint32_t(a.V) ? a.scale : 0.f;  // zeros for padding, whatever the scale
       float y[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = float(x[u].v[j]) * a.scale;
+      for (int j = 0; j < 8; ++j) y[j] = float(x[u].v[j]) * scale;
       Part<half_t, 8>::template store<PAST>(a.out + (i0 + u * G) * a.ldo + f, a.F - f, y);
     }
   }

@@ -76,6 +76,15 @@ def test_lookup_takes_values_as_they_are(hgnn, dev):
     assert np.array_equal(got[0], np.array([np.inf, -np.inf, np.nan, 65504, np.inf, 0], np.float16), equal_nan=True) and np.all(got[1] == 0)
 
 
+@pytest.mark.parametrize("scale", [float("inf"), float("nan"), 1e30])
+def test_padding_is_zero_whatever_the_scale(hgnn, dev, scale):
+    T = np.ones((3, 11), np.float32)
+    out = torch.full((5, 11), FILL, dtype=torch.float16, device=dev)
+    hgnn.hgnn_embedding(up(np.array([3, 2, -1, 0, -2 ** 31], np.int32), dev), up(T, dev), out, scale=scale)
+    got = down(out)
+    assert np.all(got[[0, 2, 4]] == 0) and np.array_equal(got[[1, 3]], np.full((2, 11), np.inf if scale == scale else np.nan, np.float16), equal_nan=True)
+
+
 def test_lookup_far_rows(hgnn, dev):
     """Rows beyond 2^31 elements of a table, and beyond 2^31 bytes of the output."""
     V, F = 2 ** 31 // 256 + 7, 256

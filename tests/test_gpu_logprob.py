@@ -285,6 +285,26 @@ def test_parts_alone(hgnn, dev):
         assert torch.equal(dx, dz)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("C", [6, 300, 5000])
+def test_gradient_of_masked_rows(hgnn, dev, C, dtype):
+    """A row of -inf alone has no gradient, whatever comes from above; a masked label has its row's."""
+    x = np.full((4, C), -np.inf, NP[dtype])
+    x[1, :3] = 1.0  # and the label 4 is masked
+    x[3] = 0.5
+    labels = np.array([1, 4, 0, -1], np.int32)
+    t, y, out = run(hgnn, dev, x, labels, 0, C)
+    g = np.array([np.nan, 2.0, np.inf, np.nan], np.float32)  # the last row has no label
+    h = np.array([np.nan, 0.0, -np.inf, 0.0], np.float32)
+    dx = torch.full_like(t, FILL)
+    hgnn.hgnn_logprob_grad(t, y, out["stats"], up(g, dev), dx, entropy=out["entropy"], dentropy=up(h, dev))
+    got = down(dx).astype(np.float64)
+    assert np.all(got[[0, 2, 3]] == 0)
+    want = np.zeros(C)
+    want[:3], want[4] = -2 / 3, 2.0
+    assert np.all(np.abs(got[1] - want) <= np.abs(want) * (2.0 ** -11 if dtype == torch.float16 else 16 * U))
+
+
 def test_gradient_by_differences(hgnn, dev):
     """Of the values themselves: central differences of log probability and entropy in 64 bits of the host against the gradient of the call."""
     rng = np.random.default_rng(4)
