@@ -309,3 +309,37 @@ def test_tensors_of_another_device(hgnn, dev, monkeypatch):
     for call in calls:
         call()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_nothing_and_the_least(hgnn, dev, native, monkeypatch):
+    """No positions, no rows, no classes asked for, no tensors, tensors without elements, of no axis or several: every one is a call like another."""
+    if not native:
+        monkeypatch.setattr(hgnn.binding, "_calls", None)
+    zeros = lambda *s, t=torch.float32: torch.zeros(s, dtype=t, device=dev)  # noqa: E731
+    ones = lambda *s, t=torch.float32: torch.ones(s, dtype=t, device=dev)  # noqa: E731
+    h, i = torch.float16, torch.int32
+    hgnn.hgnn_embedding(zeros(0, t=i), zeros(5, 8), zeros(0, 8, t=h))
+    for table, want in ((zeros(0, 8), 0), (ones(1, 8), 24), (ones(2, 9)[:, 1:], 24)):
+        out = ones(3, 8, t=h)
+        hgnn.hgnn_embedding(zeros(3, t=i), table, out)
+        assert float(out.sum()) == want
+    dT = ones(5, 8)
+    hgnn.hgnn_embedding_grad(zeros(0, t=i), zeros(0, 8, t=h), dT, None)
+    assert float(dT.abs().sum()) == 0
+    hgnn.hgnn_embedding_grad(zeros(3, t=i), zeros(3, 8, t=h), zeros(0, 8), zeros(4096, t=torch.uint8))
+    hgnn.hgnn_logprob(zeros(0, 7, t=h), zeros(0, t=i), zeros(0), stats=zeros(0, 2), entropy=zeros(0), top_logprob=zeros(0, 3), top_class=zeros(0, 3, t=i))
+    hgnn.hgnn_logprob(zeros(3, 7, t=h), None, None)
+    hgnn.hgnn_logprob(zeros(3, 7, t=h), None, None, top_logprob=zeros(3, 0), top_class=zeros(3, 0, t=i))
+    hgnn.hgnn_logprob_grad(zeros(0, 7, t=h), zeros(0, t=i), zeros(0, 2), zeros(0), zeros(0, 7, t=h))
+    dx = ones(3, 7, t=h)
+    hgnn.hgnn_logprob_grad(zeros(3, 7, t=h), None, zeros(3, 2), None, dx)
+    assert float(dx.abs().sum()) == 0
+    ws, norm = torch.empty(hgnn.hgnn_grad_norm_workspace(), dtype=torch.uint8, device=dev), ones(1)
+    for tensors, want in (([], 0.0), ([zeros(0), zeros(4, 0), zeros(0, 4)], 0.0), ([zeros(0), ones(), ones(2, 3, 4)], 5.0), ([ones(5, 8)[:, :3], ones(1, t=h)], 4.0)):
+        for call in (lambda: hgnn.hgnn_grad_norm(tensors, norm, ws), lambda: hgnn.hgnn_grad_clip(tensors, 2.0, norm, ws)):
+            norm.fill_(7)
+            call()
+            assert float(norm) == want
+        assert all(bool((t == min(1.0, 2.0 / max(want, 1e-9))).all()) for t in tensors)
+    torch.cuda.synchronize()
