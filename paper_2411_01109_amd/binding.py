@@ -671,6 +671,13 @@ def _two(name: str, t: torch.Tensor):
     return t.shape[0], t.shape[1]
 
 
+def _int32(name: str, n: int) -> int:
+    """A number for a 32-bit argument (ctypes would cut it)."""
+    if not 0 <= n < 1 << 31:
+        raise ValueError(f"{name} = {n} does not fit an int32")
+    return n
+
+
 def hgnn_embedding(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0, stream=None) -> None:
     """out[i] = scale * table[ids[i]]: int32 ids, a table of fp16 or fp32 rows, out fp16; an id that is no row of the table gives zeros."""
     if _calls is not None and _done(_calls.embedding(ids, table, out, scale, stream)):
@@ -681,11 +688,11 @@ def hgnn_embedding(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, sc
     T, ldt = _rows("table", table, V, F)
     o, ldo = _rows("out", out, n, F)
     _ptr(out, torch.float16)
-    _check(load().hgnn_embedding(n, F, _dense("ids", ids, torch.int32, n), V, _type(table), T, ldt, scale, o, ldo, _stream(stream)))
+    _check(load().hgnn_embedding(n, _int32("F", F), _dense("ids", ids, torch.int32, n), _int32("the number of rows of the table", V), _type(table), T, ldt, scale, o, ldo, _stream(stream)))
 
 
 def hgnn_embedding_grad_workspace(n: int, F: int, V: int) -> int:
-    return load().hgnn_embedding_grad_workspace(n, F, V)
+    return load().hgnn_embedding_grad_workspace(n, _int32("F", F), _int32("V", V))
 
 
 def hgnn_embedding_grad(ids: torch.Tensor, dY: torch.Tensor, dT: torch.Tensor, workspace: Optional[torch.Tensor], scale: float = 1.0,
@@ -701,12 +708,12 @@ def hgnn_embedding_grad(ids: torch.Tensor, dY: torch.Tensor, dT: torch.Tensor, w
     T, ldt = _rows("dT", dT, V, F)
     _ptr(dY, torch.float16)
     ws, bytes = _room(workspace)
-    _check(load().hgnn_embedding_grad(n, F, _dense("ids", ids, torch.int32, n), V, y, ldy, scale, 1 if accumulate else 0, _type(dT), T, ldt, ws, bytes,
+    _check(load().hgnn_embedding_grad(n, _int32("F", F), _dense("ids", ids, torch.int32, n), _int32("the number of rows of dT", V), y, ldy, scale, 1 if accumulate else 0, _type(dT), T, ldt, ws, bytes,
                                       _stream(stream)))
 
 
 def hgnn_logprob_workspace(n: int, C: int, k: int = 0) -> int:
-    return load().hgnn_logprob_workspace(n, C, k)
+    return load().hgnn_logprob_workspace(n, _int32("C", C), _int32("k", k))
 
 
 def hgnn_logprob(logits: torch.Tensor, labels: Optional[torch.Tensor], logprob: Optional[torch.Tensor], stats: Optional[torch.Tensor] = None,
@@ -724,8 +731,8 @@ def hgnn_logprob(logits: torch.Tensor, labels: Optional[torch.Tensor], logprob: 
     single = torch.float32
     if (top_class is None) != (top_logprob is None):
         raise ValueError("top_logprob and top_class go together")
-    _check(load().hgnn_logprob(n, C, _type(logits), x, ld, _dense("labels", labels, torch.int32, n), _dense("logprob", logprob, single, n),
-                               _dense("stats", stats, single, n, 2), _dense("entropy", entropy, single, n), k,
+    _check(load().hgnn_logprob(n, _int32("the number of classes", C), _type(logits), x, ld, _dense("labels", labels, torch.int32, n), _dense("logprob", logprob, single, n),
+                               _dense("stats", stats, single, n, 2), _dense("entropy", entropy, single, n), _int32("k", k),
                                _dense("top_logprob", top_logprob, single, n, k), _dense("top_class", top_class, torch.int32, n, k), ws, bytes, _stream(stream)))
 
 
@@ -740,7 +747,7 @@ def hgnn_logprob_grad(logits: torch.Tensor, labels: Optional[torch.Tensor], stat
     d, ldd = _rows("dlogits", dlogits, n, C)
     _ptr(dlogits, logits.dtype)
     single = torch.float32
-    _check(load().hgnn_logprob_grad(n, C, _type(logits), x, ld, _dense("labels", labels, torch.int32, n), _dense("stats", stats, single, n, 2),
+    _check(load().hgnn_logprob_grad(n, _int32("the number of classes", C), _type(logits), x, ld, _dense("labels", labels, torch.int32, n), _dense("stats", stats, single, n, 2),
                                     _dense("dlogprob", dlogprob, single, n), _dense("entropy", entropy, single, n),
                                     _dense("dentropy", dentropy, single, n), d, ldd, _stream(stream)))
 

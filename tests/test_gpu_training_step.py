@@ -343,3 +343,52 @@ def test_nothing_and_the_least(hgnn, dev, native, monkeypatch):
             assert float(norm) == want
         assert all(bool((t == min(1.0, 2.0 / max(want, 1e-9))).all()) for t in tensors)
     torch.cuda.synchronize()
+
+
+def test_sizes_beyond_int32(hgnn, dev):
+    """Rows and classes that a 32-bit number would cut to a few are refused, not cut."""
+    far = torch.empty(2 ** 32 + 9, dtype=torch.float16, device=dev)
+    single, ids = torch.zeros(1, device=dev), torch.zeros(1, dtype=torch.int32, device=dev)
+    stats, out = torch.zeros((1, 2), device=dev), torch.zeros((1, 1), dtype=torch.float16, device=dev)
+    ws = torch.empty(4096, dtype=torch.uint8, device=dev)
+    for call in (lambda: hgnn.hgnn_embedding(ids, far[:, None], out), lambda: hgnn.hgnn_embedding_grad(ids, out, far[:, None], ws),
+                 lambda: hgnn.hgnn_logprob(far[None], ids, single), lambda: hgnn.hgnn_logprob_grad(far[None], ids, stats, single, far[None]),
+                 lambda: hgnn.hgnn_embedding_grad_workspace(1, 1, 2 ** 32 + 9), lambda: hgnn.hgnn_logprob_workspace(1, 2 ** 32 + 9, 1)):
+        with pytest.raises(ValueError, match="int32"):
+            call()
+
+
+def test_two_graphs_share_a_workspace(hgnn, dev):
+    """Captured calls of different sizes with one workspace, replayed in turn: every one finds in it only what it has written itself."""
+    rng = np.random.default_rng(8)
+    norm_ws = torch.empty(hgnn.hgnn_grad_norm_workspace(), dtype=torch.uint8, device=dev)
+    sizes = ((3000, 400, 24, 5003), (20011, 50, 40, 3001))
+    need = max(max(hgnn.hgnn_embedding_grad_workspace(n, F, V), hgnn.hgnn_logprob_workspace(3, C, 20)) for n, V, F, C in sizes)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    runs = []
+    for n, V, F, C in sizes:
+        ids = up(rng.integers(-1, V, n).astype(np.int32), dev)
+        dY, x = up(rng.standard_normal((n, F)).astype(np.float16), dev), up(rng.standard_normal((3, C)).astype(np.float32), dev)
+        y = up(rng.integers(0, C, 3).astype(np.int32), dev)
+        outs = (torch.zeros((V, F), device=dev), torch.zeros(3, device=dev), torch.zeros((3, 20), device=dev), torch.zeros((3, 20), dtype=torch.int32, device=dev),
+                torch.zeros(1, device=dev), torch.zeros((n, F), device=dev))
+
+        def run(ids=ids, dY=dY, x=x, y=y, outs=outs):
+            hgnn.hgnn_embedding_grad(ids, dY, outs[0], ws)
+            hgnn.hgnn_logprob(x, y, outs[1], top_logprob=outs[2], top_class=outs[3], workspace=ws)
+            hgnn.hgnn_grad_clip([dY], 1.0, outs[4], norm_ws, outs=[outs[5]])
+        run()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in outs]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+        runs.append((graph, run, outs, want))
+    for turn in range(4):
+        for graph, run, outs, want in runs if turn % 2 else runs[::-1]:
+            for t in outs:
+                t.fill_(7)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, want)), turn
+        runs[turn % 2][1]()  # and an eager one between them
