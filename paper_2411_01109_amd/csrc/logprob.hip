@@ -799,8 +799,6 @@ static int row_pieces(int64_t n, int C, bool wide) {
   if (C <= 8 || n * group_lanes(C, 1) < int64_t(1) << 20) return 1;
   return wide && C > 256 ? 4 : 2;
 }
-// What a group of lanes holds: up to 512 classes, 2048 without alternatives (200 000 rows of 520 and their gradient, by waves / groups: 203 / 191 us, of 600 189 / 172).
-static bool by_groups(int C, int k) { return C <= (k > 0 ? 1 : 4) * kGroupClasses; }
 template <class Call>
 static void with_pieces(int pieces, Call&& call) {
   if (pieces == 1) call(std::integral_constant<int, 1>());
@@ -809,9 +807,17 @@ static void with_pieces(int pieces, Call&& call) {
 }
 constexpr int kWaveClasses = 4096;        // up to so many, a row is a wave's where there are rows enough
 static bool by_waves(int64_t n, int C) { return C <= kWaveClasses && n >= 4096; }
+// What a group of lanes holds: up to 512 classes, 2048 without alternatives (200 000 rows of 520 and their gradient, by waves / groups: 203 / 191 us, of 600 189 / 172).
+// Many alternatives of rows that take all lanes of a wave are found sooner among candidates (us, by groups / by waves, 100 000 rows of 500, fp32: best twenty 171 / 109, five 85 / 77; of 512, fp16, 127 / 122, 77 / 83; 400, best one
+// 60 / 75; 212 828 of 247, two to a wave, best twenty 132 / 274).
+constexpr int kGroupTop = 8;
+static bool by_groups(int64_t n, int C, int k) {
+  if (k > kGroupTop && C > kGroupClasses / 2 && by_waves(n, C)) return false;
+  return C <= (k > 0 ? 1 : 4) * kGroupClasses;
+}
 // Workgroups of a row: as many as fill the chip, of no less than a piece for every lane
 static int splits_of(int64_t n, int C, int k) {
-  if (by_groups(C, k) || by_waves(n, C)) return 1;
+  if (by_groups(n, C, k) || by_waves(n, C)) return 1;
   const int64_t most = ceil_div(C, int64_t(8) * kWave * kWavesPerBlock), want = ceil_div(1024, n), s = most < want ? most : want;
   return int(s < 1 ? 1 : (s > kMostSplits ? kMostSplits : s));
 }
@@ -856,7 +862,7 @@ static void with_group(int lanes, Call&& call) {
 template <class T>
 static hgnn_status logprob(ScoreArgs& a, hipStream_t s) {
   const char* who = "hgnn_logprob";
-  const bool group = by_groups(a.C, a.k), waves = by_waves(a.n, a.C);
+  const bool group = by_groups(a.n, a.C, a.k), waves = by_waves(a.n, a.C);
   const int N = a.k > 0 ? 1 : row_pieces(a.n, a.C, sizeof(T) == 2), L = group_lanes(a.C, N);
   const bool lanes = by_lanes(a.n, a.C, a.k);
   const int64_t blocks = lanes ? ceil_div(a.n, kBlock) : group ? ceil_div(a.n * L, kBlock) : (waves ? ceil_div(a.n, kWavesPerBlock) : a.n * a.splits);

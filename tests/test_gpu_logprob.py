@@ -153,7 +153,8 @@ def test_shapes(hgnn, dev, n, C, pitch, offset, k, dtype):
         check_grad(hgnn, dev, x, labels, pitch, offset, t, y, out, r, with_entropy, rng)
 
 
-ROWS = [(65536, 9, 9, 0, 9), (66001, 41, 48, 0, 5), (70000, 16, 17, 1, 2), (65800, 64, 64, 0, 20), (80001, 57, 59, 3, 0), (68000, 24, 24, 0, 1), (70000, 47, 47, 0, 8), (66000, 33, 40, 0, 32)]
+ROWS = [(65536, 9, 9, 0, 9), (66001, 41, 48, 0, 5), (70000, 16, 17, 1, 2), (65800, 64, 64, 0, 20), (80001, 57, 59, 3, 0), (68000, 24, 24, 0, 1), (70000, 47, 47, 0, 8), (66000, 33, 40, 0, 32),
+        (65536, 64, 64, 0, 3), (65600, 33, 40, 0, 5), (66000, 27, 29, 1, 4), (66000, 49, 50, 1, 5), (4100, 300, 300, 0, 20), (4097, 512, 513, 1, 9), (4096, 257, 264, 0, 32)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
