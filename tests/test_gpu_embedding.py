@@ -220,6 +220,21 @@ def test_table_gradient_of_large_tables(hgnn, dev, F, ldt, offset, dtype):
         assert bool((buf == FILL).all())
 
 
+@pytest.mark.parametrize("F", [65535, 65536])
+def test_widest_rows(hgnn, dev, F):
+    rng = np.random.default_rng(F)
+    n, V = 75, 6
+    ids = ids_of(n, V, "hubs", rng)
+    dY = rng.standard_normal((n, F)).astype(np.float16)
+    for dtype, add in ((torch.float32, False), (torch.float16, True)):
+        check_grad(hgnn, dev, ids, dY, V, F, dtype, 0.5, add, F + 1, F, label="widest")
+    T = up(rng.standard_normal((V, F)).astype(np.float16), dev)
+    out = torch.full((n, F), FILL, dtype=torch.float16, device=dev)
+    hgnn.hgnn_embedding(up(ids, dev), T, out)
+    real = (ids >= 0) & (ids < V)
+    assert np.array_equal(down(out), np.where(real[:, None], down(T)[np.where(real, ids, 0)], np.float16(0)))
+
+
 def test_gradient_is_the_lookups(hgnn, dev):
     """<lookup(T), dY> moves with T as the gradient says: the lookup is linear in T, so differences are exact up to the roundings of both sides."""
     rng = np.random.default_rng(3)

@@ -93,7 +93,7 @@ def test_lists(hgnn, dev, shapes, inv_scale, max_norm):
     check(hgnn, dev, a, None, inv_scale, max_norm, offsets=[i % 5 + 1 for i in range(len(a))])
 
 
-@pytest.mark.parametrize("count", [55, 56, 57, 113, 400])
+@pytest.mark.parametrize("count", [55, 56, 57, 95, 96, 97, 113, 192, 193, 400])
 def test_many_tensors(hgnn, dev, count):
     """More than the arguments of a launch hold; a small first launch and a large last one."""
     print(f"clip of {count}", flush=True)
