@@ -532,52 +532,63 @@ hgnn_status hgnn_edge_colsum(const hgnn_csr* g, const hgnn_plan* p, int32_t H, c
                              void* stream);
 
 /* ---- the two ends of a training step and its guard ------------------------------------------------------
- * What stands before the first layer (rows of a learned vertex table by id), behind the last one (log probabilities of
- * the vertices' labels) and between the gradients and the optimizer (their norm, unscaling and clipping).  These calls take
- * rows of any width and pitch: a tensor has to be aligned to its elements' type alone, nothing between or behind
- * its rows is written, nothing behind the last one read (what lies between rows may be, and never reaches a result), and an output may
- * overlap no other argument where nothing else is said. */
+ * What stands before the first layer (rows of a learned vertex table by id), behind the last one (log probabilities
+ * of the vertices' labels) and between the gradients and the optimizer (their norm, unscaling and clipping).  These
+ * calls take rows of any width and pitch: a tensor has to be aligned to its elements' type alone, nothing between or
+ * behind its rows is written, nothing behind the last one read (what lies between rows may be, and never reaches a
+ * result), and an output may overlap no other argument where nothing else is said. */
 
-/* out[i, f] = fp16(scale * table[ids[i], f]) for i < n, f < F: rows of a table [V][ldt] of fp16 or fp32 by id.  An id outside [0, V) is padding: its
- * row is zeros, whatever the scale.  out is [n][ldo].  F <= 65536 (HGNN_EUNSUPPORTED beyond). */
+/* out[i, f] = fp16(scale * table[ids[i], f]) for i < n, f < F: rows of a table [V][ldt] of fp16 or fp32 by id.  An id
+ * outside [0, V) is padding: its row is zeros, whatever the scale.  out is [n][ldo].  F <= 65536 (HGNN_EUNSUPPORTED
+ * beyond). */
 hgnn_status hgnn_embedding(int64_t n, int32_t F, const int32_t* ids, int32_t V, hgnn_type table_type, const void* table,
                            int64_t ldt, float scale, hgnn_half* out, int64_t ldo, void* stream);
 
 /* The gradient of the table of hgnn_embedding given the gradient dY [n][ldy] of its output:
- *   dT[v, f] = (accumulate ? dT[v, f] : 0) + scale * sum over i with ids[i] = v of dY[i, f]        [V][lddt], fp16 or fp32
- * Without accumulate every row is written, those without an id as zeros; with it the rows without an id are neither read nor written.  Ids
- * outside [0, V) add nothing.  The positions are sorted by id and the rows of an id are added in fp32, in an order that the sizes and ids alone decide: no atomics,
- * the same bits on every run; one rounding.  workspace is device memory of at least hgnn_embedding_grad_workspace(n, F, V) bytes (16-byte aligned), owned by
- * the caller and overwritten.  n < 2^31, F <= 65536. */
+ *   dT[v, f] = (accumulate ? dT[v, f] : 0) + scale * sum over i with ids[i] = v of dY[i, f]
+ * dT is [V][lddt], fp16 or fp32.  Without accumulate every row is written, those without an id as zeros; with it the
+ * rows without an id are neither read nor written.  Ids outside [0, V) add nothing.  The positions are sorted by id and
+ * the rows of an id are added in fp32, in an order that the sizes and ids alone decide: no atomics, the same bits on
+ * every run; one rounding.  workspace is device memory of at least hgnn_embedding_grad_workspace(n, F, V) bytes
+ * (16-byte aligned), owned by the caller and overwritten.  n < 2^31, F <= 65536. */
 size_t hgnn_embedding_grad_workspace(int64_t n, int32_t F, int32_t V);
 hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_t V, const hgnn_half* dY, int64_t ldy, float scale,
                                 int32_t accumulate, hgnn_type grad_type, void* dT, int64_t lddt, void* workspace,
                                 size_t workspace_bytes, void* stream);
 
-/* Log probabilities under a softmax over the C classes of every row of logits [n][ld] (fp16 or fp32), in one pass over them, with
+/* Log probabilities under a softmax over the C classes of every row of logits [n][ld] (fp16 or fp32), in one pass
+ * over them, with
  *   m_i = max_c x[i,c],  L_i = log sum_c exp(x[i,c] - m_i),  log p[i,c] = (x[i,c] - m_i) - L_i:
- *   logprob[i]    = log p[i, labels[i]]; a label outside [0, C) is none, and the value 0             (with labels; both or neither)
- *   stats[i]      = (m_i, L_i), what hgnn_logprob_grad needs of the row                              [n][2] or NULL
- *   entropy[i]    = -sum_c p[i,c] log p[i,c]                                                         [n] or NULL
- *   top_logprob, top_class [n][k]: the k classes of the largest scores, falling, among equal scores the lowest class first (0 <= k <= 32, k <= C)
- * all fp32, the classes int32.  A class whose score is -inf is masked out: its probability is 0, and as an alternative it comes last.  A row of -inf
- * alone has the log probability -inf everywhere, the entropy 0 and the stats (-inf, 0).  A row that holds +inf or NaN is NaN everywhere (its
- * alternatives are some k different classes).  What a launch does not hold is refused with HGNN_EUNSUPPORTED: more than 2^30 classes, 2^34 scores or so.  workspace is device memory of at least hgnn_logprob_workspace(n, C, k) bytes (4-byte aligned; 0: none is
- * needed), owned by the caller and overwritten. */
+ *   logprob [n]              log p[i, labels[i]]; a label outside [0, C) is none, and the value 0 (with labels; both or
+ *                            neither)
+ *   stats [n][2] or NULL     (m_i, L_i), what hgnn_logprob_grad needs of the row
+ *   entropy [n] or NULL      -sum_c p[i,c] log p[i,c]
+ *   top_logprob, top_class   [n][k]: the k classes of the largest scores, falling, among equal scores the lowest class
+ *                            first (0 <= k <= 32, k <= C)
+ * all fp32, the classes int32.  A class whose score is -inf is masked out: its probability is 0, and as an alternative
+ * it comes last.  A row of -inf alone has the log probability -inf everywhere, the entropy 0 and the stats (-inf, 0).
+ * A row that holds +inf or NaN is NaN everywhere (its alternatives are some k different classes).  What a launch does
+ * not hold is refused with HGNN_EUNSUPPORTED: more than 2^30 classes, 2^34 scores or so.  workspace is device memory of
+ * at least hgnn_logprob_workspace(n, C, k) bytes (4-byte aligned; 0: none is needed), owned by the caller and
+ * overwritten. */
 size_t hgnn_logprob_workspace(int64_t n, int32_t C, int32_t k);
 hgnn_status hgnn_logprob(int64_t n, int32_t C, hgnn_type type, const void* logits, int64_t ld, const int32_t* labels, float* logprob,
                          float* stats, float* entropy, int32_t k, float* top_logprob, int32_t* top_class, void* workspace,
                          size_t workspace_bytes, void* stream);
 
-/* The gradient of the logits given those of logprob (g = dlogprob, [n]) and, unless dentropy is NULL, of the entropy (h = dentropy, [n]):
- *   dlogits[i,c] = g_i (1[c = labels[i]] - p[i,c]) - h_i p[i,c] (log p[i,c] + entropy[i])            [n][ldd], the type of the logits
- * with the stats and the entropy that hgnn_logprob gave.  A row without a label has g = 0; labels and dlogprob may both be NULL.  The gradient of a masked
- * class is 0 (g_i if it is the label), and of a row of -inf alone 0 whatever g_i and h_i are.  Sizes as for hgnn_logprob.  dlogits may be the logits themselves (with the same pitch). */
+/* The gradient of the logits given those of logprob (g = dlogprob, [n]) and, unless dentropy is NULL, of the entropy
+ * (h = dentropy, [n]):
+ *   dlogits[i,c] = g_i (1[c = labels[i]] - p[i,c]) - h_i p[i,c] (log p[i,c] + entropy[i])
+ * dlogits is [n][ldd] of the type of the logits, stats and entropy are what hgnn_logprob gave.  A row without a label
+ * has g = 0; labels and dlogprob may both be NULL.  The gradient of a masked class is 0 (g_i if it is the label), and of
+ * a row of -inf alone 0 whatever g_i and h_i are.  Sizes as for hgnn_logprob.  dlogits may be the logits themselves
+ * (with the same pitch). */
 hgnn_status hgnn_logprob_grad(int64_t n, int32_t C, hgnn_type type, const void* logits, int64_t ld, const int32_t* labels,
                               const float* stats, const float* dlogprob, const float* entropy, const float* dentropy, void* dlogits,
                               int64_t ldd, void* stream);
 
-/* A gradient tensor of hgnn_grad_norm and hgnn_grad_clip: rows x cols elements in rows of pitch ld (one row where there are no gaps). */
+/* A gradient tensor of hgnn_grad_norm and hgnn_grad_clip: rows x cols elements in rows of pitch ld (one row where there
+ * are no gaps). */
 typedef struct {
   const void* grad;
   void* out; /* where hgnn_grad_clip writes it, or NULL: in place (ld_out and out_type are then not looked at) */
@@ -585,18 +596,20 @@ typedef struct {
   hgnn_type type, out_type;
 } hgnn_grad;
 
-/* norm[0] = inv_scale * sqrt(sum of the squares of all elements of `count` tensors), fp32, inv_scale = 1 / (the factor that the loss was scaled by).  `grads` is a
- * HOST array that is read before the call returns.  Squares are summed in 64 bits, in a fixed order: the norm is not finite only if an element is not, or if it is
- * beyond fp32 itself.  workspace is device memory of at least hgnn_grad_norm_workspace() bytes (8-byte aligned), owned by the caller and overwritten. */
+/* norm[0] = inv_scale * sqrt(sum of the squares of all elements of `count` tensors), fp32, inv_scale = 1 / (the factor
+ * that the loss was scaled by).  `grads` is a HOST array that is read before the call returns.  Squares are summed in
+ * 64 bits, in a fixed order: the norm is not finite only if an element is not, or if it is beyond fp32 itself.
+ * workspace is device memory of at least hgnn_grad_norm_workspace() bytes (8-byte aligned), owned by the caller and
+ * overwritten. */
 size_t hgnn_grad_norm_workspace(void);
 hgnn_status hgnn_grad_norm(int32_t count, const hgnn_grad* grads, float inv_scale, float* norm, void* workspace, size_t workspace_bytes,
                            void* stream);
 
 /* hgnn_grad_norm, and then every gradient unscaled and clipped to the norm max_norm >= 0 (infinity: unscaled alone):
  *   out = type(factor * grad),  factor = inv_scale * min(1, max_norm / norm)
- * into its own place or another of either type.  Where the norm is not finite every output is zero, so that a step which nobody looks at
- * adds nothing, inside a captured graph for instance; norm[0] says so.  No two outputs may be the same or overlap, nor may an output overlap another
- * tensor's gradient. */
+ * into its own place or another of either type.  Where the norm is not finite every output is zero, so that a step
+ * which nobody looks at adds nothing, inside a captured graph for instance; norm[0] says so.  No two outputs may be the
+ * same or overlap, nor may an output overlap another tensor's gradient. */
 hgnn_status hgnn_grad_clip(int32_t count, const hgnn_grad* grads, float inv_scale, float max_norm, float* norm, void* workspace,
                            size_t workspace_bytes, void* stream);
 

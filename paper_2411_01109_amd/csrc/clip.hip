@@ -12,7 +12,8 @@
 
 namespace hgnn {
 
-// Tensors of a launch, by value: the arguments of a kernel hold 4 KB, and a launch costs the host 3 us and more (200 tensors: eight launches of 56 39 us, four of 96 27).
+// Tensors of a launch, by value: the arguments of a kernel hold 4 KB, and a launch costs the host 3 us and more (200 tensors: eight launches of 56 39 us, four
+// of 96 27).
 constexpr int kClipTensors = 96;
 constexpr int kClipParts = 1024;   // partial sums of squares at most, one for every workgroup
 // Elements of a workgroup's turn, a multiple of kClipChunk: as many as give every workgroup one, at most kClipMost.
@@ -53,8 +54,8 @@ __device__ __forceinline__ const ClipTensor& tensor_of(const ClipArgs& a, int c)
   return a.t[i];
 }
 
-// The elements of chunk c of a tensor, row by row in pieces of V, several of a lane's fetched together: use(row, column, columns left, piece).  V: 16 bytes of the wider of what
-// is read and written, so that the lanes' 16 bytes lie beside each other.
+// The elements of chunk c of a tensor, row by row in pieces of V, several of a lane's fetched together: use(row, column, columns left, piece).  V: 16 bytes of
+// the wider of what is read and written, so that the lanes' 16 bytes lie beside each other.
 template <class I, int V, class Use>
 __device__ __forceinline__ void walk_chunk(const ClipArgs& a, const ClipTensor& t, int c, Use&& use) {
   constexpr int kAhead = kClipAhead * 8 / V, kTurn = V * kBlock;
@@ -97,8 +98,8 @@ __device__ __forceinline__ double block_sum(double v) {
   return v;
 }
 
-// Sums of squares, in 64 bits: squares of fp32 leave its range at 1.8e19, and a long sum its precision.  A workgroup's sum is its own slot's, so launches of one call
-// add in order and the bits are the same on every run.
+// Sums of squares, in 64 bits: squares of fp32 leave its range at 1.8e19, and a long sum its precision.  A workgroup's sum is its own slot's, so launches of
+// one call add in order and the bits are the same on every run.
 __global__ __launch_bounds__(kBlock) void grad_squares_kernel(ClipArgs a) {
   double sum = 0;
   for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {

@@ -50,11 +50,11 @@ __global__ __launch_bounds__(kBlock) void embedding_kernel(LookupArgs a) {
 }
 
 // ---- the gradient -------------------------------------------------------------------------------------------
-// dT[v] = scale * sum of dY[i] over the i with ids[i] = v.  The positions are sorted by id (stable, so the rows of an id keep their order).  L lanes walk a share of
-// the sorted list, 8 or 16 positions, a workgroup so many consecutive ones as it has groups of L.  A run of equal ids inside a share is stored at once.  What
-// shares hold of a run in common goes to LDS, `head` of a run that began before the share, `tail` of one that goes on behind it, and is added in order by the share where the run
-// begins; what workgroups hold in common goes to memory in the same two forms, and a second pass adds it.  No atomics: the same bits on every run.  Rows without a position
-// are zeros, which workgroups behind those of the shares write.
+// dT[v] = scale * sum of dY[i] over the i with ids[i] = v.  The positions are sorted by id (stable, so the rows of an id keep their order).  L lanes walk a
+// share of the sorted list, 8 or 16 positions, a workgroup so many consecutive ones as it has groups of L.  A run of equal ids inside a share is stored at
+// once.  What shares hold of a run in common goes to LDS, `head` of a run that began before the share, `tail` of one that goes on behind it, and is added in
+// order by the share where the run begins; what workgroups hold in common goes to memory in the same two forms, and a second pass adds it.  No atomics: the
+// same bits on every run.  Rows without a position are zeros, which workgroups behind those of the shares write.
 
 // words: (id, position), an id that is none counts as V
 struct IdWords {
@@ -174,7 +174,7 @@ __device__ __forceinline__ bool in_whole_line(const char* at, const char* from, 
 }
 
 // zeros in those of 64 rows that no position has; s_there: 64 words of the wave's own
-template <class T, int L>
+template <class T>
 __device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, int* s_there) {
   if (r0 >= a.V) return;
   const int lane = threadIdx.x & (kWave - 1);
@@ -217,8 +217,9 @@ __device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, 
   }
 }
 
-// Positions of a share: many positions leave more shares than the chip holds at once, and shares of some hundred workgroups' runs to be joined.  us, 8 / 16: 1024 of 64 into 4096 rows 15.2 / 18.5, 30 000 of 64 into
-// 233 000 36 / 39, 200 000 of 128 into 233 000 59 / 57, 1 000 003 of 128 (power law) into 2.4 M 339 / 336, into 10 000 113 / 103, into 100 97 / 86.
+// Positions of a share: many positions leave more shares than the chip holds at once, and shares of some hundred workgroups' runs to be joined.  us, 8 / 16:
+// 1024 of 64 into 4096 rows 15.2 / 18.5, 30 000 of 64 into 233 000 36 / 39, 200 000 of 128 into 233 000 59 / 57, 1 000 003 of 128 (power law) into 2.4 M 339 /
+// 336, into 10 000 113 / 103, into 100 97 / 86.
 static int share_of(int64_t n) { return n < int64_t(1) << 19 ? 8 : 16; }
 constexpr int kAhead = 4;  // rows of a share that are fetched together
 
@@ -228,7 +229,8 @@ __global__ __launch_bounds__(kBlock, 6) void table_grad_kernel(TableGradArgs a) 
   __shared__ Quads s_part[2][kBlock];  // head and tail of the shares
   if (int64_t(blockIdx.x) >= a.blocks) {
     const int wave = threadIdx.x / kWave;
-    if (blockIdx.y == 0) write_zeros<T, L>(a, ((int64_t(blockIdx.x) - a.blocks) * kWavesPerBlock + wave) * kZeroRows, reinterpret_cast<int*>(s_part) + wave * kZeroRows);
+    const int64_t r0 = ((int64_t(blockIdx.x) - a.blocks) * kWavesPerBlock + wave) * kZeroRows;
+    if (blockIdx.y == 0) write_zeros<T>(a, r0, reinterpret_cast<int*>(s_part) + wave * kZeroRows);
     return;
   }
   const int64_t block = blockIdx.x;
@@ -478,11 +480,12 @@ hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_
   a.n = n, a.blocks = w.blocks, a.share = share_of(n), a.F = F, a.V = V;
   a.pos_bits = bits_of(n), a.zero_bits = F <= 8 ? 0 : std::min(6, bits_of((F + 7) / 8));
 
-  // Large tables (kPastBytes) whose rows are whole 128-byte lines are written past the caches.  us, through the caches / zeros past them / all rows past
-  // them, 64 M elements of gradients into 200 M (rows of 8 features 1 M into 3 M): rows of 128 bytes (32 x fp32) 191 / 182 / 183, 256 (64 x fp32) 265 / 236 / 229, 512 233 / 227 / 215,
-  // 512 (256 x fp16) 162 / 153 / 143; but parts of lines cost more, rows of 32 bytes 127 / 136 / 198, of 168 bytes 312 / 343 / 371.
-  // Of rows with gaps, whose parts of lines cost more either way, zeros in the whole lines alone: 16 positions into 400 MB of fp32, rows of 64 of a pitch of 72 159 / 169, 80 of 88 154 / 119, 100 of 104 149 / 110, 200 of 208
-  // 134 / 87, 333 of 336 127 / 91, 1000 of 1008 107 / 93 (all of the row past them: 100 of 104 174, 200 of 208 136); without gaps, where the caches join the parts, 100 91 / 122, 333 92 / 129.
+  // Large tables (kPastBytes) whose rows are whole 128-byte lines are written past the caches.  us, through the caches / zeros past them / all rows past them,
+  // 64 M elements of gradients into 200 M (rows of 8 features 1 M into 3 M): rows of 128 bytes (32 x fp32) 191 / 182 / 183, 256 (64 x fp32) 265 / 236 / 229,
+  // 512 233 / 227 / 215, 512 (256 x fp16) 162 / 153 / 143; but parts of lines cost more, rows of 32 bytes 127 / 136 / 198, of 168 bytes 312 / 343 / 371. Of
+  // rows with gaps, whose parts of lines cost more either way, zeros in the whole lines alone: 16 positions into 400 MB of fp32, rows of 64 of a pitch of 72
+  // 159 / 169, 80 of 88 154 / 119, 100 of 104 149 / 110, 200 of 208 134 / 87, 333 of 336 127 / 91, 1000 of 1008 107 / 93 (all of the row past them: 100 of 104
+  // 174, 200 of 208 136); without gaps, where the caches join the parts, 100 91 / 122, 333 92 / 129.
   const size_t row_bytes = size_t(F) * (grad_type == HGNN_F16 ? 2 : 4), pitch_bytes = size_t(lddt) * (grad_type == HGNN_F16 ? 2 : 4);
   const bool lines = row_bytes % 128 == 0 && pitch_bytes % 128 == 0 && (reinterpret_cast<uintptr_t>(dT) & 127u) == 0;
   const bool gaps = pitch_bytes > row_bytes && row_bytes >= 288;

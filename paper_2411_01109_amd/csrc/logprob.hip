@@ -1,6 +1,6 @@
-// Log probabilities of labels under a softmax over classes, with the entropy and the best alternatives, and their gradient: what stands behind the last
-// layer.  m = max x, S = sum exp(x - m), L = log S; log p_c = (x_c - m) - L, entropy = L - sum exp(x - m) (x - m) / S.  The maximum and L are kept apart: their sum would
-// lose the small differences of large scores to its rounding.
+// Log probabilities of labels under a softmax over classes, with the entropy and the best alternatives, and their gradient: what stands behind the last layer.
+// m = max x, S = sum exp(x - m), L = log S; log p_c = (x_c - m) - L, entropy = L - sum exp(x - m) (x - m) / S.  The maximum and L are kept apart: their sum
+// would lose the small differences of large scores to its rounding.
 #include <math.h>
 
 #include <algorithm>
@@ -16,10 +16,10 @@ constexpr int kMostTop = 32;     // alternatives at most: a lane of a wave each
 constexpr int kMostSplits = 64;  // workgroups of a row at most: a lane of a wave each
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// What a set of classes holds: the maximum m, s = sum 2^y and t = sum 2^y y, y = (x - m) log2(e).  An empty one, or one of -inf alone, has s = 0 and a maximum below all
-// others, which is finite, so that it takes no part in inf - inf.
-// fp16: y = fma(x, log2(e), -c) in one instruction, with the conversion; c, the rounded m log2(e), is the same for all classes, so its error goes in and out with it (shift_of).
-// fp32, whose products with log2(e) may overflow: a difference and a product.
+// What a set of classes holds: the maximum m, s = sum 2^y and t = sum 2^y y, y = (x - m) log2(e).  An empty one, or one of -inf alone, has s = 0 and a maximum
+// below all others, which is finite, so that it takes no part in inf - inf. fp16: y = fma(x, log2(e), -c) in one instruction, with the conversion; c, the
+// rounded m log2(e), is the same for all classes, so its error goes in and out with it (shift_of). fp32, whose products with log2(e) may overflow: a difference
+// and a product.
 template <class T>
 struct Mass {
   static constexpr bool kHalf = sizeof(T) == 2;
@@ -253,9 +253,9 @@ __device__ __forceinline__ Best sorted(Candidates& s, int count) {  // at most 6
   return sorted(v, c, count, s);
 }
 
-// Takes those of a wave's classes c0 + 512 i + 8 lane + j (i < N, j < 8, scores x, -inf where there is none) that are among the best k; `least`, the k-th so far.  A wave comes by its
-// classes in rising order, so a score that equals the k-th is behind it.  What is better becomes candidates, of many no more than what is as good as the k-th of the lanes' best.  Where
-// there are too many all the same (equal scores), pieces are gone through in their order.
+// Takes those of a wave's classes c0 + 512 i + 8 lane + j (i < N, j < 8, scores x, -inf where there is none) that are among the best k; `least`, the k-th so
+// far.  A wave comes by its classes in rising order, so a score that equals the k-th is behind it.  What is better becomes candidates, of many no more than
+// what is as good as the k-th of the lanes' best.  Where there are too many all the same (equal scores), pieces are gone through in their order.
 template <class T, int N>
 __device__ __forceinline__ void take_best(Best& best, float& least, int k, const RawPiece<T> (&x)[N], const float (&top)[N], int c0, Candidates& s) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -407,8 +407,9 @@ __device__ __forceinline__ Best merge_lists(int k, int n, Entry&& entry) {
   return out;
 }
 
-// ---- the best k of a row that a group of lanes holds, a piece each: every lane puts its eight in order once, then the row's best is the best of the lanes' first, k times.  us, with rounds that looked
-// for score and class among all that is left / this: 212 828 rows of 247 (fp16) best five 137 / 82, twenty 461 / 135; 19 rows of 16, all sixteen 14 / 4.3
+// ---- the best k of a row that a group of lanes holds, a piece each
+// Every lane puts its eight in order once, then the row's best is the best of the lanes' first, k times.  us, with rounds that looked for score and class
+// among all that is left / this: 212 828 rows of 247 (fp16) best five 137 / 82, twenty 461 / 135; 19 rows of 16, all sixteen 14 / 4.3.
 // A score and its class.  NaN counts as -inf, and what is behind the row's end comes after both.
 template <class T>
 struct Place;
@@ -423,7 +424,8 @@ struct Place<half_t> {  // in one number, that rises with the score and falls wi
     key = there ? int(uint32_t(b >= 0 ? b : b ^ 0x7fff) << 16) | (0xffff - c) : int(0x80000000u);
   }
   static __device__ __forceinline__ void order(Place (&e)[8]) {
-    constexpr int kPairs[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6}, {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
+    constexpr int kPairs[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
+                                   {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
 #pragma unroll
     for (int q = 0; q < 19; ++q) {
       const int x = e[kPairs[q][0]].key, y = e[kPairs[q][1]].key;
@@ -469,8 +471,8 @@ struct Place<float> {
   __device__ __forceinline__ int cls() const { return c; }
 };
 
-// Rows of up to 512 classes: L lanes hold a row, N pieces each.  What a row costs beside its classes (reductions, logarithm, stores) is a wave's for all of its 64 / L rows at once: 262 144 rows
-// of 512, 64 lanes with a piece / 16 with four, 78 / 51 us.
+// Rows of up to 512 classes: L lanes hold a row, N pieces each.  What a row costs beside its classes (reductions, logarithm, stores) is a wave's for all of its
+// 64 / L rows at once: 262 144 rows of 512, 64 lanes with a piece / 16 with four, 78 / 51 us.
 template <class T, int L, int N, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(kBlock) void logprob_group_kernel(ScoreArgs a) {
   const int64_t i = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / L, row = i < a.n ? i : a.n - 1;
@@ -500,8 +502,9 @@ __global__ __launch_bounds__(kBlock) void logprob_group_kernel(ScoreArgs a) {
   __shared__ Place<T> s_best[TOP ? kWavesPerBlock : 1][TOP ? kRows * kMost : 1];
   __shared__ RowStats s_stats[TOP ? kWavesPerBlock : 1][TOP ? kRows : 1];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, r = lane / L;
-  Place<T> e[8] = {{p[0].v[0], 8 * l, 8 * l < a.C},         {p[0].v[1], 8 * l + 1, 8 * l + 1 < a.C}, {p[0].v[2], 8 * l + 2, 8 * l + 2 < a.C}, {p[0].v[3], 8 * l + 3, 8 * l + 3 < a.C},
-                   {p[0].v[4], 8 * l + 4, 8 * l + 4 < a.C}, {p[0].v[5], 8 * l + 5, 8 * l + 5 < a.C}, {p[0].v[6], 8 * l + 6, 8 * l + 6 < a.C}, {p[0].v[7], 8 * l + 7, 8 * l + 7 < a.C}};
+  Place<T> e[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e[j] = Place<T>(p[0].v[j], 8 * l + j, 8 * l + j < a.C);
   Place<T>::order(e);
   const Place<T> none(T(0), 0, false);
   for (int k = 0; k < a.k; ++k) {
@@ -523,9 +526,10 @@ __global__ __launch_bounds__(kBlock) void logprob_group_kernel(ScoreArgs a) {
   }
 }
 
-// Few alternatives of few classes, many rows: a lane takes a row by itself, with no reduction across lanes.  The 64 rows of a wave come in whole pieces through LDS (rows of P pieces and a pad
-// word, so that lanes that read their own rows meet on no bank).  us, lanes in groups / a lane a row, 233 000 rows of 41 (fp16): the best one 18.5 / 11.2, five 22 / 18.3, eight 26.2 / 25.5, twenty
-// 34 / 76; of 16 five 9.5 / 8.8, eight 11 / 15; without alternatives 8.8 / 8.3 and the gradient, which would go back that way, 9.9 / 12.5: not kept.
+// Few alternatives of few classes, many rows: a lane takes a row by itself, with no reduction across lanes.  The 64 rows of a wave come in whole pieces through
+// LDS (rows of P pieces and a pad word, so that lanes that read their own rows meet on no bank).  us, lanes in groups / a lane a row, 233 000 rows of 41
+// (fp16): the best one 18.5 / 11.2, five 22 / 18.3, eight 26.2 / 25.5, twenty 34 / 76; of 16 five 9.5 / 8.8, eight 11 / 15; without alternatives 8.8 / 8.3 and
+// the gradient, which would go back that way, 9.9 / 12.5: not kept.
 template <class T, int P>
 struct LaneRows {
   static constexpr int kPitch = 8 * P + 4 / int(sizeof(T));  // elements
@@ -792,8 +796,8 @@ __global__ __launch_bounds__(kBlock) void logprob_grad_kernel(ScoreGradArgs a) {
 
 constexpr int kGroupClasses = 8 * kWave;  // most classes that the lanes of a wave hold at once
 static int group_lanes(int C, int pieces) { return std::min(kWave, pow2_at_least(int(ceil_div(C, 8 * pieces)))); }
-// Pieces of a lane, more than one where rows fill the chip all the same.  us, 1 / 2 / 4: 233 000 rows of 41 (fp16) 10.2 / 8.4 / 8.8, their gradient 11.5 / 11.2 / 13.3; 262 144 of 512 78 / 57 / 51,
-// gradient 97 / 94 / 94; 100 000 of 200 18 / 12.8 / 13.6; fp32, 100 000 of 512 - / 34.8 / 36.8, gradient - / 77.7 / 81.9.
+// Pieces of a lane, more than one where rows fill the chip all the same.  us, 1 / 2 / 4: 233 000 rows of 41 (fp16) 10.2 / 8.4 / 8.8, their gradient 11.5 / 11.2
+// / 13.3; 262 144 of 512 78 / 57 / 51, gradient 97 / 94 / 94; 100 000 of 200 18 / 12.8 / 13.6; fp32, 100 000 of 512 - / 34.8 / 36.8, gradient - / 77.7 / 81.9.
 static int row_pieces(int64_t n, int C, bool wide) {
   if (C > kGroupClasses) return C <= 2 * kGroupClasses ? 2 : 4;
   if (C <= 8 || n * group_lanes(C, 1) < int64_t(1) << 20) return 1;
@@ -807,9 +811,9 @@ static void with_pieces(int pieces, Call&& call) {
 }
 constexpr int kWaveClasses = 4096;        // up to so many, a row is a wave's where there are rows enough
 static bool by_waves(int64_t n, int C) { return C <= kWaveClasses && n >= 4096; }
-// What a group of lanes holds: up to 512 classes, 2048 without alternatives (200 000 rows of 520 and their gradient, by waves / groups: 203 / 191 us, of 600 189 / 172).
-// Many alternatives of rows that take all lanes of a wave are found sooner among candidates (us, by groups / by waves, 100 000 rows of 500, fp32: best twenty 171 / 109, five 85 / 77; of 512, fp16, 127 / 122, 77 / 83; 400, best one
-// 60 / 75; 212 828 of 247, two to a wave, best twenty 132 / 274).
+// What a group of lanes holds: up to 512 classes, 2048 without alternatives (200 000 rows of 520 and their gradient, by waves / groups: 203 / 191 us, of 600
+// 189 / 172). Many alternatives of rows that take all lanes of a wave are found sooner among candidates (us, by groups / by waves, 100 000 rows of 500, fp32:
+// best twenty 171 / 109, five 85 / 77; of 512, fp16, 127 / 122, 77 / 83; 400, best one 60 / 75; 212 828 of 247, two to a wave, best twenty 132 / 274).
 constexpr int kGroupTop = 8;
 static bool by_groups(int64_t n, int C, int k) {
   if (k > kGroupTop && C > kGroupClasses / 2 && by_waves(n, C)) return false;

@@ -5,8 +5,9 @@
 
 namespace hgnn {
 
-// The hardware takes 16-byte accesses to global memory at any element's address, so rows of any pitch go in whole pieces.  The last piece of a row is read whole, too, where
-// that stays inside the tensor (what it brings from beyond the row never reaches a result), else, and when it is written, in parts of four, two and one elements.
+// The hardware takes 16-byte accesses to global memory at any element's address, so rows of any pitch go in whole pieces.  The last piece of a row is read
+// whole, too, where that stays inside the tensor (what it brings from beyond the row never reaches a result), else, and when it is written, in parts of four,
+// two and one elements.
 typedef half8_t half8_any_t __attribute__((aligned(2)));
 typedef half4_t half4_any_t __attribute__((aligned(2)));
 typedef half2_t half2_any_t __attribute__((aligned(2)));
@@ -202,8 +203,8 @@ struct Part<T, 4> {
   static __device__ __forceinline__ void store(T* p, int left, const float (&x)[4]) { store_quad<T, PAST>(p, left, float4_t{x[0], x[1], x[2], x[3]}); }
 };
 
-// Outputs of so many bytes are written past the caches: the last-level cache (256 MiB) would have lost most of them before they are read.  us, rows of 128 by id and then a reader of them, through / past: 61 MB
-// 35 / 38, 122 MB 62 / 66, 244 MB 126 / 121 (the rows alone: 20 / 16, 41 / 31, 81 / 58).
+// Outputs of so many bytes are written past the caches: the last-level cache (256 MiB) would have lost most of them before they are read.  us, rows of 128 by
+// id and then a reader of them, through / past: 61 MB 35 / 38, 122 MB 62 / 66, 244 MB 126 / 121 (the rows alone: 20 / 16, 41 / 31, 81 / 58).
 constexpr double kPastBytes = 192. * (1 << 20);
 
 // what a launch holds: fewer than 2^32 lanes
