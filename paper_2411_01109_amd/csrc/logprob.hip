@@ -758,7 +758,7 @@ __device__ __forceinline__ RowGrad<T> row_grad(const ScoreGradArgs& a, int64_t r
   const float shift = none ? 0.f : kLn2 * Mass<T>::shift(m), p = none ? 0.f : expf(shift - ls);  // p is this times e, log p = ln2 y + shift - ls
   r.at0 = -r.g * p;
   if (ENTROPY) {
-    const float h = none ? 0.f : a.dentropy[row] * p;
+    const float above = a.dentropy[row], h = none ? 0.f : above * p;  // (loaded with the stats, not behind them: 4096 rows of 50 021 165 / 145 us)
     r.slope = -h * kLn2;
     r.at0 -= h * (a.entropy[row] + shift - ls);
   }
