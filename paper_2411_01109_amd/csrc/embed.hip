@@ -173,9 +173,9 @@ __device__ __forceinline__ bool in_whole_line(const char* at, const char* from, 
   return line >= from && line + 128 <= to;
 }
 
-// zeros in those of 64 rows that no position has; s_there: 64 words of the wave's own
+// zeros in features f0 to f1 of those of 64 rows that no position has; s_there: 64 words of the wave's own
 template <class T>
-__device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, int* s_there) {
+__device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, int f0, int f1, int* s_there) {
   if (r0 >= a.V) return;
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t r = r0 + lane, ids[2] = {r0, r0 + kZeroRows};
@@ -211,7 +211,7 @@ __device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, 
     T* const p = static_cast<T*>(a.dT) + (r0 + k) * a.lddt;
     const char* const from = reinterpret_cast<const char*>(p);
     const char* const to = reinterpret_cast<const char*>(p + a.F);
-    for (int f = 4 * (lane & ((1 << a.zero_bits) - 1)); f < a.F; f += 4 << a.zero_bits)
+    for (int f = f0 + 4 * (lane & ((1 << a.zero_bits) - 1)); f < f1; f += 4 << a.zero_bits)
       if (const char* const at = reinterpret_cast<const char*>(p + f); a.past != 0 && in_whole_line(at, from, to)) store_quad<T, true>(p + f, a.F - f, float4_t{});
       else store_quad(p + f, a.F - f, float4_t{});
   }
@@ -230,7 +230,8 @@ __global__ __launch_bounds__(kBlock, 6) void table_grad_kernel(TableGradArgs a) 
   if (int64_t(blockIdx.x) >= a.blocks) {
     const int wave = threadIdx.x / kWave;
     const int64_t r0 = ((int64_t(blockIdx.x) - a.blocks) * kWavesPerBlock + wave) * kZeroRows;
-    if (blockIdx.y == 0) write_zeros<T>(a, r0, reinterpret_cast<int*>(s_part) + wave * kZeroRows);
+    const int f0 = 8 * L * int(blockIdx.y);
+    write_zeros<T>(a, r0, f0, min(a.F, f0 + 8 * L), reinterpret_cast<int*>(s_part) + wave * kZeroRows);
     return;
   }
   const int64_t block = blockIdx.x;
