@@ -81,7 +81,8 @@ struct TableGradArgs {
   const uint64_t* words;  // sorted
   int64_t n;
   int pos_bits, F, V;
-  int zero_bits;  // 2^zero_bits lanes write the zeros of a row
+  int zero_bits;   // 2^zero_bits lanes write the zeros of a row
+  int zero_waves;  // waves that share 64 rows
   const half_t* dY;
   int64_t ldy, inside;  // elements from the first of dY to its last
   float scale;
@@ -175,7 +176,7 @@ __device__ __forceinline__ bool in_whole_line(const char* at, const char* from, 
 
 // zeros in features f0 to f1 of those of 64 rows that no position has; s_there: 64 words of the wave's own
 template <class T>
-__device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, int f0, int f1, int* s_there) {
+__device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, int part, int f0, int f1, int* s_there) {
   if (r0 >= a.V) return;
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t r = r0 + lane, ids[2] = {r0, r0 + kZeroRows};
@@ -206,7 +207,8 @@ __device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, 
     mine = mine || (lo < range[1] && a.id(lo) == r);
   }
   const uint64_t there = __ballot(mine);
-  for (int k = lane >> a.zero_bits; k < kZeroRows; k += kWave >> a.zero_bits) {
+  const int rows = kWave >> a.zero_bits;
+  for (int k = (lane >> a.zero_bits) + part * rows; k < kZeroRows; k += rows * a.zero_waves) {
     if (there >> k & 1) continue;
     T* const p = static_cast<T*>(a.dT) + (r0 + k) * a.lddt;
     const char* const from = reinterpret_cast<const char*>(p);
@@ -229,9 +231,9 @@ __global__ __launch_bounds__(kBlock, 6) void table_grad_kernel(TableGradArgs a) 
   __shared__ Quads s_part[2][kBlock];  // head and tail of the shares
   if (int64_t(blockIdx.x) >= a.blocks) {
     const int wave = threadIdx.x / kWave;
-    const int64_t r0 = ((int64_t(blockIdx.x) - a.blocks) * kWavesPerBlock + wave) * kZeroRows;
+    const int64_t r0 = ((int64_t(blockIdx.x) - a.blocks) * (kWavesPerBlock / a.zero_waves) + wave / a.zero_waves) * kZeroRows;
     const int f0 = 8 * L * int(blockIdx.y);
-    write_zeros<T>(a, r0, f0, min(a.F, f0 + 8 * L), reinterpret_cast<int*>(s_part) + wave * kZeroRows);
+    write_zeros<T>(a, r0, wave % a.zero_waves, f0, min(a.F, f0 + 8 * L), reinterpret_cast<int*>(s_part) + wave * kZeroRows);
     return;
   }
   const int64_t block = blockIdx.x;
@@ -393,7 +395,7 @@ static hgnn_status table_grad(const TableGradArgs& a, hipStream_t s) {
   hgnn_status st = HGNN_OK;
   with_lanes<kShareLanes>(a.F, [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
-    const int64_t zeros = ADD ? 0 : ceil_div(a.V, int64_t(kZeroRows) * kWavesPerBlock);
+    const int64_t zeros = ADD ? 0 : ceil_div(a.V, int64_t(kZeroRows) * (kWavesPerBlock / a.zero_waves));
     const unsigned fy = unsigned(ceil_div(a.F, 8 * L));  // 1 up to 512 features
     auto go = [&]() -> hgnn_status {
       HGNN_REQUIRE(a.blocks + zeros <= kMostBlocks, HGNN_EUNSUPPORTED, "hgnn_embedding_grad: grid too large");
@@ -480,6 +482,9 @@ hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_
   TableGradArgs a{};
   a.n = n, a.blocks = w.blocks, a.share = share_of(n), a.F = F, a.V = V;
   a.pos_bits = bits_of(n), a.zero_bits = F <= 8 ? 0 : std::min(6, bits_of((F + 7) / 8));
+  // Waves of a workgroup share 64 wide rows, a wave alone takes narrow ones.  us, alone / shared, 16 positions: 100 rows of 1000 (fp32) 22 / 12, 60 000 of 333 30 / 21,
+  // 300 000 of 333 92 / 90, 1 M of 100 at a pitch of 104 118 / 109, of 128 102 / 103; 40 000 of 64 12.1 / 12.4; 100 000 positions of 233 000 rows of 128 54 / 56.
+  a.zero_waves = F > 64 ? kWavesPerBlock : 1;
 
   // Large tables (kPastBytes) whose rows are whole 128-byte lines are written past the caches.  us, through the caches / zeros past them / all rows past them,
   // 64 M elements of gradients into 200 M (rows of 8 features 1 M into 3 M): rows of 128 bytes (32 x fp32) 191 / 182 / 183, 256 (64 x fp32) 265 / 236 / 229,
