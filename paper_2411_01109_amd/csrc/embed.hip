@@ -83,6 +83,7 @@ struct TableGradArgs {
   int pos_bits, F, V;
   int zero_bits;   // 2^zero_bits lanes write the zeros of a row
   int zero_waves;  // waves that share 64 rows
+  int zero_span;   // features of a workgroup's zeros
   const half_t* dY;
   int64_t ldy, inside;  // elements from the first of dY to its last
   float scale;
@@ -177,7 +178,7 @@ __device__ __forceinline__ bool in_whole_line(const char* at, const char* from, 
 // zeros in features f0 to f1 of those of 64 rows that no position has; s_there: 64 words of the wave's own
 template <class T>
 __device__ __forceinline__ void write_zeros(const TableGradArgs& a, int64_t r0, int part, int f0, int f1, int* s_there) {
-  if (r0 >= a.V) return;
+  if (r0 >= a.V || f0 >= f1) return;
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t r = r0 + lane, ids[2] = {r0, r0 + kZeroRows};
   int64_t range[2] = {0, 0};
@@ -232,8 +233,8 @@ __global__ __launch_bounds__(kBlock, 6) void table_grad_kernel(TableGradArgs a) 
   if (int64_t(blockIdx.x) >= a.blocks) {
     const int wave = threadIdx.x / kWave;
     const int64_t r0 = ((int64_t(blockIdx.x) - a.blocks) * (kWavesPerBlock / a.zero_waves) + wave / a.zero_waves) * kZeroRows;
-    const int f0 = 8 * L * int(blockIdx.y);
-    write_zeros<T>(a, r0, wave % a.zero_waves, f0, min(a.F, f0 + 8 * L), reinterpret_cast<int*>(s_part) + wave * kZeroRows);
+    const int f0 = min(a.F, a.zero_span * int(blockIdx.y));
+    write_zeros<T>(a, r0, wave % a.zero_waves, f0, min(a.F, f0 + a.zero_span), reinterpret_cast<int*>(s_part) + wave * kZeroRows);
     return;
   }
   const int64_t block = blockIdx.x;
@@ -485,6 +486,10 @@ hgnn_status hgnn_embedding_grad(int64_t n, int32_t F, const int32_t* ids, int32_
   // Waves of a workgroup share 64 wide rows, a wave alone takes narrow ones.  us, alone / shared, 16 positions: 100 rows of 1000 (fp32) 22 / 12, 60 000 of 333 30 / 21,
   // 300 000 of 333 92 / 90, 1 M of 100 at a pitch of 104 118 / 109, of 128 102 / 103; 40 000 of 64 12.1 / 12.4; 100 000 positions of 233 000 rows of 128 54 / 56.
   a.zero_waves = F > 64 ? kWavesPerBlock : 1;
+  // Of wide rows a workgroup for every 512 features writes zeros where rows are few; many are written from end to end (us, 512 / whole: 64 rows of 65 536, fp32, 12 /
+  // 350, 10 000 of 1000 16 / 20, 20 000 21 / 21, 200 000 239 / 166).
+  constexpr int kFewRows = 16384;
+  a.zero_span = V < kFewRows ? 8 * kWave : F;
 
   // Large tables (kPastBytes) whose rows are whole 128-byte lines are written past the caches.  us, through the caches / zeros past them / all rows past them,
   // 64 M elements of gradients into 200 M (rows of 8 features 1 M into 3 M): rows of 128 bytes (32 x fp32) 191 / 182 / 183, 256 (64 x fp32) 265 / 236 / 229,

@@ -199,7 +199,7 @@ def test_table_gradient_far_rows(hgnn, dev):
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
-@pytest.mark.parametrize("F,ldt,offset", [(100, 104, 0), (333, 333, 0), (256, 256, 0), (161, 200, 3), (1000, 1008, 0)])
+@pytest.mark.parametrize("F,ldt,offset", [(100, 104, 0), (333, 333, 0), (256, 256, 0), (161, 200, 3), (1000, 1008, 0), (1300, 1301, 1)])
 def test_table_gradient_of_large_tables(hgnn, dev, F, ldt, offset, dtype):
     """Tables too large for the last-level cache: rows and zeros in whole lines and in parts of lines, what lies between the rows as it was, NaN at positions without an id."""
     size = 2 if dtype == torch.float16 else 4
