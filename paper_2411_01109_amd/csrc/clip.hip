@@ -133,14 +133,25 @@ __global__ __launch_bounds__(kBlock) void grad_norm_kernel(ClipArgs a) {
   if (threadIdx.x == 0) *a.norm = float(norm);
 }
 
+// What gradients are multiplied by: factor 2^exponent.  The exponent is not zero only below 2^-100, where the factor alone may leave fp32's normal numbers though
+// the products do not (gradients near the largest fp32 values): there it is a number of [0.5, 1), whose product with a gradient is exact to its rounding.
+struct ClipFactor {
+  float factor;
+  int exponent;
+  __device__ __forceinline__ explicit ClipFactor(double f) : factor(float(f)), exponent(0) {
+    if (f < 0x1p-100) factor = float(frexp(f, &exponent));
+  }
+  __device__ __forceinline__ float of(float g) const { return factor == 0.f ? 0.f : __builtin_ldexpf(g * factor, exponent); }
+};
+
 template <class I, class O, bool PAST>
-__device__ __forceinline__ void clip_chunk(const ClipArgs& a, const ClipTensor& t, int c, float factor) {
+__device__ __forceinline__ void clip_chunk(const ClipArgs& a, const ClipTensor& t, int c, const ClipFactor& factor) {
   constexpr int V = sizeof(I) == 2 && sizeof(O) == 2 ? 8 : 4;
   walk_chunk<I, V>(a, t, c, [&](int64_t row, int64_t col, int left, const Part<I, V>& x) __attribute__((always_inline)) {
     O* const o = static_cast<O*>(t.o) + row * t.ldo() + col;
     float y[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) y[j] = factor == 0.f ? 0.f : float(x.v[j]) * factor;
+    for (int j = 0; j < V; ++j) y[j] = factor.of(float(x.v[j]));
     Part<O, V>::template store<PAST>(o, left, y);
   });
 }
@@ -152,7 +163,7 @@ __global__ __launch_bounds__(kBlock) void grad_clip_kernel(ClipArgs a) {
   // a norm that is none: zeros, so that a step that nobody looks at adds nothing
   double f = isfinite(float(norm)) ? double(a.inv_scale) : 0.;
   if (norm > double(a.max_norm)) f *= double(a.max_norm) / norm;
-  const float factor = float(f);
+  const ClipFactor factor(f);
   // from the end: what the sums of squares read last is still in the last-level cache
   for (int c = a.chunks - 1 - int(blockIdx.x); c >= 0; c -= gridDim.x) {
     const ClipTensor& t = tensor_of(a, c);
