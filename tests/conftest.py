@@ -12,6 +12,16 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu)")
 
 
+# Tests that assert nothing but how long calls take.  They come last: a run that stops at its first failure has been through all that tells right from wrong
+# before a moment's delay of the host can end it (a pair of calls of 11 us that once took 18, whose kernels take 5.7 and 5.5).
+TIMED = {"test_linear_ragged_weight_costs_as_much_as_a_whole_one", "test_rows_in_order_of_their_lengths", "test_kernels_of_rows_in_order_of_their_lengths", "test_backward_of_short_rows",
+         "test_middle_rows_in_order_of_lengths", "test_time_of_a_long_gap", "test_time_of_few_words"}
+
+
+def pytest_collection_modifyitems(items):
+    items.sort(key=lambda item: getattr(item, "originalname", item.name) in TIMED)  # stable: each part in its order
+
+
 def parse_golden(name):
     """tests/golden/<name>: '#' comments, then 'key: v v v ...' lines (ints or floats, a/b fractions allowed)."""
     out = {}
