@@ -40,16 +40,6 @@ __device__ __forceinline__ float exp2_of(float y) { return __builtin_amdgcn_exp2
 // (-inf comes with a factor of zero, whose product would be no number)
 __device__ __forceinline__ float bounded(float y) { return fmaxf(y, -1e4f); }
 
-template <class T>
-__device__ __forceinline__ Mass<T> joined(const Mass<T>& a, const Mass<T>& b) {
-  Mass<T> r;
-  r.m = fmaxf(a.m, b.m);
-  const float da = Mass<T>::step(a.m, r.m), db = Mass<T>::step(b.m, r.m), fa = exp2_of(da), fb = exp2_of(db);
-  r.s = fa * a.s + fb * b.s;
-  r.t = fa * (a.t + bounded(da) * a.s) + fb * (b.t + bounded(db) * b.s);
-  return r;
-}
-
 // ---- over L lanes, L a power of two: pairs of lanes by data-parallel primitives (common.h), beyond a row of 16 by swaps
 enum class Over { kSum, kMax, kMin };
 template <Over OP>

@@ -84,27 +84,6 @@ template <class T>
 __device__ __forceinline__ RawPiece<T> load_raw(const T* p, int left, int64_t inside) {
   return inside >= 8 ? load_raw(p) : load_raw_part(p, left);
 }
-template <class T>
-__device__ __forceinline__ Piece floats(const RawPiece<T>& r) {
-  Piece x;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x.v[i] = float(r.v[i]);
-  return x;
-}
-template <class T>
-__device__ __forceinline__ Piece load_piece(const T* p) {
-  return floats(load_raw(p));
-}
-// the first `left` elements, the others as `none`
-template <class T>
-__device__ __forceinline__ Piece load_piece(const T* p, int left, float none) {
-  if (left >= 8) return load_piece(p);
-  Piece x = floats(load_raw_part(p, left));
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x.v[i] = i < left ? x.v[i] : none;
-  return x;
-}
-
 __device__ __forceinline__ void store_piece(half_t* p, const Piece& x) {
   half8_t h;
 #pragma unroll
