@@ -75,7 +75,8 @@ __device__ __forceinline__ void walk_chunk(const ClipArgs& a, const ClipTensor& 
     for (; p < c1; p += kTurn) use(0, p, int(c1 - p), P::load(g + p, int(c1 - p), c1 - p));
     return;
   }
-  // a band of rows; rows that are longer than a chunk alone
+  // A band of rows; rows that are longer than a chunk alone.  A lane has one piece on its way: us, fp32 in place, 2.4 M x 100 of a pitch of 104 / without gaps 607 / 541,
+  // 100 000 x 42 of 48 24.5 / 19.0.
   const int band = band_of(t.cols, a.chunk), r0 = k * band, nr = min(band, t.rows - r0);
   const uint32_t per = uint32_t((t.cols + V - 1) / V);
   for (uint32_t q = threadIdx.x; q < per * uint32_t(nr); q += kBlock) {

@@ -801,15 +801,17 @@ static void with_pieces(int pieces, Call&& call) {
 }
 constexpr int kWaveClasses = 4096;        // up to so many, a row is a wave's where there are rows enough
 static bool by_waves(int64_t n, int C) { return C <= kWaveClasses && n >= 4096; }
-// What a group of lanes holds: up to 512 classes, 2048 without alternatives (200 000 rows of 520 and their gradient, by waves / groups: 203 / 191 us, of 600
-// 189 / 172). Many alternatives of rows that take all lanes of a wave are found sooner among candidates (us, by groups / by waves, 100 000 rows of 500, fp32:
+// What a group of lanes holds: up to 512 classes, 2048 without alternatives (rows and their gradient, by waves / groups, us, fp16: 200 000 of 520 172 / 155, of 600
+// 176 / 158, of 1000 233 / 216, 100 000 of 1500 170 / 174, of 2000 204 / 203, 5000 of 1000 10.3 / 9.4; fp32, 100 000 of 520 112 / 112, of 2000 407 / 408). Many alternatives of rows that take all lanes of a wave are found sooner among candidates (us, by groups / by waves, 100 000 rows of 500, fp32:
 // best twenty 171 / 109, five 85 / 77; of 512, fp16, 127 / 122, 77 / 83; 400, best one 60 / 75; 212 828 of 247, two to a wave, best twenty 132 / 274).
 constexpr int kGroupTop = 8;
 static bool by_groups(int64_t n, int C, int k) {
   if (k > kGroupTop && C > kGroupClasses / 2 && by_waves(n, C)) return false;
   return C <= (k > 0 ? 1 : 4) * kGroupClasses;
 }
-// Workgroups of a row: as many as fill the chip, of no less than a piece for every lane
+// Workgroups of a row: as many as make 1024 in all, 64 at most, for no less than 2048 classes each.  Their waves take a part's classes by kStep in turn, so of a part
+// of 2048 one wave of the four has classes in fp16 and two in fp32: one row of 100 003 is 49 workgroups (best eight 10.3 us in fp16, 10.4 in fp32; none 6.5, 6.3),
+// rows of 513 to 2048 with alternatives one each where they are fewer than 4096 (best five of 1000: 100 rows 6.2 us, 1000 7.1, 4000 14.6).
 static int splits_of(int64_t n, int C, int k) {
   if (by_groups(n, C, k) || by_waves(n, C)) return 1;
   const int64_t most = ceil_div(C, int64_t(8) * kWave * kWavesPerBlock), want = ceil_div(1024, n), s = most < want ? most : want;
@@ -892,8 +894,10 @@ static hgnn_status logprob_grad(ScoreGradArgs& a, hipStream_t s) {
   const int N = group ? row_pieces(a.n, a.C, false) : 1, L = group ? group_lanes(a.C, N) : kWave;
   constexpr int V = 16 / int(sizeof(T)), W = 4;  // of long rows: 16 bytes, four of them
   a.chunks = group ? 1 : int(ceil_div(a.C, V * kWave * W));
-  // Long rows of large outputs are written past the caches.  us, the log probabilities and this, through / past: 4096 rows of 50 021 (fp16) 257 / 232,
-  // 1024 68.5 / 59; rows of 41 and 100 classes, whose ends share lines, 19 / 28, 159 / 214.
+  // Long rows of large outputs are written past the caches, whether they are whole lines or not.  us, the log probabilities and this, through / past, 208 MB: fp16,
+  // rows of 513 165 / 160, 520 152 / 151, 600 138 / 138, 777 126 / 121 (of a pitch of 784 128 / 122), 1000 116 / 108, 1500 119 / 114, 2000 126 / 101, 4000 126 / 99,
+  // 16 001 133 / 110, 50 021 136 / 112; fp32, 520 120 / 112, 1001 126 / 101, 4000 124 / 98, 16 001 126 / 102.  Rows that a group of lanes holds go through: past
+  // the caches those of 41 and 100 classes, whose ends share lines, took 28 for 19 and 214 for 159.
   const bool past = a.n * double(a.C) * sizeof(T) >= kPastBytes;
   HGNN_REQUIRE(double(a.n) * a.chunks * L <= double(kMostBlocks) * kBlock, HGNN_EUNSUPPORTED, "hgnn_logprob_grad: grid too large");
   const dim3 grid{unsigned(ceil_div(a.n * a.chunks * L, kBlock))};
