@@ -75,3 +75,34 @@ def test_accumulated_gradients_of_many_positions(hgnn, dev, n, V, F, ldy, ldt, o
     assert torch.equal(T, want.to(dtype))
     T.fill_(FILL)
     assert bool((buf == FILL).all()), "something beside the rows was written"
+
+
+@pytest.mark.parametrize("n,V,F,ldy", [(26000003, 5003, 1, 1), (2 ** 24 + 77, 300007, 126, 130)])
+@pytest.mark.parametrize("hub", [False, True])
+def test_gradients_of_very_many_positions(hgnn, dev, n, V, F, ldy, hub):
+    """More tiles of the sort than its sums are taken of at once, and rows of dY beyond 2^31 elements.  Whole numbers from -1 to 1, whose sums are
+    exact in fp32 in any order while an id has fewer than 2^24 positions."""
+    print(f"table gradient of {n} positions V={V} F={F} hub={hub}", flush=True)
+    gen = torch.Generator(device=dev).manual_seed(n % 1000 + F)
+    ids = torch.randint(0, V, (n,), generator=gen, device=dev, dtype=torch.int32)
+    if hub:
+        ids[torch.rand(n, generator=gen, device=dev) < 0.45] = V // 3
+    ids[torch.rand(n, generator=gen, device=dev) < 0.01] = -1
+    ids[-3:] = torch.tensor([V - 1, 0, V - 1], dtype=torch.int32, device=dev)
+    assert int((ids == V // 3).sum()) < 1 << 24
+    dY = torch.empty((n, ldy), dtype=HALF, device=dev)[:, :F]
+    for r in range(0, n, 1 << 20):
+        part = dY[r:r + (1 << 20)]
+        part.copy_(torch.randint(-1, 2, part.shape, generator=gen, device=dev, dtype=torch.int8))
+    T = torch.full((V, F), FILL, device=dev)
+    ws = torch.full((hgnn.hgnn_embedding_grad_workspace(n, F, V),), 255, dtype=torch.uint8, device=dev)
+    hgnn.hgnn_embedding_grad(ids, dY, T, ws)
+    torch.cuda.synchronize()
+    print("  sums on the device are there", flush=True)
+    want = torch.zeros((V, F), dtype=torch.float64, device=dev)
+    for r in range(0, n, 1 << 20):
+        i, y = ids[r:r + (1 << 20)].long(), dY[r:r + (1 << 20)].double()
+        rest = (i >= 0) & (i != V // 3)  # (torch adds rows of one index one by one: half a million of the same would take seconds)
+        want.index_add_(0, i[rest], y[rest])
+        want[V // 3] += y[i == V // 3].sum(0)
+    assert torch.equal(T.double(), want)

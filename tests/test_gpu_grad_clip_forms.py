@@ -52,3 +52,40 @@ def test_outputs_past_the_caches(hgnn, dev, in_place, inv_scale, max_norm):
             assert torch.equal(g, c), "what was read is as it was"
         o.fill_(FILL)
         assert bool((buf == FILL).all()), "something beside the rows was written"
+
+
+def test_many_tensors_captured(hgnn, dev):
+    """Several launches of each pass in a graph, replayed over other gradients, with a number among them that is none and without."""
+    gen = torch.Generator(device=dev).manual_seed(5)
+    sizes = [1 + 977 * i % 4099 for i in range(230)] + [1500007]
+    grads = [torch.zeros(n, dtype=(HALF, SINGLE)[i % 2], device=dev) for i, n in enumerate(sizes)]
+    outs = [torch.empty(n, dtype=(SINGLE, HALF)[i % 3 == 0], device=dev) for i, n in enumerate(sizes)]
+    ws = torch.empty(hgnn.hgnn_grad_norm_workspace(), dtype=torch.uint8, device=dev)
+    norm, alone = torch.zeros(1, device=dev), torch.zeros(1, device=dev)
+    call = lambda: (hgnn.hgnn_grad_clip(grads, 2.0, norm, ws, outs=outs, inv_scale=0.25), hgnn.hgnn_grad_norm(grads, alone, ws, inv_scale=0.25))  # noqa: E731
+    call()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call()
+    for turn in range(5):
+        for g in grads:
+            g.copy_(torch.randn(g.shape, generator=gen, device=dev) * 3 ** turn)
+        if turn == 2:
+            grads[150][0] = math.nan
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [norm.clone(), alone.clone()] + [o.clone() for o in outs]
+        for o in outs:
+            o.fill_(FILL)
+        call()
+        assert all(torch.equal(a.nan_to_num(nan=-1.0), b.nan_to_num(nan=-1.0)) for a, b in zip(got, [norm, alone] + outs))
+        if turn == 2:
+            assert math.isnan(float(norm)) and all(bool((o == 0).all()) for o in outs)
+            continue
+        ref = 0.25 * math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+        assert abs(float(norm) - ref) <= 6 * U * ref and torch.equal(norm, alone)
+        for g, o in zip(grads, outs):
+            want = g.double() * (0.25 * min(1.0, 2.0 / ref))
+            tol = 8 * U * want.abs() + 2.0 ** -149 + (want.abs() * 2.0 ** -11 + 2.0 ** -25 if o.dtype == HALF else 0.0)
+            assert bool(((o.double() - want).abs() <= tol).all())

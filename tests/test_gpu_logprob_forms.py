@@ -154,6 +154,8 @@ FORMS = [  # n, C, pitch, offset, k: a wave to a row with alternatives, of one t
     (33000, 511, 513, 1, 0), (40001, 257, 257, 0, 0), (140001, 57, 59, 3, 0), (262145, 31, 32, 0, 0), (70001, 200, 201, 1, 0),
     # workgroups to a row: a wave or two with classes, a last part that is short
     (3000, 1500, 1501, 1, 5), (700, 2500, 2501, 0, 9), (20, 30011, 30013, 1, 32), (1025, 4097, 4097, 0, 7),
+    # very many short rows
+    (17000003, 3, 3, 1, 2), (9000001, 9, 11, 0, 2), (9000001, 10, 10, 0, 7),
 ]
 
 
