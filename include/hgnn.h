@@ -25,7 +25,7 @@
  *    compute entry points are asynchronous on that stream, never synchronize and
  *    never allocate: scratch memory comes from the plan or from a workspace argument
  *    that the caller owns (hgnn_spmm, hgnn_linear_wgrad, hgnn_gat_feature_grad, hgnn_embedding_grad, hgnn_logprob,
- *    hgnn_grad_norm, hgnn_grad_clip).
+ *    hgnn_grad_norm, hgnn_grad_clip, hgnn_residual_norm_grad, hgnn_gated, hgnn_gated_grad, hgnn_orthogonalize).
  *    hgnn_plan_create, hgnn_plan_add_groups, hgnn_plan_add_slices, the export calls, hgnn_transpose,
  *    hgnn_coo_to_csr and hgnn_csr_validate allocate and/or synchronize (one-off set-up calls).
  *  - A plan owns scratch that the calls using it write (staging rows, per-vertex
@@ -612,6 +612,101 @@ hgnn_status hgnn_grad_norm(int32_t count, const hgnn_grad* grads, float inv_scal
  * same or overlap, nor may an output overlap another tensor's gradient. */
 hgnn_status hgnn_grad_clip(int32_t count, const hgnn_grad* grads, float inv_scale, float max_norm, float* norm, void* workspace,
                            size_t workspace_bytes, void* stream);
+
+/* ---- between two aggregations of a network, and between the clipped gradient and the weight ---------------------
+ * The norms around a block with its gate and residual, the gated projection, and updates of weights made orthogonal. */
+
+/* a norm of the rows of a tensor: RMS x / sqrt(mean(x^2) + eps), LAYER (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) */
+typedef enum { HGNN_NORM_NONE = 0, HGNN_NORM_RMS = 1, HGNN_NORM_LAYER = 2 } hgnn_norm_kind;
+
+/* What a block of a network does around its branch Y = f(...) (HOST structure, device arrays):
+ *   b = post(Y) * post_w + post_b,   H = alpha R + gate * b,   Z = pre(H) * pre_w + pre_b
+ * post: the norm of the branch; pre: the norm of the sum, for the next block.  Weights are fp32 [F]; one that is NULL counts
+ * as 1, a bias that is NULL as 0, and so does the gate: `gate` is fp32 [F] (one for every feature), gate_rows fp16
+ * [n][ld_gate] (one for every element); at most one of the two. */
+typedef struct {
+  hgnn_norm_kind post;
+  const float *post_w, *post_b;
+  const float* gate;
+  const hgnn_half* gate_rows;
+  int64_t ld_gate;
+  float alpha;
+  hgnn_norm_kind pre;
+  const float *pre_w, *pre_b;
+  float eps; /* > 0 */
+} hgnn_block;
+
+/* H and Z of a block (above) in one pass.  R and H are the residual stream, fp16 or fp32 [n][ld] (type); Y and Z are fp16
+ * [n][ld].  R or Y may be NULL and count as 0 (without Y no post and no gate); H may be NULL where it is not wanted, and may
+ * be R itself (with the same pitch); Z is there if and only if there is a norm `pre`, which takes H as it is stored, rounded
+ * to its type.  Statistics and all arithmetic are fp32.  Rows have any width up to 8192 (HGNN_EUNSUPPORTED beyond) and any
+ * pitch, arrays are aligned to their elements, nothing between or behind rows is written, nothing behind the last one read. */
+hgnn_status hgnn_residual_norm(int64_t n, int32_t F, const hgnn_block* block, hgnn_type type, const void* R, int64_t ldr, const hgnn_half* Y,
+                               int64_t ldy, void* H, int64_t ldh, hgnn_half* Z, int64_t ldz, void* stream);
+
+/* Where the gradients of a block go (HOST structure); those that are NULL are not formed.  With e = dH + (the gradient of Z
+ * through pre):  dR = alpha e,  dgate = sum over rows of e b (dgate_rows: e b),  dY = the gradient gate * e through post. */
+typedef struct {
+  void* dR; /* of the stream's type; may be dH itself (with the same pitch) */
+  int64_t lddr;
+  hgnn_half* dY;
+  int64_t lddy;
+  float* dgate; /* [F] */
+  hgnn_half* dgate_rows;
+  int64_t ldd_gate;
+  float *dpost_w, *dpost_b, *dpre_w, *dpre_b; /* [F] */
+} hgnn_block_grad;
+
+/* The gradients of a block given those of H (dH, of the stream's type, or NULL: 0; required without `pre`) and of Z (dZ,
+ * with `pre`), from H as hgnn_residual_norm stored it (where there is a norm `pre`) and Y (where there is a norm `post` or a
+ * gate).  The statistics of the rows are formed again.  Sums over rows are fp32, in a fixed order: no atomics, the same bits
+ * on every run.  workspace is device memory of at least hgnn_residual_norm_grad_workspace(n, F) bytes (16-byte aligned),
+ * owned by the caller and overwritten; it may be NULL where no sum over rows is wanted. */
+size_t hgnn_residual_norm_grad_workspace(int64_t n, int32_t F);
+hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* block, hgnn_type type, const void* H, int64_t ldh, const hgnn_half* Y,
+                                    int64_t ldy, const void* dH, int64_t lddh, const hgnn_half* dZ, int64_t lddz, const hgnn_block_grad* grads,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* what a gated projection does to the gate's side: x / (1 + exp(-x)), x Phi(x) (the normal distribution), 1 / (1 + exp(-x)), max(x, 0) */
+typedef enum { HGNN_SILU = 0, HGNN_GELU = 1, HGNN_SIGMOID = 2, HGNN_RELU = 3 } hgnn_activation;
+
+/* Y[i, f] = fp16( act(G[i, f]) * U[i, f] ),  G = X Wg,  U = X Wu:  both projections of a gated block, the activation and
+ * their product in one kernel; G and U stay in fp32 registers.  X is [n][ldx] with K columns, Y [n][ldy] with F; Wg and Wu
+ * are [K][ldw >= F] (trans_w = 0) or [F][ldw >= K] (trans_w != 0), all fp16.  K and F are any numbers up to 65536
+ * (HGNN_EUNSUPPORTED beyond).  All tensors need 16-byte aligned addresses and pitches that are multiples of 8
+ * (HGNN_EUNSUPPORTED otherwise); rows are read in 16-byte pieces up to the pitch, whatever the padding columns hold never
+ * reaches a result, and padding columns of outputs are not written.  Y may overlap no input.  workspace is device memory of
+ * at least hgnn_gated_workspace(n, K, F) bytes (16-byte aligned; 0: none is needed), owned by the caller and overwritten. */
+size_t hgnn_gated_workspace(int64_t n, int32_t K, int32_t F);
+hgnn_status hgnn_gated(int64_t n, int32_t K, int32_t F, hgnn_activation act, const hgnn_half* X, int64_t ldx, const hgnn_half* Wg, const hgnn_half* Wu,
+                       int64_t ldw, int32_t trans_w, hgnn_half* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gradients of hgnn_gated given that of Y:  dG = dY U act'(G), dU = dY act(G),  dX = dG Wg^T + dU Wu^T (fp16 [n][lddx]),
+ * dWg = X^T dG, dWu = X^T dU (fp16, laid out as the weights, pitch lddw; HGNN_RELU has the derivative 0 at 0).  dX, or dWg and
+ * dWu together, may be NULL: not wanted.  G and U are formed again; dG and dU pass through the workspace in fp16 as all
+ * vertex-level gradients here do (scale the loss as for those), and sums are fp32 in a fixed order.  Tensors as for
+ * hgnn_gated; workspace at least hgnn_gated_grad_workspace(n, K, F) bytes (16-byte aligned). */
+size_t hgnn_gated_grad_workspace(int64_t n, int32_t K, int32_t F);
+hgnn_status hgnn_gated_grad(int64_t n, int32_t K, int32_t F, hgnn_activation act, const hgnn_half* X, int64_t ldx, const hgnn_half* Wg,
+                            const hgnn_half* Wu, int64_t ldw, int32_t trans_w, const hgnn_half* dY, int64_t lddy, hgnn_half* dX, int64_t lddx,
+                            hgnn_half* dWg, hgnn_half* dWu, int64_t lddw, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Matrices made orthogonal by Newton-Schulz products, what an optimizer of that kind does to the (clipped, averaged) gradients
+ * of weight matrices before they are added:  with X = G / |G| (the 2-norm of all elements),
+ *   `steps` times  A = X X^T,  X <- a X + (b A + c A A) X     (a, b, c = coef[3 step ..]),   out = scale X
+ * which is a X + b X A' + c X A' A' from the other side (A' = X^T X): the shorter side is taken.  Every singular value s of X
+ * passes through a s + b s^3 + c s^5.  `grads` is a HOST array of `count` matrices, read before the call returns: rows x cols
+ * of fp16 or fp32 with a pitch, the output of either type, in place where it is NULL (as for hgnn_grad_clip).  coef is a HOST
+ * array of 3 * steps numbers (0 <= steps <= 64), scales a HOST array of one number for each matrix, or NULL: 1.  Products
+ * are formed from two fp16 numbers for each value (22 bits) with fp32 sums: the accuracy of fp32 products.  A matrix whose
+ * norm is 0 or not finite gives zeros.  Coefficients that let a singular value that was at most 1 pass 8 (or a product 64) on
+ * its way are HGNN_EINVAL, a side of more than 65536 HGNN_EUNSUPPORTED.  No two outputs may be the same or overlap, nor
+ * may an output overlap another matrix's gradient.  workspace is device memory of at least
+ * hgnn_orthogonalize_workspace(count, grads) bytes (16-byte aligned), owned by the caller and overwritten; only the sizes in
+ * `grads` count for it (0 where they are none that the call takes). */
+size_t hgnn_orthogonalize_workspace(int32_t count, const hgnn_grad* grads);
+hgnn_status hgnn_orthogonalize(int32_t count, const hgnn_grad* grads, int32_t steps, const float* coef, const float* scales, void* workspace,
+                               size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -23,6 +23,8 @@ HGNN_OK, HGNN_EINVAL, HGNN_EUNSUPPORTED, HGNN_ENOMEM, HGNN_EHIP = range(5)
 HGNN_SUM, HGNN_MEAN = 0, 1
 HGNN_SDDMM_DOT, HGNN_SDDMM_GAT_SCORE = 0, 1
 HGNN_F16, HGNN_F32 = 0, 1
+HGNN_NORM_NONE, HGNN_NORM_RMS, HGNN_NORM_LAYER = 0, 1, 2
+HGNN_SILU, HGNN_GELU, HGNN_SIGMOID, HGNN_RELU = 0, 1, 2, 3
 
 EXPORTS = (
     "hgnn_status_str", "hgnn_last_error", "hgnn_csr_validate", "hgnn_transpose", "hgnn_coo_to_csr", "hgnn_plan_create",
@@ -36,7 +38,9 @@ EXPORTS = (
     "hgnn_edge_to_transposed", "hgnn_scale_rows", "hgnn_linear", "hgnn_linear_padded", "hgnn_linear_wgrad", "hgnn_linear_wgrad_workspace",
     "hgnn_gat_feature_grad", "hgnn_gat_feature_grad_workspace", "hgnn_gat_forward_fused_save",
     "hgnn_gat_backward_fused_saved", "hgnn_embedding", "hgnn_embedding_grad", "hgnn_embedding_grad_workspace", "hgnn_logprob", "hgnn_logprob_workspace",
-    "hgnn_logprob_grad", "hgnn_grad_norm", "hgnn_grad_norm_workspace", "hgnn_grad_clip",
+    "hgnn_logprob_grad", "hgnn_grad_norm", "hgnn_grad_norm_workspace", "hgnn_grad_clip", "hgnn_residual_norm", "hgnn_residual_norm_grad",
+    "hgnn_residual_norm_grad_workspace", "hgnn_gated", "hgnn_gated_workspace", "hgnn_gated_grad", "hgnn_gated_grad_workspace", "hgnn_orthogonalize",
+    "hgnn_orthogonalize_workspace",
 )
 
 HGNN_EDGE_SEGMENTS, HGNN_EDGE_SEGMENTS_ATOMIC, HGNN_VERTEX_GROUPS, HGNN_VERTEX_GROUPS_HALF2 = 0, 1, 2, 3
@@ -63,6 +67,18 @@ class _CsrStruct(ctypes.Structure):
 class _GradStruct(ctypes.Structure):
     _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
                 ("ld", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("type", ctypes.c_int), ("out_type", ctypes.c_int)]
+
+
+class _BlockStruct(ctypes.Structure):
+    _fields_ = [("post", ctypes.c_int), ("post_w", ctypes.c_void_p), ("post_b", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("gate_rows", ctypes.c_void_p),
+                ("ld_gate", ctypes.c_int64), ("alpha", ctypes.c_float), ("pre", ctypes.c_int), ("pre_w", ctypes.c_void_p), ("pre_b", ctypes.c_void_p),
+                ("eps", ctypes.c_float)]
+
+
+class _BlockGradStruct(ctypes.Structure):
+    _fields_ = [("dR", ctypes.c_void_p), ("lddr", ctypes.c_int64), ("dY", ctypes.c_void_p), ("lddy", ctypes.c_int64), ("dgate", ctypes.c_void_p),
+                ("dgate_rows", ctypes.c_void_p), ("ldd_gate", ctypes.c_int64), ("dpost_w", ctypes.c_void_p), ("dpost_b", ctypes.c_void_p),
+                ("dpre_w", ctypes.c_void_p), ("dpre_b", ctypes.c_void_p)]
 
 
 _lib = None
@@ -165,6 +181,18 @@ def load() -> ctypes.CDLL:
     lib.hgnn_grad_norm_workspace.restype = ctypes.c_size_t
     lib.hgnn_grad_norm.argtypes = [i32, grads, f32, vp, vp, ctypes.c_size_t, vp]
     lib.hgnn_grad_clip.argtypes = [i32, grads, f32, f32, vp, vp, ctypes.c_size_t, vp]
+    block, sz, grad_list = ctypes.POINTER(_BlockStruct), ctypes.c_size_t, ctypes.POINTER(_GradStruct)
+    lib.hgnn_residual_norm.argtypes = [i64, i32, block, ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.hgnn_residual_norm_grad_workspace.restype = sz
+    lib.hgnn_residual_norm_grad_workspace.argtypes = [i64, i32]
+    lib.hgnn_residual_norm_grad.argtypes = [i64, i32, block, ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, i64, ctypes.POINTER(_BlockGradStruct), vp, sz, vp]
+    lib.hgnn_gated_workspace.restype = lib.hgnn_gated_grad_workspace.restype = sz
+    lib.hgnn_gated_workspace.argtypes = lib.hgnn_gated_grad_workspace.argtypes = [i64, i32, i32]
+    lib.hgnn_gated.argtypes = [i64, i32, i32, ctypes.c_int, vp, i64, vp, vp, i64, i32, vp, i64, vp, sz, vp]
+    lib.hgnn_gated_grad.argtypes = [i64, i32, i32, ctypes.c_int, vp, i64, vp, vp, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp, sz, vp]
+    lib.hgnn_orthogonalize_workspace.restype = sz
+    lib.hgnn_orthogonalize_workspace.argtypes = [i32, grad_list]
+    lib.hgnn_orthogonalize.argtypes = [i32, grad_list, i32, vp, vp, vp, sz, vp]
     for name in EXPORTS:
         getattr(lib, name)  # every declared entry point must be exported
     _calls = _load_calls(lib)
@@ -801,3 +829,185 @@ def hgnn_grad_clip(grads, max_norm: float, norm: torch.Tensor, workspace: torch.
     _here(norm, workspace)
     ws, bytes = _room(workspace)
     _check(load().hgnn_grad_clip(len(grads), a, inv_scale, max_norm, _dense("norm", norm, torch.float32, 1), ws, bytes, _stream(stream)))
+
+
+# ---- between two aggregations, and between the clipped gradient and the weight
+def _rows_or_none(name: str, t: Optional[torch.Tensor], rows: int, cols: int, dtype):
+    if t is None:
+        return None, 0
+    _ptr(t, dtype)
+    return _rows(name, t, rows, cols)
+
+
+def _norm_block(n: int, F: int, post, post_w, post_b, gate, alpha, pre, pre_w, pre_b, eps) -> _BlockStruct:
+    single = torch.float32
+    if post not in (0, 1, 2) or pre not in (0, 1, 2):
+        raise ValueError("post and pre must be HGNN_NORM_NONE, HGNN_NORM_RMS or HGNN_NORM_LAYER")
+    rows = gate is not None and gate.dim() == 2
+    g, ldg = _rows_or_none("gate", gate, n, F, torch.float16) if rows else (_dense("gate", gate, single, F), 0)
+    return _BlockStruct(post, _dense("post_w", post_w, single, F), _dense("post_b", post_b, single, F), None if rows else g, g if rows else None, ldg, alpha, pre,
+                        _dense("pre_w", pre_w, single, F), _dense("pre_b", pre_b, single, F), eps)
+
+
+def _size_and_type(rows, streams):
+    """(n, F) of the first tensor there is, and the type of the residual stream."""
+    t = next((t for t in rows if t is not None), None)
+    if t is None:
+        raise ValueError("no tensor is given")
+    n, F = _two("the tensors", t)
+    s = next((s for s in streams if s is not None), None)
+    return n, _int32("F", F), torch.float16 if s is None else s.dtype
+
+
+def hgnn_residual_norm(R: Optional[torch.Tensor], Y: Optional[torch.Tensor], H: Optional[torch.Tensor], Z: Optional[torch.Tensor], post: int = HGNN_NORM_NONE,
+                       post_w: Optional[torch.Tensor] = None, post_b: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, alpha: float = 1.0,
+                       pre: int = HGNN_NORM_NONE, pre_w: Optional[torch.Tensor] = None, pre_b: Optional[torch.Tensor] = None, eps: float = 1e-5, stream=None) -> None:
+    """H = alpha R + gate * post(Y), Z = pre(H), with the weights and biases of the two norms: R and H fp16 or fp32, Y and Z fp16; the gate is fp32 [F] or fp16
+    [n][F]; H may be R."""
+    if _calls is not None and _done(_calls.residual_norm(R, Y, H, Z, post, post_w, post_b, gate, alpha, pre, pre_w, pre_b, eps, stream)):
+        return
+    _here(R, Y, H, Z, post_w, post_b, gate, pre_w, pre_b)
+    n, F, dtype = _size_and_type((R, Y, H, Z), (R, H))
+    block = _norm_block(n, F, post, post_w, post_b, gate, alpha, pre, pre_w, pre_b, eps)
+    half = torch.float16
+    (r, ldr), (h, ldh) = _rows_or_none("R", R, n, F, dtype), _rows_or_none("H", H, n, F, dtype)
+    (y, ldy), (z, ldz) = _rows_or_none("Y", Y, n, F, half), _rows_or_none("Z", Z, n, F, half)
+    _check(load().hgnn_residual_norm(n, F, block, HGNN_F16 if R is None and H is None else _type(H if R is None else R), r, ldr, y, ldy, h, ldh, z, ldz, _stream(stream)))
+
+
+def hgnn_residual_norm_grad_workspace(n: int, F: int) -> int:
+    return load().hgnn_residual_norm_grad_workspace(n, _int32("F", F))
+
+
+def hgnn_residual_norm_grad(H: Optional[torch.Tensor], Y: Optional[torch.Tensor], dH: Optional[torch.Tensor], dZ: Optional[torch.Tensor], dR: Optional[torch.Tensor],
+                            dY: Optional[torch.Tensor], workspace: Optional[torch.Tensor], post: int = HGNN_NORM_NONE, post_w: Optional[torch.Tensor] = None,
+                            post_b: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, alpha: float = 1.0, pre: int = HGNN_NORM_NONE,
+                            pre_w: Optional[torch.Tensor] = None, pre_b: Optional[torch.Tensor] = None, eps: float = 1e-5, dgate: Optional[torch.Tensor] = None,
+                            dpost_w: Optional[torch.Tensor] = None, dpost_b: Optional[torch.Tensor] = None, dpre_w: Optional[torch.Tensor] = None,
+                            dpre_b: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The gradients of hgnn_residual_norm from those of H and Z, into the tensors that are given (dgate like the gate, dR may be dH); workspace: device tensor of
+    hgnn_residual_norm_grad_workspace(n, F) bytes, or None without sums over rows."""
+    if _calls is not None and _done(_calls.residual_norm_grad(H, Y, dH, dZ, dR, dY, workspace, post, post_w, post_b, gate, alpha, pre, pre_w, pre_b, eps, dgate,
+                                                              dpost_w, dpost_b, dpre_w, dpre_b, stream)):
+        return
+    _here(H, Y, dH, dZ, dR, dY, workspace, post_w, post_b, gate, pre_w, pre_b, dgate, dpost_w, dpost_b, dpre_w, dpre_b)
+    n, F, dtype = _size_and_type((H, Y, dH, dZ), (H, dH, dR))
+    block = _norm_block(n, F, post, post_w, post_b, gate, alpha, pre, pre_w, pre_b, eps)
+    half, single = torch.float16, torch.float32
+    (h, ldh), (y, ldy) = _rows_or_none("H", H, n, F, dtype), _rows_or_none("Y", Y, n, F, half)
+    (dh, lddh), (dz, lddz) = _rows_or_none("dH", dH, n, F, dtype), _rows_or_none("dZ", dZ, n, F, half)
+    (dr, lddr), (dy, lddy) = _rows_or_none("dR", dR, n, F, dtype), _rows_or_none("dY", dY, n, F, half)
+    if dgate is not None and (gate is None or gate.dim() != dgate.dim()):
+        raise ValueError("dgate goes with a gate of as many dimensions")
+    rows = dgate is not None and dgate.dim() == 2
+    dg, ldg = _rows_or_none("dgate", dgate, n, F, half) if rows else (_dense("dgate", dgate, single, F), 0)
+    grads = _BlockGradStruct(dr, lddr, dy, lddy, None if rows else dg, dg if rows else None, ldg, _dense("dpost_w", dpost_w, single, F),
+                             _dense("dpost_b", dpost_b, single, F), _dense("dpre_w", dpre_w, single, F), _dense("dpre_b", dpre_b, single, F))
+    ws, bytes = _room(workspace)
+    stream_type = next((t for t in (H, dH, dR) if t is not None), None)
+    _check(load().hgnn_residual_norm_grad(n, F, block, HGNN_F16 if stream_type is None else _type(stream_type), h, ldh, y, ldy, dh, lddh, dz, lddz, grads, ws, bytes,
+                                          _stream(stream)))
+
+
+def _padded(name: str, t: torch.Tensor, rows: int, cols: int, read: bool = True):
+    """-> (address, pitch) of fp16 rows that are read in pieces of eight elements: what the last piece brings from behind the row has to be there."""
+    p, ld = _rows(name, t, rows, cols)
+    _ptr(t, torch.float16)
+    whole = (cols + 7) // 8 * 8
+    if rows <= 1:
+        ld = whole
+    if read and rows > 0 and (t.storage_offset() + (rows - 1) * ld + whole) * 2 > t.untyped_storage().nbytes():
+        raise ValueError(f"{name}: rows of {cols} elements are read in pieces of eight, and behind the last one there is not room enough")
+    return p, ld
+
+
+def _gated_weights(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, F: int, trans_w: bool):
+    n, K = _two("X", X)
+    shape = (F, K) if trans_w else (K, F)
+    x, ldx = _padded("X", X, n, K)
+    (g, ldw), (u, ldu) = _padded("Wg", Wg, *shape), _padded("Wu", Wu, *shape)
+    if ldw != ldu:
+        raise ValueError(f"Wg and Wu must have the same pitch, got {ldw} and {ldu}")
+    return n, _int32("K", K), _int32("F", F), x, ldx, g, u, ldw
+
+
+def hgnn_gated_workspace(n: int, K: int, F: int) -> int:
+    return load().hgnn_gated_workspace(n, _int32("K", K), _int32("F", F))
+
+
+def hgnn_gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Y: torch.Tensor, act: int = HGNN_SILU, trans_w: bool = False,
+               workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Y = act(X Wg) * (X Wu), all fp16, the weights [K][F] (or [F][K] with trans_w); workspace: device tensor of hgnn_gated_workspace(n, K, F) bytes."""
+    if _calls is not None and _done(_calls.gated(X, Wg, Wu, Y, act, trans_w, workspace, stream)):
+        return
+    _here(X, Wg, Wu, Y, workspace)
+    n, K, F, x, ldx, g, u, ldw = _gated_weights(X, Wg, Wu, _two("Y", Y)[1], trans_w)
+    y, ldy = _padded("Y", Y, n, F, read=False)
+    ws, bytes = _room(workspace)
+    _check(load().hgnn_gated(n, K, F, act, x, ldx, g, u, ldw, 1 if trans_w else 0, y, ldy, ws, bytes, _stream(stream)))
+
+
+def hgnn_gated_grad_workspace(n: int, K: int, F: int) -> int:
+    return load().hgnn_gated_grad_workspace(n, _int32("K", K), _int32("F", F))
+
+
+def hgnn_gated_grad(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, dY: torch.Tensor, dX: Optional[torch.Tensor], dWg: Optional[torch.Tensor],
+                    dWu: Optional[torch.Tensor], workspace: torch.Tensor, act: int = HGNN_SILU, trans_w: bool = False, stream=None) -> None:
+    """The gradients of hgnn_gated from that of Y, all fp16; dX, or dWg and dWu, may be None; workspace: device tensor of hgnn_gated_grad_workspace(n, K, F) bytes."""
+    if _calls is not None and _done(_calls.gated_grad(X, Wg, Wu, dY, dX, dWg, dWu, workspace, act, trans_w, stream)):
+        return
+    _here(X, Wg, Wu, dY, dX, dWg, dWu, workspace)
+    n, K, F, x, ldx, g, u, ldw = _gated_weights(X, Wg, Wu, _two("dY", dY)[1], trans_w)
+    dy, lddy = _padded("dY", dY, n, F)
+    dx, lddx = (None, 0) if dX is None else _padded("dX", dX, n, K, read=False)
+    if (dWg is None) != (dWu is None):
+        raise ValueError("dWg and dWu go together")
+    shape = (F, K) if trans_w else (K, F)
+    (dg, lddw), (du, lddu) = ((None, 0), (None, 0)) if dWg is None else (_padded("dWg", dWg, *shape, read=False), _padded("dWu", dWu, *shape, read=False))
+    if lddw != lddu:
+        raise ValueError(f"dWg and dWu must have the same pitch, got {lddw} and {lddu}")
+    ws, bytes = _room(workspace)
+    _check(load().hgnn_gated_grad(n, K, F, act, x, ldx, g, u, ldw, 1 if trans_w else 0, dy, lddy, dx, lddx, dg, du, lddw, ws, bytes, _stream(stream)))
+
+
+def _matrices(grads, outs=None):
+    """A list of matrices and where they go, as the C side takes it."""
+    if outs is not None and len(outs) != len(grads):
+        raise ValueError("grads and outs must have the same length")
+    a = (_GradStruct * max(len(grads), 1))()
+    for i, t in enumerate(grads):
+        o = t if outs is None else outs[i]
+        rows, cols = _two(f"grads[{i}]", t)
+        if t.numel() == 0 and o.shape == t.shape:  # nothing, whatever its strides
+            a[i] = _GradStruct(_ptr(t), _ptr(o), rows, cols, cols, cols, _type(t), _type(o))
+            continue
+        p, ld = _rows(f"grads[{i}]", t, rows, cols)
+        q, ldo = _rows(f"outs[{i}]", o, rows, cols)
+        a[i] = _GradStruct(p, q, rows, cols, ld, ldo, _type(t), _type(o))
+    return a
+
+
+def hgnn_orthogonalize_workspace(grads) -> int:
+    """Bytes of the workspace for matrices of these shapes (tensors)."""
+    a = (_GradStruct * max(len(grads), 1))()
+    for i, t in enumerate(grads):
+        rows, cols = _two(f"grads[{i}]", t)
+        a[i] = _GradStruct(None, None, rows, cols, cols, cols, _type(t), _type(t))
+    return load().hgnn_orthogonalize_workspace(len(grads), a)
+
+
+def hgnn_orthogonalize(grads, outs, coef, workspace: Optional[torch.Tensor], scales=None, stream=None) -> None:
+    """A list of fp16 or fp32 matrices, each divided by its norm, through len(coef) steps x <- a x + (b A + c A A) x with A = x x^T and (a, b, c) of coef, times
+    scales[i] (or 1), into outs (fp16 or fp32) or, where that is None, in place; workspace: device tensor of hgnn_orthogonalize_workspace(grads) bytes."""
+    if _calls is not None and _done(_calls.orthogonalize(grads, outs, coef, workspace, scales, stream)):
+        return
+    a = _matrices(grads, outs)
+    _here(*grads, *(outs or ()), workspace)
+    steps = [float(v) for step in coef for v in step]
+    if any(len(step) != 3 for step in coef):
+        raise ValueError("coef must be a list of (a, b, c)")
+    if scales is not None and len(scales) != len(grads):
+        raise ValueError("grads and scales must have the same length")
+    ws, bytes = _room(workspace)
+    _check(load().hgnn_orthogonalize(len(grads), a, len(coef), (ctypes.c_float * max(len(steps), 1))(*steps),
+                                     None if scales is None else (ctypes.c_float * max(len(scales), 1))(*scales), ws, bytes, _stream(stream)))

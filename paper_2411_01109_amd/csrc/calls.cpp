@@ -14,6 +14,7 @@
 #include <cstdint>
 #include <cstring>
 #include <exception>
+#include <initializer_list>
 #include <new>
 #include <optional>
 #include <vector>
@@ -32,6 +33,14 @@ struct Table {  // a vertex-level tensor: rows of a pitch, unit stride along the
   int64_t ld = 0, rows = 0, cols = 0;
   hgnn_half* half() const { return static_cast<hgnn_half*>(p); }
   float* single() const { return static_cast<float*>(p); }
+};
+
+struct Size {
+  int64_t rows = 0, cols = 0;
+};
+struct Gate {  // one for every feature, or for every element
+  const float* one = nullptr;
+  Table rows;
 };
 
 // Reads arguments; ok turns false with the first that is not plain.
@@ -163,6 +172,92 @@ struct Reader {
     }
     return r;
   }
+  // for the calls between two aggregations: the size of the first tensor there is, the type of the residual stream
+  Size first_size(std::initializer_list<PyObject*> list) {
+    for (PyObject* const o : list) {
+      if (o == Py_None) continue;
+      const at::Tensor* const t = tensor(o);
+      if (t && t->dim() == 2) return {t->size(0), t->size(1)};
+      break;
+    }
+    ok = false;
+    return {};
+  }
+  hgnn_type stream_type(std::initializer_list<PyObject*> list) {
+    for (PyObject* const o : list)
+      if (o != Py_None) return tensor(o) ? type_of(o) : HGNN_F16;
+    return HGNN_F16;
+  }
+  Table rows_or_null(PyObject* o, Size z, hgnn_type type) {
+    if (o == Py_None || !ok) return Table();
+    const Table t = rows(o, z.rows, z.cols);
+    if (type_of(o) != type) ok = false;
+    return t;
+  }
+  Gate gate(PyObject* o, Size z) {
+    Gate g;
+    if (o == Py_None) return g;
+    const at::Tensor* const t = tensor(o);
+    if (t && t->dim() == 2) g.rows = rows_or_null(o, z, HGNN_F16);
+    else if (t) g.one = static_cast<const float*>(dense(o, at::kFloat, z.cols));
+    return g;
+  }
+  // post, post_w, post_b, gate, alpha, pre, pre_w, pre_b, eps
+  hgnn_block block(PyObject* const* a, Size z) {
+    const auto kind = [&](PyObject* o) {
+      const int k = integer(o);
+      if (k < 0 || k > 2) ok = false;
+      return hgnn_norm_kind(k);
+    };
+    const auto vector = [&](PyObject* o) { return ok ? static_cast<const float*>(dense(o, at::kFloat, z.cols)) : nullptr; };
+    hgnn_block b{};
+    b.post = kind(a[0]), b.post_w = vector(a[1]), b.post_b = vector(a[2]);
+    const Gate g = gate(a[3], z);
+    b.gate = g.one, b.gate_rows = g.rows.half(), b.ld_gate = g.rows.ld;
+    b.alpha = real(a[4]), b.pre = kind(a[5]), b.pre_w = vector(a[6]), b.pre_b = vector(a[7]), b.eps = real(a[8]);
+    return b;
+  }
+  // fp16 rows that are read in pieces of eight: what the last piece brings from behind its row has to be there
+  Table padded(PyObject* o, Size z, bool read) {
+    Table t = ok ? rows(o, z.rows, z.cols) : Table();
+    if (!ok || type_of(o) != HGNN_F16 || !ok) {
+      ok = false;
+      return t;
+    }
+    const int64_t whole = (z.cols + 7) / 8 * 8;
+    if (z.rows <= 1) t.ld = whole;
+    const at::Tensor& x = THPVariable_Unpack(o);
+    if (read && z.rows > 0 && uint64_t(x.storage_offset() + (z.rows - 1) * t.ld + whole) * 2 > x.storage().nbytes()) ok = false;
+    return t;
+  }
+  std::vector<hgnn_grad> matrices(PyObject* o, PyObject* outs) {
+    std::vector<hgnn_grad> r;
+    const auto listed = [](PyObject* x) { return PyList_CheckExact(x) || PyTuple_CheckExact(x); };
+    if (!listed(o) || (outs != Py_None && (!listed(outs) || PySequence_Fast_GET_SIZE(outs) != PySequence_Fast_GET_SIZE(o)))) {
+      ok = false;
+      return r;
+    }
+    r.resize(size_t(PySequence_Fast_GET_SIZE(o)));
+    for (size_t i = 0; i < r.size() && ok; ++i) {
+      PyObject *const a = PySequence_Fast_GET_ITEM(o, Py_ssize_t(i)), *const b = outs == Py_None ? a : PySequence_Fast_GET_ITEM(outs, Py_ssize_t(i));
+      const Table t = rows(a), u = ok ? rows(b, t.rows, t.cols) : t;
+      if (ok) r[i] = hgnn_grad{t.p, u.p, t.rows, t.cols, t.ld, u.ld, type_of(a), type_of(b)};
+    }
+    return r;
+  }
+  std::vector<float> reals(PyObject* o, Py_ssize_t n) {
+    std::vector<float> r;
+    if (!(PyList_CheckExact(o) || PyTuple_CheckExact(o)) || PySequence_Fast_GET_SIZE(o) != n) ok = false;
+    for (Py_ssize_t i = 0; ok && i < n; ++i) r.push_back(real(PySequence_Fast_GET_ITEM(o, i)));
+    return r;
+  }
+  std::vector<float> triples(PyObject* o) {
+    std::vector<float> r;
+    if (!(PyList_CheckExact(o) || PyTuple_CheckExact(o))) ok = false;
+    for (Py_ssize_t i = 0; ok && i < PySequence_Fast_GET_SIZE(o); ++i)
+      for (const float v : reals(PySequence_Fast_GET_ITEM(o, i), 3)) r.push_back(v);
+    return r;
+  }
   Table table_or_null(PyObject* o) { return o == Py_None ? Table() : table(o); }
   void* workspace(PyObject* o, size_t* bytes) {
     *bytes = 0;
@@ -281,7 +376,8 @@ PyObject* run(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F&& f) {
 #define HGNN_ENTRIES(X)                                                                                                          \
   X(linear) X(linear_padded) X(linear_wgrad) X(spmm) X(spmm_discretized) X(spmm_discretized_fused) X(sddmm) X(edge_softmax)       \
   X(edge_softmax_bwd) X(edge_rowsum) X(edge_colsum) X(gat_forward_fused) X(gat_forward_fused_save) X(gat_backward_fused_saved) \
-  X(gat_feature_grad) X(embedding) X(embedding_grad) X(logprob) X(logprob_grad) X(grad_norm) X(grad_clip)
+  X(gat_feature_grad) X(embedding) X(embedding_grad) X(logprob) X(logprob_grad) X(grad_norm) X(grad_clip) X(residual_norm)       \
+  X(residual_norm_grad) X(gated) X(gated_grad) X(orthogonalize)
 #define HGNN_ENTRY(name) decltype(&hgnn_##name) f_##name = nullptr;
 HGNN_ENTRIES(HGNN_ENTRY)
 
@@ -551,6 +647,80 @@ HGNN_CALL(grad_clip, 7) {
   return [=] { return f_grad_clip(n, g.data(), inv_scale, max_norm, norm, ws, bytes, s); };
 } HGNN_END
 
+HGNN_CALL(residual_norm, 14) {
+  const Size z = r.first_size({a[0], a[1], a[2], a[3]});
+  const hgnn_type type = r.stream_type({a[0], a[2]});
+  const Table R = r.rows_or_null(a[0], z, type), Y = r.rows_or_null(a[1], z, HGNN_F16), H = r.rows_or_null(a[2], z, type), Z = r.rows_or_null(a[3], z, HGNN_F16);
+  const hgnn_block b = r.block(a + 4, z);
+  const int32_t F = r.count(z.cols);
+  void* const s = r.stream_here(a[13]);
+  return [=] { return f_residual_norm(z.rows, F, &b, type, R.p, R.ld, Y.half(), Y.ld, H.p, H.ld, Z.half(), Z.ld, s); };
+} HGNN_END
+
+HGNN_CALL(residual_norm_grad, 22) {
+  const Size z = r.first_size({a[0], a[1], a[2], a[3]});
+  const hgnn_type type = r.stream_type({a[0], a[2], a[4]});
+  const Table H = r.rows_or_null(a[0], z, type), Y = r.rows_or_null(a[1], z, HGNN_F16), dH = r.rows_or_null(a[2], z, type), dZ = r.rows_or_null(a[3], z, HGNN_F16);
+  const Table dR = r.rows_or_null(a[4], z, type), dY = r.rows_or_null(a[5], z, HGNN_F16);
+  size_t bytes;
+  void* const ws = r.room(a[6], &bytes);
+  const hgnn_block b = r.block(a + 7, z);
+  hgnn_block_grad g{};
+  g.dR = dR.p, g.lddr = dR.ld, g.dY = dY.half(), g.lddy = dY.ld;
+  const Gate d = r.gate(a[16], z);
+  if ((d.one && !b.gate) || (d.rows.p && !b.gate_rows)) r.ok = false;
+  g.dgate = const_cast<float*>(d.one), g.dgate_rows = d.rows.half(), g.ldd_gate = d.rows.ld;
+  float** const vectors[] = {&g.dpost_w, &g.dpost_b, &g.dpre_w, &g.dpre_b};
+  for (int i = 0; i < 4; ++i) *vectors[i] = static_cast<float*>(r.dense(a[17 + i], at::kFloat, z.cols));
+  const int32_t F = r.count(z.cols);
+  void* const s = r.stream_here(a[21]);
+  return [=] { return f_residual_norm_grad(z.rows, F, &b, type, H.p, H.ld, Y.half(), Y.ld, dH.p, dH.ld, dZ.half(), dZ.ld, &g, ws, bytes, s); };
+} HGNN_END
+
+HGNN_CALL(gated, 8) {
+  const Size x = r.first_size({a[0]}), y = r.first_size({a[3]});
+  const bool trans = r.truth(a[5]);
+  const Size w = trans ? Size{y.cols, x.cols} : Size{x.cols, y.cols};
+  const Table X = r.padded(a[0], x, true), Wg = r.padded(a[1], w, true), Wu = r.padded(a[2], w, true), Y = r.padded(a[3], {x.rows, y.cols}, false);
+  if (Wg.ld != Wu.ld) r.ok = false;
+  const auto act = hgnn_activation(r.integer(a[4]));
+  size_t bytes;
+  void* const ws = r.room(a[6], &bytes);
+  const int32_t K = r.count(x.cols), F = r.count(y.cols);
+  void* const s = r.stream_here(a[7]);
+  return [=] { return f_gated(x.rows, K, F, act, X.half(), X.ld, Wg.half(), Wu.half(), Wg.ld, trans, Y.half(), Y.ld, ws, bytes, s); };
+} HGNN_END
+
+HGNN_CALL(gated_grad, 11) {
+  const Size x = r.first_size({a[0]}), y = r.first_size({a[3]});
+  const bool trans = r.truth(a[9]);
+  const Size w = trans ? Size{y.cols, x.cols} : Size{x.cols, y.cols};
+  const Table X = r.padded(a[0], x, true), Wg = r.padded(a[1], w, true), Wu = r.padded(a[2], w, true), dY = r.padded(a[3], {x.rows, y.cols}, true);
+  const Table dX = a[4] == Py_None ? Table() : r.padded(a[4], x, false);
+  if ((a[5] == Py_None) != (a[6] == Py_None)) r.ok = false;
+  const Table dWg = a[5] == Py_None ? Table() : r.padded(a[5], w, false), dWu = a[6] == Py_None ? Table() : r.padded(a[6], w, false);
+  if (Wg.ld != Wu.ld || dWg.ld != dWu.ld) r.ok = false;
+  size_t bytes;
+  void* const ws = r.room(a[7], &bytes);
+  const auto act = hgnn_activation(r.integer(a[8]));
+  const int32_t K = r.count(x.cols), F = r.count(y.cols);
+  void* const s = r.stream_here(a[10]);
+  return [=] {
+    return f_gated_grad(x.rows, K, F, act, X.half(), X.ld, Wg.half(), Wu.half(), Wg.ld, trans, dY.half(), dY.ld, dX.half(), dX.ld, dWg.half(), dWu.half(), dWg.ld, ws, bytes, s);
+  };
+} HGNN_END
+
+HGNN_CALL(orthogonalize, 6) {
+  const std::vector<hgnn_grad> g = r.matrices(a[0], a[1]);
+  const std::vector<float> coef = r.triples(a[2]);
+  size_t bytes;
+  void* const ws = r.room(a[3], &bytes);
+  const std::vector<float> scales = a[4] == Py_None ? std::vector<float>() : r.reals(a[4], Py_ssize_t(g.size()));
+  const int32_t n = r.count(int64_t(g.size())), steps = r.count(int64_t(coef.size() / 3));
+  void* const s = r.stream_here(a[5]);
+  return [=] { return f_orthogonalize(n, g.data(), steps, coef.data(), scales.empty() ? nullptr : scales.data(), ws, bytes, s); };
+} HGNN_END
+
 // bind({entry point: address}, raw stream of a device, current device)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 3 || !PyDict_Check(a[0])) {
@@ -578,7 +748,8 @@ PyMethodDef methods[] = {HGNN_METHOD(bind), HGNN_METHOD(linear), HGNN_METHOD(lin
                          HGNN_METHOD(spmm_discretized_fused), HGNN_METHOD(sddmm), HGNN_METHOD(edge_softmax), HGNN_METHOD(edge_softmax_bwd),
                          HGNN_METHOD(edge_rowsum), HGNN_METHOD(edge_colsum), HGNN_METHOD(gat_forward_fused), HGNN_METHOD(gat_forward_fused_save),
                          HGNN_METHOD(gat_backward_fused_saved), HGNN_METHOD(gat_feature_grad), HGNN_METHOD(embedding), HGNN_METHOD(embedding_grad),
-                         HGNN_METHOD(logprob), HGNN_METHOD(logprob_grad), HGNN_METHOD(grad_norm), HGNN_METHOD(grad_clip), {nullptr, nullptr, 0, nullptr}};
+                         HGNN_METHOD(logprob), HGNN_METHOD(logprob_grad), HGNN_METHOD(grad_norm), HGNN_METHOD(grad_clip), HGNN_METHOD(residual_norm),
+                         HGNN_METHOD(residual_norm_grad), HGNN_METHOD(gated), HGNN_METHOD(gated_grad), HGNN_METHOD(orthogonalize), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

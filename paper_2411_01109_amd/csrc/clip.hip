@@ -199,7 +199,7 @@ static hgnn_status check_grads(const char* who, int32_t count, const hgnn_grad* 
   return HGNN_OK;
 }
 
-static hgnn_status check_outputs(const char* who, int32_t count, const hgnn_grad* g) {
+hgnn_status check_outputs(const char* who, int32_t count, const hgnn_grad* g) {
   if (count < 2) return HGNN_OK;
   const std::unique_ptr<const void*[]> outs(new (std::nothrow) const void*[size_t(count)]);
   HGNN_REQUIRE(outs != nullptr, HGNN_ENOMEM, "%s: host allocation failed", who);

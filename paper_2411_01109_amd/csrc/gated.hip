@@ -1,0 +1,346 @@
+// The gated projection  Y = act(G) * U,  G = X Wg,  U = X Wu,  and its gradients
+//   dG = dY U act'(G),  dU = dY act(G),  dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU
+// on the product kernel of product.h.  The forward forms both sums of an element in the same lane, so the activation and the product cost no pass of their own.
+// The gradients form G and U once more (two of their six products) and leave dG and dU beside each other in the workspace, [n][2 Fp] in fp16: a rounding of
+// 2^-11 of each value, as every vertex-level gradient of this library takes it; then dX is one product over both halves and (dWg, dWu) is one, too.
+// Where C has too few tiles for the chip the contraction is cut; the parts' fp32 sums go through the workspace and are added in their order.
+#include <algorithm>
+#include <cmath>
+
+#include "product.h"
+
+namespace hgnn {
+
+// ---- activations
+__device__ __forceinline__ float gate_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f)); }
+__device__ __forceinline__ float gate_value(int act, float x) {  // act: uniform
+  switch (act) {
+    case HGNN_SILU: return x * gate_sigmoid(x);
+    case HGNN_GELU: return 0.5f * x * (1.f + erff(x * 0.70710678f));
+    case HGNN_SIGMOID: return gate_sigmoid(x);
+    default: return x > 0.f ? x : x == x ? 0.f : x;
+  }
+}
+__device__ __forceinline__ void gate_both(int act, float x, float& value, float& slope) {
+  switch (act) {
+    case HGNN_SILU: {
+      const float p = gate_sigmoid(x);
+      value = x * p, slope = p * (1.f + x * (1.f - p));
+      return;
+    }
+    case HGNN_GELU: {
+      const float phi = 0.5f * (1.f + erff(x * 0.70710678f));
+      value = x * phi, slope = fmaf(x * 0.39894228f, __builtin_amdgcn_exp2f(x * x * -0.72134752f), phi);
+      return;
+    }
+    case HGNN_SIGMOID: {
+      value = gate_sigmoid(x), slope = value * (1.f - value);
+      return;
+    }
+    default: value = x > 0.f ? x : x == x ? 0.f : x, slope = x > 0.f ? 1.f : 0.f;
+  }
+}
+
+// the first `left` of four values (all of them where it is four or more), at 8-byte aligned places
+__device__ __forceinline__ void store_four(half_t* p, int64_t left, const float4_t& v) {
+  const half4_t h = {half_t(v[0]), half_t(v[1]), half_t(v[2]), half_t(v[3])};
+  if (left >= 4) {
+    *reinterpret_cast<half4_t*>(p) = h;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < left) p[e] = h[e];
+  }
+}
+
+// ---- what becomes of the two sums of an element
+struct GatedOut {
+  int act, F;
+  half_t* Y;
+  int64_t ldy;
+  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& g, const float4_t& u) const {
+    float4_t y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = gate_value(act, g[e]) * u[e];
+    store_four(Y + q * ldy + p, F - p, y);
+  }
+};
+struct GatedGradOut {
+  int act;
+  const half_t* dY;
+  int64_t lddy;
+  half_t* D;  // [n][2 Fp]
+  int64_t Fp;
+  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& g, const float4_t& u) const {
+    const half4_t dy = *reinterpret_cast<const half4_t*>(dY + q * lddy + p);  // what is behind F reaches what is behind F
+    float4_t dg, du;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float value, slope;
+      gate_both(act, g[e], value, slope);
+      dg[e] = float(dy[e]) * u[e] * slope, du[e] = float(dy[e]) * value;
+    }
+    store_four(D + q * 2 * Fp + p, 4, dg);
+    store_four(D + q * 2 * Fp + Fp + p, 4, du);
+  }
+};
+struct GatedPart {  // [parts][n][2][Fp]
+  float* part;
+  int64_t n, Fp;
+  __device__ void operator()(int64_t k, int64_t q, int64_t p, const float4_t& g, const float4_t& u) const {
+    float* const at = part + ((k * n + q) * 2) * Fp + p;
+    *reinterpret_cast<float4_t*>(at) = g;
+    *reinterpret_cast<float4_t*>(at + Fp) = u;
+  }
+};
+template <class Out>
+__global__ __launch_bounds__(kBlock) void gated_join_kernel(const float* part, int parts, int64_t n, int F, int64_t Fp, Out out) {
+  const int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x, each = (F + 3) / 4, q = t / each, p = 4 * (t - q * each);
+  if (q >= n) return;
+  const float* at = part + q * 2 * Fp + p;
+  const int64_t stride = n * 2 * Fp;
+  float4_t g = *reinterpret_cast<const float4_t*>(at), u = *reinterpret_cast<const float4_t*>(at + Fp);
+#pragma unroll 4
+  for (int k = 1; k < parts; ++k) {
+    at += stride;
+    g += *reinterpret_cast<const float4_t*>(at), u += *reinterpret_cast<const float4_t*>(at + Fp);
+  }
+  out(0, q, p, g, u);
+}
+
+// ---- products into one fp16 matrix, or into two that are the halves of C's lines or of its items along a line
+struct HalfOut {
+  half_t *a, *b;
+  int64_t ld;
+  int64_t split_q, split_p;  // from there on b's; beyond C: none
+  int64_t lines, cols;       // of either
+  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const {
+    half_t* to = a;
+    if (q >= split_q) to = b, q -= split_q;
+    if (p >= split_p) to = b, p -= split_p;
+    if (q < lines && p < cols) store_four(to + q * ld + p, cols - p, v);
+  }
+};
+struct HalfPart {  // [parts][nq][pitch]
+  float* part;
+  int64_t nq, pitch;
+  __device__ void operator()(int64_t k, int64_t q, int64_t p, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * pitch + p) = v; }
+};
+__global__ __launch_bounds__(kBlock) void half_join_kernel(const float* part, int parts, int64_t nq, int64_t pitch, HalfOut out) {
+  const int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x, each = pitch / 4, q = t / each, p = 4 * (t - q * each);
+  if (q >= nq) return;
+  const float* at = part + q * pitch + p;
+  const int64_t stride = nq * pitch;
+  float4_t v = *reinterpret_cast<const float4_t*>(at);
+#pragma unroll 4
+  for (int k = 1; k < parts; ++k) {
+    at += stride;
+    v += *reinterpret_cast<const float4_t*>(at);
+  }
+  out(0, q, p, v);
+}
+
+__global__ __launch_bounds__(kBlock) void half_zero_kernel(half_t* out, int64_t lines, int64_t cols, int64_t ld) {
+  const int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x, each = (cols + 3) / 4, q = t / each, p = 4 * (t - q * each);
+  if (q < lines) store_four(out + q * ld + p, cols - p, float4_t{0.f, 0.f, 0.f, 0.f});
+}
+
+static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// ---- shapes.  A product of few rows takes tiles of 64, one whose tiles of 256 x 256 fill the chip those, any other 128 x 128.
+enum Size { kFew, kMid, kWide };
+constexpr int kFull = 256;  // compute units
+template <ProductKind KIND, bool QCOL, bool PCOL, class Call>
+static hgnn_status with_product(Size size, Call&& call) {
+  constexpr int two = KIND == kTwo ? 2 : 1;  // two results: half as many items of P
+  if (size == kFew) return call(ProductShape<2, 2, 2, 2, KIND, QCOL, PCOL, 4>());
+  if (size == kMid) return call(ProductShape<2, 2, 4, 4 / two, KIND, QCOL, PCOL, 4>());
+  return call(ProductShape<2, 4, 8, 4 / two, KIND, QCOL, PCOL, 4>());
+}
+struct Split {
+  Size size;
+  int parts;
+  int64_t part;  // contraction steps of a part
+};
+// nq x np sums over K steps (`two`: a pair of each).  Parts of at least 128 steps until the chip has two workgroups a compute unit.
+static Split split_of(int64_t nq, int64_t np, int64_t K, bool two) {
+  const auto tiles = [&](int64_t b) { return ceil_div(nq, b) * ceil_div(np, two ? b / 2 : b); };
+  Split s;
+  s.size = nq <= 64 || np <= (two ? 32 : 64) ? kFew : tiles(256) >= kFull ? kWide : kMid;
+  const int64_t t = s.size == kFew ? ceil_div(nq, 64) * ceil_div(np, 64) : tiles(s.size == kWide ? 256 : 128);
+  int64_t parts = t >= kFull ? 1 : std::min(ceil_div(2 * kFull, t), ceil_div(K, 128));
+  s.part = std::max<int64_t>(32, up(ceil_div(K, std::max<int64_t>(parts, 1)), 32));
+  s.parts = int(std::max<int64_t>(1, ceil_div(K, s.part)));
+  return s;
+}
+
+struct GatedSizes {
+  int64_t n, Fp;
+  int K, F;
+  Split gate, dx, dw;
+  size_t gate_part, dx_part, dw_part, d;
+};
+static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
+  GatedSizes z{};
+  z.n = n, z.K = K, z.F = F, z.Fp = up(F, 64);
+  z.gate = split_of(n, F, K, true);
+  z.dx = split_of(n, K, F, false);
+  z.dw = split_of(K, 2 * z.Fp, n, false);
+  z.gate_part = z.gate.parts > 1 ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
+  z.dx_part = z.dx.parts > 1 ? size_t(z.dx.parts) * size_t(n) * size_t(up(K, 4)) * 4 : 0;
+  z.dw_part = z.dw.parts > 1 ? size_t(z.dw.parts) * size_t(up(K, 4)) * 2 * size_t(z.Fp) * 4 : 0;
+  z.d = size_t(up(n * 2 * z.Fp * 2, 256));
+  return z;
+}
+
+static hgnn_status join_grid(const char* who, int64_t threads, unsigned* blocks) {
+  HGNN_REQUIRE(ceil_div(threads, kBlock) <= 0xffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
+  *blocks = unsigned(ceil_div(threads, kBlock));
+  return HGNN_OK;
+}
+
+// both projections and `out` of their pairs of sums
+template <class Out>
+static hgnn_status gated_pairs(const char* who, const GatedSizes& z, const half_t* X, int64_t ldx, const half_t* Wg, const half_t* Wu, int64_t ldw, bool trans, float* part,
+                               const Out& out, hipStream_t s) {
+  ProductArgs a{};
+  a.Q0 = X, a.Q1 = X, a.P0 = Wg, a.P1 = Wu, a.ldq = ldx, a.ldp = ldw, a.nq = z.n, a.np = z.F, a.K = z.K, a.part = z.gate.part, a.parts = z.gate.parts;
+  const auto go = [&](auto shape) -> hgnn_status {
+    typedef decltype(shape) S;
+    if (z.gate.parts == 1) return product<S>(who, a, out, s);
+    hgnn_status st = product<S>(who, a, GatedPart{part, z.n, z.Fp}, s);
+    unsigned blocks;
+    if (st == HGNN_OK) st = join_grid(who, z.n * ((z.F + 3) / 4), &blocks);
+    if (st != HGNN_OK) return st;
+    gated_join_kernel<<<blocks, kBlock, 0, s>>>(part, z.gate.parts, z.n, z.F, z.Fp, out);
+    HGNN_LAUNCH_CHECK("gated_join_kernel");
+    return HGNN_OK;
+  };
+  return trans ? with_product<kTwo, false, false>(z.gate.size, go) : with_product<kTwo, false, true>(z.gate.size, go);
+}
+
+template <ProductKind KIND, bool QCOL, bool PCOL>
+static hgnn_status half_product(const char* who, ProductArgs& a, const Split& split, float* part, const HalfOut& out, hipStream_t s) {
+  a.part = split.part, a.parts = split.parts;
+  return with_product<KIND, QCOL, PCOL>(split.size, [&](auto shape) -> hgnn_status {
+    typedef decltype(shape) S;
+    if (split.parts == 1) return product<S>(who, a, out, s);
+    const int64_t pitch = up(a.np, 4);
+    hgnn_status st = product<S>(who, a, HalfPart{part, a.nq, pitch}, s);
+    unsigned blocks;
+    if (st == HGNN_OK) st = join_grid(who, a.nq * (pitch / 4), &blocks);
+    if (st != HGNN_OK) return st;
+    half_join_kernel<<<blocks, kBlock, 0, s>>>(part, split.parts, a.nq, pitch, out);
+    HGNN_LAUNCH_CHECK("half_join_kernel");
+    return HGNN_OK;
+  });
+}
+
+static hgnn_status check_gated(const char* who, int64_t n, int32_t K, int32_t F, hgnn_activation act, int64_t ldx, int64_t ldw, int32_t trans_w, int64_t ldy) {
+  HGNN_REQUIRE(n >= 0 && K > 0 && F > 0, HGNN_EINVAL, "%s: n = %lld, K = %d, F = %d", who, static_cast<long long>(n), K, F);
+  HGNN_REQUIRE(act >= HGNN_SILU && act <= HGNN_RELU, HGNN_EINVAL, "%s: unknown activation %d", who, int(act));
+  HGNN_REQUIRE(ldx >= K && ldy >= F && ldw >= (trans_w ? K : F), HGNN_EINVAL, "%s: leading dimension smaller than the row", who);
+  HGNN_REQUIRE(K <= 65536 && F <= 65536 && n < (int64_t(1) << 31), HGNN_EUNSUPPORTED, "%s: K = %d / F = %d above 65536, or n = %lld from 2^31 on", who, K, F, static_cast<long long>(n));
+  return HGNN_OK;
+}
+static bool fits(const void* p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
+
+}  // namespace hgnn
+
+using namespace hgnn;
+
+extern "C" {
+
+size_t hgnn_gated_workspace(int64_t n, int32_t K, int32_t F) {
+  if (n <= 0 || n > 0x7fffffff || K <= 0 || F <= 0 || K > 65536 || F > 65536) return 0;
+  return gated_sizes(n, K, F).gate_part;
+}
+
+hgnn_status hgnn_gated(int64_t n, int32_t K, int32_t F, hgnn_activation act, const hgnn_half* X, int64_t ldx, const hgnn_half* Wg, const hgnn_half* Wu, int64_t ldw,
+                       int32_t trans_w, hgnn_half* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  const char* who = "hgnn_gated";
+  hgnn_status st = check_gated(who, n, K, F, act, ldx, ldw, trans_w, ldy);
+  if (st != HGNN_OK) return st;
+  if (n == 0) return HGNN_OK;
+  HGNN_REQUIRE(X && Wg && Wu && Y, HGNN_EINVAL, "%s: NULL argument", who);
+  HGNN_REQUIRE(fits(X, ldx) && fits(Wg, ldw) && fits(Wu, ldw) && fits(Y, ldy), HGNN_EUNSUPPORTED, "%s: needs 16-byte aligned tensors and pitches that are multiples of 8", who);
+  const GatedSizes z = gated_sizes(n, K, F);
+  HGNN_REQUIRE(z.gate_part == 0 || (workspace && workspace_bytes >= z.gate_part && aligned16(workspace)), HGNN_EINVAL,
+               "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_gated_workspace)", who, workspace_bytes, z.gate_part);
+  const auto half = [](const hgnn_half* p) { return reinterpret_cast<const half_t*>(p); };
+  return gated_pairs(who, z, half(X), ldx, half(Wg), half(Wu), ldw, trans_w != 0, static_cast<float*>(workspace),
+                     GatedOut{int(act), F, reinterpret_cast<half_t*>(Y), ldy}, static_cast<hipStream_t>(stream));
+}
+
+size_t hgnn_gated_grad_workspace(int64_t n, int32_t K, int32_t F) {
+  if (n <= 0 || n > 0x7fffffff || K <= 0 || F <= 0 || K > 65536 || F > 65536) return 0;
+  const GatedSizes z = gated_sizes(n, K, F);
+  return z.d + std::max({z.gate_part, z.dx_part, z.dw_part});
+}
+
+hgnn_status hgnn_gated_grad(int64_t n, int32_t K, int32_t F, hgnn_activation act, const hgnn_half* X, int64_t ldx, const hgnn_half* Wg, const hgnn_half* Wu, int64_t ldw,
+                            int32_t trans_w, const hgnn_half* dY, int64_t lddy, hgnn_half* dX, int64_t lddx, hgnn_half* dWg, hgnn_half* dWu, int64_t lddw, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  clear_error();
+  const char* who = "hgnn_gated_grad";
+  hgnn_status st = check_gated(who, n, K, F, act, ldx, ldw, trans_w, lddy);
+  if (st != HGNN_OK) return st;
+  HGNN_REQUIRE((dWg == nullptr) == (dWu == nullptr), HGNN_EINVAL, "%s: dWg and dWu go together", who);
+  HGNN_REQUIRE((!dX || lddx >= K) && (!dWg || lddw >= (trans_w ? K : F)), HGNN_EINVAL, "%s: leading dimension smaller than the row", who);
+  HGNN_REQUIRE((!dX || fits(dX, lddx)) && (!dWg || (fits(dWg, lddw) && fits(dWu, lddw))), HGNN_EUNSUPPORTED,
+               "%s: needs 16-byte aligned tensors and pitches that are multiples of 8", who);
+  HGNN_REQUIRE(!dWg || dWg != dWu, HGNN_EINVAL, "%s: the same output twice", who);
+  const bool trans = trans_w != 0;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const auto half = [](const hgnn_half* p) { return reinterpret_cast<const half_t*>(p); };
+  const auto out = [](hgnn_half* p) { return reinterpret_cast<half_t*>(p); };
+  const int64_t lines = trans ? F : K, cols = trans ? K : F;
+  if (n == 0) {  // sums of nothing
+    if (!dWg) return HGNN_OK;
+    for (half_t* w : {out(dWg), out(dWu)}) {
+      unsigned blocks;
+      st = join_grid(who, lines * ceil_div(cols, 4), &blocks);
+      if (st != HGNN_OK) return st;
+      half_zero_kernel<<<blocks, kBlock, 0, s>>>(w, lines, cols, lddw);
+      HGNN_LAUNCH_CHECK("half_zero_kernel");
+    }
+    return HGNN_OK;
+  }
+  HGNN_REQUIRE(X && Wg && Wu && dY, HGNN_EINVAL, "%s: NULL argument", who);
+  HGNN_REQUIRE(fits(X, ldx) && fits(Wg, ldw) && fits(Wu, ldw) && fits(dY, lddy), HGNN_EUNSUPPORTED,
+               "%s: needs 16-byte aligned tensors and pitches that are multiples of 8", who);
+  const GatedSizes z = gated_sizes(n, K, F);
+  const size_t need = hgnn_gated_grad_workspace(n, K, F);
+  HGNN_REQUIRE(workspace && workspace_bytes >= need && aligned16(workspace), HGNN_EINVAL, "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_gated_grad_workspace)", who,
+               workspace_bytes, need);
+  if (!dX && !dWg) return HGNN_OK;
+  half_t* const D = static_cast<half_t*>(workspace);
+  float* const part = reinterpret_cast<float*>(static_cast<char*>(workspace) + z.d);
+  st = gated_pairs(who, z, half(X), ldx, half(Wg), half(Wu), ldw, trans, part, GatedGradOut{int(act), half(dY), lddy, D, z.Fp}, s);
+  if (st != HGNN_OK) return st;
+  constexpr int64_t kNone = int64_t(1) << 62;
+  if (dX) {
+    ProductArgs a{};
+    a.Q0 = D, a.Q1 = D + z.Fp, a.ldq = 2 * z.Fp, a.P0 = half(Wg), a.P1 = half(Wu), a.ldp = ldw, a.nq = n, a.np = K, a.K = F;
+    const HalfOut to{out(dX), nullptr, lddx, kNone, kNone, n, K};
+    st = trans ? half_product<kSegments, false, true>(who, a, z.dx, part, to, s) : half_product<kSegments, false, false>(who, a, z.dx, part, to, s);
+    if (st != HGNN_OK) return st;
+  }
+  if (dWg) {
+    ProductArgs a{};
+    a.K = n;
+    HalfOut to{out(dWg), out(dWu), lddw, kNone, kNone, lines, cols};
+    if (trans) {
+      a.Q0 = a.Q1 = D, a.ldq = 2 * z.Fp, a.nq = 2 * z.Fp, a.P0 = a.P1 = half(X), a.ldp = ldx, a.np = K;
+      to.split_q = z.Fp;
+    } else {
+      a.Q0 = a.Q1 = half(X), a.ldq = ldx, a.nq = K, a.P0 = a.P1 = D, a.ldp = 2 * z.Fp, a.np = 2 * z.Fp;
+      to.split_p = z.Fp;
+    }
+    st = half_product<kOne, true, true>(who, a, z.dw, part, to, s);
+  }
+  return st;
+}
+
+}  // extern "C"

@@ -1,0 +1,561 @@
+// The norms around a block of a network, with the gate of its branch and the residual, in one pass, and the gradients of all of that in another:
+//   b = N1(Y),  H = alpha R + g b,  Z = N2(H),   N(x) = (x - mean(x)) r w + c,  r = 1 / sqrt(mean((x - mean(x))^2) + eps)   (mean(x) = 0 without centring)
+// and with u = d w, xh = (x - mean) r, the gradient through a norm
+//   N^T(d) = r (u - xh mean(u xh) - [centred] mean(u)),   dw = sum_rows d xh,   dc = sum_rows d.
+// A row stays in registers from its load to its stores, so every tensor crosses the memory once, which is what bounds both kernels; sums over a row and all
+// that is formed from them are fp32, the variance is formed from the differences to the mean.  The gradients recompute the statistics from the rows that they
+// read in any case: two more reductions over lanes, no array of statistics that a caller could hand over stale.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "rows.h"
+
+namespace hgnn {
+
+struct BlockArgs {
+  int64_t n;
+  int F;
+  int post, pre;  // hgnn_norm_kind
+  float alpha, eps;
+  const float *post_w, *post_b, *gate, *pre_w, *pre_b;
+  const half_t* gate_rows;
+  int64_t ld_gate;
+  const void* R;
+  int64_t ldr;
+  const half_t* Y;
+  int64_t ldy;
+  void* H;  // the forward's output, the gradients' input
+  int64_t ldh;
+  half_t* Z;
+  int64_t ldz;
+};
+struct BlockGradArgs : BlockArgs {
+  const void* dH;
+  int64_t lddh;
+  const half_t* dZ;
+  int64_t lddz;
+  void* dR;
+  int64_t lddr;
+  half_t* dY;
+  int64_t lddy;
+  half_t* dgate_rows;
+  int64_t ldd_gate;
+  int vectors;  // kPreW | ...: which sums over rows are wanted
+  float* part;  // [gridDim.x][kVectors][pitch]
+  int pitch;
+};
+enum { kPreW = 0, kPreB, kGate, kPostW, kPostB, kVectors };
+
+// ---- sums over the lanes of a row: L lanes of a wave, or W waves
+__device__ __forceinline__ float lanes_sum(float v, int L) {
+  if (L >= 2) v = dpp_add<0xB1>(v);
+  if (L >= 4) v = dpp_add<0x4E>(v);
+  if (L >= 8) v = dpp_add<0x141>(v);
+  if (L >= 16) v = dpp_add<0x140>(v);
+  typedef unsigned uint2_t __attribute__((ext_vector_type(2)));
+  if (L >= 32) {
+    const uint2_t r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if (L >= 64) {
+    const uint2_t r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return v;
+}
+
+// Rows of L lanes (W = 1), or of W waves; P pieces of eight elements a lane.
+template <int L, int P, int W>
+struct RowShape {
+  static constexpr int kRows = W > 1 ? 1 : kBlock / L;       // rows of a workgroup at a time
+  static constexpr int kThreads = W > 1 ? W * kWave : kBlock;
+  static constexpr int kLanes = W > 1 ? W * kWave : L;       // of a row
+  static constexpr bool kKeep = P == 1 && W <= 4;            // weights stay in registers over the rows of a workgroup
+  __device__ static int lane() { return threadIdx.x % kLanes; }
+  __device__ static int row() { return W > 1 ? 0 : threadIdx.x / L; }
+  // of both at once: where the row is several waves', one turn through LDS
+  __device__ static void sum(float& a, float& b, float* lds) {
+    a = lanes_sum(a, W > 1 ? kWave : L), b = lanes_sum(b, W > 1 ? kWave : L);
+    if constexpr (W > 1) {
+      __syncthreads();  // what the turn before left has been read
+      if (threadIdx.x % kWave == 0) lds[2 * (threadIdx.x / kWave)] = a, lds[2 * (threadIdx.x / kWave) + 1] = b;
+      __syncthreads();
+      a = 0.f, b = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) a += lds[2 * w], b += lds[2 * w + 1];
+    }
+  }
+  __device__ static float sum(float a, float* lds) {
+    float none = 0.f;
+    if constexpr (W > 1) sum(a, none, lds);
+    else a = lanes_sum(a, L);
+    return a;
+  }
+};
+
+struct Eight {
+  float v[8];
+};
+
+// columns of piece p of the lane: [col, col + 8), `left` of them in the row
+template <class S, int P>
+__device__ __forceinline__ int col_of(int p) { return 8 * (S::lane() + p * S::kLanes); }
+
+// of row `row` of n rows; nothing behind the tensor is read
+template <class T>
+__device__ __forceinline__ Eight load_eight(const T* x0, int64_t ld, int64_t row, int64_t n, int col, int F) {
+  Eight r;
+  const int left = F - col;
+  const T* const at = x0 + row * ld + col;
+  RawPiece<T> x;
+  x.v = 0;
+  if (left >= 8) x = load_raw(at);
+  else if (left > 0) x = load_raw(at, left, (n - 1 - row) * ld + left);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.v[i] = i < left ? float(x.v[i]) : 0.f;
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void store_eight(T* row, int col, int F, const Eight& x) {
+  if (col >= F) return;
+  store_piece(row + col, F - col, Piece{{x.v[0], x.v[1], x.v[2], x.v[3], x.v[4], x.v[5], x.v[6], x.v[7]}});
+}
+__device__ __forceinline__ Eight weights_at(const float* w, int col, int F, float otherwise) {
+  if (w) return load_eight(w, 0, 0, 1, col, F);
+  Eight r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.v[i] = otherwise;
+  return r;
+}
+
+// (x - mean) r in the place of x, zeros behind the row; returns r
+template <class S, int P>
+__device__ __forceinline__ float normed(Eight (&x)[P], int kind, int F, float eps, float* lds) {
+  const float inv = 1.f / float(F);
+  if (kind == HGNN_NORM_LAYER) {
+    float s = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += x[p].v[i];
+    const float mean = S::sum(s, lds) * inv;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int left = F - col_of<S, P>(p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[p].v[i] = i < left ? x[p].v[i] - mean : 0.f;
+    }
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q = fmaf(x[p].v[i], x[p].v[i], q);
+  const float r = 1.f / sqrtf(S::sum(q, lds) * inv + eps);
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[p].v[i] *= r;
+  return r;
+}
+
+// N^T(d) in the place of d: what comes back through a norm whose output was xh w + c
+template <class S, int P>
+__device__ __forceinline__ void through(Eight (&d)[P], const Eight (&xh)[P], const Eight (&w)[P], float r, int kind, int F, float* lds) {
+  float su = 0.f, sx = 0.f;
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      d[p].v[i] *= w[p].v[i];
+      su += d[p].v[i];
+      sx = fmaf(d[p].v[i], xh[p].v[i], sx);
+    }
+  if (kind == HGNN_NORM_LAYER) {
+    S::sum(su, sx, lds);
+  } else {
+    sx = S::sum(sx, lds), su = 0.f;
+  }
+  const float inv = 1.f / float(F);
+  su *= inv, sx *= inv;
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[p].v[i] = r * (fmaf(-xh[p].v[i], sx, d[p].v[i]) - su);
+}
+
+template <class T, int L, int P, int W>
+__global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_kernel(BlockArgs a) {
+  typedef RowShape<L, P, W> S;
+  __shared__ float lds[2 * W];
+  Eight post_w[P], post_b[P], gate[P], pre_w[P], pre_b[P];
+  const auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = col_of<S, P>(p);
+      post_w[p] = weights_at(a.post_w, c, a.F, 1.f), post_b[p] = weights_at(a.post_b, c, a.F, 0.f), gate[p] = weights_at(a.gate, c, a.F, 1.f);
+      pre_w[p] = weights_at(a.pre_w, c, a.F, 1.f), pre_b[p] = weights_at(a.pre_b, c, a.F, 0.f);
+    }
+  };
+  if (S::kKeep) weights();
+  for (int64_t row0 = int64_t(blockIdx.x) * S::kRows; row0 < a.n; row0 += int64_t(gridDim.x) * S::kRows) {  // all waves alike: the sums meet
+    if (!S::kKeep) weights();
+    const int64_t row = min(row0 + S::row(), a.n - 1);
+    const bool live = row0 + S::row() < a.n;  // else the last row once more, which is not stored
+    Eight b[P], h[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = col_of<S, P>(p);
+      b[p] = a.Y ? load_eight(a.Y, a.ldy, row, a.n, c, a.F) : Eight{};
+      h[p] = a.R ? load_eight(static_cast<const T*>(a.R), a.ldr, row, a.n, c, a.F) : Eight{};
+      if (a.gate_rows) gate[p] = load_eight(a.gate_rows, a.ld_gate, row, a.n, c, a.F);
+    }
+    if (a.post != HGNN_NORM_NONE) {
+      normed<S, P>(b, a.post, a.F, a.eps, lds);
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[p].v[i] = fmaf(b[p].v[i], post_w[p].v[i], post_b[p].v[i]);
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int left = a.F - col_of<S, P>(p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[p].v[i] = i < left ? float(T(fmaf(gate[p].v[i], b[p].v[i], a.alpha * h[p].v[i]))) : 0.f;  // as it is stored
+      if (a.H && live) store_eight(static_cast<T*>(a.H) + row * a.ldh, col_of<S, P>(p), a.F, h[p]);
+    }
+    if (a.pre == HGNN_NORM_NONE) continue;
+    normed<S, P>(h, a.pre, a.F, a.eps, lds);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[p].v[i] = fmaf(h[p].v[i], pre_w[p].v[i], pre_b[p].v[i]);
+      if (live) store_eight(a.Z + row * a.ldz, col_of<S, P>(p), a.F, h[p]);
+    }
+  }
+}
+
+// Sums over rows: a lane keeps those of its columns over all rows of its workgroup, the row groups of the workgroup are added in LDS in order, and the
+// workgroup leaves one partial result, which block_sums_kernel adds in order: no atomics, the same bits on every run.
+template <class T, int L, int P, int W>
+__global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_grad_kernel(BlockGradArgs a) {
+  typedef RowShape<L, P, W> S;
+  __shared__ float lds[2 * W];
+  __shared__ float sums[S::kRows > 1 ? S::kThreads * 9 : 1];
+  Eight post_w[P], post_b[P], gate[P], pre_w[P], total[kVectors][P] = {};
+  const auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = col_of<S, P>(p);
+      post_w[p] = weights_at(a.post_w, c, a.F, 1.f), post_b[p] = weights_at(a.post_b, c, a.F, 0.f), gate[p] = weights_at(a.gate, c, a.F, 1.f);
+      pre_w[p] = weights_at(a.pre_w, c, a.F, 1.f);
+    }
+  };
+  if (S::kKeep) weights();
+  for (int64_t row0 = int64_t(blockIdx.x) * S::kRows; row0 < a.n; row0 += int64_t(gridDim.x) * S::kRows) {
+    if (!S::kKeep) weights();
+    const int64_t row = min(row0 + S::row(), a.n - 1);
+    const bool live = row0 + S::row() < a.n;  // else the last row once more, which is not stored and adds nothing
+    Eight e[P], h[P], d[P], b[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = col_of<S, P>(p);
+      e[p] = a.dH ? load_eight(static_cast<const T*>(a.dH), a.lddh, row, a.n, c, a.F) : Eight{};
+      if (a.pre != HGNN_NORM_NONE) {
+        h[p] = load_eight(static_cast<const T*>(a.H), a.ldh, row, a.n, c, a.F);
+        d[p] = load_eight(a.dZ, a.lddz, row, a.n, c, a.F);
+      }
+      if (a.Y) b[p] = load_eight(a.Y, a.ldy, row, a.n, c, a.F);
+      if (a.gate_rows) gate[p] = load_eight(a.gate_rows, a.ld_gate, row, a.n, c, a.F);
+    }
+    if (a.pre != HGNN_NORM_NONE) {
+      const float r = normed<S, P>(h, a.pre, a.F, a.eps, lds);
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float v = live ? d[p].v[i] : 0.f;
+          total[kPreW][p].v[i] = fmaf(v, h[p].v[i], total[kPreW][p].v[i]);
+          total[kPreB][p].v[i] += v;
+        }
+      through<S, P>(d, h, pre_w, r, a.pre, a.F, lds);
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[p].v[i] += d[p].v[i];
+    }
+    if (a.dR && live) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        Eight out;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out.v[i] = a.alpha * e[p].v[i];
+        store_eight(static_cast<T*>(a.dR) + row * a.lddr, col_of<S, P>(p), a.F, out);
+      }
+    }
+    if (!a.dY && !a.dgate_rows && !(a.vectors & (1 << kGate | 1 << kPostW | 1 << kPostB))) continue;
+    float r = 1.f;
+    if (a.post != HGNN_NORM_NONE) r = normed<S, P>(b, a.post, a.F, a.eps, lds);  // b: xh
+    if (a.gate || a.gate_rows) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int left = a.F - col_of<S, P>(p);
+        Eight g;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          g.v[i] = e[p].v[i] * (a.post != HGNN_NORM_NONE ? fmaf(b[p].v[i], post_w[p].v[i], post_b[p].v[i]) : b[p].v[i]);
+          total[kGate][p].v[i] += live && i < left ? g.v[i] : 0.f;
+          e[p].v[i] *= gate[p].v[i];
+        }
+        if (a.dgate_rows && live) store_eight(a.dgate_rows + row * a.ldd_gate, col_of<S, P>(p), a.F, g);
+      }
+    }
+    if (a.post != HGNN_NORM_NONE) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int left = a.F - col_of<S, P>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[p].v[i] = i < left ? e[p].v[i] : 0.f;
+          const float v = live ? e[p].v[i] : 0.f;
+          total[kPostW][p].v[i] = fmaf(v, b[p].v[i], total[kPostW][p].v[i]);
+          total[kPostB][p].v[i] += v;
+        }
+      }
+      through<S, P>(e, b, post_w, r, a.post, a.F, lds);
+    }
+    if (a.dY && live) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) store_eight(a.dY + row * a.lddy, col_of<S, P>(p), a.F, e[p]);
+    }
+  }
+  float* const part = a.part + int64_t(blockIdx.x) * kVectors * a.pitch;
+#pragma unroll
+  for (int k = 0; k < kVectors; ++k) {
+    if (!(a.vectors & (1 << k))) continue;  // uniform
+    if constexpr (S::kRows > 1) {  // P = 1: lanes of a row, groups of rows
+      static_assert(P <= 2, "pieces");
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[threadIdx.x * 9 + i] = total[k][p].v[i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < 8 * L; c += S::kThreads) {
+          float s = 0.f;
+          for (int g = 0; g < S::kRows; ++g) s += sums[(g * L + c / 8) * 9 + c % 8];
+          const int col = 8 * p * L + c;
+          if (col < a.F) part[k * a.pitch + col] = s;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < P; ++p) store_eight(part + k * a.pitch, col_of<S, P>(p), a.F, total[k][p]);
+    }
+  }
+}
+
+struct BlockSumsArgs {
+  const float* part;
+  int parts, pitch, F;
+  float* out[kVectors];
+};
+constexpr int kSumCols = 64, kSumRows = 16;
+__global__ __launch_bounds__(kSumCols* kSumRows) void block_sums_kernel(BlockSumsArgs a) {
+  __shared__ float lds[kSumRows][kSumCols];
+  const int k = blockIdx.y, x = threadIdx.x % kSumCols, y = threadIdx.x / kSumCols, col = blockIdx.x * kSumCols + x;
+  float* out = nullptr;
+#pragma unroll
+  for (int j = 0; j < kVectors; ++j) out = j == k ? a.out[j] : out;
+  if (!out) return;  // uniform
+  float s = 0.f;
+  if (col < a.F) {
+    const float* const in = a.part + int64_t(k) * a.pitch + col;
+    const int64_t stride = int64_t(kVectors) * a.pitch;
+    int j = y;
+    for (; j + 7 * kSumRows < a.parts; j += 8 * kSumRows) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = in[(j + u * kSumRows) * stride];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; j < a.parts; j += kSumRows) s += in[j * stride];
+  }
+  lds[y][x] = s;
+  __syncthreads();
+  if (y != 0 || col >= a.F) return;
+  s = 0.f;
+#pragma unroll
+  for (int j = 0; j < kSumRows; ++j) s += lds[j][x];
+  out[col] = s;
+}
+
+constexpr int kMostNormed = 8192;
+
+// The shape of a row of F elements: a piece of eight elements a lane, up to 512 elements of a wave's lanes, then of as many waves as it takes.
+template <class Call>
+static hgnn_status with_shape(int F, Call&& call) {
+  const int lanes = pow2_at_least((F + 7) / 8);
+  switch (lanes) {
+    case 1: return call(RowShape<1, 1, 1>());
+    case 2: return call(RowShape<2, 1, 1>());
+    case 4: return call(RowShape<4, 1, 1>());
+    case 8: return call(RowShape<8, 1, 1>());
+    case 16: return call(RowShape<16, 1, 1>());
+    case 32: return call(RowShape<32, 1, 1>());
+    case 64: return call(RowShape<64, 1, 1>());
+    case 128: return call(RowShape<64, 1, 2>());
+    case 256: return call(RowShape<64, 1, 4>());
+    case 512: return call(RowShape<64, 1, 8>());
+    default: return call(RowShape<64, 1, 16>());
+  }
+}
+template <class S>
+struct ShapeOf;
+template <int l, int p, int w>
+struct ShapeOf<RowShape<l, p, w>> {
+  static constexpr int L = l, P = p, W = w;
+};
+
+// Workgroups of the gradients: as many as fill the chip, each with rows enough that its partial sums (as many bytes as three rows or so) cost little.
+constexpr int kGradBlocks = 1024;
+template <class S>
+static int64_t grad_blocks(int64_t n) {
+  const int64_t most = S::kThreads > kBlock ? kGradBlocks / 4 : kGradBlocks;
+  const int64_t per = std::max(S::kRows, S::kLanes >= 64 ? 8 : 1);
+  return std::max<int64_t>(1, std::min(most, ceil_div(n, per)));
+}
+
+static hgnn_status check_block(const char* who, int64_t n, int32_t F, const hgnn_block* b, hgnn_type type, bool branch) {
+  HGNN_REQUIRE(n >= 0 && F > 0, HGNN_EINVAL, "%s: n = %lld, F = %d", who, static_cast<long long>(n), F);
+  HGNN_REQUIRE(b != nullptr, HGNN_EINVAL, "%s: block is NULL", who);
+  HGNN_REQUIRE(known_type(type), HGNN_EINVAL, "%s: unknown type %d", who, int(type));
+  const auto known = [](hgnn_norm_kind k) { return k == HGNN_NORM_NONE || k == HGNN_NORM_RMS || k == HGNN_NORM_LAYER; };
+  HGNN_REQUIRE(known(b->post) && known(b->pre), HGNN_EINVAL, "%s: unknown norm %d or %d", who, int(b->post), int(b->pre));
+  HGNN_REQUIRE(F <= kMostNormed && n <= (int64_t(1) << 40), HGNN_EUNSUPPORTED, "%s: F = %d above %d, or n = %lld above 2^40", who, F, kMostNormed, static_cast<long long>(n));
+  HGNN_REQUIRE(std::isfinite(b->alpha) && b->eps > 0.f && std::isfinite(b->eps), HGNN_EINVAL, "%s: alpha = %g, eps = %g", who, double(b->alpha), double(b->eps));
+  HGNN_REQUIRE(b->post != HGNN_NORM_NONE || (!b->post_w && !b->post_b), HGNN_EINVAL, "%s: weights of a norm behind the branch that is none", who);
+  HGNN_REQUIRE(b->pre != HGNN_NORM_NONE || (!b->pre_w && !b->pre_b), HGNN_EINVAL, "%s: weights of a norm of the sum that is none", who);
+  HGNN_REQUIRE(!b->gate || !b->gate_rows, HGNN_EINVAL, "%s: gate and gate_rows exclude each other", who);
+  HGNN_REQUIRE(!b->gate_rows || b->ld_gate >= F, HGNN_EINVAL, "%s: leading dimension of the gate smaller than F", who);
+  HGNN_REQUIRE(branch || (b->post == HGNN_NORM_NONE && !b->gate && !b->gate_rows), HGNN_EINVAL, "%s: a norm or a gate of a branch that is not there", who);
+  HGNN_REQUIRE(aligned_to_type(b->post_w, HGNN_F32) && aligned_to_type(b->post_b, HGNN_F32) && aligned_to_type(b->gate, HGNN_F32) && aligned_to_type(b->pre_w, HGNN_F32) &&
+                   aligned_to_type(b->pre_b, HGNN_F32) && aligned_to_type(b->gate_rows, HGNN_F16),
+               HGNN_EINVAL, "%s: an array that is not aligned to its type", who);
+  return HGNN_OK;
+}
+static void block_args(BlockArgs& a, int64_t n, int32_t F, const hgnn_block* b) {
+  a.n = n, a.F = F, a.post = b->post, a.pre = b->pre, a.alpha = b->alpha, a.eps = b->eps;
+  a.post_w = b->post_w, a.post_b = b->post_b, a.gate = b->gate, a.pre_w = b->pre_w, a.pre_b = b->pre_b;
+  a.gate_rows = reinterpret_cast<const half_t*>(b->gate_rows), a.ld_gate = b->ld_gate;
+}
+
+}  // namespace hgnn
+
+using namespace hgnn;
+
+extern "C" {
+
+hgnn_status hgnn_residual_norm(int64_t n, int32_t F, const hgnn_block* block, hgnn_type type, const void* R, int64_t ldr, const hgnn_half* Y, int64_t ldy, void* H,
+                               int64_t ldh, hgnn_half* Z, int64_t ldz, void* stream) {
+  clear_error();
+  const char* who = "hgnn_residual_norm";
+  hgnn_status st = check_block(who, n, F, block, type, Y != nullptr || n == 0);
+  if (st != HGNN_OK) return st;
+  HGNN_REQUIRE((!R || ldr >= F) && (!Y || ldy >= F) && (!H || ldh >= F) && (!Z || ldz >= F), HGNN_EINVAL, "%s: leading dimension smaller than F", who);
+  if (n == 0) return HGNN_OK;
+  HGNN_REQUIRE(R || Y, HGNN_EINVAL, "%s: neither R nor Y is given", who);
+  HGNN_REQUIRE((block->pre == HGNN_NORM_NONE) == (Z == nullptr) && (H || Z), HGNN_EINVAL, "%s: Z goes with a norm of the sum, and one of H and Z has to be there", who);
+  HGNN_REQUIRE(aligned_to_type(R, type) && aligned_to_type(H, type) && aligned_to_type(Y, HGNN_F16) && aligned_to_type(Z, HGNN_F16), HGNN_EINVAL,
+               "%s: an array that is not aligned to its type", who);
+  HGNN_REQUIRE(!H || H != R || ldh == ldr, HGNN_EINVAL, "%s: in place with another leading dimension", who);
+  BlockArgs a{};
+  block_args(a, n, F, block);
+  a.R = R, a.ldr = ldr, a.Y = reinterpret_cast<const half_t*>(Y), a.ldy = ldy, a.H = H, a.ldh = ldh, a.Z = reinterpret_cast<half_t*>(Z), a.ldz = ldz;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return with_shape(F, [&](auto shape) -> hgnn_status {
+    typedef decltype(shape) S;
+    typedef ShapeOf<S> D;
+    const unsigned blocks = unsigned(std::min<int64_t>(ceil_div(n, S::kRows), 2048));
+    if (type == HGNN_F16) block_norm_kernel<half_t, D::L, D::P, D::W><<<blocks, S::kThreads, 0, s>>>(a);
+    else block_norm_kernel<float, D::L, D::P, D::W><<<blocks, S::kThreads, 0, s>>>(a);
+    HGNN_LAUNCH_CHECK("block_norm_kernel");
+    return HGNN_OK;
+  });
+}
+
+size_t hgnn_residual_norm_grad_workspace(int64_t n, int32_t F) {
+  if (n <= 0 || F <= 0 || F > kMostNormed) return 0;
+  int64_t blocks = 0;
+  with_shape(F, [&](auto shape) -> hgnn_status {
+    blocks = grad_blocks<decltype(shape)>(n);
+    return HGNN_OK;
+  });
+  return size_t(blocks) * kVectors * size_t((F + 7) / 8 * 8) * sizeof(float);
+}
+
+hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* block, hgnn_type type, const void* H, int64_t ldh, const hgnn_half* Y, int64_t ldy,
+                                    const void* dH, int64_t lddh, const hgnn_half* dZ, int64_t lddz, const hgnn_block_grad* grads, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  clear_error();
+  const char* who = "hgnn_residual_norm_grad";
+  HGNN_REQUIRE(grads != nullptr, HGNN_EINVAL, "%s: grads is NULL", who);
+  const hgnn_block_grad& g = *grads;
+  hgnn_status st = check_block(who, n, F, block, type, true);
+  if (st != HGNN_OK) return st;
+  HGNN_REQUIRE((!H || ldh >= F) && (!Y || ldy >= F) && (!dH || lddh >= F) && (!dZ || lddz >= F) && (!g.dR || g.lddr >= F) && (!g.dY || g.lddy >= F) &&
+                   (!g.dgate_rows || g.ldd_gate >= F),
+               HGNN_EINVAL, "%s: leading dimension smaller than F", who);
+  HGNN_REQUIRE((block->pre != HGNN_NORM_NONE) || (!dZ && !g.dpre_w && !g.dpre_b), HGNN_EINVAL, "%s: gradients of a norm of the sum that is none", who);
+  HGNN_REQUIRE(block->post != HGNN_NORM_NONE || (!g.dpost_w && !g.dpost_b), HGNN_EINVAL, "%s: gradients of a norm behind the branch that is none", who);
+  HGNN_REQUIRE((!g.dgate || block->gate) && (!g.dgate_rows || block->gate_rows), HGNN_EINVAL, "%s: the gradient of a gate that is none", who);
+  HGNN_REQUIRE(aligned_to_type(H, type) && aligned_to_type(dH, type) && aligned_to_type(g.dR, type) && aligned_to_type(Y, HGNN_F16) && aligned_to_type(dZ, HGNN_F16) &&
+                   aligned_to_type(g.dY, HGNN_F16) && aligned_to_type(g.dgate_rows, HGNN_F16) && aligned_to_type(g.dgate, HGNN_F32) && aligned_to_type(g.dpost_w, HGNN_F32) &&
+                   aligned_to_type(g.dpost_b, HGNN_F32) && aligned_to_type(g.dpre_w, HGNN_F32) && aligned_to_type(g.dpre_b, HGNN_F32),
+               HGNN_EINVAL, "%s: an array that is not aligned to its type", who);
+  HGNN_REQUIRE(!g.dR || g.dR != dH || g.lddr == lddh, HGNN_EINVAL, "%s: in place with another leading dimension", who);
+  const bool branch = g.dY || g.dgate || g.dgate_rows || g.dpost_w || g.dpost_b;
+  // what the branch's gradients need of it
+  const bool needs_Y = branch && (block->post != HGNN_NORM_NONE || block->gate || block->gate_rows);
+  if (n > 0) {
+    HGNN_REQUIRE(block->pre == HGNN_NORM_NONE ? dH != nullptr : (H && dZ), HGNN_EINVAL, "%s: NULL argument", who);
+    HGNN_REQUIRE(!needs_Y || Y, HGNN_EINVAL, "%s: Y is NULL", who);
+  }
+  BlockGradArgs a{};
+  block_args(a, n, F, block);
+  float* const out[kVectors] = {g.dpre_w, g.dpre_b, g.dgate, g.dpost_w, g.dpost_b};
+  for (int k = 0; k < kVectors; ++k) a.vectors |= out[k] ? 1 << k : 0;
+  const size_t need = hgnn_residual_norm_grad_workspace(n, F);
+  HGNN_REQUIRE(a.vectors == 0 || need == 0 || (workspace && workspace_bytes >= need && aligned16(workspace)), HGNN_EINVAL,
+               "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_residual_norm_grad_workspace)", who, workspace_bytes, need);
+  if (n == 0 && a.vectors == 0) return HGNN_OK;
+  a.H = const_cast<void*>(H), a.ldh = ldh, a.Y = needs_Y ? reinterpret_cast<const half_t*>(Y) : nullptr, a.ldy = ldy;
+  a.dH = dH, a.lddh = lddh, a.dZ = reinterpret_cast<const half_t*>(dZ), a.lddz = lddz;
+  a.dR = g.dR, a.lddr = g.lddr, a.dY = reinterpret_cast<half_t*>(g.dY), a.lddy = g.lddy;
+  a.dgate_rows = reinterpret_cast<half_t*>(g.dgate_rows), a.ldd_gate = g.ldd_gate;
+  a.part = static_cast<float*>(workspace), a.pitch = (F + 7) / 8 * 8;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  int64_t blocks = 0;  // no rows: sums of nothing
+  if (n > 0) {
+    st = with_shape(F, [&](auto shape) -> hgnn_status {
+      typedef decltype(shape) S;
+      typedef ShapeOf<S> D;
+      blocks = grad_blocks<S>(n);
+      if (type == HGNN_F16) block_norm_grad_kernel<half_t, D::L, D::P, D::W><<<unsigned(blocks), S::kThreads, 0, s>>>(a);
+      else block_norm_grad_kernel<float, D::L, D::P, D::W><<<unsigned(blocks), S::kThreads, 0, s>>>(a);
+      HGNN_LAUNCH_CHECK("block_norm_grad_kernel");
+      return HGNN_OK;
+    });
+    if (st != HGNN_OK) return st;
+  }
+  if (a.vectors) {
+    BlockSumsArgs q{a.part, int(blocks), a.pitch, F, {out[0], out[1], out[2], out[3], out[4]}};
+    block_sums_kernel<<<dim3(unsigned(ceil_div(F, kSumCols)), kVectors), kSumCols * kSumRows, 0, s>>>(q);
+    HGNN_LAUNCH_CHECK("block_sums_kernel");
+  }
+  return HGNN_OK;
+}
+
+}  // extern "C"

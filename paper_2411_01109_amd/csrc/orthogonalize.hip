@@ -1,0 +1,355 @@
+// Matrices made orthogonal by Newton-Schulz products:  X = G / |G|, then `steps` times  A = X X^T,  B = b A + c A A,  X <- a X + B X,  out = scale X
+// (of the transpose where the matrix is higher than wide, so that A is the smaller product).
+//
+// The polynomial multiplies small singular values by a at each step, so an error of the first products comes out a^steps times as large: half precision products
+// leave a result that is off by percents.  Every value is therefore kept as two fp16 numbers, v = hi + lo with hi = fp16(v) and lo = fp16(v - hi), some 22 bits, and
+// a product is hi hi + hi lo + lo hi in fp32 sums (lo lo is below the last bit): three products on the matrix cores, a fifth of what fp32's own rate would take.
+// Powers of two bring the values into fp16's range: X at 2^11 (values up to 8 x 2^11 fit, what is lost at the small end is 2^-36), A and B at 2^9 (up to 64).
+// A and B are symmetric: tiles on and below the diagonal alone, each written to its mirror place, too (a tile on the diagonal only once: its two triangles are
+// summed in different orders, and two writers would make the result a race).
+// All matrices are padded to multiples of 32 with zeros, which stay zeros through every product.
+#include <algorithm>
+#include <cmath>
+
+#include "product.h"
+#include "rows.h"
+
+namespace hgnn {
+
+constexpr float kX = 2048.f, kA = 512.f;  // what X, and A and B, are stored times
+constexpr int kNormParts = 256;
+
+__device__ __forceinline__ void split_value(float v, half_t& hi, half_t& lo) {
+  hi = half_t(v);
+  lo = half_t(v - float(hi));
+}
+// a matrix of values in two parts, pitch ld
+struct Pairs {
+  half_t *hi, *lo;
+  int64_t ld;
+  __device__ float4_t get(int64_t q, int64_t p) const {
+    const half4_t h = *reinterpret_cast<const half4_t*>(hi + q * ld + p), l = *reinterpret_cast<const half4_t*>(lo + q * ld + p);
+    float4_t v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = float(h[e]) + float(l[e]);
+    return v;
+  }
+  __device__ void put(int64_t q, int64_t p, const float4_t& v, bool mirror) const {
+    half4_t h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      half_t a, b;
+      split_value(v[e], a, b);
+      h[e] = a, l[e] = b;
+    }
+    *reinterpret_cast<half4_t*>(hi + q * ld + p) = h;
+    *reinterpret_cast<half4_t*>(lo + q * ld + p) = l;
+    if (!mirror) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) hi[(p + e) * ld + q] = h[e], lo[(p + e) * ld + q] = l[e];
+  }
+};
+
+// ---- what becomes of the sums
+struct GramOut {  // A, or b A where that is all of B
+  Pairs to;
+  float factor;
+  int tile;
+  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const { to.put(q, p, v * factor, q / tile != p / tile); }
+};
+struct SquareOut {  // B = b A + c A A
+  Pairs to, A;
+  float b, c;
+  int tile;
+  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const { to.put(q, p, A.get(q, p) * b + v * c, q / tile != p / tile); }
+};
+struct StepOut {  // X = a X + B X
+  Pairs to, X;
+  float a;
+  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const { to.put(q, p, X.get(q, p) * a + v * (1.f / kA), false); }
+};
+struct LastOut {  // the same into the caller's matrix
+  Pairs X;
+  float a, scale;
+  void* out;
+  int64_t ld, rows, cols;  // of X without its padding
+  int type, flip;
+  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const {
+    if (q >= rows) return;
+    const float4_t x = (X.get(q, p) * a + v * (1.f / kA)) * scale;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (p + e >= cols) return;
+      const int64_t at = flip ? (p + e) * ld + q : q * ld + p + e;
+      if (type == HGNN_F16) static_cast<half_t*>(out)[at] = half_t(x[e]);
+      else static_cast<float*>(out)[at] = x[e];
+    }
+  }
+};
+struct SumsPart {  // [parts][nq][np]
+  float* part;
+  int64_t nq, np;
+  __device__ void operator()(int64_t k, int64_t q, int64_t p, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * np + p) = v; }
+};
+template <class Out>
+__global__ __launch_bounds__(kBlock) void sums_join_kernel(const float* part, int parts, int64_t nq, int64_t np, int lower, Out out) {
+  const int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x, each = np / 4, q = t / each, p = 4 * (t - q * each);
+  if (q >= nq || (lower && p / lower > q / lower)) return;
+  const float* at = part + q * np + p;
+  float4_t v = *reinterpret_cast<const float4_t*>(at);
+#pragma unroll 4
+  for (int k = 1; k < parts; ++k) {
+    at += nq * np;
+    v += *reinterpret_cast<const float4_t*>(at);
+  }
+  out(0, q, p, v);
+}
+
+// ---- the way in: the norm, X = G / |G|
+struct OrthMatrix {
+  const void* grad;
+  void* out;
+  int64_t rows, cols, ld, ldo;
+  int type, out_type;
+};
+__device__ __forceinline__ double value_at(const OrthMatrix& m, int64_t r, int64_t c) {
+  return m.type == HGNN_F16 ? double(static_cast<const half_t*>(m.grad)[r * m.ld + c]) : double(static_cast<const float*>(m.grad)[r * m.ld + c]);
+}
+// sum over a workgroup of kBlock, on all threads
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double lds[kBlock];
+  lds[threadIdx.x] = v;
+  __syncthreads();
+  for (int w = kBlock / 2; w > 0; w >>= 1) {
+    if (int(threadIdx.x) < w) lds[threadIdx.x] += lds[threadIdx.x + w];
+    __syncthreads();
+  }
+  return lds[0];
+}
+// the partial sums of squares, in 64 bits: no element's square is lost or overflows
+__global__ __launch_bounds__(kBlock) void orth_squares_kernel(OrthMatrix m, double* part) {
+  const int64_t all = m.rows * m.cols, step = int64_t(gridDim.x) * kBlock;
+  double s = 0.;
+  int64_t e = int64_t(blockIdx.x) * kBlock + threadIdx.x, r = e / m.cols, c = e - r * m.cols;
+  const int64_t dr = step / m.cols, dc = step - dr * m.cols;
+  for (; e < all; e += step) {
+    const double v = value_at(m, r, c);
+    s += v * v;
+    r += dr, c += dc;
+    if (c >= m.cols) c -= m.cols, ++r;
+  }
+  s = block_sum(s);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+// 1 / |G|, or 0 where that is none
+__device__ __forceinline__ double inverse_norm(const double* part, int parts) {
+  double s = 0.;
+  for (int k = threadIdx.x; k < parts; k += kBlock) s += part[k];
+  s = block_sum(s);
+  return s > 0. && s < double(INFINITY) ? 1. / sqrt(s) : 0.;
+}
+constexpr int kTurn = 32;  // a workgroup takes 32 x 32 elements, through LDS where they change sides
+// X (of hq x hp with its padding) at kX times its values; with `last` the scaled result itself
+__global__ __launch_bounds__(kBlock) void orth_begin_kernel(OrthMatrix m, int flip, const double* part, int parts, Pairs X, int last, float scale) {
+  __shared__ float tile[kTurn][kTurn + 1];
+  const double inv = inverse_norm(part, parts);
+  const int64_t r0 = int64_t(flip ? blockIdx.x : blockIdx.y) * kTurn, c0 = int64_t(flip ? blockIdx.y : blockIdx.x) * kTurn;
+  const int x = threadIdx.x % kTurn, y = threadIdx.x / kTurn;
+  for (int i = y; i < kTurn; i += kBlock / kTurn) {
+    const int64_t r = r0 + i, c = c0 + x;
+    float v = 0.f;
+    if (r < m.rows && c < m.cols && inv > 0.) v = float(value_at(m, r, c) * inv * (last ? double(scale) : double(kX)));
+    if (last) {
+      if (r < m.rows && c < m.cols) {
+        if (m.out_type == HGNN_F16) static_cast<half_t*>(m.out)[r * m.ldo + c] = half_t(v);
+        else static_cast<float*>(m.out)[r * m.ldo + c] = v;
+      }
+    }
+    tile[i][x] = v;
+  }
+  if (last) return;
+  __syncthreads();
+  for (int i = y; i < kTurn; i += kBlock / kTurn) {
+    const int64_t q = int64_t(blockIdx.y) * kTurn + i, p = int64_t(blockIdx.x) * kTurn + x;
+    half_t hi, lo;
+    split_value(flip ? tile[x][i] : tile[i][x], hi, lo);
+    X.hi[q * X.ld + p] = hi, X.lo[q * X.ld + p] = lo;
+  }
+}
+
+static int64_t up32(int64_t n) { return (n + 31) / 32 * 32; }
+
+// ---- shapes: tiles of 64 where a side is short, else of 128
+template <bool PCOL>
+using SplitSmall = ProductShape<2, 2, 2, 2, kSplit, false, PCOL, 4>;
+template <bool PCOL>
+using SplitMid = ProductShape<2, 2, 4, 4, kSplit, false, PCOL, 2>;
+constexpr int kOrthFull = 256;
+struct OrthSplit {
+  int tile, parts;
+  int64_t part;
+};
+static OrthSplit orth_split(int64_t nq, int64_t np, int64_t K, bool lower) {
+  const auto tiles = [&](int64_t b) {
+    const int64_t l = ceil_div(nq, b);
+    return lower ? l * (l + 1) / 2 : l * ceil_div(np, b);
+  };
+  OrthSplit s;
+  s.tile = tiles(128) < kOrthFull / 4 || nq <= 64 ? 64 : 128;
+  const int64_t t = tiles(s.tile), parts = t >= kOrthFull ? 1 : std::min(ceil_div(2 * kOrthFull, t), ceil_div(K, 256));
+  s.part = std::max<int64_t>(32, up32(ceil_div(K, std::max<int64_t>(parts, 1))));
+  s.parts = int(std::max<int64_t>(1, ceil_div(K, s.part)));
+  return s;
+}
+struct OrthSizes {
+  int64_t m, k;  // padded, m <= k
+  int flip;
+  OrthSplit gram, square, step;
+  size_t x, a, part, bytes;
+};
+static OrthSizes orth_sizes(int64_t rows, int64_t cols) {
+  OrthSizes z{};
+  z.flip = rows > cols;
+  z.m = up32(std::min(rows, cols)), z.k = up32(std::max(rows, cols));
+  z.gram = orth_split(z.m, z.m, z.k, true), z.square = orth_split(z.m, z.m, z.m, true), z.step = orth_split(z.m, z.k, z.m, false);
+  const auto part = [](const OrthSplit& s, int64_t q, int64_t p) { return s.parts > 1 ? size_t(s.parts) * size_t(q) * size_t(p) * 4 : 0; };
+  z.x = size_t(z.m) * size_t(z.k) * 2, z.a = size_t(z.m) * size_t(z.m) * 2;
+  z.part = std::max({part(z.gram, z.m, z.m), part(z.square, z.m, z.m), part(z.step, z.m, z.k)});
+  z.bytes = kNormParts * sizeof(double) + 4 * z.x + 4 * z.a + z.part;
+  return z;
+}
+
+template <bool PCOL, class Out>
+static hgnn_status orth_product(const char* who, const Pairs& Q, const Pairs& P, int64_t nq, int64_t np, int64_t K, bool lower, const OrthSplit& split, float* part, const Out& out,
+                                hipStream_t s) {
+  ProductArgs a{};
+  a.Q0 = Q.hi, a.Q1 = Q.lo, a.ldq = Q.ld, a.P0 = P.hi, a.P1 = P.lo, a.ldp = P.ld, a.nq = nq, a.np = np, a.K = K, a.part = split.part, a.parts = split.parts, a.lower = lower;
+  if (split.parts == 1) return split.tile == 64 ? product<SplitSmall<PCOL>>(who, a, out, s) : product<SplitMid<PCOL>>(who, a, out, s);
+  const SumsPart sums{part, nq, np};
+  const hgnn_status st = split.tile == 64 ? product<SplitSmall<PCOL>>(who, a, sums, s) : product<SplitMid<PCOL>>(who, a, sums, s);
+  if (st != HGNN_OK) return st;
+  const int64_t blocks = ceil_div(nq * (np / 4), kBlock);
+  HGNN_REQUIRE(blocks <= 0xffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
+  sums_join_kernel<<<unsigned(blocks), kBlock, 0, s>>>(part, split.parts, nq, np, lower ? split.tile : 0, out);
+  HGNN_LAUNCH_CHECK("sums_join_kernel");
+  return HGNN_OK;
+}
+
+static hgnn_status orth_matrix(const char* who, const hgnn_grad& g, int32_t steps, const float* coef, float scale, char* ws, hipStream_t s) {
+  const OrthSizes z = orth_sizes(g.rows, g.cols);
+  double* const squares = reinterpret_cast<double*>(ws);
+  half_t* at = reinterpret_cast<half_t*>(ws + kNormParts * sizeof(double));
+  const auto pairs = [&](int64_t q, int64_t p) {
+    const Pairs r{at, at + q * p, p};
+    at += 2 * q * p;
+    return r;
+  };
+  Pairs X = pairs(z.m, z.k), next = pairs(z.m, z.k);
+  const Pairs A = pairs(z.m, z.m), B = pairs(z.m, z.m);
+  float* const part = reinterpret_cast<float*>(at);
+  const OrthMatrix m{g.grad, g.out ? g.out : const_cast<void*>(g.grad), g.rows, g.cols, g.ld, g.out ? g.ld_out : g.ld, int(g.type), int(g.out ? g.out_type : g.type)};
+  const unsigned parts = unsigned(std::min<int64_t>(kNormParts, ceil_div(g.rows * g.cols, 4 * kBlock)));
+  orth_squares_kernel<<<parts, kBlock, 0, s>>>(m, squares);
+  HGNN_LAUNCH_CHECK("orth_squares_kernel");
+  orth_begin_kernel<<<dim3(unsigned(z.k / kTurn), unsigned(z.m / kTurn)), kBlock, 0, s>>>(m, z.flip, squares, int(parts), X, steps == 0, scale);
+  HGNN_LAUNCH_CHECK("orth_begin_kernel");
+  for (int i = 0; i < steps; ++i) {
+    const float a = coef[3 * i], b = coef[3 * i + 1], c = coef[3 * i + 2];
+    hgnn_status st = orth_product<false>(who, X, X, z.m, z.m, z.k, true, z.gram, part, GramOut{c == 0.f ? B : A, (c == 0.f ? b : 1.f) * (kA / (kX * kX)), z.gram.tile}, s);
+    if (st == HGNN_OK && c != 0.f) st = orth_product<false>(who, A, A, z.m, z.m, z.m, true, z.square, part, SquareOut{B, A, b, c / kA, z.square.tile}, s);
+    if (st != HGNN_OK) return st;
+    if (i + 1 < steps) st = orth_product<true>(who, B, X, z.m, z.k, z.m, false, z.step, part, StepOut{next, X, a}, s);
+    else
+      st = orth_product<true>(who, B, X, z.m, z.k, z.m, false, z.step, part,
+                              LastOut{X, a, scale / kX, m.out, m.ldo, std::min(g.rows, g.cols), std::max(g.rows, g.cols), m.out_type, z.flip}, s);
+    if (st != HGNN_OK) return st;
+    std::swap(X, next);
+  }
+  return HGNN_OK;
+}
+
+// The largest of |f| on [0, t] for f = t (b + c t)
+static double largest_square(double b, double c, double t) {
+  double most = std::fabs(t * (b + c * t));
+  if (c != 0.) {
+    const double v = -b / (2 * c);
+    if (v > 0. && v < t) most = std::max(most, std::fabs(v * (b + c * v)));
+  }
+  return most;
+}
+// ... and of |s (a + b s^2 + c s^4)| on [0, s]
+static double largest_value(double a, double b, double c, double s) {
+  const auto f = [&](double v) { return std::fabs(v * (a + b * v * v + c * v * v * v * v)); };
+  double most = f(s);
+  const auto look = [&](double t) {  // a place where the slope a + 3 b t + 5 c t^2 is 0, t = s^2
+    if (t > 0. && t < s * s) most = std::max(most, f(std::sqrt(t)));
+  };
+  if (c != 0.) {
+    const double d = 9 * b * b - 20 * a * c;
+    if (d >= 0.) look((-3 * b + std::sqrt(d)) / (10 * c)), look((-3 * b - std::sqrt(d)) / (10 * c));
+  } else if (b != 0.) {
+    look(-a / (3 * b));
+  }
+  return most;
+}
+
+static hgnn_status check_matrices(const char* who, int32_t count, const hgnn_grad* g) {
+  HGNN_REQUIRE(count >= 0 && (g || count == 0), HGNN_EINVAL, "%s: count = %d, grads %s", who, count, g ? "given" : "NULL");
+  for (int i = 0; i < count; ++i) {
+    const hgnn_grad& t = g[i];
+    HGNN_REQUIRE(t.rows >= 0 && t.cols >= 0, HGNN_EINVAL, "%s: matrix %d: %lld x %lld", who, i, static_cast<long long>(t.rows), static_cast<long long>(t.cols));
+    HGNN_REQUIRE(known_type(t.type) && (!t.out || known_type(t.out_type)), HGNN_EINVAL, "%s: matrix %d: unknown type %d or %d", who, i, int(t.type), int(t.out_type));
+    HGNN_REQUIRE(t.ld >= t.cols && (!t.out || t.ld_out >= t.cols), HGNN_EINVAL, "%s: matrix %d: leading dimension smaller than the row", who, i);
+    HGNN_REQUIRE(t.rows <= 65536 && t.cols <= 65536, HGNN_EUNSUPPORTED, "%s: matrix %d: a side above 65536", who, i);
+    if (t.rows == 0 || t.cols == 0) continue;
+    HGNN_REQUIRE(t.grad && aligned_to_type(t.grad, t.type), HGNN_EINVAL, "%s: matrix %d: NULL, or not aligned to its type", who, i);
+    if (!t.out) continue;
+    HGNN_REQUIRE(aligned_to_type(t.out, t.out_type), HGNN_EINVAL, "%s: matrix %d: an output that is not aligned to its type", who, i);
+    HGNN_REQUIRE(t.out != t.grad || (t.type == t.out_type && t.ld == t.ld_out), HGNN_EINVAL, "%s: matrix %d: in place as another type or with another leading dimension", who, i);
+  }
+  return check_outputs(who, count, g);
+}
+
+}  // namespace hgnn
+
+using namespace hgnn;
+
+extern "C" {
+
+size_t hgnn_orthogonalize_workspace(int32_t count, const hgnn_grad* grads) {
+  size_t most = 0;
+  for (int i = 0; grads && i < count; ++i) {
+    const hgnn_grad& g = grads[i];
+    if (g.rows < 0 || g.cols < 0 || g.rows > 65536 || g.cols > 65536) return 0;
+    if (g.rows > 0 && g.cols > 0) most = std::max(most, orth_sizes(g.rows, g.cols).bytes);
+  }
+  return most;
+}
+
+hgnn_status hgnn_orthogonalize(int32_t count, const hgnn_grad* grads, int32_t steps, const float* coef, const float* scales, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  clear_error();
+  const char* who = "hgnn_orthogonalize";
+  hgnn_status st = check_matrices(who, count, grads);
+  if (st != HGNN_OK) return st;
+  HGNN_REQUIRE(steps >= 0 && steps <= 64 && (steps == 0 || coef), HGNN_EINVAL, "%s: steps = %d, coef %s", who, steps, coef ? "given" : "NULL");
+  double s = 1.;
+  for (int i = 0; i < steps; ++i) {
+    const double a = coef[3 * i], b = coef[3 * i + 1], c = coef[3 * i + 2];
+    HGNN_REQUIRE(std::isfinite(a) && std::isfinite(b) && std::isfinite(c), HGNN_EINVAL, "%s: coefficients of step %d that are not finite", who, i);
+    HGNN_REQUIRE(largest_square(b, c, s * s) <= 64., HGNN_EINVAL, "%s: step %d: b A + c A A may pass 64", who, i);
+    s = largest_value(a, b, c, s);
+    HGNN_REQUIRE(s <= 8., HGNN_EINVAL, "%s: step %d: singular values may pass 8", who, i);
+    s *= 1. + 1e-5;  // what roundings may add
+  }
+  for (int i = 0; scales && i < count; ++i) HGNN_REQUIRE(std::isfinite(scales[i]), HGNN_EINVAL, "%s: scales[%d] = %g", who, i, double(scales[i]));
+  const size_t need = hgnn_orthogonalize_workspace(count, grads);
+  HGNN_REQUIRE(need == 0 || (workspace && workspace_bytes >= need && aligned16(workspace)), HGNN_EINVAL,
+               "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_orthogonalize_workspace)", who, workspace_bytes, need);
+  for (int i = 0; i < count && st == HGNN_OK; ++i)
+    if (grads[i].rows > 0 && grads[i].cols > 0)
+      st = orth_matrix(who, grads[i], steps, coef, scales ? scales[i] : 1.f, static_cast<char*>(workspace), static_cast<hipStream_t>(stream));
+  return st;
+}
+
+}  // extern "C"

@@ -191,6 +191,8 @@ constexpr int64_t kMostBlocks = 0xffffffffll / kBlock;
 
 inline bool known_type(hgnn_type t) { return t == HGNN_F16 || t == HGNN_F32; }
 inline bool aligned_to_type(const void* p, hgnn_type t) { return (reinterpret_cast<uintptr_t>(p) & (t == HGNN_F32 ? 3u : 1u)) == 0; }
+// that no two of a list's outputs that hold anything are the same (clip.hip)
+hgnn_status check_outputs(const char* who, int32_t count, const hgnn_grad* g);
 // elements from a tensor's first to its last: what a row's last piece may be read from
 inline int64_t extent_of(int64_t rows, int64_t cols, int64_t ld) { return rows > 0 ? (rows - 1) * ld + cols : 0; }
 
