@@ -153,9 +153,9 @@ constexpr int kFull = 256;  // compute units
 template <ProductKind KIND, bool QCOL, bool PCOL, class Call>
 static hgnn_status with_product(Size size, Call&& call) {
   constexpr int two = KIND == kTwo ? 2 : 1;  // two results: half as many items of P
-  if (size == kFew) return call(ProductShape<2, 2, 2, 2, KIND, QCOL, PCOL, 4>());
-  if (size == kMid) return call(ProductShape<2, 2, 4, 4 / two, KIND, QCOL, PCOL, 4>());
-  return call(ProductShape<2, 4, 8, 4 / two, KIND, QCOL, PCOL, 4>());
+  if (size == kFew) return call(ProductShape<2, 2, 2, 2, KIND, QCOL, PCOL, 3>());
+  if (size == kMid) return call(ProductShape<2, 2, 4, 4 / two, KIND, QCOL, PCOL, 2>());
+  return call(ProductShape<2, 4, 8, 4 / two, KIND, QCOL, PCOL, 2>());
 }
 struct Split {
   Size size;
@@ -169,7 +169,7 @@ static Split split_of(int64_t nq, int64_t np, int64_t K, bool two) {
   s.size = nq <= 64 || np <= (two ? 32 : 64) ? kFew : tiles(256) >= kFull ? kWide : kMid;
   const int64_t t = s.size == kFew ? ceil_div(nq, 64) * ceil_div(np, 64) : tiles(s.size == kWide ? 256 : 128);
   int64_t parts = t >= kFull ? 1 : std::min(ceil_div(2 * kFull, t), ceil_div(K, 128));
-  s.part = std::max<int64_t>(32, up(ceil_div(K, std::max<int64_t>(parts, 1)), 32));
+  s.part = std::max<int64_t>(64, up(ceil_div(K, std::max<int64_t>(parts, 1)), 64));
   s.parts = int(std::max<int64_t>(1, ceil_div(K, s.part)));
   return s;
 }

@@ -23,16 +23,18 @@ __device__ __forceinline__ void split_value(float v, half_t& hi, half_t& lo) {
   hi = half_t(v);
   lo = half_t(v - float(hi));
 }
-// a matrix of values in two parts, pitch ld
+// a matrix of values in two parts, 32 high ones and their 32 low ones in turn; ld: halves of a line
 struct Pairs {
-  half_t *hi, *lo;
+  half_t* at;
   int64_t ld;
+  __device__ half_t* place(int64_t q, int64_t p) const { return at + q * ld + 2 * p - (p & 31); }
   __device__ float4_t get(int64_t q, int64_t p) const {
-    const half4_t h = *reinterpret_cast<const half4_t*>(hi + q * ld + p), l = *reinterpret_cast<const half4_t*>(lo + q * ld + p);
-    float4_t v;
+    const half_t* const v = place(q, p);
+    const half4_t h = *reinterpret_cast<const half4_t*>(v), l = *reinterpret_cast<const half4_t*>(v + 32);
+    float4_t r;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = float(h[e]) + float(l[e]);
-    return v;
+    for (int e = 0; e < 4; ++e) r[e] = float(h[e]) + float(l[e]);
+    return r;
   }
   __device__ void put(int64_t q, int64_t p, const float4_t& v, bool mirror) const {
     half4_t h, l;
@@ -42,11 +44,13 @@ struct Pairs {
       split_value(v[e], a, b);
       h[e] = a, l[e] = b;
     }
-    *reinterpret_cast<half4_t*>(hi + q * ld + p) = h;
-    *reinterpret_cast<half4_t*>(lo + q * ld + p) = l;
+    half_t* const to = place(q, p);
+    *reinterpret_cast<half4_t*>(to) = h;
+    *reinterpret_cast<half4_t*>(to + 32) = l;
     if (!mirror) return;
+    half_t* const over = place(p, q);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) hi[(p + e) * ld + q] = h[e], lo[(p + e) * ld + q] = l[e];
+    for (int e = 0; e < 4; ++e) over[e * ld] = h[e], over[e * ld + 32] = l[e];
   }
 };
 
@@ -173,7 +177,8 @@ __global__ __launch_bounds__(kBlock) void orth_begin_kernel(OrthMatrix m, int fl
     const int64_t q = int64_t(blockIdx.y) * kTurn + i, p = int64_t(blockIdx.x) * kTurn + x;
     half_t hi, lo;
     split_value(flip ? tile[x][i] : tile[i][x], hi, lo);
-    X.hi[q * X.ld + p] = hi, X.lo[q * X.ld + p] = lo;
+    half_t* const to = X.place(q, p);
+    to[0] = hi, to[32] = lo;
   }
 }
 
@@ -181,7 +186,7 @@ static int64_t up32(int64_t n) { return (n + 31) / 32 * 32; }
 
 // ---- shapes: tiles of 64 where a side is short, else of 128
 template <bool PCOL>
-using SplitSmall = ProductShape<2, 2, 2, 2, kSplit, false, PCOL, 4>;
+using SplitSmall = ProductShape<2, 2, 2, 2, kSplit, false, PCOL, 3>;
 template <bool PCOL>
 using SplitMid = ProductShape<2, 2, 4, 4, kSplit, false, PCOL, 2>;
 constexpr int kOrthFull = 256;
@@ -223,7 +228,7 @@ template <bool PCOL, class Out>
 static hgnn_status orth_product(const char* who, const Pairs& Q, const Pairs& P, int64_t nq, int64_t np, int64_t K, bool lower, const OrthSplit& split, float* part, const Out& out,
                                 hipStream_t s) {
   ProductArgs a{};
-  a.Q0 = Q.hi, a.Q1 = Q.lo, a.ldq = Q.ld, a.P0 = P.hi, a.P1 = P.lo, a.ldp = P.ld, a.nq = nq, a.np = np, a.K = K, a.part = split.part, a.parts = split.parts, a.lower = lower;
+  a.Q0 = a.Q1 = Q.at, a.ldq = Q.ld, a.P0 = a.P1 = P.at, a.ldp = P.ld, a.nq = nq, a.np = np, a.K = K, a.part = split.part, a.parts = split.parts, a.lower = lower;
   if (split.parts == 1) return split.tile == 64 ? product<SplitSmall<PCOL>>(who, a, out, s) : product<SplitMid<PCOL>>(who, a, out, s);
   const SumsPart sums{part, nq, np};
   const hgnn_status st = split.tile == 64 ? product<SplitSmall<PCOL>>(who, a, sums, s) : product<SplitMid<PCOL>>(who, a, sums, s);
@@ -240,7 +245,7 @@ static hgnn_status orth_matrix(const char* who, const hgnn_grad& g, int32_t step
   double* const squares = reinterpret_cast<double*>(ws);
   half_t* at = reinterpret_cast<half_t*>(ws + kNormParts * sizeof(double));
   const auto pairs = [&](int64_t q, int64_t p) {
-    const Pairs r{at, at + q * p, p};
+    const Pairs r{at, 2 * p};
     at += 2 * q * p;
     return r;
   };

@@ -1,11 +1,14 @@
 // Dense products on the matrix cores for matrices of any size:  C[q][p] = sum_k Q(q, k) P(p, k), fp16 operands, fp32 sums, and an epilogue that takes the
 // sums out of the registers.  Used by the gated projection (gated.hip) and the orthogonal updates (orthogonalize.hip).
 //
-// An operand lies with the contraction along its rows ([items][k], "rows") or across them ([k][items], "columns").  Both come into LDS as 32 contraction steps
-// of 64 or more items by loads that write LDS directly, a kilobyte an instruction, 16 bytes a lane, a ring of kStages ahead of the products, so that no register
-// and no instruction of a lane carries them; lanes choose WHICH 16 bytes they ask for, such that the reads behind meet on no bank:
-//  - rows: an instruction is 16 items of 32 steps; lane l asks for item l / 4, piece (l % 4) ^ (l / 16), and ds_read_b128 gives a lane eight steps of an item;
-//  - columns: an instruction is 8 steps of 64 items; piece u of step r stands at place u ^ turn(r), and ds_read_b64_tr_b16 gives a lane four steps of an item.
+// An operand lies with the contraction along its rows ([items][k], "rows") or across them ([k][items], "columns").  Both come into LDS by loads that write LDS
+// directly, a kilobyte an instruction, 16 bytes a lane, 128 consecutive bytes of eight rows, a ring of stages ahead of the products, so that no register and no
+// instruction of a lane carries them; lanes choose WHICH 16 bytes they ask for, such that the reads behind meet on no bank:
+//  - rows: 64 steps of 8 items; piece u of item i (of 16) stands at place u ^ (i / 2), and ds_read_b128 gives a lane eight steps of an item (it serves lanes 0-3 and
+//    12-15 of 16 together with 4-11 of the next 16);
+//  - columns: 64 items of 8 steps; piece u of step r stands at place u ^ turn(r), and ds_read_b64_tr_b16 gives a lane four steps of an item.
+// Values that are two fp16 numbers each lie as 32 high parts and 32 low parts in turn, so that the same 128 bytes are 32 steps (items) of both.
+// (With 64 bytes of 16 rows an instruction, at pitches that are multiples of 4 KB, requests met on the L2's channels: 8192 x 16384 x 2048 592 us.)
 // What is behind the contraction's end is asked for at a place that holds zeros; where the end lies inside a piece, the rest of the piece is cleared in LDS
 // (the bytes there are the caller's padding and may be NaN).  Items that do not exist are asked for at the last one that does: they meet only results that
 // are not stored.
@@ -23,8 +26,8 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef short short8_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) short4_t lds_short4_t;
 
-// Two operands each where the kernel takes two: of P for two results at once (kTwo), the second segment of the contraction (kSegments), or the low parts of
-// values that are two fp16 numbers each (kSplit: Q0 P0 + Q0 P1 + Q1 P0).
+// Two operands each where the kernel takes two: of P for two results at once (kTwo), the second segment of the contraction (kSegments).  kSplit: values of two
+// parts, Q P = Qhi Phi + Qhi Plo + Qlo Phi; its contraction is a multiple of 32 and its items are, too.
 enum ProductKind { kOne, kTwo, kSegments, kSplit };
 
 struct ProductArgs {
@@ -32,7 +35,7 @@ struct ProductArgs {
   int64_t ldq, ldp;
   int64_t nq, np;   // items
   int64_t K;        // of a segment
-  int64_t part;     // contraction steps of a workgroup (blocks beyond the first take the next ones); a multiple of 32, or K where there is one part
+  int64_t part;     // contraction steps of a workgroup (blocks beyond the first take the next ones); a multiple of 64 (kSplit: 32), or K where there is one part
   int64_t tiles;    // of C, tiles_p of them on a line
   int32_t tiles_p;
   int32_t parts;
@@ -48,9 +51,10 @@ struct ProductShape {
   static constexpr bool QCOL = QCOL_, PCOL = PCOL_;
   static constexpr int kWaves = WQ * WP, kThreads = kWaves * kWave;
   static constexpr int BQ = 16 * TQ * WQ, BP = 16 * TP * WP;
-  static constexpr int NQ = KIND == kSplit ? 2 : 1, NP = KIND == kSplit || KIND == kTwo ? 2 : 1;  // operands in LDS
-  static constexpr int NR = KIND == kTwo ? 2 : 1;                                                 // results
-  static constexpr int CQ = NQ * BQ / 16, CP = NP * BP / 16;  // kilobytes of a stage
+  static constexpr bool SPLIT = KIND == kSplit;
+  static constexpr int NP = KIND == kTwo ? 2 : 1, NR = NP;        // operands of P in LDS, results
+  static constexpr int kStep = SPLIT ? 32 : 64, kSubs = kStep / 32;  // contraction of a stage, instructions along it
+  static constexpr int CQ = BQ / 8, CP = NP * BP / 8;              // kilobytes of a stage
   static constexpr int JQ = CQ / kWaves, JP = CP / kWaves, J = JQ + JP;
   static constexpr int kStageBytes = (CQ + CP) * 1024;
   static constexpr int kLds = kStageBytes * kStages;
@@ -62,9 +66,12 @@ struct ProductShape {
 // place of 16 bytes of step r (0..31) among the eight of 64 items
 __device__ __forceinline__ int product_turn(int r) { return 2 * ((r >> 1) & 1) | 4 * ((r >> 3) & 1); }
 
-// 16 bytes a lane from src to LDS at `to` (uniform) + 16 * lane.  Written out, because behind the builtin the compiler waits for all of them before every
-// read of LDS; what it does not know of is waited for by product_wait.  (Nothing else in these kernels uses m0.)
-__device__ __forceinline__ void load_to_lds(const void* src, uint32_t to) {
+// 16 bytes a lane from base (uniform) + off to LDS at `to` (uniform) + 16 * lane.  Written out, because behind the builtin the compiler waits for all of them before
+// every read of LDS; what it does not know of is waited for by product_wait.  (Nothing else in these kernels uses m0.)
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1" ::"s"(to), "s"(base), "v"(off) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(const char* src, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src) : "memory");
 }
 // at most N of this wave's loads to LDS are left in flight, its reads of LDS have ended, and so have those of all waves
@@ -76,32 +83,34 @@ __device__ __forceinline__ void product_wait() {
   asm volatile("" ::: "memory");
 }
 
-// one operand's kilobytes that a wave brings in
+// One operand's kilobytes that a wave brings in: where they begin is uniform and moves with the steps, a lane's place behind it stays.
 template <int N, bool COL>
 struct ProductLoads {
-  const char* at[N];
+  const char* base[N];
+  uint32_t off[N];
   int k[N];  // step of the lane's piece inside 32
   int64_t inc;
 };
-template <int N, bool COL, int CHUNKS, int WAVES>
+template <int N, bool COL, bool SPLIT, int WAVES>
 __device__ __forceinline__ void product_loads(ProductLoads<N, COL>& s, const half_t* first, const half_t* second, int64_t ld, int64_t item0, int64_t items, int64_t k0, int wave,
                                               int lane, int half) {
-  s.inc = (COL ? 32 * ld : 32) * int64_t(sizeof(half_t));
+  constexpr int kStep = SPLIT ? 32 : 64, kParts = SPLIT ? 2 : 1;
+  s.inc = (COL ? kStep * ld : 64) * int64_t(sizeof(half_t));
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     int c = wave + j * WAVES;
-    const half_t* base = first;
-    if (c >= half) c -= half, base = second;  // uniform
+    const half_t* from = first;
+    if (c >= half) c -= half, from = second;
     if (COL) {
-      const int r = 8 * (c % 4) + (lane >> 3), u = (lane & 7) ^ product_turn(r);
-      int64_t item = item0 + 64 * (c / 4) + 8 * u;
-      if (item >= items) item = 0;
+      const int r = 8 * (c % (kStep / 8)) + (lane >> 3), u = (lane & 7) ^ product_turn(r), item = 64 * (c / (kStep / 8)) + 8 * u;
       s.k[j] = r;
-      s.at[j] = reinterpret_cast<const char*>(base + (k0 + r) * ld + item);
+      s.base[j] = reinterpret_cast<const char*>(from + k0 * ld + item0 * kParts);
+      s.off[j] = uint32_t(r * uint32_t(ld) + (item0 * kParts + item < items * kParts ? item : 0)) * 2u;
     } else {
-      const int64_t item = min(item0 + 16 * c + (lane >> 2), items - 1);
-      s.k[j] = 8 * ((lane & 3) ^ (lane >> 4));
-      s.at[j] = reinterpret_cast<const char*>(base + item * ld + k0 + s.k[j]);
+      const int n = 8 * (c & 1) + (lane >> 3), u = (lane & 7) ^ (n >> 1), item = int(min(int64_t(8 * c + (lane >> 3)), items - 1 - item0));
+      s.k[j] = SPLIT ? 0 : 8 * u;
+      s.base[j] = reinterpret_cast<const char*>(from + item0 * ld + k0 * kParts);
+      s.off[j] = (uint32_t(item) * uint32_t(ld) + 8 * u) * 2u;
     }
   }
 }
@@ -121,14 +130,35 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, int64_t t, in
   tq = g * kGroup + (in - tp * rows);
 }
 
-template <class S>
-__device__ __forceinline__ half8_t product_fragment(const unsigned char* tile, int f, bool col, const int (&off)[4]) {
-  if (!col) return *reinterpret_cast<const half8_t*>(tile + f * 1024 + off[0]);
-  const unsigned char* p = tile + (f / 4) * 4096 + off[f % 4];
-  const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)p);
-  const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(p + 512));
-  return __builtin_bit_cast(half8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
+// Where a lane reads its share of the T fragments (16 items of 32 steps) of a wave that begin with number f0; h: the stage's first or second 32 steps, or the high or
+// low parts.
+template <bool COL, bool SPLIT, int T>
+struct ProductReads {
+  static constexpr int A = !COL ? 2 : SPLIT || T >= 4 ? 4 : T;
+  int at[A];
+  __device__ __forceinline__ ProductReads(int f0, int lane) {
+    const int i = lane & 15, qq = lane >> 4, r = 8 * qq + (i >> 2);
+#pragma unroll
+    for (int t = 0; t < A; ++t) {
+      if (!COL) {
+        at[t] = f0 * 2048 + i * 128 + ((4 * t + qq) ^ (i >> 1)) * 16;
+      } else {
+        const int f = f0 + t, place = SPLIT ? t : f & 3;  // of 16 items among the 64 (32 and their low parts)
+        at[t] = (SPLIT ? (f0 >> 1) * 4096 : (f >> 2) * 8192) + r * 128 + (((2 * place + ((i & 3) >> 1)) ^ product_turn(r)) * 16) + (i & 1) * 8;
+      }
+    }
+  }
+  __device__ __forceinline__ half8_t get(const unsigned char* tile, int t, int h) const {
+    if constexpr (!COL) {
+      return *reinterpret_cast<const half8_t*>(tile + at[h] + t * 2048);
+    } else {
+      const unsigned char* p = tile + (SPLIT ? at[2 * h + t % 2] + (t / 2) * 4096 : at[t % A] + (t / 4) * 8192 + h * 4096);
+      const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)p);
+      const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(p + 512));
+      return __builtin_bit_cast(half8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
 
 template <class S, class Epilogue>
 __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs a, Epilogue epilogue) {
@@ -138,18 +168,20 @@ __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs a, 
   // consecutive workgroups go to the XCDs in turn: each takes a run of tiles of its own
   const int64_t all = a.tiles * a.parts, id = blockIdx.x, x = id & 7, base = all >> 3, more = all & 7;
   const int64_t work = x * base + min(x, more) + (id >> 3);
-  const int64_t part = work / a.tiles;
+  const int64_t part = __builtin_amdgcn_readfirstlane(int(work / a.tiles));
   int64_t tq, tp;
   product_tile(a, work - part * a.tiles, tq, tp);
-  const int64_t q0 = tq * S::BQ, p0 = tp * S::BP;
+  // (the divisions go through vector registers: back to scalar ones, which the loads to LDS take their places from)
+  const int64_t q0 = int64_t(__builtin_amdgcn_readfirstlane(int(tq))) * S::BQ, p0 = int64_t(__builtin_amdgcn_readfirstlane(int(tp))) * S::BP;
   const int64_t k_begin = part * a.part, k_end = min(a.K, k_begin + a.part), count = k_end - k_begin;  // of a segment
-  const int per = int((count + 31) / 32), steps = S::KIND == kSegments ? 2 * per : per;
+  const int per = int((count + S::kStep - 1) / S::kStep), steps = S::KIND == kSegments ? 2 * per : per;
 
   ProductLoads<S::JQ, S::QCOL> lq;
   ProductLoads<S::JP, S::PCOL> lp;
+  // steps of S::kStep
   const auto start = [&](bool second) __attribute__((always_inline)) {
-    product_loads<S::JQ, S::QCOL, S::CQ, S::kWaves>(lq, second ? a.Q1 : a.Q0, a.Q1, a.ldq, q0, a.nq, k_begin, wave, lane, S::BQ / 16);
-    product_loads<S::JP, S::PCOL, S::CP, S::kWaves>(lp, second ? a.P1 : a.P0, a.P1, a.ldp, p0, a.np, k_begin, wave, lane, S::BP / 16);
+    product_loads<S::JQ, S::QCOL, S::SPLIT, S::kWaves>(lq, second ? a.Q1 : a.Q0, a.Q1, a.ldq, q0, a.nq, k_begin, wave, lane, S::BQ / 8);
+    product_loads<S::JP, S::PCOL, S::SPLIT, S::kWaves>(lp, second ? a.P1 : a.P0, a.P1, a.ldp, p0, a.np, k_begin, wave, lane, S::BP / 8);
   };
   start(false);
   const char* const zero = reinterpret_cast<const char*>(&g_product_zero);
@@ -158,30 +190,30 @@ __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs a, 
   uint32_t to = lds0 + wave * 1024;
   const auto ask = [&]() __attribute__((always_inline)) {
     if (S::KIND == kSegments && in_segment == per) in_segment = 0, start(true);
-    const int left = int(min(count - int64_t(in_segment) * 32, int64_t(32)));
+    const int left = int(min(count - int64_t(in_segment) * S::kStep, int64_t(S::kStep)));
+    if (S::SPLIT || left == S::kStep) {  // uniform
 #pragma unroll
-    for (int j = 0; j < S::JQ; ++j) {
-      load_to_lds(lq.k[j] < left ? lq.at[j] : zero, to + j * S::kWaves * 1024);
-      lq.at[j] += lq.inc;
+      for (int j = 0; j < S::JQ; ++j) load_to_lds(lq.base[j], lq.off[j], to + j * S::kWaves * 1024);
+#pragma unroll
+      for (int j = 0; j < S::JP; ++j) load_to_lds(lp.base[j], lp.off[j], to + (S::JQ + j) * S::kWaves * 1024);
+    } else {
+#pragma unroll
+      for (int j = 0; j < S::JQ; ++j) load_to_lds(lq.k[j] < left ? lq.base[j] + lq.off[j] : zero, to + j * S::kWaves * 1024);
+#pragma unroll
+      for (int j = 0; j < S::JP; ++j) load_to_lds(lp.k[j] < left ? lp.base[j] + lp.off[j] : zero, to + (S::JQ + j) * S::kWaves * 1024);
     }
 #pragma unroll
-    for (int j = 0; j < S::JP; ++j) {
-      load_to_lds(lp.k[j] < left ? lp.at[j] : zero, to + (S::JQ + j) * S::kWaves * 1024);
-      lp.at[j] += lp.inc;
-    }
+    for (int j = 0; j < S::JQ; ++j) lq.base[j] += lq.inc;
+#pragma unroll
+    for (int j = 0; j < S::JP; ++j) lp.base[j] += lp.inc;
     ++asked, ++in_segment;
     to += S::kStageBytes;
     if (to >= lds0 + S::kLds) to -= S::kLds;
   };
 
   const int wq = wave / S::WP, wp = wave % S::WP;
-  int off_row[4], off_col[4];
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int r = 8 * qq + (i >> 2);
-    off_row[t] = 16 * (4 * i + (qq ^ (i >> 2)));
-    off_col[t] = r * 128 + (((2 * t + ((i & 3) >> 1)) ^ product_turn(r)) * 16) + (i & 1) * 8;
-  }
+  const ProductReads<S::QCOL, S::SPLIT, S::TQ> read_q(wq * S::TQ, lane);
+  const ProductReads<S::PCOL, S::SPLIT, S::TP> read_p(wp * S::TP, lane);
 
   float4_t acc[S::NR][S::TQ][S::TP];
 #pragma unroll
@@ -192,63 +224,99 @@ __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs a, 
       for (int u = 0; u < S::TP; ++u) acc[r][t][u] = float4_t{0.f, 0.f, 0.f, 0.f};
 
 #pragma unroll
-  for (int s = 0; s < S::kStages - 1; ++s)
+  for (int s = 0; s < S::kStages; ++s)
     if (s < steps) ask();
-  const unsigned char* stage = lds;
-  for (int s = 0, at = 0; s < steps; ++s) {
-    // the stages behind this one that have been asked for stay in flight
+  int at = 0;
+  // step s is in LDS, as all waves see it; the stages behind it that have been asked for stay in flight
+  const auto arrive = [&](int s, unsigned char* stage) __attribute__((always_inline)) {
     const int behind = asked - 1 - s;
     if (S::kStages > 3 && behind >= 2) product_wait<(S::kStages > 3 ? 2 : 0) * S::J>();
     else if (S::kStages > 2 && behind >= 1) product_wait<(S::kStages > 2 ? 1 : 0) * S::J>();
     else product_wait<0>();
-    if (asked < steps) ask();
-    if (++at == per) {  // a segment's last step
-      at = 0;
-      const int left = int(count - int64_t(per - 1) * 32);
-      if ((left & 7) && (!S::QCOL || !S::PCOL)) {
-        const auto clear = [&](unsigned char* tiles, int items) __attribute__((always_inline)) {
-          for (int t = threadIdx.x; t < items; t += S::kThreads) {
-            const int n = t & 15;
-            half8_t* const p = reinterpret_cast<half8_t*>(tiles + (t >> 4) * 1024 + 16 * (4 * n + ((left >> 3) ^ (n >> 2))));
-            half8_t v = *p;
+    if (++at < per) return;  // else a segment's last step
+    at = 0;
+    const int left = int(count - int64_t(per - 1) * S::kStep);
+    if (S::SPLIT || !(left & 7) || (S::QCOL && S::PCOL)) return;
+    const auto clear = [&](unsigned char* tiles, int items) __attribute__((always_inline)) {
+      for (int t = threadIdx.x; t < items; t += S::kThreads) {
+        half8_t* const p = reinterpret_cast<half8_t*>(tiles + t * 128 + ((left >> 3) ^ ((t & 15) >> 1)) * 16);
+        half8_t v = *p;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (e >= (left & 7)) v[e] = half_t(0);
-            *p = v;
-          }
-        };
-        unsigned char* const here = const_cast<unsigned char*>(stage);
-        if (!S::QCOL) clear(here, S::NQ * S::BQ);
-        if (!S::PCOL) clear(here + S::CQ * 1024, S::NP * S::BP);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        for (int e = 0; e < 8; ++e)
+          if (e >= (left & 7)) v[e] = half_t(0);
+        *p = v;
+      }
+    };
+    if (!S::QCOL) clear(stage, S::BQ);
+    if (!S::PCOL) clear(stage + S::CQ * 1024, S::NP * S::BP);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // A wave's block in two halves of its lines: while the products of one half run, the operands of the next are on their way out of LDS.
+  constexpr int HQ = S::TQ / 2;
+  static_assert(S::TQ % 2 == 0, "halves");
+  constexpr int NV = S::SPLIT ? 2 : 1;  // parts of a value
+  half8_t p0s[NV * S::NP][S::TP], p1s[NV * S::NP][S::TP], fa[NV][HQ], fb[NV][HQ];
+  typedef half8_t PValues[NV * S::NP][S::TP];
+  typedef half8_t QValues[NV][HQ];
+  const auto get_p = [&](PValues& f, const unsigned char* stage, int h, int u) __attribute__((always_inline)) {
+#pragma unroll
+    for (int o = 0; o < NV * S::NP; ++o) f[o][u] = read_p.get(stage + (S::CQ + (S::SPLIT ? 0 : o) * (S::BP / 8)) * 1024, u, S::SPLIT ? o : h);
+  };
+  const auto get_q = [&](QValues& f, const unsigned char* stage, int h, int half, int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int o = 0; o < NV; ++o) f[o][t] = read_q.get(stage, half * HQ + t, S::SPLIT ? o : h);
+  };
+  const auto multiply = [&](const PValues& p, const QValues& q, int half, int t) __attribute__((always_inline)) {
+    const int line = half * HQ + t;
+#pragma unroll
+    for (int u = 0; u < S::TP; ++u) {
+      if (S::SPLIT) {
+        acc[0][line][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[NV - 1][u], q[0][t], acc[0][line][u], 0, 0, 0);
+        acc[0][line][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0][u], q[NV - 1][t], acc[0][line][u], 0, 0, 0);
+        acc[0][line][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0][u], q[0][t], acc[0][line][u], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int r = 0; r < S::NR; ++r) acc[r][line][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[r][u], q[0][t], acc[r][line][u], 0, 0, 0);
       }
     }
-    half8_t fp[S::NP][S::TP];
+  };
+  unsigned char* stage = lds;
+  arrive(0, stage);
 #pragma unroll
-    for (int o = 0; o < S::NP; ++o)
+  for (int u = 0; u < S::TP; ++u) get_p(p0s, stage, 0, u);
 #pragma unroll
-      for (int u = 0; u < S::TP; ++u) fp[o][u] = product_fragment<S>(stage + (S::CQ + o * (S::BP / 16)) * 1024, wp * S::TP + u, S::PCOL, S::PCOL ? off_col : off_row);
+  for (int t = 0; t < HQ; ++t) get_q(fa, stage, 0, 0, t);
+  // 32 steps of stage s, with P's values in `p`; those of the next 32 go into `next`.  (Reads in a row would fill the queue to LDS, and products wait behind them: a few
+  // at a time.)
+  const auto sub = [&](int s, int h, const PValues& p, PValues& next) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < S::TQ; ++t) {
-      half8_t fq[S::NQ];
-#pragma unroll
-      for (int o = 0; o < S::NQ; ++o) fq[o] = product_fragment<S>(stage + o * (S::BQ / 16) * 1024, wq * S::TQ + t, S::QCOL, S::QCOL ? off_col : off_row);
-#pragma unroll
-      for (int u = 0; u < S::TP; ++u) {
-        if (S::KIND == kSplit) {
-          acc[0][t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[S::NP - 1][u], fq[0], acc[0][t][u], 0, 0, 0);
-          acc[0][t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[0][u], fq[S::NQ - 1], acc[0][t][u], 0, 0, 0);
-          acc[0][t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[0][u], fq[0], acc[0][t][u], 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int r = 0; r < S::NR; ++r) acc[r][t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[r][u], fq[0], acc[r][t][u], 0, 0, 0);
-        }
-      }
+    for (int t = 0; t < HQ; ++t) {
+      get_q(fb, stage, h, 1, t);
+      multiply(p, fa, 0, t);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    stage += S::kStageBytes;
-    if (stage >= lds + S::kLds) stage -= S::kLds;
+    if (h == S::kSubs - 1 && s + 1 < steps) {
+      stage += S::kStageBytes;
+      if (stage >= lds + S::kLds) stage -= S::kLds;
+      arrive(s + 1, stage);
+      if (asked < steps) ask();  // into the place of stage s, which all waves have left
+    }
+    const int then = (h + 1) % S::kSubs;
+#pragma unroll
+    for (int t = 0; t < HQ; ++t) {  // (behind the last stage: what is there once more)
+      get_q(fa, stage, then, 0, t);
+#pragma unroll
+      for (int u = t * S::TP / HQ; u < (t + 1) * S::TP / HQ; ++u) get_p(next, stage, then, u);
+      multiply(p, fb, 1, t);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  for (int s = 0; s < steps; ++s) {
+    sub(s, 0, p0s, p1s);
+    if (S::kSubs == 1 && ++s >= steps) break;
+    sub(s, S::kSubs - 1, p1s, p0s);
   }
 #pragma unroll
   for (int t = 0; t < S::TQ; ++t) {
