@@ -58,11 +58,14 @@ struct GatedOut {
   int act, F;
   half_t* Y;
   int64_t ldy;
-  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& g, const float4_t& u) const {
+  typedef ProductNothing Read;
+  __device__ Read read(int64_t, int64_t) const { return {}; }
+  template <bool WHOLE>
+  __device__ void put(int64_t, int64_t q, int64_t p, const Read&, const float4_t& g, const float4_t& u) const {
     float4_t y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = gate_value(act, g[e]) * u[e];
-    store_four(Y + q * ldy + p, F - p, y);
+    store_four(Y + q * ldy + p, WHOLE ? 4 : F - p, y);
   }
 };
 struct GatedGradOut {
@@ -71,8 +74,10 @@ struct GatedGradOut {
   int64_t lddy;
   half_t* D;  // [n][2 Fp]
   int64_t Fp;
-  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& g, const float4_t& u) const {
-    const half4_t dy = *reinterpret_cast<const half4_t*>(dY + q * lddy + p);  // what is behind F reaches what is behind F
+  typedef half4_t Read;
+  __device__ Read read(int64_t q, int64_t p) const { return *reinterpret_cast<const half4_t*>(dY + q * lddy + p); }  // what is behind F reaches what is behind F
+  template <bool WHOLE>
+  __device__ void put(int64_t, int64_t q, int64_t p, const Read& dy, const float4_t& g, const float4_t& u) const {
     float4_t dg, du;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -87,7 +92,10 @@ struct GatedGradOut {
 struct GatedPart {  // [parts][n][2][Fp]
   float* part;
   int64_t n, Fp;
-  __device__ void operator()(int64_t k, int64_t q, int64_t p, const float4_t& g, const float4_t& u) const {
+  typedef ProductNothing Read;
+  __device__ Read read(int64_t, int64_t) const { return {}; }
+  template <bool WHOLE>
+  __device__ void put(int64_t k, int64_t q, int64_t p, const Read&, const float4_t& g, const float4_t& u) const {
     float* const at = part + ((k * n + q) * 2) * Fp + p;
     *reinterpret_cast<float4_t*>(at) = g;
     *reinterpret_cast<float4_t*>(at + Fp) = u;
@@ -105,7 +113,7 @@ __global__ __launch_bounds__(kBlock) void gated_join_kernel(const float* part, i
     at += stride;
     g += *reinterpret_cast<const float4_t*>(at), u += *reinterpret_cast<const float4_t*>(at + Fp);
   }
-  out(0, q, p, g, u);
+  out.template put<false>(0, q, p, out.read(q, p), g, u);
 }
 
 // ---- products into one fp16 matrix, or into two that are the halves of C's lines or of its items along a line
@@ -114,7 +122,10 @@ struct HalfOut {
   int64_t ld;
   int64_t split_q, split_p;  // from there on b's; beyond C: none
   int64_t lines, cols;       // of either
-  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const {
+  typedef ProductNothing Read;
+  __device__ Read read(int64_t, int64_t) const { return {}; }
+  template <bool WHOLE>
+  __device__ void put(int64_t, int64_t q, int64_t p, const Read&, const float4_t& v) const {
     half_t* to = a;
     if (q >= split_q) to = b, q -= split_q;
     if (p >= split_p) to = b, p -= split_p;
@@ -124,7 +135,10 @@ struct HalfOut {
 struct HalfPart {  // [parts][nq][pitch]
   float* part;
   int64_t nq, pitch;
-  __device__ void operator()(int64_t k, int64_t q, int64_t p, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * pitch + p) = v; }
+  typedef ProductNothing Read;
+  __device__ Read read(int64_t, int64_t) const { return {}; }
+  template <bool WHOLE>
+  __device__ void put(int64_t k, int64_t q, int64_t p, const Read&, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * pitch + p) = v; }
 };
 __global__ __launch_bounds__(kBlock) void half_join_kernel(const float* part, int parts, int64_t nq, int64_t pitch, HalfOut out) {
   const int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x, each = pitch / 4, q = t / each, p = 4 * (t - q * each);
@@ -137,7 +151,7 @@ __global__ __launch_bounds__(kBlock) void half_join_kernel(const float* part, in
     at += stride;
     v += *reinterpret_cast<const float4_t*>(at);
   }
-  out(0, q, p, v);
+  out.template put<false>(0, q, p, out.read(q, p), v);
 }
 
 __global__ __launch_bounds__(kBlock) void half_zero_kernel(half_t* out, int64_t lines, int64_t cols, int64_t ld) {
@@ -150,6 +164,7 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // ---- shapes.  A product of few rows takes tiles of 64, one whose tiles of 256 x 256 fill the chip those, any other 128 x 128.
 enum Size { kFew, kMid, kWide };
 constexpr int kFull = 256;  // compute units
+constexpr int kLong = 512;
 template <ProductKind KIND, bool QCOL, bool PCOL, class Call>
 static hgnn_status with_product(Size size, Call&& call) {
   constexpr int two = KIND == kTwo ? 2 : 1;  // two results: half as many items of P
@@ -166,7 +181,7 @@ struct Split {
 static Split split_of(int64_t nq, int64_t np, int64_t K, bool two) {
   const auto tiles = [&](int64_t b) { return ceil_div(nq, b) * ceil_div(np, two ? b / 2 : b); };
   Split s;
-  s.size = nq <= 64 || np <= (two ? 32 : 64) ? kFew : tiles(256) >= kFull ? kWide : kMid;
+  s.size = nq <= 64 || np <= (two ? 32 : 64) ? kFew : K >= kLong && tiles(256) >= kFull ? kWide : kMid;
   const int64_t t = s.size == kFew ? ceil_div(nq, 64) * ceil_div(np, 64) : tiles(s.size == kWide ? 256 : 128);
   int64_t parts = t >= kFull ? 1 : std::min(ceil_div(2 * kFull, t), ceil_div(K, 128));
   s.part = std::max<int64_t>(64, up(ceil_div(K, std::max<int64_t>(parts, 1)), 64));

@@ -28,13 +28,18 @@ struct Pairs {
   half_t* at;
   int64_t ld;
   __device__ half_t* place(int64_t q, int64_t p) const { return at + q * ld + 2 * p - (p & 31); }
-  __device__ float4_t get(int64_t q, int64_t p) const {
-    const half_t* const v = place(q, p);
-    const half4_t h = *reinterpret_cast<const half4_t*>(v), l = *reinterpret_cast<const half4_t*>(v + 32);
-    float4_t r;
+  struct Four {
+    half4_t h, l;
+    __device__ float4_t value() const {
+      float4_t r;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = float(h[e]) + float(l[e]);
-    return r;
+      for (int e = 0; e < 4; ++e) r[e] = float(h[e]) + float(l[e]);
+      return r;
+    }
+  };
+  __device__ Four get(int64_t q, int64_t p) const {
+    const half_t* const v = place(q, p);
+    return {*reinterpret_cast<const half4_t*>(v), *reinterpret_cast<const half4_t*>(v + 32)};
   }
   __device__ void put(int64_t q, int64_t p, const float4_t& v, bool mirror) const {
     half4_t h, l;
@@ -59,18 +64,27 @@ struct GramOut {  // A, or b A where that is all of B
   Pairs to;
   float factor;
   int tile;
-  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const { to.put(q, p, v * factor, q / tile != p / tile); }
+  typedef ProductNothing Read;
+  __device__ Read read(int64_t, int64_t) const { return {}; }
+  template <bool WHOLE>
+  __device__ void put(int64_t, int64_t q, int64_t p, const Read&, const float4_t& v) const { to.put(q, p, v * factor, q / tile != p / tile); }
 };
 struct SquareOut {  // B = b A + c A A
   Pairs to, A;
   float b, c;
   int tile;
-  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const { to.put(q, p, A.get(q, p) * b + v * c, q / tile != p / tile); }
+  typedef Pairs::Four Read;
+  __device__ Read read(int64_t q, int64_t p) const { return A.get(q, p); }
+  template <bool WHOLE>
+  __device__ void put(int64_t, int64_t q, int64_t p, const Read& x, const float4_t& v) const { to.put(q, p, x.value() * b + v * c, q / tile != p / tile); }
 };
 struct StepOut {  // X = a X + B X
   Pairs to, X;
   float a;
-  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const { to.put(q, p, X.get(q, p) * a + v * (1.f / kA), false); }
+  typedef Pairs::Four Read;
+  __device__ Read read(int64_t q, int64_t p) const { return X.get(q, p); }
+  template <bool WHOLE>
+  __device__ void put(int64_t, int64_t q, int64_t p, const Read& x, const float4_t& v) const { to.put(q, p, x.value() * a + v * (1.f / kA), false); }
 };
 struct LastOut {  // the same into the caller's matrix
   Pairs X;
@@ -78,9 +92,12 @@ struct LastOut {  // the same into the caller's matrix
   void* out;
   int64_t ld, rows, cols;  // of X without its padding
   int type, flip;
-  __device__ void operator()(int64_t, int64_t q, int64_t p, const float4_t& v) const {
+  typedef Pairs::Four Read;
+  __device__ Read read(int64_t q, int64_t p) const { return X.get(q, p); }
+  template <bool WHOLE>
+  __device__ void put(int64_t, int64_t q, int64_t p, const Read& old, const float4_t& v) const {
     if (q >= rows) return;
-    const float4_t x = (X.get(q, p) * a + v * (1.f / kA)) * scale;
+    const float4_t x = (old.value() * a + v * (1.f / kA)) * scale;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (p + e >= cols) return;
@@ -93,7 +110,10 @@ struct LastOut {  // the same into the caller's matrix
 struct SumsPart {  // [parts][nq][np]
   float* part;
   int64_t nq, np;
-  __device__ void operator()(int64_t k, int64_t q, int64_t p, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * np + p) = v; }
+  typedef ProductNothing Read;
+  __device__ Read read(int64_t, int64_t) const { return {}; }
+  template <bool WHOLE>
+  __device__ void put(int64_t k, int64_t q, int64_t p, const Read&, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * np + p) = v; }
 };
 template <class Out>
 __global__ __launch_bounds__(kBlock) void sums_join_kernel(const float* part, int parts, int64_t nq, int64_t np, int lower, Out out) {
@@ -106,7 +126,7 @@ __global__ __launch_bounds__(kBlock) void sums_join_kernel(const float* part, in
     at += nq * np;
     v += *reinterpret_cast<const float4_t*>(at);
   }
-  out(0, q, p, v);
+  out.template put<false>(0, q, p, out.read(q, p), v);
 }
 
 // ---- the way in: the norm, X = G / |G|

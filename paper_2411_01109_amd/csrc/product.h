@@ -17,6 +17,8 @@
 // from LDS, and that is what bounds the large shape (256 x 256: 8 waves of 128 x 64, (128 + 64) 64 bytes a step for 32 products of 16 cycles).
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace hgnn {
@@ -318,19 +320,36 @@ __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs a, 
     if (S::kSubs == 1 && ++s >= steps) break;
     sub(s, S::kSubs - 1, p1s, p0s);
   }
+  // What the epilogue reads is asked for first, half of the block at a time: behind its stores every load would wait for them.
+  const auto finish = [&](auto whole) __attribute__((always_inline)) {  // whole: all of the tile exists, and nothing is asked about it
+    constexpr bool kWhole = decltype(whole)::value;
 #pragma unroll
-  for (int t = 0; t < S::TQ; ++t) {
-    const int64_t q = q0 + 16 * (wq * S::TQ + t) + i;
-    if (q >= a.nq) continue;
+    for (int half = 0; half < 2; ++half) {
+      typename Epilogue::Read read[HQ][S::TP];
+      const auto each = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < S::TP; ++u) {
-      const int64_t p = p0 + 16 * (wp * S::TP + u) + 4 * qq;
-      if (p >= a.np) continue;
-      if constexpr (S::NR == 2) epilogue(part, q, p, acc[0][t][u], acc[1][t][u]);
-      else epilogue(part, q, p, acc[0][t][u]);
+        for (int t = 0; t < HQ; ++t) {
+          const int64_t q = q0 + 16 * (wq * S::TQ + half * HQ + t) + i;
+#pragma unroll
+          for (int u = 0; u < S::TP; ++u) {
+            const int64_t p = p0 + 16 * (wp * S::TP + u) + 4 * qq;
+            if (kWhole || (q < a.nq && p < a.np)) f(q, p, t, u);
+          }
+        }
+      };
+      each([&](int64_t q, int64_t p, int t, int u) __attribute__((always_inline)) { read[t][u] = epilogue.read(q, p); });
+      each([&](int64_t q, int64_t p, int t, int u) __attribute__((always_inline)) {
+        const int line = half * HQ + t;
+        if constexpr (S::NR == 2) epilogue.template put<kWhole>(part, q, p, read[t][u], acc[0][line][u], acc[1][line][u]);
+        else epilogue.template put<kWhole>(part, q, p, read[t][u], acc[0][line][u]);
+      });
     }
-  }
+  };
+  if (q0 + S::BQ <= a.nq && p0 + S::BP <= a.np) finish(std::true_type());
+  else finish(std::false_type());
 }
+
+struct ProductNothing {};
 
 // tiles and workgroups of a product, and its launch
 template <class S>
