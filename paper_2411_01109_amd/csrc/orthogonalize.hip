@@ -17,7 +17,7 @@
 namespace hgnn {
 
 constexpr float kX = 2048.f, kA = 512.f;  // what X, and A and B, are stored times
-constexpr int kNormParts = 256;
+constexpr int kNormParts = 1024;
 
 __device__ __forceinline__ void split_value(float v, half_t& hi, half_t& lo) {
   hi = half_t(v);
@@ -136,70 +136,119 @@ struct OrthMatrix {
   int64_t rows, cols, ld, ldo;
   int type, out_type;
 };
-__device__ __forceinline__ double value_at(const OrthMatrix& m, int64_t r, int64_t c) {
-  return m.type == HGNN_F16 ? double(static_cast<const half_t*>(m.grad)[r * m.ld + c]) : double(static_cast<const float*>(m.grad)[r * m.ld + c]);
-}
-// sum over a workgroup of kBlock, on all threads
+// sum over a workgroup of N threads, on all threads
+template <int N = kBlock>
 __device__ __forceinline__ double block_sum(double v) {
-  __shared__ double lds[kBlock];
+  __shared__ double lds[N];
   lds[threadIdx.x] = v;
   __syncthreads();
-  for (int w = kBlock / 2; w > 0; w >>= 1) {
+  for (int w = N / 2; w > 0; w >>= 1) {
     if (int(threadIdx.x) < w) lds[threadIdx.x] += lds[threadIdx.x + w];
     __syncthreads();
   }
   return lds[0];
 }
-// the partial sums of squares, in 64 bits: no element's square is lost or overflows
-__global__ __launch_bounds__(kBlock) void orth_squares_kernel(OrthMatrix m, double* part) {
-  const int64_t all = m.rows * m.cols, step = int64_t(gridDim.x) * kBlock;
+// The sum of the squares of a share of a matrix, number `share` of `shares`, in 64 bits: no element's square is lost or overflows.  Pieces of eight elements, four
+// of them on their way at a time.
+template <class T>
+__device__ __forceinline__ double squares_of(const OrthMatrix& m, int share, int shares) {
+  const T* const g = static_cast<const T*>(m.grad);
+  const bool flat = m.ld == m.cols;  // one row of all elements
+  const int64_t rows = flat ? 1 : m.rows, cols = flat ? m.rows * m.cols : m.cols, each = (cols + 7) / 8, all = rows * each, extent = (rows - 1) * m.ld + cols;
+  const int64_t step = int64_t(shares) * blockDim.x;
   double s = 0.;
-  int64_t e = int64_t(blockIdx.x) * kBlock + threadIdx.x, r = e / m.cols, c = e - r * m.cols;
-  const int64_t dr = step / m.cols, dc = step - dr * m.cols;
-  for (; e < all; e += step) {
-    const double v = value_at(m, r, c);
-    s += v * v;
-    r += dr, c += dc;
-    if (c >= m.cols) c -= m.cols, ++r;
+  for (int64_t e = int64_t(share) * blockDim.x + threadIdx.x; e < all; e += 4 * step) {
+    RawPiece<T> x[4];
+    int left[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t at = e + u * step, r = flat ? 0 : at / each, c = 8 * (at - r * each);
+      left[u] = at < all ? int(min(cols - c, int64_t(8))) : 0;
+      x[u].v = 0;
+      if (left[u] > 0) x[u] = load_raw(g + r * m.ld + c, left[u], extent - (r * m.ld + c));
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double v = i < left[u] ? double(x[u].v[i]) : 0.;
+        s = fma(v, v, s);
+      }
   }
-  s = block_sum(s);
+  return s;
+}
+__device__ __forceinline__ double squares_of(const OrthMatrix& m, int share, int shares) {
+  return m.type == HGNN_F16 ? squares_of<half_t>(m, share, shares) : squares_of<float>(m, share, shares);
+}
+__global__ __launch_bounds__(kBlock) void orth_squares_kernel(OrthMatrix m, double* part) {
+  const double s = block_sum(squares_of(m, blockIdx.x, gridDim.x));
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 // 1 / |G|, or 0 where that is none
+__device__ __forceinline__ double inverse_root(double s) { return s > 0. && s < double(INFINITY) ? 1. / sqrt(s) : 0.; }
 __device__ __forceinline__ double inverse_norm(const double* part, int parts) {
   double s = 0.;
   for (int k = threadIdx.x; k < parts; k += kBlock) s += part[k];
   s = block_sum(s);
-  return s > 0. && s < double(INFINITY) ? 1. / sqrt(s) : 0.;
+  return inverse_root(s);
 }
-constexpr int kTurn = 32;  // a workgroup takes 32 x 32 elements, through LDS where they change sides
-// X (of hq x hp with its padding) at kX times its values; with `last` the scaled result itself
-__global__ __launch_bounds__(kBlock) void orth_begin_kernel(OrthMatrix m, int flip, const double* part, int parts, Pairs X, int last, float scale) {
+// 64 x 64 elements of X = G / |G| (of its transpose with `flip`) at kX times their values, zeros in the padding (hq x hp in all), by N threads; with `last` the scaled
+// elements of the result in their place.  Through LDS, so that lines are read and written along themselves in pieces of eight either way.
+constexpr int kTurn = 64;
+template <class T>
+__device__ __forceinline__ void load_turn(const OrthMatrix& m, int64_t r, int64_t c, double f, float (&v)[8]) {
+  const T* const g = static_cast<const T*>(m.grad) + r * m.ld + c;
+  const int left = r < m.rows && c < m.cols ? int(min(m.cols - c, int64_t(8))) : 0;
+  RawPiece<T> x;
+  x.v = 0;
+  if (left > 0) x = load_raw(g, left, (m.rows - 1 - r) * m.ld + m.cols - c);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < left && f > 0. ? float(double(x.v[e]) * f) : 0.f;
+}
+template <int N>
+__device__ __forceinline__ void orth_turn(const OrthMatrix& m, int flip, double inv, int64_t q0, int64_t p0, const Pairs& X, int64_t hq, int64_t hp, int last, float scale) {
   __shared__ float tile[kTurn][kTurn + 1];
-  const double inv = inverse_norm(part, parts);
-  const int64_t r0 = int64_t(flip ? blockIdx.x : blockIdx.y) * kTurn, c0 = int64_t(flip ? blockIdx.y : blockIdx.x) * kTurn;
-  const int x = threadIdx.x % kTurn, y = threadIdx.x / kTurn;
-  for (int i = y; i < kTurn; i += kBlock / kTurn) {
-    const int64_t r = r0 + i, c = c0 + x;
-    float v = 0.f;
-    if (r < m.rows && c < m.cols && inv > 0.) v = float(value_at(m, r, c) * inv * (last ? double(scale) : double(kX)));
-    if (last) {
-      if (r < m.rows && c < m.cols) {
-        if (m.out_type == HGNN_F16) static_cast<half_t*>(m.out)[r * m.ldo + c] = half_t(v);
-        else static_cast<float*>(m.out)[r * m.ldo + c] = v;
+  const int64_t r0 = flip ? p0 : q0, c0 = flip ? q0 : p0;
+#pragma unroll
+  for (int e = threadIdx.x; e < kTurn * 8; e += N) {
+    const int r = e / 8, c = 8 * (e % 8);
+    float v[8];
+    if (m.type == HGNN_F16) load_turn<half_t>(m, r0 + r, c0 + c, inv * double(kX), v);
+    else load_turn<float>(m, r0 + r, c0 + c, inv * double(kX), v);
+    if (last && r0 + r < m.rows) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float y = v[k] * (scale / kX);
+        if (c0 + c + k >= m.cols) break;
+        const int64_t at = (r0 + r) * m.ldo + c0 + c + k;
+        if (m.out_type == HGNN_F16) static_cast<half_t*>(m.out)[at] = half_t(y);
+        else static_cast<float*>(m.out)[at] = y;
       }
     }
-    tile[i][x] = v;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) tile[r][c + k] = v[k];
   }
   if (last) return;
   __syncthreads();
-  for (int i = y; i < kTurn; i += kBlock / kTurn) {
-    const int64_t q = int64_t(blockIdx.y) * kTurn + i, p = int64_t(blockIdx.x) * kTurn + x;
-    half_t hi, lo;
-    split_value(flip ? tile[x][i] : tile[i][x], hi, lo);
-    half_t* const to = X.place(q, p);
-    to[0] = hi, to[32] = lo;
+#pragma unroll
+  for (int e = threadIdx.x; e < kTurn * 8; e += N) {
+    const int q = e / 8, p = 8 * (e % 8);
+    if (q0 + q >= hq || p0 + p >= hp) continue;
+    half8_t h, l;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      half_t a, b;
+      split_value(flip ? tile[p + k][q] : tile[q][p + k], a, b);
+      h[k] = a, l[k] = b;
+    }
+    half_t* const to = X.place(q0 + q, p0 + p);
+    *reinterpret_cast<half8_t*>(to) = h;
+    *reinterpret_cast<half8_t*>(to + 32) = l;
   }
+}
+__global__ __launch_bounds__(kBlock) void orth_begin_kernel(OrthMatrix m, int flip, const double* part, int parts, Pairs X, int64_t hq, int64_t hp, int last, float scale) {
+  const double inv = inverse_norm(part, parts);
+  orth_turn<kBlock>(m, flip, inv, int64_t(blockIdx.y) * kTurn, int64_t(blockIdx.x) * kTurn, X, hq, hp, last, scale);
 }
 
 static int64_t up32(int64_t n) { return (n + 31) / 32 * 32; }
@@ -221,7 +270,8 @@ static OrthSplit orth_split(int64_t nq, int64_t np, int64_t K, bool lower) {
   };
   OrthSplit s;
   s.tile = tiles(128) < kOrthFull / 4 || nq <= 64 ? 64 : 128;
-  const int64_t t = tiles(s.tile), parts = t >= kOrthFull ? 1 : std::min(ceil_div(2 * kOrthFull, t), ceil_div(K, 256));
+  // a part of 1024 steps at least: sums that go through memory and another launch cost about as much
+  const int64_t t = tiles(s.tile), parts = t >= kOrthFull ? 1 : std::min(ceil_div(2 * kOrthFull, t), ceil_div(K, 1024));
   s.part = std::max<int64_t>(32, up32(ceil_div(K, std::max<int64_t>(parts, 1))));
   s.parts = int(std::max<int64_t>(1, ceil_div(K, s.part)));
   return s;
@@ -242,6 +292,176 @@ static OrthSizes orth_sizes(int64_t rows, int64_t cols) {
   z.part = std::max({part(z.gram, z.m, z.m), part(z.square, z.m, z.m), part(z.step, z.m, z.k)});
   z.bytes = kNormParts * sizeof(double) + 4 * z.x + 4 * z.a + z.part;
   return z;
+}
+
+// ---- matrices of at most 64 x 1024: a launch for a step of all of them.  A workgroup owns 64 columns of X, forms A and B by itself (each of a matrix's workgroups
+// the same: their sums over up to 1024 columns out of the L2 cost less than two launches more) and multiplies its columns.  X is padded to 64 rows and whole
+// 64 columns.  Four waves, 32 x 32 of the 64 x 64 each; A and B stand in LDS as the products read them.
+constexpr int kNarrowM = 64, kNarrowK = 1024, kNarrowMany = 24, kNarrowRing = 6, kNarrowTile = 64 * 128;
+struct NarrowMatrix {
+  OrthMatrix m;
+  half_t *X, *next;
+  int32_t first;  // workgroup
+  int32_t k;      // padded columns
+  float scale;
+  int32_t flip;
+};
+struct NarrowArgs {
+  NarrowMatrix m[kNarrowMany];
+  int count;
+  float a, b, c;
+  int last;
+};
+__device__ __forceinline__ const NarrowMatrix& narrow_matrix(const NarrowArgs& a, int block) {
+  int i = 0;
+  while (i + 1 < a.count && a.m[i + 1].first <= block) ++i;  // uniform
+  return a.m[i];
+}
+// the norm (each of a matrix's workgroups the same) and X = G / |G|; without steps the result
+__global__ __launch_bounds__(1024) void narrow_begin_kernel(NarrowArgs a) {
+  const NarrowMatrix& n = narrow_matrix(a, blockIdx.x);
+  const double inv = inverse_root(block_sum<1024>(squares_of(n.m, 0, 1)));
+  orth_turn<1024>(n.m, n.flip, inv, 0, 64 * int64_t(int(blockIdx.x) - n.first), Pairs{n.X, 2 * int64_t(n.k)}, kNarrowM, n.k, a.last, n.scale);
+}
+// four values (q, p .. p + 3) of a 64 x 64 matrix to where ProductReads<false, true> finds them
+__device__ __forceinline__ void narrow_put(unsigned char* at, int q, int p, const float4_t& v) {
+  half4_t h, l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    half_t a, b;
+    split_value(v[e], a, b);
+    h[e] = a, l[e] = b;
+  }
+  unsigned char* const line = at + (p >> 5) * kNarrowTile + q * 128 + (p & 4) * 2;
+  const int piece = (p & 31) >> 3, turn = (q & 15) >> 1;
+  *reinterpret_cast<half4_t*>(line + (piece ^ turn) * 16) = h;
+  *reinterpret_cast<half4_t*>(line + ((piece + 4) ^ turn) * 16) = l;
+}
+template <class Q, class P>
+__device__ __forceinline__ void narrow_multiply(float4_t (&acc)[2][2], const Q& q, const unsigned char* qs, const P& p, const unsigned char* ps) {
+  half8_t a[2][2], b[2][2];  // [part][16 items]
+#pragma unroll
+  for (int o = 0; o < 2; ++o)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) a[o][t] = q.get(qs, t, o), b[o][t] = p.get(ps, t, o);
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][u], a[0][t], acc[t][u], 0, 0, 0);
+      acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][u], a[1][t], acc[t][u], 0, 0, 0);
+      acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][u], a[0][t], acc[t][u], 0, 0, 0);
+    }
+}
+__global__ __launch_bounds__(kBlock) void narrow_step_kernel(NarrowArgs a) {
+  extern __shared__ __align__(1024) unsigned char lds[];
+  unsigned char *const columns = lds + kNarrowRing * kNarrowTile, *const gram = columns + 2 * kNarrowTile, *const poly = gram + 2 * kNarrowTile;
+  const NarrowMatrix& n = narrow_matrix(a, blockIdx.x);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wq = wave >> 1, wp = wave & 1, i = lane & 15, qq = lane >> 4;
+  const int k = n.k, steps = k / 32, p0 = 64 * (int(blockIdx.x) - n.first);
+  const int64_t ld = 2 * int64_t(k);
+  const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) unsigned char*)lds)) + wave * 1024;
+  const half_t* const x = n.X;
+  {  // the workgroup's own columns, 64 steps
+    ProductLoads<2, true> own;
+    product_loads<2, true, true, kWavesPerBlock>(own, x, x, ld, p0, k, 0, wave, lane, 8);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_to_lds(own.base[j] + s * own.inc, own.off[j], lds0 + (kNarrowRing + s) * kNarrowTile + j * 4096);
+  }
+  ProductLoads<2, false> lines;
+  product_loads<2, false, true, kWavesPerBlock>(lines, x, x, ld, 0, kNarrowM, 0, wave, lane, 8);
+  uint32_t to = lds0;
+  const auto ask = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) load_to_lds(lines.base[j], lines.off[j], to + j * 4096), lines.base[j] += lines.inc;
+    to += kNarrowTile;
+    if (to >= lds0 + kNarrowRing * kNarrowTile) to -= kNarrowRing * kNarrowTile;
+  };
+  const ProductReads<false, true, 2> read_q(2 * wq, lane), read_p(2 * wp, lane);
+  const ProductReads<true, true, 2> read_columns(2 * wp, lane);
+  const float4_t none = {0.f, 0.f, 0.f, 0.f};
+  float4_t A[2][2] = {{none, none}, {none, none}}, B[2][2] = {{none, none}, {none, none}};
+  int asked = 0;
+  for (; asked < kNarrowRing - 1 && asked < steps; ++asked) ask();
+  const unsigned char* stage = lds;
+  for (int s = 0; s < steps; ++s) {
+    const int behind = asked - 1 - s;
+    if (behind >= 4) product_wait<8>();
+    else if (behind == 3) product_wait<6>();
+    else if (behind == 2) product_wait<4>();
+    else if (behind == 1) product_wait<2>();
+    else product_wait<0>();
+    if (asked < steps) ask(), ++asked;  // into the place of the stage before, which all waves have left
+    narrow_multiply(A, read_q, stage, read_p, stage);
+    stage += kNarrowTile;
+    if (stage >= columns) stage = lds;
+  }
+  const auto each = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) f(16 * (2 * wq + t) + i, 16 * (2 * wp + u) + 4 * qq, t, u);
+  };
+  each([&](int q, int p, int t, int u) __attribute__((always_inline)) {
+    A[t][u] *= kA / (kX * kX);
+    narrow_put(gram, q, p, A[t][u]);
+  });
+  __syncthreads();
+  if (a.c != 0.f) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) narrow_multiply(B, read_q, gram + s * kNarrowTile, read_p, gram + s * kNarrowTile);
+  }
+  each([&](int q, int p, int t, int u) __attribute__((always_inline)) { narrow_put(poly, q, p, A[t][u] * a.b + B[t][u] * (a.c / kA)); });
+  __syncthreads();
+  float4_t Y[2][2] = {{none, none}, {none, none}};
+#pragma unroll
+  for (int s = 0; s < 2; ++s) narrow_multiply(Y, read_q, poly + s * kNarrowTile, read_columns, columns + s * kNarrowTile);
+  const Pairs X{n.X, ld};
+  if (a.last) {
+    const LastOut out{X, a.a, n.scale / kX, n.m.out, n.m.ldo, n.flip ? n.m.cols : n.m.rows, n.flip ? n.m.rows : n.m.cols, n.m.out_type, n.flip};
+    each([&](int q, int p, int t, int u) __attribute__((always_inline)) { out.put<false>(0, q, p0 + p, out.read(q, p0 + p), Y[t][u]); });
+  } else {
+    const StepOut out{Pairs{n.next, ld}, X, a.a};
+    each([&](int q, int p, int t, int u) __attribute__((always_inline)) { out.put<false>(0, q, p0 + p, out.read(q, p0 + p), Y[t][u]); });
+  }
+}
+static bool is_narrow(int64_t rows, int64_t cols) { return std::min(rows, cols) <= kNarrowM && std::max(rows, cols) <= kNarrowK; }
+static int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
+static size_t narrow_bytes(int64_t rows, int64_t cols) { return 2 * size_t(kNarrowM) * size_t(up64(std::max(rows, cols))) * 4; }
+
+// all narrow ones of a list; their X lie one behind the other at ws
+static hgnn_status orth_narrow(const char* who, int32_t count, const hgnn_grad* grads, int32_t steps, const float* coef, const float* scales, char* ws, hipStream_t s) {
+  static uint64_t told = 0;
+  constexpr int kBytes = (kNarrowRing + 6) * kNarrowTile;
+  const hgnn_status st = product_lds(reinterpret_cast<const void*>(&narrow_step_kernel), kBytes, &told);
+  if (st != HGNN_OK) return st;
+  for (int i = 0; i < count;) {
+    NarrowArgs a{};
+    int64_t blocks = 0;
+    for (; i < count && a.count < kNarrowMany; ++i) {
+      const hgnn_grad& g = grads[i];
+      if (g.rows == 0 || g.cols == 0 || !is_narrow(g.rows, g.cols)) continue;
+      NarrowMatrix& n = a.m[a.count++];
+      n.m = OrthMatrix{g.grad, g.out ? g.out : const_cast<void*>(g.grad), g.rows, g.cols, g.ld, g.out ? g.ld_out : g.ld, int(g.type), int(g.out ? g.out_type : g.type)};
+      n.flip = g.rows > g.cols, n.k = int32_t(up64(std::max(g.rows, g.cols))), n.scale = scales ? scales[i] : 1.f, n.first = int32_t(blocks);
+      blocks += n.k / 64;
+      n.X = reinterpret_cast<half_t*>(ws), n.next = n.X + 2 * kNarrowM * int64_t(n.k);
+      ws += narrow_bytes(g.rows, g.cols);
+    }
+    if (a.count == 0) break;
+    a.last = steps == 0;
+    narrow_begin_kernel<<<unsigned(blocks), 1024, 0, s>>>(a);
+    HGNN_LAUNCH_CHECK("narrow_begin_kernel");
+    for (int k = 0; k < steps; ++k) {
+      a.a = coef[3 * k], a.b = coef[3 * k + 1], a.c = coef[3 * k + 2], a.last = k + 1 == steps;
+      narrow_step_kernel<<<unsigned(blocks), kBlock, kBytes, s>>>(a);
+      HGNN_LAUNCH_CHECK("narrow_step_kernel");
+      for (int j = 0; j < a.count; ++j) std::swap(a.m[j].X, a.m[j].next);
+    }
+  }
+  return HGNN_OK;
 }
 
 template <bool PCOL, class Out>
@@ -273,10 +493,10 @@ static hgnn_status orth_matrix(const char* who, const hgnn_grad& g, int32_t step
   const Pairs A = pairs(z.m, z.m), B = pairs(z.m, z.m);
   float* const part = reinterpret_cast<float*>(at);
   const OrthMatrix m{g.grad, g.out ? g.out : const_cast<void*>(g.grad), g.rows, g.cols, g.ld, g.out ? g.ld_out : g.ld, int(g.type), int(g.out ? g.out_type : g.type)};
-  const unsigned parts = unsigned(std::min<int64_t>(kNormParts, ceil_div(g.rows * g.cols, 4 * kBlock)));
+  const unsigned parts = unsigned(std::min<int64_t>(kNormParts, ceil_div(g.rows * g.cols, 32 * kBlock)));
   orth_squares_kernel<<<parts, kBlock, 0, s>>>(m, squares);
   HGNN_LAUNCH_CHECK("orth_squares_kernel");
-  orth_begin_kernel<<<dim3(unsigned(z.k / kTurn), unsigned(z.m / kTurn)), kBlock, 0, s>>>(m, z.flip, squares, int(parts), X, steps == 0, scale);
+  orth_begin_kernel<<<dim3(unsigned(ceil_div(z.k, kTurn)), unsigned(ceil_div(z.m, kTurn))), kBlock, 0, s>>>(m, z.flip, squares, int(parts), X, z.m, z.k, steps == 0, scale);
   HGNN_LAUNCH_CHECK("orth_begin_kernel");
   for (int i = 0; i < steps; ++i) {
     const float a = coef[3 * i], b = coef[3 * i + 1], c = coef[3 * i + 2];
@@ -342,13 +562,15 @@ using namespace hgnn;
 extern "C" {
 
 size_t hgnn_orthogonalize_workspace(int32_t count, const hgnn_grad* grads) {
-  size_t most = 0;
+  size_t most = 0, narrow = 0;
   for (int i = 0; grads && i < count; ++i) {
     const hgnn_grad& g = grads[i];
     if (g.rows < 0 || g.cols < 0 || g.rows > 65536 || g.cols > 65536) return 0;
-    if (g.rows > 0 && g.cols > 0) most = std::max(most, orth_sizes(g.rows, g.cols).bytes);
+    if (g.rows == 0 || g.cols == 0) continue;
+    if (is_narrow(g.rows, g.cols)) narrow += narrow_bytes(g.rows, g.cols);
+    else most = std::max(most, orth_sizes(g.rows, g.cols).bytes);
   }
-  return most;
+  return std::max(narrow, most);  // the narrow ones are done before the others begin
 }
 
 hgnn_status hgnn_orthogonalize(int32_t count, const hgnn_grad* grads, int32_t steps, const float* coef, const float* scales, void* workspace, size_t workspace_bytes,
@@ -371,8 +593,9 @@ hgnn_status hgnn_orthogonalize(int32_t count, const hgnn_grad* grads, int32_t st
   const size_t need = hgnn_orthogonalize_workspace(count, grads);
   HGNN_REQUIRE(need == 0 || (workspace && workspace_bytes >= need && aligned16(workspace)), HGNN_EINVAL,
                "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_orthogonalize_workspace)", who, workspace_bytes, need);
+  st = orth_narrow(who, count, grads, steps, coef, scales, static_cast<char*>(workspace), static_cast<hipStream_t>(stream));
   for (int i = 0; i < count && st == HGNN_OK; ++i)
-    if (grads[i].rows > 0 && grads[i].cols > 0)
+    if (grads[i].rows > 0 && grads[i].cols > 0 && !is_narrow(grads[i].rows, grads[i].cols))
       st = orth_matrix(who, grads[i], steps, coef, scales ? scales[i] : 1.f, static_cast<char*>(workspace), static_cast<hipStream_t>(stream));
   return st;
 }

@@ -358,19 +358,23 @@ inline void product_tiles(ProductArgs& a) {
   a.tiles_p = int32_t(ceil_div(a.np, S::BP));
   a.tiles = a.lower ? lines * (lines + 1) / 2 : lines * a.tiles_p;
 }
+// beyond 64 KB of dynamic LDS the runtime wants to be told, once for a kernel and a device (told: a bit a device; two threads write the same at worst)
+inline hgnn_status product_lds(const void* kernel, int bytes, uint64_t* told) {
+  if (bytes <= 65536) return HGNN_OK;
+  int dev = 0;
+  HGNN_HIP(hipGetDevice(&dev));
+  if (dev < 64 && (__atomic_load_n(told, __ATOMIC_ACQUIRE) >> dev & 1)) return HGNN_OK;
+  HGNN_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  if (dev < 64) __atomic_fetch_or(told, uint64_t(1) << dev, __ATOMIC_RELEASE);
+  return HGNN_OK;
+}
 template <class S, class Epilogue>
 inline hgnn_status product(const char* who, ProductArgs& a, const Epilogue& e, hipStream_t s) {
   product_tiles<S>(a);
   HGNN_REQUIRE(a.tiles * a.parts <= 0x7ffffe, HGNN_EUNSUPPORTED, "%s: grid too large", who);
-  if (S::kLds > 65536) {
-    int dev = 0;
-    HGNN_HIP(hipGetDevice(&dev));
-    static uint64_t told = 0;  // devices, a bit each: the same value is written again at worst
-    if (dev >= 64 || !(__atomic_load_n(&told, __ATOMIC_ACQUIRE) >> dev & 1)) {
-      HGNN_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&product_kernel<S, Epilogue>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds));
-      if (dev < 64) __atomic_fetch_or(&told, uint64_t(1) << dev, __ATOMIC_RELEASE);
-    }
-  }
+  static uint64_t told = 0;
+  const hgnn_status st = product_lds(reinterpret_cast<const void*>(&product_kernel<S, Epilogue>), S::kLds, &told);
+  if (st != HGNN_OK) return st;
   product_kernel<S, Epilogue><<<dim3(unsigned(a.tiles * a.parts)), S::kThreads, S::kLds, s>>>(a, e);
   HGNN_LAUNCH_CHECK("product_kernel");
   return HGNN_OK;
