@@ -29,6 +29,7 @@ struct BlockArgs {
   int64_t ldh;
   half_t* Z;
   int64_t ldz;
+  int past;  // 1: H (dR), 2: Z (dY)
 };
 struct BlockGradArgs : BlockArgs {
   const void* dH;
@@ -102,27 +103,69 @@ struct Eight {
 template <class S, int P>
 __device__ __forceinline__ int col_of(int p) { return 8 * (S::lane() + p * S::kLanes); }
 
-// of row `row` of n rows; nothing behind the tensor is read
-template <class T>
-__device__ __forceinline__ Eight load_eight(const T* x0, int64_t ld, int64_t row, int64_t n, int col, int F) {
-  Eight r;
-  const int left = F - col;
-  const T* const at = x0 + row * ld + col;
+// Eight elements of a row as they are in memory, `left` of them the row's; zeros behind the row and for rows that do not exist, which then stay zeros through all that
+// follows and add nothing anywhere.  after(): the elements from here to the tensor's end, behind which nothing is read.
+template <class T, class After>
+__device__ __forceinline__ RawPiece<T> fetch_eight(const T* at, int left, After&& after) {
   RawPiece<T> x;
   x.v = 0;
   if (left >= 8) x = load_raw(at);
-  else if (left > 0) x = load_raw(at, left, (n - 1 - row) * ld + left);
+  else if (left > 0) x = load_raw(at, left, after());  // with what is behind the row: eight_of takes that off, once the piece is there
+  return x;
+}
+// a lane's place in a tensor, which moves with the rows that its workgroup takes
+template <class T>
+struct Place {
+  T* at;
+  int64_t ld, step;
+  __device__ __forceinline__ Place(const void* base, int64_t ld_, int64_t row, int64_t rows, int col)
+      : at(static_cast<T*>(const_cast<void*>(base)) + (base ? row * ld_ + col : 0)), ld(ld_), step(base ? rows * ld_ : 0) {}
+  __device__ __forceinline__ void move() { at += step; }
+  __device__ __forceinline__ RawPiece<T> fetch(int64_t row, int64_t n, int left) const {
+    return fetch_eight(at, row < n ? left : 0, [&] { return (n - 1 - row) * ld + left; });
+  }
+};
+template <class T>
+__device__ __forceinline__ Eight eight_of(const RawPiece<T>& x, int left) {
+  Eight r;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) r.v[i] = i < left ? float(x.v[i]) : 0.f;
+  for (int i = 0; i < 8; ++i) r.v[i] = float(x.v[i]);
+  if (left > 0 && left < 8) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) r.v[i] = i < left ? r.v[i] : 0.f;
+  }
   return r;
 }
+// x - v inside the row; what is behind it stays zero
+__device__ __forceinline__ void less(Eight& x, float v, int left) {
+  v = left > 0 ? v : 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x.v[i] -= v;
+  if (left > 0 && left < 8) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) x.v[i] = i < left ? x.v[i] : 0.f;
+  }
+}
+// past: whole lines past the caches (kPastBytes)
 template <class T>
-__device__ __forceinline__ void store_eight(T* row, int col, int F, const Eight& x) {
-  if (col >= F) return;
-  store_piece(row + col, F - col, Piece{{x.v[0], x.v[1], x.v[2], x.v[3], x.v[4], x.v[5], x.v[6], x.v[7]}});
+__device__ __forceinline__ void store_eight(T* at, int left, const Eight& x, bool past = false) {
+  if (left <= 0) return;
+  if (past) {  // uniform; F is a multiple of eight
+    if constexpr (sizeof(T) == 2) {
+      half8_t h;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] = half_t(x.v[i]);
+      __builtin_nontemporal_store(h, reinterpret_cast<half8_t*>(at));
+    } else {
+      __builtin_nontemporal_store(float4_t{x.v[0], x.v[1], x.v[2], x.v[3]}, reinterpret_cast<float4_t*>(at));
+      __builtin_nontemporal_store(float4_t{x.v[4], x.v[5], x.v[6], x.v[7]}, reinterpret_cast<float4_t*>(at + 4));
+    }
+    return;
+  }
+  store_piece(at, left, Piece{{x.v[0], x.v[1], x.v[2], x.v[3], x.v[4], x.v[5], x.v[6], x.v[7]}});
 }
 __device__ __forceinline__ Eight weights_at(const float* w, int col, int F, float otherwise) {
-  if (w) return load_eight(w, 0, 0, 1, col, F);
+  if (w) return eight_of(fetch_eight(w + col, F - col, [&] { return int64_t(F - col); }), F - col);
   Eight r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.v[i] = otherwise;
@@ -141,18 +184,14 @@ __device__ __forceinline__ float normed(Eight (&x)[P], int kind, int F, float ep
       for (int i = 0; i < 8; ++i) s += x[p].v[i];
     const float mean = S::sum(s, lds) * inv;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int left = F - col_of<S, P>(p);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[p].v[i] = i < left ? x[p].v[i] - mean : 0.f;
-    }
+    for (int p = 0; p < P; ++p) less(x[p], mean, F - col_of<S, P>(p));
   }
   float q = 0.f;
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
     for (int i = 0; i < 8; ++i) q = fmaf(x[p].v[i], x[p].v[i], q);
-  const float r = 1.f / sqrtf(S::sum(q, lds) * inv + eps);
+  const float r = __builtin_amdgcn_rsqf(S::sum(q, lds) * inv + eps);
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
@@ -160,29 +199,29 @@ __device__ __forceinline__ float normed(Eight (&x)[P], int kind, int F, float ep
   return r;
 }
 
-// N^T(d) in the place of d: what comes back through a norm whose output was xh w + c
-template <class S, int P>
-__device__ __forceinline__ void through(Eight (&d)[P], const Eight (&xh)[P], const Eight (&w)[P], float r, int kind, int F, float* lds) {
+// to + N^T(d) in the place of `to`: what comes back through a norm whose output was xh w + c
+template <class S, int P, class Weight>
+__device__ __forceinline__ void through(Eight (&to)[P], Eight (&d)[P], const Eight (&xh)[P], Weight&& weight, float r, int kind, int F, float* lds) {
   float su = 0.f, sx = 0.f;
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+  for (int p = 0; p < P; ++p) {
+    const Eight w = weight(p);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      d[p].v[i] *= w[p].v[i];
+      d[p].v[i] *= w.v[i];
       su += d[p].v[i];
       sx = fmaf(d[p].v[i], xh[p].v[i], sx);
     }
-  if (kind == HGNN_NORM_LAYER) {
-    S::sum(su, sx, lds);
-  } else {
-    sx = S::sum(sx, lds), su = 0.f;
   }
-  const float inv = 1.f / float(F);
-  su *= inv, sx *= inv;
+  if (kind == HGNN_NORM_LAYER) S::sum(su, sx, lds);
+  else sx = S::sum(sx, lds);
+  sx *= r / float(F), su *= r / float(F);
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+  for (int p = 0; p < P; ++p) {
+    if (kind == HGNN_NORM_LAYER) less(to[p], su, F - col_of<S, P>(p));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) d[p].v[i] = r * (fmaf(-xh[p].v[i], sx, d[p].v[i]) - su);
+    for (int i = 0; i < 8; ++i) to[p].v[i] = fmaf(d[p].v[i], r, fmaf(-xh[p].v[i], sx, to[p].v[i]));
+  }
 }
 
 template <class T, int L, int P, int W>
@@ -199,40 +238,34 @@ __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_kernel(
     }
   };
   if (S::kKeep) weights();
-  for (int64_t row0 = int64_t(blockIdx.x) * S::kRows; row0 < a.n; row0 += int64_t(gridDim.x) * S::kRows) {  // all waves alike: the sums meet
+  // (asking for the next rows ahead, as the gradients do, costs registers and with them waves: 2.4 M x 128 512 -> 567 us)
+  static_assert(P == 1, "pieces");
+  const int64_t first = int64_t(blockIdx.x) * S::kRows + S::row(), stride = int64_t(gridDim.x) * S::kRows;
+  const int col = col_of<S, P>(0), left = a.F - col;
+  Place<half_t> Y(a.Y, a.ldy, first, stride, col), G(a.gate_rows, a.ld_gate, first, stride, col), Z(a.Z, a.ldz, first, stride, col);
+  Place<T> R(a.R, a.ldr, first, stride, col), H(a.H, a.ldh, first, stride, col);
+  for (int64_t row = first; row - S::row() < a.n; row += stride) {  // all waves alike: the sums meet
     if (!S::kKeep) weights();
-    const int64_t row = min(row0 + S::row(), a.n - 1);
-    const bool live = row0 + S::row() < a.n;  // else the last row once more, which is not stored
-    Eight b[P], h[P];
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int c = col_of<S, P>(p);
-      b[p] = a.Y ? load_eight(a.Y, a.ldy, row, a.n, c, a.F) : Eight{};
-      h[p] = a.R ? load_eight(static_cast<const T*>(a.R), a.ldr, row, a.n, c, a.F) : Eight{};
-      if (a.gate_rows) gate[p] = load_eight(a.gate_rows, a.ld_gate, row, a.n, c, a.F);
-    }
+    const int mine = row < a.n ? left : 0;
+    Eight b[1], h[1];
+    b[0] = a.Y ? eight_of(Y.fetch(row, a.n, left), left) : Eight{};
+    h[0] = a.R ? eight_of(R.fetch(row, a.n, left), left) : Eight{};
+    if (a.gate_rows) gate[0] = eight_of(G.fetch(row, a.n, left), left);
     if (a.post != HGNN_NORM_NONE) {
       normed<S, P>(b, a.post, a.F, a.eps, lds);
 #pragma unroll
-      for (int p = 0; p < P; ++p)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b[p].v[i] = fmaf(b[p].v[i], post_w[p].v[i], post_b[p].v[i]);
+      for (int i = 0; i < 8; ++i) b[0].v[i] = fmaf(b[0].v[i], post_w[0].v[i], post_b[0].v[i]);
     }
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int left = a.F - col_of<S, P>(p);
+    for (int i = 0; i < 8; ++i) h[0].v[i] = float(T(fmaf(gate[0].v[i], b[0].v[i], a.alpha * h[0].v[i])));  // as it is stored
+    if (a.H) store_eight(H.at, mine, h[0], a.past & 1);
+    if (a.pre != HGNN_NORM_NONE) {
+      normed<S, P>(h, a.pre, a.F, a.eps, lds);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[p].v[i] = i < left ? float(T(fmaf(gate[p].v[i], b[p].v[i], a.alpha * h[p].v[i]))) : 0.f;  // as it is stored
-      if (a.H && live) store_eight(static_cast<T*>(a.H) + row * a.ldh, col_of<S, P>(p), a.F, h[p]);
+      for (int i = 0; i < 8; ++i) h[0].v[i] = fmaf(h[0].v[i], pre_w[0].v[i], pre_b[0].v[i]);
+      store_eight(Z.at, mine, h[0], a.past & 2);
     }
-    if (a.pre == HGNN_NORM_NONE) continue;
-    normed<S, P>(h, a.pre, a.F, a.eps, lds);
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[p].v[i] = fmaf(h[p].v[i], pre_w[p].v[i], pre_b[p].v[i]);
-      if (live) store_eight(a.Z + row * a.ldz, col_of<S, P>(p), a.F, h[p]);
-    }
+    Y.move(), R.move(), G.move(), H.move(), Z.move();
   }
 }
 
@@ -243,92 +276,99 @@ __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_grad_ke
   typedef RowShape<L, P, W> S;
   __shared__ float lds[2 * W];
   __shared__ float sums[S::kRows > 1 ? S::kThreads * 9 : 1];
-  Eight post_w[P], post_b[P], gate[P], pre_w[P], total[kVectors][P] = {};
-  const auto weights = [&]() __attribute__((always_inline)) {
+  Eight gate[P], total[kVectors][P] = {};
+  // Weights stand in LDS: as registers of every lane they would cost a wave of three (153 registers, 2.4 M x 128 911 us).
+  enum { kAtPreW, kAtPostW, kAtPostB, kAtGate, kWeights };
+  __shared__ __align__(16) float s_weights[kWeights][P * S::kLanes * 8];
+  if (S::row() == 0) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = col_of<S, P>(p);
-      post_w[p] = weights_at(a.post_w, c, a.F, 1.f), post_b[p] = weights_at(a.post_b, c, a.F, 0.f), gate[p] = weights_at(a.gate, c, a.F, 1.f);
-      pre_w[p] = weights_at(a.pre_w, c, a.F, 1.f);
+      *reinterpret_cast<Eight*>(&s_weights[kAtPreW][c]) = weights_at(a.pre_w, c, a.F, 1.f);
+      *reinterpret_cast<Eight*>(&s_weights[kAtPostW][c]) = weights_at(a.post_w, c, a.F, 1.f);
+      *reinterpret_cast<Eight*>(&s_weights[kAtPostB][c]) = weights_at(a.post_b, c, a.F, 0.f);
+      *reinterpret_cast<Eight*>(&s_weights[kAtGate][c]) = weights_at(a.gate, c, a.F, 1.f);
     }
+  }
+  __syncthreads();
+  const auto weight = [&](int k, int p) __attribute__((always_inline)) {
+    const float4_t* const at = reinterpret_cast<const float4_t*>(&s_weights[k][col_of<S, P>(p)]);
+    const float4_t lo = at[0], hi = at[1];
+    return Eight{{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
   };
-  if (S::kKeep) weights();
-  for (int64_t row0 = int64_t(blockIdx.x) * S::kRows; row0 < a.n; row0 += int64_t(gridDim.x) * S::kRows) {
-    if (!S::kKeep) weights();
-    const int64_t row = min(row0 + S::row(), a.n - 1);
-    const bool live = row0 + S::row() < a.n;  // else the last row once more, which is not stored and adds nothing
-    Eight e[P], h[P], d[P], b[P];
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int c = col_of<S, P>(p);
-      e[p] = a.dH ? load_eight(static_cast<const T*>(a.dH), a.lddh, row, a.n, c, a.F) : Eight{};
-      if (a.pre != HGNN_NORM_NONE) {
-        h[p] = load_eight(static_cast<const T*>(a.H), a.ldh, row, a.n, c, a.F);
-        d[p] = load_eight(a.dZ, a.lddz, row, a.n, c, a.F);
-      }
-      if (a.Y) b[p] = load_eight(a.Y, a.ldy, row, a.n, c, a.F);
-      if (a.gate_rows) gate[p] = load_eight(a.gate_rows, a.ld_gate, row, a.n, c, a.F);
-    }
-    if (a.pre != HGNN_NORM_NONE) {
+  static_assert(P == 1, "pieces");
+  const int64_t first = int64_t(blockIdx.x) * S::kRows + S::row(), stride = int64_t(gridDim.x) * S::kRows;
+  const int col = col_of<S, P>(0), left = a.F - col;
+  const bool pre = a.pre != HGNN_NORM_NONE, post = a.post != HGNN_NORM_NONE;
+  struct {
+    RawPiece<half_t> dZ, Y, gate;
+    RawPiece<T> dH, H;
+  } next = {};
+  Place<T> in_dH(a.dH, a.lddh, first, stride, col), in_H(a.H, a.ldh, first, stride, col), out_R(a.dR, a.lddr, first, stride, col);
+  Place<half_t> in_dZ(a.dZ, a.lddz, first, stride, col), in_Y(a.Y, a.ldy, first, stride, col), in_gate(a.gate_rows, a.ld_gate, first, stride, col),
+      out_Y(a.dY, a.lddy, first, stride, col), out_gate(a.dgate_rows, a.ldd_gate, first, stride, col);
+  const auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+    if (a.dH) next.dH = in_dH.fetch(row, a.n, left);
+    if (pre) next.H = in_H.fetch(row, a.n, left), next.dZ = in_dZ.fetch(row, a.n, left);
+    if (a.Y) next.Y = in_Y.fetch(row, a.n, left);
+    if (a.gate_rows) next.gate = in_gate.fetch(row, a.n, left);
+    in_dH.move(), in_H.move(), in_dZ.move(), in_Y.move(), in_gate.move();
+  };
+  constexpr bool kAhead = W <= 8;  // the next rows are on their way while these are worked on (where there are registers for it)
+  if (kAhead) fetch(first);
+  for (int64_t row = first; row - S::row() < a.n; row += stride) {
+    asm volatile("" ::: "memory");  // weights are read again, not kept
+    if (!kAhead) fetch(row);
+    const int mine = row < a.n ? left : 0;
+    Eight e[1] = {eight_of(next.dH, left)}, h[1] = {eight_of(next.H, left)}, d[1] = {eight_of(next.dZ, left)}, b[1] = {eight_of(next.Y, left)};
+    if (a.gate_rows) gate[0] = eight_of(next.gate, left);
+    if (kAhead && row - S::row() + stride < a.n) fetch(row + stride);
+    if (pre) {
       const float r = normed<S, P>(h, a.pre, a.F, a.eps, lds);
 #pragma unroll
-      for (int p = 0; p < P; ++p)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float v = live ? d[p].v[i] : 0.f;
-          total[kPreW][p].v[i] = fmaf(v, h[p].v[i], total[kPreW][p].v[i]);
-          total[kPreB][p].v[i] += v;
-        }
-      through<S, P>(d, h, pre_w, r, a.pre, a.F, lds);
-#pragma unroll
-      for (int p = 0; p < P; ++p)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[p].v[i] += d[p].v[i];
+      for (int i = 0; i < 8; ++i) {
+        total[kPreW][0].v[i] = fmaf(d[0].v[i], h[0].v[i], total[kPreW][0].v[i]);
+        total[kPreB][0].v[i] += d[0].v[i];
+      }
+      through<S, P>(e, d, h, [&](int p) { return weight(kAtPreW, p); }, r, a.pre, a.F, lds);
     }
-    if (a.dR && live) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
+    if (a.dR) {
+      if (a.alpha == 1.f) {
+        store_eight(out_R.at, mine, e[0], a.past & 1);
+      } else {
         Eight out;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out.v[i] = a.alpha * e[p].v[i];
-        store_eight(static_cast<T*>(a.dR) + row * a.lddr, col_of<S, P>(p), a.F, out);
+        for (int i = 0; i < 8; ++i) out.v[i] = a.alpha * e[0].v[i];
+        store_eight(out_R.at, mine, out, a.past & 1);
       }
+      out_R.move();
     }
     if (!a.dY && !a.dgate_rows && !(a.vectors & (1 << kGate | 1 << kPostW | 1 << kPostB))) continue;
     float r = 1.f;
-    if (a.post != HGNN_NORM_NONE) r = normed<S, P>(b, a.post, a.F, a.eps, lds);  // b: xh
+    if (post) r = normed<S, P>(b, a.post, a.F, a.eps, lds);  // b: xh
     if (a.gate || a.gate_rows) {
+      const Eight w = weight(kAtPostW, 0), c = weight(kAtPostB, 0);
+      if (!a.gate_rows) gate[0] = weight(kAtGate, 0);
+      Eight g;
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const int left = a.F - col_of<S, P>(p);
-        Eight g;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          g.v[i] = e[p].v[i] * (a.post != HGNN_NORM_NONE ? fmaf(b[p].v[i], post_w[p].v[i], post_b[p].v[i]) : b[p].v[i]);
-          total[kGate][p].v[i] += live && i < left ? g.v[i] : 0.f;
-          e[p].v[i] *= gate[p].v[i];
-        }
-        if (a.dgate_rows && live) store_eight(a.dgate_rows + row * a.ldd_gate, col_of<S, P>(p), a.F, g);
+      for (int i = 0; i < 8; ++i) {
+        g.v[i] = e[0].v[i] * (post ? fmaf(b[0].v[i], w.v[i], c.v[i]) : b[0].v[i]);
+        total[kGate][0].v[i] += g.v[i];
+        e[0].v[i] *= gate[0].v[i];
       }
+      if (a.dgate_rows) store_eight(out_gate.at, mine, g), out_gate.move();
     }
-    if (a.post != HGNN_NORM_NONE) {
+    if (post) {
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const int left = a.F - col_of<S, P>(p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          e[p].v[i] = i < left ? e[p].v[i] : 0.f;
-          const float v = live ? e[p].v[i] : 0.f;
-          total[kPostW][p].v[i] = fmaf(v, b[p].v[i], total[kPostW][p].v[i]);
-          total[kPostB][p].v[i] += v;
-        }
+      for (int i = 0; i < 8; ++i) {
+        total[kPostW][0].v[i] = fmaf(e[0].v[i], b[0].v[i], total[kPostW][0].v[i]);
+        total[kPostB][0].v[i] += e[0].v[i];
       }
-      through<S, P>(e, b, post_w, r, a.post, a.F, lds);
+      Eight y[1] = {};
+      through<S, P>(y, e, b, [&](int p) { return weight(kAtPostW, p); }, r, a.post, a.F, lds);
+      e[0] = y[0];
     }
-    if (a.dY && live) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) store_eight(a.dY + row * a.lddy, col_of<S, P>(p), a.F, e[p]);
-    }
+    if (a.dY) store_eight(out_Y.at, mine, e[0], a.past & 2), out_Y.move();
   }
   float* const part = a.part + int64_t(blockIdx.x) * kVectors * a.pitch;
 #pragma unroll
@@ -351,7 +391,7 @@ __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_grad_ke
       }
     } else {
 #pragma unroll
-      for (int p = 0; p < P; ++p) store_eight(part + k * a.pitch, col_of<S, P>(p), a.F, total[k][p]);
+      for (int p = 0; p < P; ++p) store_eight(part + k * a.pitch + col_of<S, P>(p), a.F - col_of<S, P>(p), total[k][p]);
     }
   }
 }
@@ -419,13 +459,18 @@ struct ShapeOf<RowShape<l, p, w>> {
   static constexpr int L = l, P = p, W = w;
 };
 
-// Workgroups of the gradients: as many as fill the chip, each with rows enough that its partial sums (as many bytes as three rows or so) cost little.
-constexpr int kGradBlocks = 1024;
+// Workgroups that are resident at once where a SIMD holds so many waves of a kernel: with more, the last ones run by themselves (the gradients of 2.4 M x 128 by
+// 1024 workgroups, 768 of them at once, 910 us).
+constexpr int kUnits = 256;
 template <class S>
-static int64_t grad_blocks(int64_t n) {
-  const int64_t most = S::kThreads > kBlock ? kGradBlocks / 4 : kGradBlocks;
+static int64_t resident(int waves) {
+  return kUnits * int64_t(std::max(1, waves * 4 * kWave / S::kThreads));
+}
+// ... of the gradients: each with rows enough that its partial sums (as many bytes as three rows or so) cost little.
+template <class S>
+static int64_t grad_blocks(int64_t n, hgnn_type type) {
   const int64_t per = std::max(S::kRows, S::kLanes >= 64 ? 8 : 1);
-  return std::max<int64_t>(1, std::min(most, ceil_div(n, per)));
+  return std::max<int64_t>(1, std::min(resident<S>(type == HGNN_F16 ? 3 : 2), ceil_div(n, per)));
 }
 
 static hgnn_status check_block(const char* who, int64_t n, int32_t F, const hgnn_block* b, hgnn_type type, bool branch) {
@@ -435,7 +480,7 @@ static hgnn_status check_block(const char* who, int64_t n, int32_t F, const hgnn
   const auto known = [](hgnn_norm_kind k) { return k == HGNN_NORM_NONE || k == HGNN_NORM_RMS || k == HGNN_NORM_LAYER; };
   HGNN_REQUIRE(known(b->post) && known(b->pre), HGNN_EINVAL, "%s: unknown norm %d or %d", who, int(b->post), int(b->pre));
   HGNN_REQUIRE(F <= kMostNormed && n <= (int64_t(1) << 40), HGNN_EUNSUPPORTED, "%s: F = %d above %d, or n = %lld above 2^40", who, F, kMostNormed, static_cast<long long>(n));
-  HGNN_REQUIRE(std::isfinite(b->alpha) && b->eps > 0.f && std::isfinite(b->eps), HGNN_EINVAL, "%s: alpha = %g, eps = %g", who, double(b->alpha), double(b->eps));
+  HGNN_REQUIRE(std::isfinite(b->alpha) && b->eps >= 1.17549435e-38f && std::isfinite(b->eps), HGNN_EINVAL, "%s: alpha = %g, eps = %g", who, double(b->alpha), double(b->eps));
   HGNN_REQUIRE(b->post != HGNN_NORM_NONE || (!b->post_w && !b->post_b), HGNN_EINVAL, "%s: weights of a norm behind the branch that is none", who);
   HGNN_REQUIRE(b->pre != HGNN_NORM_NONE || (!b->pre_w && !b->pre_b), HGNN_EINVAL, "%s: weights of a norm of the sum that is none", who);
   HGNN_REQUIRE(!b->gate || !b->gate_rows, HGNN_EINVAL, "%s: gate and gate_rows exclude each other", who);
@@ -445,6 +490,11 @@ static hgnn_status check_block(const char* who, int64_t n, int32_t F, const hgnn
                    aligned_to_type(b->pre_b, HGNN_F32) && aligned_to_type(b->gate_rows, HGNN_F16),
                HGNN_EINVAL, "%s: an array that is not aligned to its type", who);
   return HGNN_OK;
+}
+// whether an output goes past the caches: large, and in whole lines
+static bool block_past(double bytes, const void* p, int64_t F, int64_t ld, hgnn_type type) {
+  const int64_t size = type == HGNN_F16 ? 2 : 4;
+  return p && bytes >= kPastBytes && F * size % 128 == 0 && ld * size % 128 == 0 && (reinterpret_cast<uintptr_t>(p) & 127u) == 0;
 }
 static void block_args(BlockArgs& a, int64_t n, int32_t F, const hgnn_block* b) {
   a.n = n, a.F = F, a.post = b->post, a.pre = b->pre, a.alpha = b->alpha, a.eps = b->eps;
@@ -478,7 +528,7 @@ hgnn_status hgnn_residual_norm(int64_t n, int32_t F, const hgnn_block* block, hg
   return with_shape(F, [&](auto shape) -> hgnn_status {
     typedef decltype(shape) S;
     typedef ShapeOf<S> D;
-    const unsigned blocks = unsigned(std::min<int64_t>(ceil_div(n, S::kRows), 2048));
+    const unsigned blocks = unsigned(std::min<int64_t>(ceil_div(n, S::kRows), resident<S>(S::kThreads > 512 ? 4 : 5)));
     if (type == HGNN_F16) block_norm_kernel<half_t, D::L, D::P, D::W><<<blocks, S::kThreads, 0, s>>>(a);
     else block_norm_kernel<float, D::L, D::P, D::W><<<blocks, S::kThreads, 0, s>>>(a);
     HGNN_LAUNCH_CHECK("block_norm_kernel");
@@ -490,7 +540,7 @@ size_t hgnn_residual_norm_grad_workspace(int64_t n, int32_t F) {
   if (n <= 0 || F <= 0 || F > kMostNormed) return 0;
   int64_t blocks = 0;
   with_shape(F, [&](auto shape) -> hgnn_status {
-    blocks = grad_blocks<decltype(shape)>(n);
+    blocks = grad_blocks<decltype(shape)>(n, HGNN_F16);  // the more of the two
     return HGNN_OK;
   });
   return size_t(blocks) * kVectors * size_t((F + 7) / 8 * 8) * sizeof(float);
@@ -535,6 +585,8 @@ hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* bloc
   a.dH = dH, a.lddh = lddh, a.dZ = reinterpret_cast<const half_t*>(dZ), a.lddz = lddz;
   a.dR = g.dR, a.lddr = g.lddr, a.dY = reinterpret_cast<half_t*>(g.dY), a.lddy = g.lddy;
   a.dgate_rows = reinterpret_cast<half_t*>(g.dgate_rows), a.ldd_gate = g.ldd_gate;
+  const double bytes = double(n) * F * ((g.dR ? (type == HGNN_F16 ? 2 : 4) : 0) + (g.dY ? 2 : 0));
+  a.past = (block_past(bytes, g.dR, F, g.lddr, type) ? 1 : 0) | (block_past(bytes, g.dY, F, g.lddy, HGNN_F16) ? 2 : 0);
   a.part = static_cast<float*>(workspace), a.pitch = (F + 7) / 8 * 8;
   hipStream_t s = static_cast<hipStream_t>(stream);
   int64_t blocks = 0;  // no rows: sums of nothing
@@ -542,7 +594,7 @@ hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* bloc
     st = with_shape(F, [&](auto shape) -> hgnn_status {
       typedef decltype(shape) S;
       typedef ShapeOf<S> D;
-      blocks = grad_blocks<S>(n);
+      blocks = grad_blocks<S>(n, type);
       if (type == HGNN_F16) block_norm_grad_kernel<half_t, D::L, D::P, D::W><<<unsigned(blocks), S::kThreads, 0, s>>>(a);
       else block_norm_grad_kernel<float, D::L, D::P, D::W><<<unsigned(blocks), S::kThreads, 0, s>>>(a);
       HGNN_LAUNCH_CHECK("block_norm_grad_kernel");
