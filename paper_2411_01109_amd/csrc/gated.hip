@@ -13,32 +13,28 @@ namespace hgnn {
 
 // ---- activations
 __device__ __forceinline__ float gate_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f)); }
-__device__ __forceinline__ float gate_value(int act, float x) {  // act: uniform
+// Four at a time behind one question about the kind, which is uniform: a question for each value keeps the four from running beside each other.
+__device__ __forceinline__ float4_t gate_value(int act, const float4_t& x) {
+  float4_t y;
+#define HGNN_EACH(...) { _Pragma("unroll") for (int e = 0; e < 4; ++e) { __VA_ARGS__; } break; }
   switch (act) {
-    case HGNN_SILU: return x * gate_sigmoid(x);
-    case HGNN_GELU: return 0.5f * x * (1.f + erff(x * 0.70710678f));
-    case HGNN_SIGMOID: return gate_sigmoid(x);
-    default: return x > 0.f ? x : x == x ? 0.f : x;
+    case HGNN_SILU: HGNN_EACH(y[e] = x[e] * gate_sigmoid(x[e]))
+    case HGNN_GELU: HGNN_EACH(y[e] = 0.5f * x[e] * (1.f + erff(x[e] * 0.70710678f)))
+    case HGNN_SIGMOID: HGNN_EACH(y[e] = gate_sigmoid(x[e]))
+    default: HGNN_EACH(y[e] = x[e] > 0.f ? x[e] : x[e] == x[e] ? 0.f : x[e])
   }
+  return y;
 }
-__device__ __forceinline__ void gate_both(int act, float x, float& value, float& slope) {
+__device__ __forceinline__ void gate_both(int act, const float4_t& x, float4_t& value, float4_t& slope) {
   switch (act) {
-    case HGNN_SILU: {
-      const float p = gate_sigmoid(x);
-      value = x * p, slope = p * (1.f + x * (1.f - p));
-      return;
-    }
-    case HGNN_GELU: {
-      const float phi = 0.5f * (1.f + erff(x * 0.70710678f));
-      value = x * phi, slope = fmaf(x * 0.39894228f, __builtin_amdgcn_exp2f(x * x * -0.72134752f), phi);
-      return;
-    }
-    case HGNN_SIGMOID: {
-      value = gate_sigmoid(x), slope = value * (1.f - value);
-      return;
-    }
-    default: value = x > 0.f ? x : x == x ? 0.f : x, slope = x > 0.f ? 1.f : 0.f;
+    case HGNN_SILU: HGNN_EACH(const float p = gate_sigmoid(x[e]); value[e] = x[e] * p; slope[e] = p * (1.f + x[e] * (1.f - p)))
+    case HGNN_GELU:
+      HGNN_EACH(const float phi = 0.5f * (1.f + erff(x[e] * 0.70710678f)); value[e] = x[e] * phi;
+                slope[e] = fmaf(x[e] * 0.39894228f, __builtin_amdgcn_exp2f(x[e] * x[e] * -0.72134752f), phi))
+    case HGNN_SIGMOID: HGNN_EACH(value[e] = gate_sigmoid(x[e]); slope[e] = value[e] * (1.f - value[e]))
+    default: HGNN_EACH(value[e] = x[e] > 0.f ? x[e] : x[e] == x[e] ? 0.f : x[e]; slope[e] = x[e] > 0.f ? 1.f : 0.f)
   }
+#undef HGNN_EACH
 }
 
 // the first `left` of four values (all of them where it is four or more), at 8-byte aligned places
@@ -62,9 +58,7 @@ struct GatedOut {
   __device__ Read read(int64_t, int64_t) const { return {}; }
   template <bool WHOLE>
   __device__ void put(int64_t, int64_t q, int64_t p, const Read&, const float4_t& g, const float4_t& u) const {
-    float4_t y;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = gate_value(act, g[e]) * u[e];
+    const float4_t y = gate_value(act, g) * u;
     store_four(Y + q * ldy + p, WHOLE ? 4 : F - p, y);
   }
 };
@@ -78,13 +72,9 @@ struct GatedGradOut {
   __device__ Read read(int64_t q, int64_t p) const { return *reinterpret_cast<const half4_t*>(dY + q * lddy + p); }  // what is behind F reaches what is behind F
   template <bool WHOLE>
   __device__ void put(int64_t, int64_t q, int64_t p, const Read& dy, const float4_t& g, const float4_t& u) const {
-    float4_t dg, du;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float value, slope;
-      gate_both(act, g[e], value, slope);
-      dg[e] = float(dy[e]) * u[e] * slope, du[e] = float(dy[e]) * value;
-    }
+    float4_t value, slope;
+    gate_both(act, g, value, slope);
+    const float4_t d = {float(dy[0]), float(dy[1]), float(dy[2]), float(dy[3])}, dg = d * u * slope, du = d * value;
     store_four(D + q * 2 * Fp + p, 4, dg);
     store_four(D + q * 2 * Fp + Fp + p, 4, du);
   }
@@ -165,6 +155,7 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 enum Size { kFew, kMid, kWide };
 constexpr int kFull = 256;  // compute units
 constexpr int kLong = 512;
+constexpr int64_t kManyRows = 16384;
 template <ProductKind KIND, bool QCOL, bool PCOL, class Call>
 static hgnn_status with_product(Size size, Call&& call) {
   constexpr int two = KIND == kTwo ? 2 : 1;  // two results: half as many items of P
@@ -189,10 +180,176 @@ static Split split_of(int64_t nq, int64_t np, int64_t K, bool two) {
   return s;
 }
 
+// ---- many rows through a narrow weight (K up to 256): bound by the rows of X and Y, which the product kernel's workgroups, a tile and two steps each, do not stream
+// (233 000 x 128 -> 256 96 us, of it 35 by the bytes at a copy's rate).  Eight waves keep their features of both weights in registers for all rows of the
+// workgroup, 32 features for K <= 128, 16 beyond; a ninth brings X into a ring in LDS, 64 rows at a time, and is the only one that waits for loads to LDS, so that
+// the other waves' stores are never waited for.  A barrier a tile hands it over and takes back the one before.  (Two
+// workgroups of four waves and one do not fit a compute unit's registers: 65 -> 100 us.)  Features are dealt out such that a lane's 2 x 4 sums are eight consecutive ones.
+constexpr int kRowsWaves = 8, kRowsTile = 64;
+struct GatedRowsArgs {
+  const half_t *X, *Wg, *Wu;
+  int64_t ldx, ldw, n;
+  int32_t K, F, chunks;  // of features: a workgroup takes number blockIdx.x % chunks
+};
+template <int KS_, int TP_, bool PCOL_, int RING_>
+struct GatedRowsShape {  // KS: 64 steps of the contraction, TP: 16 features of a wave
+  static constexpr int KS = KS_, TP = TP_, kRing = RING_, kFeatures = 16 * TP * kRowsWaves, kStage = KS * kRowsTile * 128;
+  static constexpr bool PCOL = PCOL_;
+  static constexpr int kWeights = KS * 2 * kFeatures * 128;
+  static constexpr int kLds = kWeights > RING_ * kStage ? kWeights : RING_ * kStage;
+  static constexpr int kChunks = KS * kRowsTile / 8;  // kilobytes of a tile of X
+  static constexpr int kThreads = (kRowsWaves + 1) * kWave;
+  static_assert(kLds <= 160 * 1024 && (RING_ - 2) * kChunks < 64, "LDS, vmcnt");
+};
+// fragment u of a wave's 16 TP features, whose items are dealt out, from where product_loads put them
+template <bool COL, int TP>
+__device__ __forceinline__ half8_t gated_weight(const unsigned char* tile, int wave, int lane, int u, int h) {
+  const int i = lane & 15, qq = lane >> 4;
+  if (!COL) {
+    const int item = 16 * TP * wave + (TP == 2 ? 8 * (i >> 2) + 4 * u + (i & 3) : i);
+    return *reinterpret_cast<const half8_t*>(tile + item * 128 + ((4 * h + qq) ^ ((item & 15) >> 1)) * 16);
+  }
+  const int r = 8 * qq + (i >> 2), item = 16 * TP * wave + (TP == 2 ? 8 * (i & 3) + 4 * u : 4 * (i & 3));  // the first of four
+  const unsigned char* const p = tile + (item >> 6) * 8192 + h * 4096 + r * 128 + (((item & 63) >> 3) ^ product_turn(r)) * 16 + (item & 4) * 2;
+  const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)p);
+  const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(p + 512));
+  return __builtin_bit_cast(half8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+template <class S, class Out>
+__global__ __launch_bounds__(S::kThreads) void gated_rows_kernel(GatedRowsArgs a, Out out) {
+  extern __shared__ __align__(1024) unsigned char lds[];
+  constexpr int KS = S::KS, TP = S::TP;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, qq = lane >> 4;
+  const int chunk = blockIdx.x % a.chunks, first = blockIdx.x / a.chunks, stride = gridDim.x / a.chunks;
+  const int64_t f0 = int64_t(chunk) * S::kFeatures;
+  const int tiles = int((a.n + kRowsTile - 1) / kRowsTile);
+  const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) unsigned char*)lds));
+  const char* const zero = reinterpret_cast<const char*>(&g_product_zero);
+  const auto meet = [] {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  half8_t weight[2][TP][2 * KS];
+  {  // both weights' features of the workgroup into LDS, and a wave's into its registers
+    constexpr int kOperand = S::kFeatures * 128;  // 64 steps of one weight
+    constexpr int N = 2 * S::kFeatures / 8 / kRowsWaves;
+    if (wave < kRowsWaves) {
+      ProductLoads<N, S::PCOL> l;
+      product_loads<N, S::PCOL, false, kRowsWaves>(l, a.Wg, a.Wu, a.ldw, f0, a.F, 0, wave, lane, S::kFeatures / 8);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          load_to_lds(l.k[j] + 64 * s < a.K ? l.base[j] + s * l.inc + l.off[j] : zero, lds0 + s * 2 * kOperand + (wave + j * kRowsWaves) * 1024);
+    }
+    product_wait<0>();
+    if (wave < kRowsWaves) {
+#pragma unroll
+      for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int u = 0; u < TP; ++u)
+#pragma unroll
+          for (int h = 0; h < 2 * KS; ++h) {
+            half8_t v = gated_weight<S::PCOL, TP>(lds + (h / 2) * 2 * kOperand + o * kOperand, wave, lane, u, h % 2);
+            // what stands behind the contraction's end inside a piece is the caller's padding
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (!S::PCOL && 32 * h + 8 * qq + e >= a.K) v[e] = half_t(0);
+            weight[o][u][h] = v;
+          }
+    }
+    meet();
+  }
+  const int mine = first < tiles ? (tiles - 1 - first) / stride + 1 : 0;  // tiles of the workgroup
+  if (wave == kRowsWaves) {
+    const auto ask = [&](int t) __attribute__((always_inline)) {
+      const int64_t row0 = (int64_t(first) + int64_t(t) * stride) * kRowsTile;
+      const uint32_t to = lds0 + (t % S::kRing) * S::kStage;
+#pragma unroll
+      for (int c = 0; c < S::kChunks; ++c) {  // eight rows, 64 steps
+        const int s = c / 8, r = 8 * (c % 8) + (lane >> 3), u = (lane & 7) ^ ((r & 15) >> 1), k = 64 * s + 8 * u;
+        const char* const src = reinterpret_cast<const char*>(a.X + min(row0 + r, a.n - 1) * a.ldx + k);
+        load_to_lds(k < a.K ? src : zero, to + c * 1024);
+      }
+    };
+    int asked = 0;
+    for (; asked < S::kRing - 1 && asked < mine; ++asked) ask(asked);
+    for (int t = 0; t < mine; ++t) {
+      const int behind = asked - 1 - t;
+      if (S::kRing > 3 && behind >= 2) product_wait<(S::kRing > 3 ? 2 : 0) * S::kChunks>();
+      else if (S::kRing > 2 && behind >= 1) product_wait<(S::kRing > 2 ? 1 : 0) * S::kChunks>();
+      else product_wait<0>();
+      if (asked < mine) ask(asked), ++asked;  // in the place of the tile before, which all waves have left
+    }
+    return;
+  }
+  const ProductReads<false, false, kRowsTile / 16> read(0, lane);
+  // behind the contraction's end inside a piece: nothing of the rows, either
+  const int h_end = a.K / 32, e_end = a.K - 32 * h_end - 8 * qq;
+  const bool ragged = a.K & 7;
+  const int64_t p0 = f0 + 16 * TP * wave + 4 * TP * qq;
+  const bool whole_p = f0 + 16 * TP * (wave + 1) <= a.F;  // uniform
+  for (int t = 0; t < mine; ++t) {
+    const int64_t row0 = (int64_t(first) + int64_t(t) * stride) * kRowsTile;
+    meet();
+    const unsigned char* const stage = lds + (t % S::kRing) * S::kStage;
+    const auto tile = [&](auto whole, auto cut) __attribute__((always_inline)) {
+      constexpr bool kWhole = decltype(whole)::value, kCut = decltype(cut)::value;
+      typename Out::Read early[kRowsTile / 16][TP];
+      const auto each = [&](int x, auto&& f) __attribute__((always_inline)) {
+        const int64_t q = row0 + 16 * x + i;
+#pragma unroll
+        for (int u = 0; u < TP; ++u)
+          if (kWhole || (q < a.n && p0 + 4 * u < a.F)) f(q, p0 + 4 * u, u);
+      };
+#pragma unroll
+      for (int x = 0; x < kRowsTile / 16; ++x) each(x, [&](int64_t q, int64_t p, int u) __attribute__((always_inline)) { early[x][u] = out.read(q, p); });
+#pragma unroll
+      for (int x = 0; x < kRowsTile / 16; ++x) {
+        float4_t acc[2][TP];
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+#pragma unroll
+          for (int u = 0; u < TP; ++u) acc[o][u] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 2 * KS; ++h) {
+          half8_t v = read.get(stage + (h / 2) * (kRowsTile * 128), x, h % 2);
+          if (kCut && h == h_end) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e >= e_end) v[e] = half_t(0);
+          }
+#pragma unroll
+          for (int o = 0; o < 2; ++o)
+#pragma unroll
+            for (int u = 0; u < TP; ++u) acc[o][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(weight[o][u][h], v, acc[o][u], 0, 0, 0);
+        }
+        each(x, [&](int64_t q, int64_t p, int u) __attribute__((always_inline)) { out.template put<kWhole>(0, q, p, early[x][u], acc[0][u], acc[1][u]); });
+      }
+    };
+    if (ragged) tile(std::false_type(), std::true_type());
+    else if (whole_p && row0 + kRowsTile <= a.n) tile(std::true_type(), std::false_type());
+    else tile(std::false_type(), std::false_type());
+  }
+}
+template <class S, class Out>
+static hgnn_status gated_rows(const char* who, GatedRowsArgs& a, const Out& out, hipStream_t s) {
+  a.chunks = int32_t(ceil_div(a.F, S::kFeatures));
+  const int64_t blocks = std::max<int64_t>(1, kFull / a.chunks) * a.chunks;
+  static uint64_t told = 0;
+  const hgnn_status st = product_lds(reinterpret_cast<const void*>(&gated_rows_kernel<S, Out>), S::kLds, &told);
+  if (st != HGNN_OK) return st;
+  gated_rows_kernel<S, Out><<<unsigned(blocks), S::kThreads, S::kLds, s>>>(a, out);
+  HGNN_LAUNCH_CHECK("gated_rows_kernel");
+  return HGNN_OK;
+}
+
 struct GatedSizes {
   int64_t n, Fp;
   int K, F;
   Split gate, dx, dw;
+  bool rows;  // gated_rows_kernel
   size_t gate_part, dx_part, dw_part, d;
 };
 static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
@@ -201,7 +358,8 @@ static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
   z.gate = split_of(n, F, K, true);
   z.dx = split_of(n, K, F, false);
   z.dw = split_of(K, 2 * z.Fp, n, false);
-  z.gate_part = z.gate.parts > 1 ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
+  z.rows = K <= 256 && F <= 2048 && n >= kManyRows;
+  z.gate_part = z.gate.parts > 1 && !z.rows ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
   z.dx_part = z.dx.parts > 1 ? size_t(z.dx.parts) * size_t(n) * size_t(up(K, 4)) * 4 : 0;
   z.dw_part = z.dw.parts > 1 ? size_t(z.dw.parts) * size_t(up(K, 4)) * 2 * size_t(z.Fp) * 4 : 0;
   z.d = size_t(up(n * 2 * z.Fp * 2, 256));
@@ -218,6 +376,16 @@ static hgnn_status join_grid(const char* who, int64_t threads, unsigned* blocks)
 template <class Out>
 static hgnn_status gated_pairs(const char* who, const GatedSizes& z, const half_t* X, int64_t ldx, const half_t* Wg, const half_t* Wu, int64_t ldw, bool trans, float* part,
                                const Out& out, hipStream_t s) {
+  if (z.rows) {
+    GatedRowsArgs r{X, Wg, Wu, ldx, ldw, z.n, z.K, z.F, 1};
+    const auto go = [&](auto pcol) -> hgnn_status {
+      constexpr bool P = decltype(pcol)::value;
+      if (z.K <= 64) return gated_rows<GatedRowsShape<1, 2, P, 4>>(who, r, out, s);
+      if (z.K <= 128) return gated_rows<GatedRowsShape<2, 2, P, 4>>(who, r, out, s);
+      return gated_rows<GatedRowsShape<4, 1, P, 3>>(who, r, out, s);
+    };
+    return trans ? go(std::false_type()) : go(std::true_type());
+  }
   ProductArgs a{};
   a.Q0 = X, a.Q1 = X, a.P0 = Wg, a.P1 = Wu, a.ldq = ldx, a.ldp = ldw, a.nq = z.n, a.np = z.F, a.K = z.K, a.part = z.gate.part, a.parts = z.gate.parts;
   const auto go = [&](auto shape) -> hgnn_status {
