@@ -91,19 +91,36 @@ struct GatedPart {  // [parts][n][2][Fp]
     *reinterpret_cast<float4_t*>(at + Fp) = u;
   }
 };
+// The parts of four sums in order: a workgroup takes 64 fours and cuts the parts in four, so that enough loads are on their way.  (121 parts of 100 x 512 by a
+// thread a four 13 us.)  N values, `apart` floats from each other; those of thread < 64 are the sums.
+constexpr int kJoinWays = 4, kJoinFours = kBlock / kJoinWays;
+template <int N>
+__device__ __forceinline__ void join_parts(float4_t (&v)[N], const float* at, int64_t apart, int64_t stride, int parts, bool in) {
+  __shared__ __align__(16) float4_t lds[kJoinWays][N][kJoinFours];
+  const int x = threadIdx.x % kJoinFours, way = threadIdx.x / kJoinFours, per = (parts + kJoinWays - 1) / kJoinWays, from = way * per, to = min(parts, from + per);
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = float4_t{0.f, 0.f, 0.f, 0.f};
+  if (in) {
+#pragma unroll 8
+    for (int p = from; p < to; ++p)
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] += *reinterpret_cast<const float4_t*>(at + p * stride + k * apart);
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) lds[way][k][x] = v[k];
+  __syncthreads();
+  if (way) return;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int w = 1; w < kJoinWays; ++w) v[k] += lds[w][k][x];
+}
 template <class Out>
 __global__ __launch_bounds__(kBlock) void gated_join_kernel(const float* part, int parts, int64_t n, int F, int64_t Fp, Out out) {
-  const int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x, each = (F + 3) / 4, q = t / each, p = 4 * (t - q * each);
-  if (q >= n) return;
-  const float* at = part + q * 2 * Fp + p;
-  const int64_t stride = n * 2 * Fp;
-  float4_t g = *reinterpret_cast<const float4_t*>(at), u = *reinterpret_cast<const float4_t*>(at + Fp);
-#pragma unroll 4
-  for (int k = 1; k < parts; ++k) {
-    at += stride;
-    g += *reinterpret_cast<const float4_t*>(at), u += *reinterpret_cast<const float4_t*>(at + Fp);
-  }
-  out.template put<false>(0, q, p, out.read(q, p), g, u);
+  const int64_t t = int64_t(blockIdx.x) * kJoinFours + threadIdx.x % kJoinFours, each = (F + 3) / 4, q = t / each, p = 4 * (t - q * each);
+  float4_t v[2];
+  join_parts(v, part + q * 2 * Fp + p, Fp, n * 2 * Fp, parts, q < n);
+  if (q < n && threadIdx.x < kJoinFours) out.template put<false>(0, q, p, out.read(q, p), v[0], v[1]);
 }
 
 // ---- products into one fp16 matrix, or into two that are the halves of C's lines or of its items along a line
@@ -131,19 +148,11 @@ struct HalfPart {  // [parts][nq][pitch]
   __device__ void put(int64_t k, int64_t q, int64_t p, const Read&, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * pitch + p) = v; }
 };
 __global__ __launch_bounds__(kBlock) void half_join_kernel(const float* part, int parts, int64_t nq, int64_t pitch, HalfOut out) {
-  const int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x, each = pitch / 4, q = t / each, p = 4 * (t - q * each);
-  if (q >= nq) return;
-  const float* at = part + q * pitch + p;
-  const int64_t stride = nq * pitch;
-  float4_t v = *reinterpret_cast<const float4_t*>(at);
-#pragma unroll 4
-  for (int k = 1; k < parts; ++k) {
-    at += stride;
-    v += *reinterpret_cast<const float4_t*>(at);
-  }
-  out.template put<false>(0, q, p, out.read(q, p), v);
+  const int64_t t = int64_t(blockIdx.x) * kJoinFours + threadIdx.x % kJoinFours, each = pitch / 4, q = t / each, p = 4 * (t - q * each);
+  float4_t v[1];
+  join_parts(v, part + q * pitch + p, 0, nq * pitch, parts, q < nq);
+  if (q < nq && threadIdx.x < kJoinFours) out.put<false>(0, q, p, out.read(q, p), v[0]);
 }
-
 __global__ __launch_bounds__(kBlock) void half_zero_kernel(half_t* out, int64_t lines, int64_t cols, int64_t ld) {
   const int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x, each = (cols + 3) / 4, q = t / each, p = 4 * (t - q * each);
   if (q < lines) store_four(out + q * ld + p, cols - p, float4_t{0.f, 0.f, 0.f, 0.f});
@@ -328,9 +337,12 @@ __global__ __launch_bounds__(S::kThreads) void gated_rows_kernel(GatedRowsArgs a
         each(x, [&](int64_t q, int64_t p, int u) __attribute__((always_inline)) { out.template put<kWhole>(0, q, p, early[x][u], acc[0][u], acc[1][u]); });
       }
     };
-    if (ragged) tile(std::false_type(), std::true_type());
-    else if (whole_p && row0 + kRowsTile <= a.n) tile(std::true_type(), std::false_type());
-    else tile(std::false_type(), std::false_type());
+    if (whole_p && row0 + kRowsTile <= a.n) {
+      if (ragged) tile(std::true_type(), std::true_type());
+      else tile(std::true_type(), std::false_type());
+    } else {
+      tile(std::false_type(), std::true_type());
+    }
   }
 }
 template <class S, class Out>
@@ -342,6 +354,158 @@ static hgnn_status gated_rows(const char* who, GatedRowsArgs& a, const Out& out,
   if (st != HGNN_OK) return st;
   gated_rows_kernel<S, Out><<<unsigned(blocks), S::kThreads, S::kLds, s>>>(a, out);
   HGNN_LAUNCH_CHECK("gated_rows_kernel");
+  return HGNN_OK;
+}
+
+// ---- few rows (up to 64), a served model's: bound by reading the two weights once.  A workgroup owns 32 features of both, its sixteen waves share the contraction, 32
+// steps at a time, and take the weights straight into the registers that the products read, a stage ahead for up to 16 rows; their sums meet in LDS.  One launch: by the
+// product kernel the contraction is cut over workgroups, and joining the parts is a launch of 3.5 us (1 row of 1024 -> 4096 9.3 us, 13 of 2048 -> 5461 16).
+// Fragment e, item i is feature 2 i + e of the 32: of [K][F] a lane takes two neighbouring features of eight steps, 64 bytes of a line a load, and a lane's sums are
+// eight consecutive features.
+constexpr int kFewWaves = 16, kFewRows = 64, kFewFeatures = 32;
+struct GatedFewArgs {
+  const half_t *X, *Wg, *Wu;
+  int64_t ldx, ldw;
+  int32_t n, K, F;
+};
+template <int RT, bool COL>
+struct FewStage {  // what a wave has in hand of 32 steps
+  typedef unsigned uint4_t __attribute__((ext_vector_type(4)));
+  uint4_t w[2][2];  // of both weights: [K][F] 2 x 4 lines of two features, [F][K] fragments
+  half8_t x[RT];
+};
+template <int RT, bool COL>
+__device__ __forceinline__ void few_fetch(const GatedFewArgs& a, FewStage<RT, COL>& st, int s, int f0, int lane) {
+  const int i = lane & 15, qq = lane >> 4, k = 32 * s + 8 * qq;
+#pragma unroll
+  for (int o = 0; o < 2; ++o) {
+    const half_t* const W = o ? a.Wu : a.Wg;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if (COL) {
+        const int f = f0 + 2 * i < a.F ? f0 + 2 * i : 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st.w[o][e][j] = *reinterpret_cast<const uint32_t*>(W + int64_t(min(k + 4 * e + j, a.K - 1)) * a.ldw + f);
+      } else {
+        st.w[o][e] = *reinterpret_cast<const typename FewStage<RT, COL>::uint4_t*>(W + int64_t(min(f0 + 2 * i + e, a.F - 1)) * a.ldw + (k < a.K ? k : 0));
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r) st.x[r] = *reinterpret_cast<const half8_t*>(a.X + int64_t(min(16 * r + i, a.n - 1)) * a.ldx + (k < a.K ? k : 0));
+}
+template <int RT, bool COL>
+__device__ __forceinline__ void few_multiply(const GatedFewArgs& a, const FewStage<RT, COL>& st, int s, int lane, float4_t (&acc)[RT][2][2]) {
+  const int left = a.K - 32 * s - 8 * (lane >> 4);  // steps of the lane that exist: the others hold padding, or lines once more
+  const bool cut = 32 * (s + 1) > a.K;              // uniform
+  const auto ended = [&](half8_t v) __attribute__((always_inline)) {
+    if (cut) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e >= left) v[e] = half_t(0);
+    }
+    return v;
+  };
+  half8_t w[2][2], x[RT];
+#pragma unroll
+  for (int o = 0; o < 2; ++o)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if (COL) {  // steps 2 j and 2 j + 1 of feature e of the pairs
+        typename FewStage<RT, COL>::uint4_t v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_perm(st.w[o][j / 2][2 * (j % 2) + 1], st.w[o][j / 2][2 * (j % 2)], e ? 0x07060302u : 0x05040100u);
+        w[o][e] = ended(__builtin_bit_cast(half8_t, v));
+      } else {
+        w[o][e] = ended(__builtin_bit_cast(half8_t, st.w[o][e]));
+      }
+    }
+#pragma unroll
+  for (int r = 0; r < RT; ++r) x[r] = ended(st.x[r]);
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) acc[r][o][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[o][e], x[r], acc[r][o][e], 0, 0, 0);
+}
+template <int RT, bool COL, class Out>
+__global__ __launch_bounds__(kFewWaves* kWave) void gated_few_kernel(GatedFewArgs a, Out out) {
+  typedef float float2_t __attribute__((ext_vector_type(2)));
+  __shared__ __align__(16) float4_t sums[kFewWaves][2][2][kWave];
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int f0 = blockIdx.x * kFewFeatures, steps = (a.K + 31) / 32;
+  float4_t acc[RT][2][2];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) acc[r][o][e] = float4_t{0.f, 0.f, 0.f, 0.f};
+  // Two neighbouring stages a wave: of [F][K] they are the two halves of a line.
+  const auto each = [&](auto&& f) __attribute__((always_inline)) {
+    for (int s = 2 * wave; s < steps; s += 2 * kFewWaves) f(s);
+  };
+  if constexpr (RT == 1) {
+    FewStage<RT, COL> one, two;
+    const auto fetch = [&](FewStage<RT, COL>& st, int s) __attribute__((always_inline)) {
+      if (s < steps) few_fetch(a, st, s, f0, lane);
+    };
+    fetch(one, 2 * wave), fetch(two, 2 * wave + 1);
+    each([&](int s) __attribute__((always_inline)) {
+      few_multiply(a, one, s, lane, acc);
+      fetch(one, s + 2 * kFewWaves);
+      if (s + 1 < steps) few_multiply(a, two, s + 1, lane, acc);
+      fetch(two, s + 1 + 2 * kFewWaves);
+    });
+  } else {  // (the registers for a stage ahead are the sums')
+    each([&](int s0) __attribute__((always_inline)) {
+      for (int s = s0; s < s0 + 2 && s < steps; ++s) {
+        FewStage<RT, COL> one;
+        few_fetch(a, one, s, f0, lane);
+        few_multiply(a, one, s, lane, acc);
+      }
+    });
+  }
+  // thread (part of the waves, row, four features): waves 2 part and 2 part + 1, and then one of them the eight parts
+  const int part = threadIdx.x >> 7, i = threadIdx.x & 15, m = (threadIdx.x >> 4) & 7, from = 16 * (m >> 1) + i, at = 2 * (m & 1);
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    if (r) __syncthreads();
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) sums[wave][o][e][lane] = acc[r][o][e];
+    __syncthreads();
+    const auto value = [&](int w, int o, int e) { return reinterpret_cast<float2_t*>(reinterpret_cast<float*>(&sums[w][o][e][from]) + at); };
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) *value(2 * part, o, e) += *value(2 * part + 1, o, e);
+    __syncthreads();
+    if (part == 0) {
+      float2_t v[2][2];
+#pragma unroll
+      for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          v[o][e] = *value(0, o, e);
+#pragma unroll
+          for (int w = 2; w < kFewWaves; w += 2) v[o][e] += *value(w, o, e);
+        }
+      const int64_t q = 16 * r + i, p = f0 + 4 * m;
+      if (q < a.n && p < a.F)
+        out.template put<false>(0, q, p, out.read(q, p), float4_t{v[0][0][0], v[0][1][0], v[0][0][1], v[0][1][1]}, float4_t{v[1][0][0], v[1][1][0], v[1][0][1], v[1][1][1]});
+    }
+  }
+}
+template <bool COL, class Out>
+static hgnn_status gated_few(const GatedFewArgs& a, const Out& out, hipStream_t s) {
+  const unsigned blocks = unsigned(ceil_div(a.F, kFewFeatures));
+  if (a.n <= 16) gated_few_kernel<1, COL><<<blocks, kFewWaves * kWave, 0, s>>>(a, out);
+  else if (a.n <= 32) gated_few_kernel<2, COL><<<blocks, kFewWaves * kWave, 0, s>>>(a, out);
+  else gated_few_kernel<4, COL><<<blocks, kFewWaves * kWave, 0, s>>>(a, out);
+  HGNN_LAUNCH_CHECK("gated_few_kernel");
   return HGNN_OK;
 }
 
@@ -359,16 +523,16 @@ static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
   z.dx = split_of(n, K, F, false);
   z.dw = split_of(K, 2 * z.Fp, n, false);
   z.rows = K <= 256 && F <= 2048 && n >= kManyRows;
-  z.gate_part = z.gate.parts > 1 && !z.rows ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
+  z.gate_part = z.gate.parts > 1 && !z.rows && n > kFewRows ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
   z.dx_part = z.dx.parts > 1 ? size_t(z.dx.parts) * size_t(n) * size_t(up(K, 4)) * 4 : 0;
   z.dw_part = z.dw.parts > 1 ? size_t(z.dw.parts) * size_t(up(K, 4)) * 2 * size_t(z.Fp) * 4 : 0;
   z.d = size_t(up(n * 2 * z.Fp * 2, 256));
   return z;
 }
 
-static hgnn_status join_grid(const char* who, int64_t threads, unsigned* blocks) {
-  HGNN_REQUIRE(ceil_div(threads, kBlock) <= 0xffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
-  *blocks = unsigned(ceil_div(threads, kBlock));
+static hgnn_status join_grid(const char* who, int64_t fours, unsigned* blocks, int per = kJoinFours) {
+  HGNN_REQUIRE(ceil_div(fours, per) <= 0xffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
+  *blocks = unsigned(ceil_div(fours, per));
   return HGNN_OK;
 }
 
@@ -376,6 +540,10 @@ static hgnn_status join_grid(const char* who, int64_t threads, unsigned* blocks)
 template <class Out>
 static hgnn_status gated_pairs(const char* who, const GatedSizes& z, const half_t* X, int64_t ldx, const half_t* Wg, const half_t* Wu, int64_t ldw, bool trans, float* part,
                                const Out& out, hipStream_t s) {
+  if (z.n <= kFewRows) {
+    const GatedFewArgs f{X, Wg, Wu, ldx, ldw, int32_t(z.n), z.K, z.F};
+    return trans ? gated_few<false>(f, out, s) : gated_few<true>(f, out, s);
+  }
   if (z.rows) {
     GatedRowsArgs r{X, Wg, Wu, ldx, ldw, z.n, z.K, z.F, 1};
     const auto go = [&](auto pcol) -> hgnn_status {
@@ -483,7 +651,7 @@ hgnn_status hgnn_gated_grad(int64_t n, int32_t K, int32_t F, hgnn_activation act
     if (!dWg) return HGNN_OK;
     for (half_t* w : {out(dWg), out(dWu)}) {
       unsigned blocks;
-      st = join_grid(who, lines * ceil_div(cols, 4), &blocks);
+      st = join_grid(who, lines * ceil_div(cols, 4), &blocks, kBlock);
       if (st != HGNN_OK) return st;
       half_zero_kernel<<<blocks, kBlock, 0, s>>>(w, lines, cols, lddw);
       HGNN_LAUNCH_CHECK("half_zero_kernel");

@@ -435,8 +435,6 @@ static size_t narrow_bytes(int64_t rows, int64_t cols) { return 2 * size_t(kNarr
 static hgnn_status orth_narrow(const char* who, int32_t count, const hgnn_grad* grads, int32_t steps, const float* coef, const float* scales, char* ws, hipStream_t s) {
   static uint64_t told = 0;
   constexpr int kBytes = (kNarrowRing + 6) * kNarrowTile;
-  const hgnn_status st = product_lds(reinterpret_cast<const void*>(&narrow_step_kernel), kBytes, &told);
-  if (st != HGNN_OK) return st;
   for (int i = 0; i < count;) {
     NarrowArgs a{};
     int64_t blocks = 0;
@@ -451,6 +449,8 @@ static hgnn_status orth_narrow(const char* who, int32_t count, const hgnn_grad* 
       ws += narrow_bytes(g.rows, g.cols);
     }
     if (a.count == 0) break;
+    const hgnn_status st = product_lds(reinterpret_cast<const void*>(&narrow_step_kernel), kBytes, &told);
+    if (st != HGNN_OK) return st;
     a.last = steps == 0;
     narrow_begin_kernel<<<unsigned(blocks), 1024, 0, s>>>(a);
     HGNN_LAUNCH_CHECK("narrow_begin_kernel");

@@ -117,7 +117,7 @@ def backward(hgnn, dev, c, extra=0, offset=0, dx=True, dw=True):
 
 
 SHAPES = [(1, 1, 1), (1, 8, 8), (3, 32, 16), (2, 33, 31), (16, 64, 64), (17, 40, 72), (1, 200, 300), (5, 7, 500), (64, 128, 64), (65, 31, 65), (63, 257, 129), (128, 128, 128), (129, 100, 200), (300, 41, 9),
-          (255, 96, 33), (1000, 64, 32), (513, 8, 130), (13, 1000, 77), (70, 515, 20), (4000, 16, 24)]
+          (255, 96, 33), (1000, 64, 32), (513, 8, 130), (13, 1000, 77), (70, 515, 20), (4000, 16, 24), (1, 1024, 640), (16, 2050, 33), (32, 700, 100), (33, 90, 47), (49, 1500, 64), (64, 33, 300)]
 
 
 @pytest.mark.parametrize("n,K,F", SHAPES)
@@ -139,7 +139,7 @@ def test_activations(hgnn, dev, act, trans):
 
 
 # (n, K, F) of each size of tile, with and without parts: few rows, a narrow side, tiles that fill the chip, and sizes around them
-@pytest.mark.parametrize("n,K,F", [(40, 700, 90), (700, 600, 500), (2100, 300, 700), (20000, 70, 20), (4099, 72, 2049), (8200, 40, 1100), (66000, 24, 40)])
+@pytest.mark.parametrize("n,K,F", [(40, 700, 90), (700, 600, 500), (2100, 300, 700), (20000, 70, 20), (4099, 72, 2049), (8200, 40, 1100), (66000, 24, 40), (17000, 128, 256), (16400, 256, 130), (16500, 99, 300), (8192, 520, 4100)])
 @pytest.mark.parametrize("trans", [False, True])
 def test_tiles(hgnn, dev, n, K, F, trans):
     c = Case(n, K, F, SILU, trans)
@@ -268,7 +268,7 @@ def test_refusals_of_the_binding(hgnn, dev):
     call = lambda x=x, g=w, u=w, y=y, ws=ws, **k: hgnn.hgnn_gated(x, g, u, y, workspace=ws, **k)  # noqa: E731
     call()
     bad = [lambda: call(x=x.float()), lambda: call(g=w.t()), lambda: call(g=h(64, 40)[:, :32]), lambda: call(y=h(99, 32)), lambda: call(act=4), lambda: call(act=-1), lambda: call(trans_w=True),
-           lambda: call(x=h(100, 66)[:, :64]), lambda: call(x=h(100, 72)[:, 4:68]), lambda: call(ws=None, x=h(2, 4000), g=h(4000, 32), u=h(4000, 32), y=h(2, 32)),
+           lambda: call(x=h(100, 66)[:, :64]), lambda: call(x=h(100, 72)[:, 4:68]), lambda: call(ws=None, x=h(100, 4000), g=h(4000, 32), u=h(4000, 32), y=h(100, 32)),
            lambda: call(x=h(100, 63), g=h(63, 32), u=h(63, 32)),
            lambda: call(x=torch.as_strided(h(99 * 64 + 61), (100, 61), (64, 1)), g=h(61, 32), u=h(61, 32)),  # no room behind the last row
            lambda: hgnn.hgnn_gated_grad(x, w, w, y, h(100, 64), h(64, 32), None, ws), lambda: hgnn.hgnn_gated_grad(x, w, w, y, h(100, 64), h(64, 32), h(64, 32), None),

@@ -59,13 +59,13 @@ def test_norm_gradient_refuses(lib, hgnn):
 
 def test_gated_refuses(lib, hgnn):
     EINVAL, EUNSUP = hgnn.HGNN_EINVAL, hgnn.HGNN_EUNSUPPORTED
-    need, need2 = hgnn.hgnn_gated_workspace(4, 4096, 64), hgnn.hgnn_gated_grad_workspace(4, 4096, 64)
+    need, need2 = hgnn.hgnn_gated_workspace(100, 4096, 64), hgnn.hgnn_gated_grad_workspace(100, 4096, 64)
     assert 0 < need <= need2
 
-    def call(n=4, K=4096, F=64, act=0, X=A, ldx=4096, Wg=B, Wu=C, ldw=64, trans=0, Y=D, ldy=64, ws=E, bytes=need):
+    def call(n=100, K=4096, F=64, act=0, X=A, ldx=4096, Wg=B, Wu=C, ldw=64, trans=0, Y=D, ldy=64, ws=E, bytes=need):
         return lib.hgnn_gated(n, K, F, act, X, ldx, Wg, Wu, ldw, trans, Y, ldy, ws, bytes, None)
 
-    def grad(n=4, K=4096, F=64, act=0, X=A, ldx=4096, Wg=B, Wu=C, ldw=64, trans=0, Y=D, ldy=64, dX=A, lddx=4096, dWg=B, dWu=C, lddw=64, ws=E, bytes=need2):
+    def grad(n=100, K=4096, F=64, act=0, X=A, ldx=4096, Wg=B, Wu=C, ldw=64, trans=0, Y=D, ldy=64, dX=A, lddx=4096, dWg=B, dWu=C, lddw=64, ws=E, bytes=need2):
         return lib.hgnn_gated_grad(n, K, F, act, X, ldx, Wg, Wu, ldw, trans, Y, ldy, dX, lddx, dWg, dWu, lddw, ws, bytes, None)
     for f, who in ((call, b"hgnn_gated"), (grad, b"hgnn_gated_grad")):
         for bad in (dict(n=-1), dict(K=0), dict(F=0), dict(act=4), dict(act=-1), dict(ldx=4088), dict(ldw=56), dict(ldy=56), dict(trans=1), dict(X=None), dict(Wg=None), dict(Wu=None), dict(Y=None), dict(ws=None),
