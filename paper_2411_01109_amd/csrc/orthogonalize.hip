@@ -68,6 +68,10 @@ struct GramOut {  // A, or b A where that is all of B
   __device__ Read read(int64_t, int64_t) const { return {}; }
   template <bool WHOLE>
   __device__ void put(int64_t, int64_t q, int64_t p, const Read&, const float4_t& v) const { to.put(q, p, v * factor, q / tile != p / tile); }
+  __device__ float4_t join(int64_t q, int64_t p, const float4_t& v) const {  // the value that stands at (q, p) then
+    to.put(q, p, v * factor, false);
+    return v * factor;
+  }
 };
 struct SquareOut {  // B = b A + c A A
   Pairs to, A;
@@ -77,6 +81,11 @@ struct SquareOut {  // B = b A + c A A
   __device__ Read read(int64_t q, int64_t p) const { return A.get(q, p); }
   template <bool WHOLE>
   __device__ void put(int64_t, int64_t q, int64_t p, const Read& x, const float4_t& v) const { to.put(q, p, x.value() * b + v * c, q / tile != p / tile); }
+  __device__ float4_t join(int64_t q, int64_t p, const float4_t& v) const {
+    const float4_t y = read(q, p).value() * b + v * c;
+    to.put(q, p, y, false);
+    return y;
+  }
 };
 struct StepOut {  // X = a X + B X
   Pairs to, X;
@@ -85,9 +94,13 @@ struct StepOut {  // X = a X + B X
   __device__ Read read(int64_t q, int64_t p) const { return X.get(q, p); }
   template <bool WHOLE>
   __device__ void put(int64_t, int64_t q, int64_t p, const Read& x, const float4_t& v) const { to.put(q, p, x.value() * a + v * (1.f / kA), false); }
+  __device__ float4_t join(int64_t q, int64_t p, const float4_t& v) const {
+    put<false>(0, q, p, read(q, p), v);
+    return v;
+  }
 };
 struct LastOut {  // the same into the caller's matrix
-  Pairs X;
+  Pairs X, to;  // to: not used
   float a, scale;
   void* out;
   int64_t ld, rows, cols;  // of X without its padding
@@ -106,6 +119,10 @@ struct LastOut {  // the same into the caller's matrix
       else static_cast<float*>(out)[at] = x[e];
     }
   }
+  __device__ float4_t join(int64_t q, int64_t p, const float4_t& v) const {
+    put<false>(0, q, p, read(q, p), v);
+    return v;
+  }
 };
 struct SumsPart {  // [parts][nq][np]
   float* part;
@@ -115,18 +132,44 @@ struct SumsPart {  // [parts][nq][np]
   template <bool WHOLE>
   __device__ void put(int64_t k, int64_t q, int64_t p, const Read&, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * np + p) = v; }
 };
+// The parts of 64 x 64 sums in order (blockIdx.x, of the tiles on and below the diagonal with `lower`), and what becomes of them; the mirror places get theirs through
+// LDS, in whole pieces (by twos the join of 1024 x 1024 took 11 us).
 template <class Out>
 __global__ __launch_bounds__(kBlock) void sums_join_kernel(const float* part, int parts, int64_t nq, int64_t np, int lower, Out out) {
-  const int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x, each = np / 4, q = t / each, p = 4 * (t - q * each);
-  if (q >= nq || (lower && p / lower > q / lower)) return;
-  const float* at = part + q * np + p;
-  float4_t v = *reinterpret_cast<const float4_t*>(at);
+  constexpr int kTile = 64;
+  __shared__ __align__(16) float tile[kTile][kTile + 4];
+  int64_t tq = blockIdx.x, tp = blockIdx.y;
+  if (lower && tp > tq) return;  // uniform
+  const int64_t q0 = tq * kTile, p0 = tp * kTile;
+  const bool mirror = lower && tp < tq;
+  float4_t v[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int64_t q = q0 + 16 * u + threadIdx.x / 16, p = p0 + 4 * (threadIdx.x % 16);
+    v[u] = float4_t{0.f, 0.f, 0.f, 0.f};
+    if (q >= nq || p >= np) continue;
+    const float* at = part + q * np + p;
 #pragma unroll 4
-  for (int k = 1; k < parts; ++k) {
-    at += nq * np;
-    v += *reinterpret_cast<const float4_t*>(at);
+    for (int k = 0; k < parts; ++k, at += nq * np) v[u] += *reinterpret_cast<const float4_t*>(at);
   }
-  out.template put<false>(0, q, p, out.read(q, p), v);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int r = 16 * u + threadIdx.x / 16, c = 4 * (threadIdx.x % 16);
+    const int64_t q = q0 + r, p = p0 + c;
+    if (q >= nq || p >= np) continue;
+    const float4_t y = out.join(q, p, v[u]);
+    if (mirror) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tile[c + e][r] = y[e];
+    }
+  }
+  if (!mirror) return;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int r = 16 * u + threadIdx.x / 16, c = 4 * (threadIdx.x % 16);
+    if (p0 + r < np && q0 + c < nq) out.to.put(p0 + r, q0 + c, *reinterpret_cast<const float4_t*>(&tile[r][c]), false);
+  }
 }
 
 // ---- the way in: the norm, X = G / |G|
@@ -258,6 +301,9 @@ template <bool PCOL>
 using SplitSmall = ProductShape<2, 2, 2, 2, kSplit, false, PCOL, 3>;
 template <bool PCOL>
 using SplitMid = ProductShape<2, 2, 4, 4, kSplit, false, PCOL, 2>;
+// ... and where there is at most one workgroup for a compute unit, all of its LDS for stages on their way
+template <bool PCOL>
+using SplitDeep = ProductShape<4, 2, 2, 4, kSplit, false, PCOL, 4>;
 constexpr int kOrthFull = 256;
 struct OrthSplit {
   int tile, parts;
@@ -269,9 +315,11 @@ static OrthSplit orth_split(int64_t nq, int64_t np, int64_t K, bool lower) {
     return lower ? l * (l + 1) / 2 : l * ceil_div(np, b);
   };
   OrthSplit s;
-  s.tile = tiles(128) < kOrthFull / 4 || nq <= 64 ? 64 : 128;
-  // a part of 1024 steps at least: sums that go through memory and another launch cost about as much
-  const int64_t t = tiles(s.tile), parts = t >= kOrthFull ? 1 : std::min(ceil_div(2 * kOrthFull, t), ceil_div(K, 1024));
+  // Tiles of 64 read LDS twice as often for their products: where a side is short, or where a compute unit has at most one of them and a short contraction (1024 x
+  // 1024, K = 1024, us: 136 of them 15, 36 of 128 in four parts 14 and the join 8; K = 4096: 136 in four parts 22.5 + 11, 36 of 128 in seven 20.5 + 10.5).  Parts until
+  // every compute unit has a workgroup, of 256 steps at least (a join costs about as much as those).
+  s.tile = std::min(nq, np) < 192 || (tiles(64) <= kOrthFull && K <= 1024) ? 64 : 128;
+  const int64_t t = tiles(s.tile), parts = t > kOrthFull / 2 || K <= 1024 ? 1 : std::min(kOrthFull / t, std::max<int64_t>(1, K / 256));
   s.part = std::max<int64_t>(32, up32(ceil_div(K, std::max<int64_t>(parts, 1))));
   s.parts = int(std::max<int64_t>(1, ceil_div(K, s.part)));
   return s;
@@ -348,6 +396,7 @@ __device__ __forceinline__ void narrow_multiply(float4_t (&acc)[2][2], const Q& 
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+      acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][u], a[1][t], acc[t][u], 0, 0, 0);
       acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][u], a[0][t], acc[t][u], 0, 0, 0);
       acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][u], a[1][t], acc[t][u], 0, 0, 0);
       acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][u], a[0][t], acc[t][u], 0, 0, 0);
@@ -420,7 +469,7 @@ __global__ __launch_bounds__(kBlock) void narrow_step_kernel(NarrowArgs a) {
   for (int s = 0; s < 2; ++s) narrow_multiply(Y, read_q, poly + s * kNarrowTile, read_columns, columns + s * kNarrowTile);
   const Pairs X{n.X, ld};
   if (a.last) {
-    const LastOut out{X, a.a, n.scale / kX, n.m.out, n.m.ldo, n.flip ? n.m.cols : n.m.rows, n.flip ? n.m.rows : n.m.cols, n.m.out_type, n.flip};
+    const LastOut out{X, X, a.a, n.scale / kX, n.m.out, n.m.ldo, n.flip ? n.m.cols : n.m.rows, n.flip ? n.m.rows : n.m.cols, n.m.out_type, n.flip};
     each([&](int q, int p, int t, int u) __attribute__((always_inline)) { out.put<false>(0, q, p0 + p, out.read(q, p0 + p), Y[t][u]); });
   } else {
     const StepOut out{Pairs{n.next, ld}, X, a.a};
@@ -469,13 +518,15 @@ static hgnn_status orth_product(const char* who, const Pairs& Q, const Pairs& P,
                                 hipStream_t s) {
   ProductArgs a{};
   a.Q0 = a.Q1 = Q.at, a.ldq = Q.ld, a.P0 = a.P1 = P.at, a.ldp = P.ld, a.nq = nq, a.np = np, a.K = K, a.part = split.part, a.parts = split.parts, a.lower = lower;
-  if (split.parts == 1) return split.tile == 64 ? product<SplitSmall<PCOL>>(who, a, out, s) : product<SplitMid<PCOL>>(who, a, out, s);
-  const SumsPart sums{part, nq, np};
-  const hgnn_status st = split.tile == 64 ? product<SplitSmall<PCOL>>(who, a, sums, s) : product<SplitMid<PCOL>>(who, a, sums, s);
+  const auto go = [&](const auto& to) {
+    if (split.tile == 64) return product<SplitSmall<PCOL>>(who, a, to, s);
+    product_tiles<SplitMid<PCOL>>(a);
+    return int64_t(a.tiles) * a.parts <= kOrthFull ? product<SplitDeep<PCOL>>(who, a, to, s) : product<SplitMid<PCOL>>(who, a, to, s);
+  };
+  if (split.parts == 1) return go(out);
+  const hgnn_status st = go(SumsPart{part, nq, np});
   if (st != HGNN_OK) return st;
-  const int64_t blocks = ceil_div(nq * (np / 4), kBlock);
-  HGNN_REQUIRE(blocks <= 0xffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
-  sums_join_kernel<<<unsigned(blocks), kBlock, 0, s>>>(part, split.parts, nq, np, lower ? split.tile : 0, out);
+  sums_join_kernel<<<dim3(unsigned(ceil_div(nq, 64)), unsigned(ceil_div(np, 64))), kBlock, 0, s>>>(part, split.parts, nq, np, lower, out);
   HGNN_LAUNCH_CHECK("sums_join_kernel");
   return HGNN_OK;
 }
@@ -506,7 +557,7 @@ static hgnn_status orth_matrix(const char* who, const hgnn_grad& g, int32_t step
     if (i + 1 < steps) st = orth_product<true>(who, B, X, z.m, z.k, z.m, false, z.step, part, StepOut{next, X, a}, s);
     else
       st = orth_product<true>(who, B, X, z.m, z.k, z.m, false, z.step, part,
-                              LastOut{X, a, scale / kX, m.out, m.ldo, std::min(g.rows, g.cols), std::max(g.rows, g.cols), m.out_type, z.flip}, s);
+                              LastOut{X, X, a, scale / kX, m.out, m.ldo, std::min(g.rows, g.cols), std::max(g.rows, g.cols), m.out_type, z.flip}, s);
     if (st != HGNN_OK) return st;
     std::swap(X, next);
   }

@@ -17,6 +17,7 @@
 // from LDS, and that is what bounds the large shape (256 x 256: 8 waves of 128 x 64, (128 + 64) 64 bytes a step for 32 products of 16 cycles).
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -38,8 +39,8 @@ struct ProductArgs {
   int64_t nq, np;   // items
   int64_t K;        // of a segment
   int64_t part;     // contraction steps of a workgroup (blocks beyond the first take the next ones); a multiple of 64 (kSplit: 32), or K where there is one part
-  int64_t tiles;    // of C, tiles_p of them on a line
-  int32_t tiles_p;
+  int32_t tiles;    // of C, lines of tiles_p of them
+  int32_t lines, tiles_p;
   int32_t parts;
   int32_t lower;    // square C of square tiles: those on and below the diagonal alone
 };
@@ -118,16 +119,16 @@ __device__ __forceinline__ void product_loads(ProductLoads<N, COL>& s, const hal
 }
 
 // where tile number t of C lies: groups of kGroup lines of tiles, walked along the lines' items, so that workgroups that run together share operands
-__device__ __forceinline__ void product_tile(const ProductArgs& a, int64_t t, int64_t& tq, int64_t& tp) {
+__device__ __forceinline__ void product_tile(const ProductArgs& a, uint32_t t, uint32_t& tq, uint32_t& tp) {
   if (a.lower) {  // t = tq (tq + 1) / 2 + tp
-    int64_t r = int64_t((sqrtf(8.f * float(t) + 1.f) - 1.f) * 0.5f);
+    uint32_t r = uint32_t((sqrtf(8.f * float(t) + 1.f) - 1.f) * 0.5f);
     while (r * (r + 1) / 2 > t) --r;
     while ((r + 1) * (r + 2) / 2 <= t) ++r;
     tq = r, tp = t - r * (r + 1) / 2;
     return;
   }
-  constexpr int64_t kGroup = 8;
-  const int64_t lines = a.tiles / a.tiles_p, per = kGroup * a.tiles_p, g = t / per, in = t - g * per, rows = min(kGroup, lines - g * kGroup);
+  constexpr uint32_t kGroup = 8;
+  const uint32_t per = kGroup * uint32_t(a.tiles_p), g = t / per, in = t - g * per, rows = min(kGroup, uint32_t(a.lines) - g * kGroup);
   tp = in / rows;
   tq = g * kGroup + (in - tp * rows);
 }
@@ -168,11 +169,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs a, 
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int i = lane & 15, qq = lane >> 4;
   // consecutive workgroups go to the XCDs in turn: each takes a run of tiles of its own
-  const int64_t all = a.tiles * a.parts, id = blockIdx.x, x = id & 7, base = all >> 3, more = all & 7;
-  const int64_t work = x * base + min(x, more) + (id >> 3);
-  const int64_t part = __builtin_amdgcn_readfirstlane(int(work / a.tiles));
-  int64_t tq, tp;
-  product_tile(a, work - part * a.tiles, tq, tp);
+  const uint32_t all = gridDim.x, id = blockIdx.x, x = id & 7, more = all & 7;
+  const uint32_t work = x * (all >> 3) + min(x, more) + (id >> 3);
+  const int64_t part = __builtin_amdgcn_readfirstlane(int(a.parts == 1 ? 0 : work / uint32_t(a.tiles)));
+  uint32_t tq, tp;
+  product_tile(a, work - uint32_t(part) * uint32_t(a.tiles), tq, tp);
   // (the divisions go through vector registers: back to scalar ones, which the loads to LDS take their places from)
   const int64_t q0 = int64_t(__builtin_amdgcn_readfirstlane(int(tq))) * S::BQ, p0 = int64_t(__builtin_amdgcn_readfirstlane(int(tp))) * S::BP;
   const int64_t k_begin = part * a.part, k_end = min(a.K, k_begin + a.part), count = k_end - k_begin;  // of a segment
@@ -354,9 +355,10 @@ struct ProductNothing {};
 // tiles and workgroups of a product, and its launch
 template <class S>
 inline void product_tiles(ProductArgs& a) {
-  const int64_t lines = ceil_div(a.nq, S::BQ);
-  a.tiles_p = int32_t(ceil_div(a.np, S::BP));
-  a.tiles = a.lower ? lines * (lines + 1) / 2 : lines * a.tiles_p;
+  const int64_t lines = ceil_div(a.nq, S::BQ), tiles_p = ceil_div(a.np, S::BP);
+  const int64_t tiles = a.lower ? lines * (lines + 1) / 2 : lines * tiles_p;
+  a.lines = int32_t(lines), a.tiles_p = int32_t(tiles_p);
+  a.tiles = int32_t(std::min<int64_t>(tiles, 0x7fffffff));
 }
 // beyond 64 KB of dynamic LDS the runtime wants to be told, once for a kernel and a device (told: a bit a device; two threads write the same at worst)
 inline hgnn_status product_lds(const void* kernel, int bytes, uint64_t* told) {
@@ -371,11 +373,11 @@ inline hgnn_status product_lds(const void* kernel, int bytes, uint64_t* told) {
 template <class S, class Epilogue>
 inline hgnn_status product(const char* who, ProductArgs& a, const Epilogue& e, hipStream_t s) {
   product_tiles<S>(a);
-  HGNN_REQUIRE(a.tiles * a.parts <= 0x7ffffe, HGNN_EUNSUPPORTED, "%s: grid too large", who);
+  HGNN_REQUIRE(int64_t(a.tiles) * a.parts <= 0x7ffffe, HGNN_EUNSUPPORTED, "%s: grid too large", who);
   static uint64_t told = 0;
   const hgnn_status st = product_lds(reinterpret_cast<const void*>(&product_kernel<S, Epilogue>), S::kLds, &told);
   if (st != HGNN_OK) return st;
-  product_kernel<S, Epilogue><<<dim3(unsigned(a.tiles * a.parts)), S::kThreads, S::kLds, s>>>(a, e);
+  product_kernel<S, Epilogue><<<dim3(unsigned(a.tiles) * unsigned(a.parts)), S::kThreads, S::kLds, s>>>(a, e);
   HGNN_LAUNCH_CHECK("product_kernel");
   return HGNN_OK;
 }
