@@ -605,7 +605,9 @@ static hgnn_status check_gated(const char* who, int64_t n, int32_t K, int32_t F,
   HGNN_REQUIRE(K <= 65536 && F <= 65536 && n < (int64_t(1) << 31), HGNN_EUNSUPPORTED, "%s: K = %d / F = %d above 65536, or n = %lld from 2^31 on", who, K, F, static_cast<long long>(n));
   return HGNN_OK;
 }
-static bool fits(const void* p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
+// (a tile's places are kept as 32-bit offsets from its first)
+constexpr int64_t kMostPitch = int64_t(1) << 22;
+static bool fits(const void* p, int64_t ld) { return aligned16(p) && ld % 8 == 0 && ld <= kMostPitch; }
 
 }  // namespace hgnn
 
@@ -626,7 +628,7 @@ hgnn_status hgnn_gated(int64_t n, int32_t K, int32_t F, hgnn_activation act, con
   if (st != HGNN_OK) return st;
   if (n == 0) return HGNN_OK;
   HGNN_REQUIRE(X && Wg && Wu && Y, HGNN_EINVAL, "%s: NULL argument", who);
-  HGNN_REQUIRE(fits(X, ldx) && fits(Wg, ldw) && fits(Wu, ldw) && fits(Y, ldy), HGNN_EUNSUPPORTED, "%s: needs 16-byte aligned tensors and pitches that are multiples of 8", who);
+  HGNN_REQUIRE(fits(X, ldx) && fits(Wg, ldw) && fits(Wu, ldw) && fits(Y, ldy), HGNN_EUNSUPPORTED, "%s: needs 16-byte aligned tensors and pitches that are multiples of 8, up to 2^22", who);
   const GatedSizes z = gated_sizes(n, K, F);
   HGNN_REQUIRE(z.gate_part == 0 || (workspace && workspace_bytes >= z.gate_part && aligned16(workspace)), HGNN_EINVAL,
                "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_gated_workspace)", who, workspace_bytes, z.gate_part);
@@ -651,7 +653,7 @@ hgnn_status hgnn_gated_grad(int64_t n, int32_t K, int32_t F, hgnn_activation act
   HGNN_REQUIRE((dWg == nullptr) == (dWu == nullptr), HGNN_EINVAL, "%s: dWg and dWu go together", who);
   HGNN_REQUIRE((!dX || lddx >= K) && (!dWg || lddw >= (trans_w ? K : F)), HGNN_EINVAL, "%s: leading dimension smaller than the row", who);
   HGNN_REQUIRE((!dX || fits(dX, lddx)) && (!dWg || (fits(dWg, lddw) && fits(dWu, lddw))), HGNN_EUNSUPPORTED,
-               "%s: needs 16-byte aligned tensors and pitches that are multiples of 8", who);
+               "%s: needs 16-byte aligned tensors and pitches that are multiples of 8, up to 2^22", who);
   HGNN_REQUIRE(!dWg || dWg != dWu, HGNN_EINVAL, "%s: the same output twice", who);
   const bool trans = trans_w != 0;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -671,7 +673,7 @@ hgnn_status hgnn_gated_grad(int64_t n, int32_t K, int32_t F, hgnn_activation act
   }
   HGNN_REQUIRE(X && Wg && Wu && dY, HGNN_EINVAL, "%s: NULL argument", who);
   HGNN_REQUIRE(fits(X, ldx) && fits(Wg, ldw) && fits(Wu, ldw) && fits(dY, lddy), HGNN_EUNSUPPORTED,
-               "%s: needs 16-byte aligned tensors and pitches that are multiples of 8", who);
+               "%s: needs 16-byte aligned tensors and pitches that are multiples of 8, up to 2^22", who);
   const GatedSizes z = gated_sizes(n, K, F);
   const size_t need = hgnn_gated_grad_workspace(n, K, F);
   HGNN_REQUIRE(workspace && workspace_bytes >= need && aligned16(workspace), HGNN_EINVAL, "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_gated_grad_workspace)", who,

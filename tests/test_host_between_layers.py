@@ -25,7 +25,7 @@ def test_norm_refuses(lib, hgnn):
     def call(n=4, F=8, kind=F16, R=B, ldr=8, Y=C, ldy=8, H=D, ldh=8, Z=E, ldz=8, none=False, **b):
         return lib.hgnn_residual_norm(n, F, None if none else block(hgnn, **b), kind, R, ldr, Y, ldy, H, ldh, Z, ldz, None)
     for bad in (dict(n=-1), dict(F=0), dict(none=True), dict(kind=2), dict(post=3), dict(pre=-1), dict(ldr=7), dict(ldy=7), dict(ldh=7), dict(ldz=7), dict(alpha=NAN), dict(alpha=INF),
-                dict(eps=0.0), dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(post=NONE), dict(post=NONE, post_w=None), dict(pre=NONE, Z=None), dict(pre=NONE, pre_w=None, pre_b=None),
+                dict(eps=0.0), dict(eps=1e-39), dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(post=NONE), dict(post=NONE, post_w=None), dict(pre=NONE, Z=None), dict(pre=NONE, pre_w=None, pre_b=None),
                 dict(gate_rows=A, ld_gate=8), dict(gate=None, gate_rows=A, ld_gate=7), dict(Y=None), dict(Z=None), dict(R=None, Y=None, post=NONE, post_w=None, post_b=None, gate=None),
                 dict(R=B + 1), dict(kind=F32, R=B + 2), dict(Y=C + 1), dict(H=D + 1), dict(Z=E + 1), dict(post_w=A + 2), dict(post_b=A + 1), dict(gate=A + 2), dict(pre_w=A + 3), dict(pre_b=A + 2),
                 dict(gate=None, gate_rows=A + 1, ld_gate=8), dict(H=B, ldh=16), dict(H=None, Z=None, pre=NONE, pre_w=None, pre_b=None)):
@@ -72,7 +72,9 @@ def test_gated_refuses(lib, hgnn):
                     dict(bytes=need - 1), dict(ws=E + 8)):
             assert f(**bad) == EINVAL, bad
             assert who in lib.hgnn_last_error()
-        for no in (dict(X=A + 2), dict(Wg=B + 8), dict(Wu=C + 2), dict(Y=D + 4), dict(ldx=4100), dict(ldw=66), dict(ldy=68), dict(K=65537, ldx=65544), dict(F=65537, ldw=65544, ldy=65544), dict(n=1 << 31)):
+        for no in (dict(X=A + 2), dict(Wg=B + 8), dict(Wu=C + 2), dict(Y=D + 4), dict(ldx=4100), dict(ldw=66), dict(ldy=68), dict(K=65537, ldx=65544),
+                   dict(F=65537, ldw=65544, ldy=65544), dict(n=1 << 31), dict(ldx=(1 << 22) + 8), dict(ldw=1 << 23),
+                   dict(ldy=1 << 40)):
             assert f(**no) == EUNSUP, no
     for bad in (dict(dWg=None), dict(dWu=None), dict(dWu=B), dict(lddx=4088), dict(lddw=56)):
         assert grad(**bad) == EINVAL, bad
