@@ -188,13 +188,14 @@ struct Split {
   int parts;
   int64_t part;  // contraction steps of a part
 };
-// nq x np sums over K steps (`two`: a pair of each).  Parts of at least 128 steps until the chip has two workgroups a compute unit.
+// nq x np sums over K steps (`two`: a pair of each).  Parts of at least 128 steps until every compute unit has a workgroup.
 static Split split_of(int64_t nq, int64_t np, int64_t K, bool two) {
   const auto tiles = [&](int64_t b) { return ceil_div(nq, b) * ceil_div(np, two ? b / 2 : b); };
   Split s;
   s.size = nq <= 64 || np <= (two ? 32 : 64) ? kFew : K >= kLong && tiles(256) >= kFull ? kWide : kMid;
   const int64_t t = s.size == kFew ? ceil_div(nq, 64) * ceil_div(np, 64) : tiles(s.size == kWide ? 256 : 128);
-  int64_t parts = t >= kFull ? 1 : std::min(ceil_div(2 * kFull, t), ceil_div(K, 128));
+  // two thirds of the units busy are enough: parts go through memory and another launch (9611 x 1402 -> 91, 152 tiles in four parts 28 us)
+  const int64_t parts = std::min(3 * t > 2 * kFull ? int64_t(1) : ceil_div(kFull, t), ceil_div(K, 128));
   s.part = std::max<int64_t>(64, up(ceil_div(K, std::max<int64_t>(parts, 1)), 64));
   s.parts = int(std::max<int64_t>(1, ceil_div(K, s.part)));
   return s;
@@ -211,9 +212,10 @@ struct GatedRowsArgs {
   int64_t ldx, ldw, n;
   int32_t K, F, chunks;  // of features: a workgroup takes number blockIdx.x % chunks
 };
-template <int KS_, int TP_, bool PCOL_, int RING_>
-struct GatedRowsShape {  // KS: 64 steps of the contraction, TP: 16 features of a wave
-  static constexpr int KS = KS_, TP = TP_, kRing = RING_, kFeatures = 16 * TP * kRowsWaves, kStage = KS * kRowsTile * 128;
+template <int KS_, int TP_, int WF_, bool PCOL_, int RING_>
+struct GatedRowsShape {  // KS: 64 steps of the contraction, TP: 16 features of a wave, WF: waves beside each other along the features, the others take other rows of the tile
+  static constexpr int KS = KS_, TP = TP_, WF = WF_, kRing = RING_, kFeatures = 16 * TP * WF, kStage = KS * kRowsTile * 128;
+  static constexpr int kGroups = kRowsWaves / WF, kBlocks = kRowsTile / 16 / kGroups;  // of waves along the rows, of 16 rows of a wave
   static constexpr bool PCOL = PCOL_;
   static constexpr int kWeights = KS * 2 * kFeatures * 128;
   static constexpr int kLds = kWeights > RING_ * kStage ? kWeights : RING_ * kStage;
@@ -251,9 +253,11 @@ __global__ __launch_bounds__(S::kThreads) void gated_rows_kernel(GatedRowsArgs a
     asm volatile("" ::: "memory");
   };
   half8_t weight[2][TP][2 * KS];
+  const int wf = wave % S::WF, group = wave / S::WF;
   {  // both weights' features of the workgroup into LDS, and a wave's into its registers
     constexpr int kOperand = S::kFeatures * 128;  // 64 steps of one weight
-    constexpr int N = 2 * S::kFeatures / 8 / kRowsWaves;
+    constexpr int N = (2 * S::kFeatures / 8 + kRowsWaves - 1) / kRowsWaves;
+    static_assert(2 * S::kFeatures / 8 % kRowsWaves == 0, "kilobytes of a wave");
     if (wave < kRowsWaves) {
       ProductLoads<N, S::PCOL> l;
       product_loads<N, S::PCOL, false, kRowsWaves>(l, a.Wg, a.Wu, a.ldw, f0, a.F, 0, wave, lane, S::kFeatures / 8);
@@ -271,7 +275,7 @@ __global__ __launch_bounds__(S::kThreads) void gated_rows_kernel(GatedRowsArgs a
         for (int u = 0; u < TP; ++u)
 #pragma unroll
           for (int h = 0; h < 2 * KS; ++h) {
-            half8_t v = gated_weight<S::PCOL, TP>(lds + (h / 2) * 2 * kOperand + o * kOperand, wave, lane, u, h % 2);
+            half8_t v = gated_weight<S::PCOL, TP>(lds + (h / 2) * 2 * kOperand + o * kOperand, wf, lane, u, h % 2);
             // what stands behind the contraction's end inside a piece is the caller's padding
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -304,29 +308,29 @@ __global__ __launch_bounds__(S::kThreads) void gated_rows_kernel(GatedRowsArgs a
     }
     return;
   }
-  const ProductReads<false, false, kRowsTile / 16> read(0, lane);
+  const ProductReads<false, false, kRowsTile / 16> read(S::kGroups > 1 ? group : 0, lane);
   // behind the contraction's end inside a piece: nothing of the rows, either
   const int h_end = a.K / 32, e_end = a.K - 32 * h_end - 8 * qq;
   const bool ragged = a.K & 7;
-  const int64_t p0 = f0 + 16 * TP * wave + 4 * TP * qq;
-  const bool whole_p = f0 + 16 * TP * (wave + 1) <= a.F;  // uniform
+  const int64_t p0 = f0 + 16 * TP * wf + 4 * TP * qq;
+  const bool whole_p = f0 + 16 * TP * (wf + 1) <= a.F;  // uniform
   for (int t = 0; t < mine; ++t) {
     const int64_t row0 = (int64_t(first) + int64_t(t) * stride) * kRowsTile;
     meet();
     const unsigned char* const stage = lds + (t % S::kRing) * S::kStage;
     const auto tile = [&](auto whole, auto cut) __attribute__((always_inline)) {
       constexpr bool kWhole = decltype(whole)::value, kCut = decltype(cut)::value;
-      typename Out::Read early[kRowsTile / 16][TP];
+      typename Out::Read early[S::kBlocks][TP];
       const auto each = [&](int x, auto&& f) __attribute__((always_inline)) {
-        const int64_t q = row0 + 16 * x + i;
+        const int64_t q = row0 + 16 * (x * S::kGroups + group) + i;
 #pragma unroll
         for (int u = 0; u < TP; ++u)
           if (kWhole || (q < a.n && p0 + 4 * u < a.F)) f(q, p0 + 4 * u, u);
       };
 #pragma unroll
-      for (int x = 0; x < kRowsTile / 16; ++x) each(x, [&](int64_t q, int64_t p, int u) __attribute__((always_inline)) { early[x][u] = out.read(q, p); });
+      for (int x = 0; x < S::kBlocks; ++x) each(x, [&](int64_t q, int64_t p, int u) __attribute__((always_inline)) { early[x][u] = out.read(q, p); });
 #pragma unroll
-      for (int x = 0; x < kRowsTile / 16; ++x) {
+      for (int x = 0; x < S::kBlocks; ++x) {
         float4_t acc[2][TP];
 #pragma unroll
         for (int o = 0; o < 2; ++o)
@@ -334,7 +338,7 @@ __global__ __launch_bounds__(S::kThreads) void gated_rows_kernel(GatedRowsArgs a
           for (int u = 0; u < TP; ++u) acc[o][u] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int h = 0; h < 2 * KS; ++h) {
-          half8_t v = read.get(stage + (h / 2) * (kRowsTile * 128), x, h % 2);
+          half8_t v = read.get(stage + (h / 2) * (kRowsTile * 128), x * S::kGroups, h % 2);
           if (kCut && h == h_end) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -533,7 +537,7 @@ static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
   z.gate = split_of(n, F, K, true);
   z.dx = split_of(n, K, F, false);
   z.dw = split_of(K, 2 * z.Fp, n, false);
-  z.rows = K <= 256 && F <= 2048 && n >= kManyRows;
+  z.rows = K <= 256 && n >= kManyRows;
   z.gate_part = z.gate.parts > 1 && !z.rows && n > kFewRows ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
   z.dx_part = z.dx.parts > 1 ? size_t(z.dx.parts) * size_t(n) * size_t(up(K, 4)) * 4 : 0;
   z.dw_part = z.dw.parts > 1 ? size_t(z.dw.parts) * size_t(up(K, 4)) * 2 * size_t(z.Fp) * 4 : 0;
@@ -559,9 +563,10 @@ static hgnn_status gated_pairs(const char* who, const GatedSizes& z, const half_
     GatedRowsArgs r{X, Wg, Wu, ldx, ldw, z.n, z.K, z.F, 1};
     const auto go = [&](auto pcol) -> hgnn_status {
       constexpr bool P = decltype(pcol)::value;
-      if (z.K <= 64) return gated_rows<GatedRowsShape<1, 2, P, 4>>(who, r, out, s);
-      if (z.K <= 128) return gated_rows<GatedRowsShape<2, 2, P, 4>>(who, r, out, s);
-      return gated_rows<GatedRowsShape<4, 1, P, 3>>(who, r, out, s);
+      if (z.K <= 64) return z.F <= 64 ? gated_rows<GatedRowsShape<1, 2, 2, P, 4>>(who, r, out, s) : z.F <= 128 ? gated_rows<GatedRowsShape<1, 2, 4, P, 4>>(who, r, out, s) : gated_rows<GatedRowsShape<1, 2, 8, P, 4>>(who, r, out, s);
+      if (z.K <= 128) return z.F <= 64 ? gated_rows<GatedRowsShape<2, 2, 2, P, 4>>(who, r, out, s) : z.F <= 128 ? gated_rows<GatedRowsShape<2, 2, 4, P, 4>>(who, r, out, s) : gated_rows<GatedRowsShape<2, 2, 8, P, 4>>(who, r, out, s);
+      if (z.F <= 64) return gated_rows<GatedRowsShape<4, 1, 4, P, 3>>(who, r, out, s);
+      return z.K <= 192 ? gated_rows<GatedRowsShape<3, 1, 8, P, 3>>(who, r, out, s) : gated_rows<GatedRowsShape<4, 1, 8, P, 3>>(who, r, out, s);
     };
     return trans ? go(std::false_type()) : go(std::true_type());
   }

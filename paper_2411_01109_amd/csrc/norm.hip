@@ -414,14 +414,14 @@ __global__ __launch_bounds__(kSumCols* kSumRows) void block_sums_kernel(BlockSum
     const float* const in = a.part + int64_t(k) * a.pitch + col;
     const int64_t stride = int64_t(kVectors) * a.pitch;
     int j = y;
-    for (; j + 7 * kSumRows < a.parts; j += 8 * kSumRows) {
-      float v[8];
+    constexpr int U = 16;  // on their way at a time
+    for (; j < a.parts; j += U * kSumRows) {
+      float v[U];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = in[(j + u * kSumRows) * stride];
+      for (int u = 0; u < U; ++u) v[u] = j + u * kSumRows < a.parts ? in[(j + u * kSumRows) * stride] : 0.f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) s += v[u];
+      for (int u = 0; u < U; ++u) s += v[u];
     }
-    for (; j < a.parts; j += kSumRows) s += in[j * stride];
   }
   lds[y][x] = s;
   __syncthreads();
@@ -466,10 +466,11 @@ template <class S>
 static int64_t resident(int waves) {
   return kUnits * int64_t(std::max(1, waves * 4 * kWave / S::kThreads));
 }
-// ... of the gradients: each with rows enough that its partial sums (as many bytes as three rows or so) cost little.
+// ... of the gradients: each with rows enough that its partial sums (as many bytes as three rows or so) cost little, up to eight in a row where a row is a wave's or more;
+// few rows are dealt out one by one, since their time is that of a chain of rows (72 rows of 4096 in fp32, eight in a row 37 us).
 template <class S>
 static int64_t grad_blocks(int64_t n, hgnn_type type) {
-  const int64_t per = std::max(S::kRows, S::kLanes >= 64 ? 8 : 1);
+  const int64_t per = std::max<int64_t>(S::kRows, S::kLanes >= 64 ? std::min<int64_t>(8, ceil_div(n, kUnits)) : 1);
   return std::max<int64_t>(1, std::min(resident<S>(type == HGNN_F16 ? 3 : 2), ceil_div(n, per)));
 }
 

@@ -342,10 +342,11 @@ static OrthSizes orth_sizes(int64_t rows, int64_t cols) {
   return z;
 }
 
-// ---- matrices of at most 64 x 1024: a launch for a step of all of them.  A workgroup owns 64 columns of X, forms A and B by itself (each of a matrix's workgroups
-// the same: their sums over up to 1024 columns out of the L2 cost less than two launches more) and multiplies its columns.  X is padded to 64 rows and whole
-// 64 columns.  Four waves, 32 x 32 of the 64 x 64 each; A and B stand in LDS as the products read them.
-constexpr int kNarrowM = 64, kNarrowK = 1024, kNarrowMany = 24, kNarrowRing = 6, kNarrowTile = 64 * 128;
+// ---- matrices of at most 64 x 4096: a launch for a step of all of them.  A workgroup owns 64 columns of X, forms A and B by itself (each of a matrix's workgroups
+// the same: their sums over the columns out of the L2 cost less than two launches more) and multiplies its columns.  X is padded to 64 rows and whole 64 columns.
+// Two teams of four waves take 32 of 64 steps of A each, 32 x 32 of the 64 x 64 a wave; behind that a wave has 32 x 16.  A and B stand in LDS as the products read
+// them.  (One team, five matrices of up to 608 x 64: 10.7 us a step.)  The low parts' product is formed here, too: it costs nothing beside the rest.
+constexpr int kNarrowM = 64, kNarrowK = 4096, kNarrowMany = 24, kNarrowRing = 5, kNarrowTile = 64 * 128, kNarrowWaves = 8;
 struct NarrowMatrix {
   OrthMatrix m;
   half_t *X, *next;
@@ -385,95 +386,130 @@ __device__ __forceinline__ void narrow_put(unsigned char* at, int q, int p, cons
   *reinterpret_cast<half4_t*>(line + (piece ^ turn) * 16) = h;
   *reinterpret_cast<half4_t*>(line + ((piece + 4) ^ turn) * 16) = l;
 }
-template <class Q, class P>
-__device__ __forceinline__ void narrow_multiply(float4_t (&acc)[2][2], const Q& q, const unsigned char* qs, const P& p, const unsigned char* ps) {
-  half8_t a[2][2], b[2][2];  // [part][16 items]
-#pragma unroll
-  for (int o = 0; o < 2; ++o)
-#pragma unroll
-    for (int t = 0; t < 2; ++t) a[o][t] = q.get(qs, t, o), b[o][t] = p.get(ps, t, o);
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][u], a[1][t], acc[t][u], 0, 0, 0);
-      acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1][u], a[0][t], acc[t][u], 0, 0, 0);
-      acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][u], a[1][t], acc[t][u], 0, 0, 0);
-      acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][u], a[0][t], acc[t][u], 0, 0, 0);
-    }
+__device__ __forceinline__ float4_t narrow_get(const unsigned char* at, int q, int p) {
+  const unsigned char* const line = at + (p >> 5) * kNarrowTile + q * 128 + (p & 4) * 2;
+  const int piece = (p & 31) >> 3, turn = (q & 15) >> 1;
+  return Pairs::Four{*reinterpret_cast<const half4_t*>(line + (piece ^ turn) * 16), *reinterpret_cast<const half4_t*>(line + ((piece + 4) ^ turn) * 16)}.value();
 }
-__global__ __launch_bounds__(kBlock) void narrow_step_kernel(NarrowArgs a) {
+// 32 x 16 U sums, 32 steps
+template <int U>
+__device__ __forceinline__ void narrow_multiply(float4_t (&acc)[2][U], const half8_t (&a)[2][2], const half8_t (&b)[2][U]) {  // [part][16 items]
+#pragma unroll
+  for (int k = 3; k >= 0; --k)  // low low, then low high, high low, high high
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int u = 0; u < U; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k >> 1][u], a[k & 1][t], acc[t][u], 0, 0, 0);
+}
+__global__ __launch_bounds__(kNarrowWaves* kWave) void narrow_step_kernel(NarrowArgs a) {
   extern __shared__ __align__(1024) unsigned char lds[];
-  unsigned char *const columns = lds + kNarrowRing * kNarrowTile, *const gram = columns + 2 * kNarrowTile, *const poly = gram + 2 * kNarrowTile;
+  constexpr int kStage = 2 * kNarrowTile;  // 64 steps
+  unsigned char *const columns = lds + kNarrowRing * kStage, *const gram = columns + 2 * kNarrowTile, *const poly = gram + 2 * kNarrowTile;
   const NarrowMatrix& n = narrow_matrix(a, blockIdx.x);
-  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wq = wave >> 1, wp = wave & 1, i = lane & 15, qq = lane >> 4;
-  const int k = n.k, steps = k / 32, p0 = 64 * (int(blockIdx.x) - n.first);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, qq = lane >> 4;
+  const int k = n.k, steps = k / 64, p0 = 64 * (int(blockIdx.x) - n.first);
   const int64_t ld = 2 * int64_t(k);
   const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) unsigned char*)lds)) + wave * 1024;
   const half_t* const x = n.X;
   {  // the workgroup's own columns, 64 steps
-    ProductLoads<2, true> own;
-    product_loads<2, true, true, kWavesPerBlock>(own, x, x, ld, p0, k, 0, wave, lane, 8);
+    ProductLoads<1, true> own;
+    product_loads<1, true, true, kNarrowWaves>(own, x, x, ld, p0, k, 0, wave, lane, 8);
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) load_to_lds(own.base[j] + s * own.inc, own.off[j], lds0 + (kNarrowRing + s) * kNarrowTile + j * 4096);
+    for (int s = 0; s < 2; ++s) load_to_lds(own.base[0] + s * own.inc, own.off[0], lds0 + kNarrowRing * kStage + s * kNarrowTile);
   }
-  ProductLoads<2, false> lines;
-  product_loads<2, false, true, kWavesPerBlock>(lines, x, x, ld, 0, kNarrowM, 0, wave, lane, 8);
+  ProductLoads<1, false> lines;
+  product_loads<1, false, true, kNarrowWaves>(lines, x, x, ld, 0, kNarrowM, 0, wave, lane, 8);
   uint32_t to = lds0;
   const auto ask = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) load_to_lds(lines.base[j], lines.off[j], to + j * 4096), lines.base[j] += lines.inc;
-    to += kNarrowTile;
-    if (to >= lds0 + kNarrowRing * kNarrowTile) to -= kNarrowRing * kNarrowTile;
+    load_to_lds(lines.base[0], lines.off[0], to);
+    load_to_lds(lines.base[0] + lines.inc, lines.off[0], to + kNarrowTile);
+    lines.base[0] += 2 * lines.inc;
+    to += kStage;
+    if (to >= lds0 + kNarrowRing * kStage) to -= kNarrowRing * kStage;
   };
-  const ProductReads<false, true, 2> read_q(2 * wq, lane), read_p(2 * wp, lane);
-  const ProductReads<true, true, 2> read_columns(2 * wp, lane);
   const float4_t none = {0.f, 0.f, 0.f, 0.f};
-  float4_t A[2][2] = {{none, none}, {none, none}}, B[2][2] = {{none, none}, {none, none}};
   int asked = 0;
   for (; asked < kNarrowRing - 1 && asked < steps; ++asked) ask();
-  const unsigned char* stage = lds;
-  for (int s = 0; s < steps; ++s) {
-    const int behind = asked - 1 - s;
-    if (behind >= 4) product_wait<8>();
-    else if (behind == 3) product_wait<6>();
-    else if (behind == 2) product_wait<4>();
-    else if (behind == 1) product_wait<2>();
-    else product_wait<0>();
-    if (asked < steps) ask(), ++asked;  // into the place of the stage before, which all waves have left
-    narrow_multiply(A, read_q, stage, read_p, stage);
-    stage += kNarrowTile;
-    if (stage >= columns) stage = lds;
+  {
+    const int team = wave >> 2, wq = (wave >> 1) & 1, wp = wave & 1;
+    const ProductReads<false, true, 2> read_q(2 * wq, lane), read_p(2 * wp, lane);
+    float4_t A[2][2] = {{none, none}, {none, none}};
+    const unsigned char* stage = lds + team * kNarrowTile;
+    for (int s = 0; s < steps; ++s) {
+      const int behind = asked - 1 - s;
+      if (behind >= 3) product_wait<6>();
+      else if (behind == 2) product_wait<4>();
+      else if (behind == 1) product_wait<2>();
+      else product_wait<0>();
+      if (asked < steps) ask(), ++asked;  // into the place of the stage before, which all waves have left
+      half8_t u[2][2], v[2][2];
+#pragma unroll
+      for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) u[o][t] = read_q.get(stage, t, o), v[o][t] = read_p.get(stage, t, o);
+      narrow_multiply<2>(A, u, v);
+      stage += kStage;
+      if (stage >= columns) stage -= kNarrowRing * kStage;
+    }
+    // the second team's sums to the first through what is B's place later
+    float4_t* const over = reinterpret_cast<float4_t*>(poly) + (wave & 3) * 4 * kWave + lane;
+    if (team == 1) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) over[t * kWave] = A[t >> 1][t & 1];
+    }
+    __syncthreads();
+    if (team == 0) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        narrow_put(gram, 16 * (2 * wq + (t >> 1)) + i, 16 * (2 * wp + (t & 1)) + 4 * qq, (A[t >> 1][t & 1] + over[t * kWave]) * (kA / (kX * kX)));
+    }
+    __syncthreads();
   }
-  const auto each = [&](auto&& f) __attribute__((always_inline)) {
+  const int wq = wave >> 2, wp = wave & 3, p = 16 * wp + 4 * qq;
+  const ProductReads<false, true, 2> read_q(2 * wq, lane);
+  const ProductReads<false, true, 1> read_p(wp, lane);
+  const auto q_of = [&](int t) { return 16 * (2 * wq + t) + i; };
+  float4_t B[2][1] = {{none}, {none}}, Y[2][1] = {{none}, {none}};
+  const auto lines_of = [&](const unsigned char* at, half8_t (&u)[2][2]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int o = 0; o < 2; ++o)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) f(16 * (2 * wq + t) + i, 16 * (2 * wp + u) + 4 * qq, t, u);
+      for (int t = 0; t < 2; ++t) u[o][t] = read_q.get(at, t, o);
   };
-  each([&](int q, int p, int t, int u) __attribute__((always_inline)) {
-    A[t][u] *= kA / (kX * kX);
-    narrow_put(gram, q, p, A[t][u]);
-  });
-  __syncthreads();
   if (a.c != 0.f) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) narrow_multiply(B, read_q, gram + s * kNarrowTile, read_p, gram + s * kNarrowTile);
-  }
-  each([&](int q, int p, int t, int u) __attribute__((always_inline)) { narrow_put(poly, q, p, A[t][u] * a.b + B[t][u] * (a.c / kA)); });
-  __syncthreads();
-  float4_t Y[2][2] = {{none, none}, {none, none}};
+    for (int s = 0; s < 2; ++s) {
+      half8_t u[2][2], v[2][1];
+      lines_of(gram + s * kNarrowTile, u);
 #pragma unroll
-  for (int s = 0; s < 2; ++s) narrow_multiply(Y, read_q, poly + s * kNarrowTile, read_columns, columns + s * kNarrowTile);
+      for (int o = 0; o < 2; ++o) v[o][0] = read_p.get(gram + s * kNarrowTile, 0, o);
+      narrow_multiply<1>(B, u, v);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) narrow_put(poly, q_of(t), p, narrow_get(gram, q_of(t), p) * a.b + B[t][0] * (a.c / kA));
+  __syncthreads();
+  const ProductReads<true, true, 2> read_columns(wp & ~1, lane);
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    half8_t u[2][2], v[2][1];
+    lines_of(poly + s * kNarrowTile, u);
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+      if (wp & 1) v[o][0] = read_columns.get(columns + s * kNarrowTile, 1, o);  // uniform
+      else v[o][0] = read_columns.get(columns + s * kNarrowTile, 0, o);
+    }
+    narrow_multiply<1>(Y, u, v);
+  }
   const Pairs X{n.X, ld};
   if (a.last) {
     const LastOut out{X, X, a.a, n.scale / kX, n.m.out, n.m.ldo, n.flip ? n.m.cols : n.m.rows, n.flip ? n.m.rows : n.m.cols, n.m.out_type, n.flip};
-    each([&](int q, int p, int t, int u) __attribute__((always_inline)) { out.put<false>(0, q, p0 + p, out.read(q, p0 + p), Y[t][u]); });
+#pragma unroll
+    for (int t = 0; t < 2; ++t) out.put<false>(0, q_of(t), p0 + p, out.read(q_of(t), p0 + p), Y[t][0]);
   } else {
     const StepOut out{Pairs{n.next, ld}, X, a.a};
-    each([&](int q, int p, int t, int u) __attribute__((always_inline)) { out.put<false>(0, q, p0 + p, out.read(q, p0 + p), Y[t][u]); });
+#pragma unroll
+    for (int t = 0; t < 2; ++t) out.put<false>(0, q_of(t), p0 + p, out.read(q_of(t), p0 + p), Y[t][0]);
   }
 }
 static bool is_narrow(int64_t rows, int64_t cols) { return std::min(rows, cols) <= kNarrowM && std::max(rows, cols) <= kNarrowK; }
@@ -483,7 +519,7 @@ static size_t narrow_bytes(int64_t rows, int64_t cols) { return 2 * size_t(kNarr
 // all narrow ones of a list; their X lie one behind the other at ws
 static hgnn_status orth_narrow(const char* who, int32_t count, const hgnn_grad* grads, int32_t steps, const float* coef, const float* scales, char* ws, hipStream_t s) {
   static uint64_t told = 0;
-  constexpr int kBytes = (kNarrowRing + 6) * kNarrowTile;
+  constexpr int kBytes = (2 * kNarrowRing + 6) * kNarrowTile;
   for (int i = 0; i < count;) {
     NarrowArgs a{};
     int64_t blocks = 0;
@@ -505,7 +541,7 @@ static hgnn_status orth_narrow(const char* who, int32_t count, const hgnn_grad* 
     HGNN_LAUNCH_CHECK("narrow_begin_kernel");
     for (int k = 0; k < steps; ++k) {
       a.a = coef[3 * k], a.b = coef[3 * k + 1], a.c = coef[3 * k + 2], a.last = k + 1 == steps;
-      narrow_step_kernel<<<unsigned(blocks), kBlock, kBytes, s>>>(a);
+      narrow_step_kernel<<<unsigned(blocks), kNarrowWaves * kWave, kBytes, s>>>(a);
       HGNN_LAUNCH_CHECK("narrow_step_kernel");
       for (int j = 0; j < a.count; ++j) std::swap(a.m[j].X, a.m[j].next);
     }

@@ -139,7 +139,8 @@ def test_activations(hgnn, dev, act, trans):
 
 
 # (n, K, F) of each size of tile, with and without parts: few rows, a narrow side, tiles that fill the chip, and sizes around them
-@pytest.mark.parametrize("n,K,F", [(40, 700, 90), (700, 600, 500), (2100, 300, 700), (20000, 70, 20), (4099, 72, 2049), (8200, 40, 1100), (66000, 24, 40), (17000, 128, 256), (16400, 256, 130), (16500, 99, 300), (8192, 520, 4100)])
+@pytest.mark.parametrize("n,K,F", [(40, 700, 90), (700, 600, 500), (2100, 300, 700), (20000, 70, 20), (4099, 72, 2049), (8200, 40, 1100), (66000, 24, 40), (17000, 128, 256), (16400, 256, 130), (16500, 99, 300), (8192, 520, 4100), (16400, 30, 60), (16401, 60, 100),
+                                   (16400, 200, 50), (17000, 150, 70), (16384, 256, 64), (16999, 100, 128), (16390, 190, 260)])
 @pytest.mark.parametrize("trans", [False, True])
 def test_tiles(hgnn, dev, n, K, F, trans):
     c = Case(n, K, F, SILU, trans)
