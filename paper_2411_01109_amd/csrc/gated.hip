@@ -188,14 +188,15 @@ struct Split {
   int parts;
   int64_t part;  // contraction steps of a part
 };
-// nq x np sums over K steps (`two`: a pair of each).  Parts of at least 128 steps until every compute unit has a workgroup.
-static Split split_of(int64_t nq, int64_t np, int64_t K, bool two) {
+// nq x np sums (`two`: a pair of each) over segments of K steps, which are cut alike.
+static Split split_of(int64_t nq, int64_t np, int64_t K, bool two, int segments) {
   const auto tiles = [&](int64_t b) { return ceil_div(nq, b) * ceil_div(np, two ? b / 2 : b); };
   Split s;
   s.size = nq <= 64 || np <= (two ? 32 : 64) ? kFew : K >= kLong && tiles(256) >= kFull ? kWide : kMid;
   const int64_t t = s.size == kFew ? ceil_div(nq, 64) * ceil_div(np, 64) : tiles(s.size == kWide ? 256 : 128);
-  // two thirds of the units busy are enough: parts go through memory and another launch (9611 x 1402 -> 91, 152 tiles in four parts 28 us)
-  const int64_t parts = std::min(3 * t > 2 * kFull ? int64_t(1) : ceil_div(kFull, t), ceil_div(K, 128));
+  // A launch of these takes 6 us and 0.6 for 64 steps, a join 4 to 6: parts of 512 steps at least, and none where half of the units have a tile (370 x 565 -> 1173, us:
+  // the pairs by 57 tiles in five parts 14.6 and 6.1 for the join, X^T D in three 13.0 and 6.0; 9611 x 1402 -> 91, 152 tiles in two 18.5 and 5.4).
+  const int64_t parts = 2 * t > kFull ? 1 : std::min(ceil_div(kFull, t), std::max<int64_t>(1, segments * K / 512));
   s.part = std::max<int64_t>(64, up(ceil_div(K, std::max<int64_t>(parts, 1)), 64));
   s.parts = int(std::max<int64_t>(1, ceil_div(K, s.part)));
   return s;
@@ -534,9 +535,9 @@ struct GatedSizes {
 static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
   GatedSizes z{};
   z.n = n, z.K = K, z.F = F, z.Fp = up(F, 32);  // rows of whole 128 bytes
-  z.gate = split_of(n, F, K, true);
-  z.dx = split_of(n, K, F, false);
-  z.dw = split_of(K, 2 * z.Fp, n, false);
+  z.gate = split_of(n, F, K, true, 1);
+  z.dx = split_of(n, K, F, false, 2);
+  z.dw = split_of(K, 2 * z.Fp, n, false, 1);
   z.rows = K <= 256 && n >= kManyRows;
   z.gate_part = z.gate.parts > 1 && !z.rows && n > kFewRows ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
   z.dx_part = z.dx.parts > 1 ? size_t(z.dx.parts) * size_t(n) * size_t(up(K, 4)) * 4 : 0;

@@ -31,6 +31,7 @@ struct BlockArgs {
   int64_t ldz;
   int past;  // 1: H (dR), 2: Z (dY)
 };
+enum { kPreW = 0, kPreB, kGate, kPostW, kPostB, kVectors };
 struct BlockGradArgs : BlockArgs {
   const void* dH;
   int64_t lddh;
@@ -45,8 +46,8 @@ struct BlockGradArgs : BlockArgs {
   int vectors;  // kPreW | ...: which sums over rows are wanted
   float* part;  // [gridDim.x][kVectors][pitch]
   int pitch;
+  float* out[kVectors];  // where the sums of a single workgroup go
 };
-enum { kPreW = 0, kPreB, kGate, kPostW, kPostB, kVectors };
 
 // ---- sums over the lanes of a row: L lanes of a wave, or W waves
 __device__ __forceinline__ float lanes_sum(float v, int L) {
@@ -370,7 +371,7 @@ __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_grad_ke
     }
     if (a.dY) store_eight(out_Y.at, mine, e[0], a.past & 2), out_Y.move();
   }
-  float* const part = a.part + int64_t(blockIdx.x) * kVectors * a.pitch;
+  const auto part = [&](int k) { return gridDim.x == 1 ? a.out[k] : a.part + (int64_t(blockIdx.x) * kVectors + k) * a.pitch; };
 #pragma unroll
   for (int k = 0; k < kVectors; ++k) {
     if (!(a.vectors & (1 << k))) continue;  // uniform
@@ -386,12 +387,12 @@ __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_grad_ke
           float s = 0.f;
           for (int g = 0; g < S::kRows; ++g) s += sums[(g * L + c / 8) * 9 + c % 8];
           const int col = 8 * p * L + c;
-          if (col < a.F) part[k * a.pitch + col] = s;
+          if (col < a.F) part(k)[col] = s;
         }
       }
     } else {
 #pragma unroll
-      for (int p = 0; p < P; ++p) store_eight(part + k * a.pitch + col_of<S, P>(p), a.F - col_of<S, P>(p), total[k][p]);
+      for (int p = 0; p < P; ++p) store_eight(part(k) + col_of<S, P>(p), a.F - col_of<S, P>(p), total[k][p]);
     }
   }
 }
@@ -577,7 +578,7 @@ hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* bloc
   BlockGradArgs a{};
   block_args(a, n, F, block);
   float* const out[kVectors] = {g.dpre_w, g.dpre_b, g.dgate, g.dpost_w, g.dpost_b};
-  for (int k = 0; k < kVectors; ++k) a.vectors |= out[k] ? 1 << k : 0;
+  for (int k = 0; k < kVectors; ++k) a.vectors |= out[k] ? 1 << k : 0, a.out[k] = out[k];
   const size_t need = hgnn_residual_norm_grad_workspace(n, F);
   HGNN_REQUIRE(a.vectors == 0 || need == 0 || (workspace && workspace_bytes >= need && aligned16(workspace)), HGNN_EINVAL,
                "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_residual_norm_grad_workspace)", who, workspace_bytes, need);
@@ -603,7 +604,7 @@ hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* bloc
     });
     if (st != HGNN_OK) return st;
   }
-  if (a.vectors) {
+  if (a.vectors && blocks != 1) {
     BlockSumsArgs q{a.part, int(blocks), a.pitch, F, {out[0], out[1], out[2], out[3], out[4]}};
     block_sums_kernel<<<dim3(unsigned(ceil_div(F, kSumCols)), kVectors), kSumCols * kSumRows, 0, s>>>(q);
     HGNN_LAUNCH_CHECK("block_sums_kernel");
