@@ -132,32 +132,26 @@ struct SumsPart {  // [parts][nq][np]
   template <bool WHOLE>
   __device__ void put(int64_t k, int64_t q, int64_t p, const Read&, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * np + p) = v; }
 };
-// The parts of 64 x 64 sums in order (blockIdx.x, of the tiles on and below the diagonal with `lower`), and what becomes of them; the mirror places get theirs through
-// LDS, in whole pieces (by twos the join of 1024 x 1024 took 11 us).
+// The parts of 32 x 32 sums in order (blockIdx.x and y, of the tiles on and below the diagonal with `lower`), four sums a lane, and what becomes of them; the mirror
+// places get theirs through LDS, in whole pieces (by twos the join of 1024 x 1024 took 11 us; tiles of 64 x 64, sixteen sums a lane, took 10.4 us for 7 parts of
+// 1024 x 1024, bound by their chains of loads, these 5.4).
+constexpr int kJoinTile = 32;
 template <class Out>
 __global__ __launch_bounds__(kBlock) void sums_join_kernel(const float* part, int parts, int64_t nq, int64_t np, int lower, Out out) {
-  constexpr int kTile = 64;
-  __shared__ __align__(16) float tile[kTile][kTile + 4];
-  int64_t tq = blockIdx.x, tp = blockIdx.y;
+  __shared__ __align__(16) float tile[kJoinTile][kJoinTile + 4];
+  static_assert(kJoinTile * kJoinTile == 4 * kBlock, "four sums a lane");
+  const int64_t tq = blockIdx.x, tp = blockIdx.y;
   if (lower && tp > tq) return;  // uniform
-  const int64_t q0 = tq * kTile, p0 = tp * kTile;
+  const int64_t q0 = tq * kJoinTile, p0 = tp * kJoinTile;
   const bool mirror = lower && tp < tq;
-  float4_t v[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int64_t q = q0 + 16 * u + threadIdx.x / 16, p = p0 + 4 * (threadIdx.x % 16);
-    v[u] = float4_t{0.f, 0.f, 0.f, 0.f};
-    if (q >= nq || p >= np) continue;
+  const int r = threadIdx.x / (kJoinTile / 4), c = 4 * (threadIdx.x % (kJoinTile / 4));
+  const int64_t q = q0 + r, p = p0 + c;
+  if (q < nq && p < np) {
+    float4_t v = {0.f, 0.f, 0.f, 0.f};
     const float* at = part + q * np + p;
-#pragma unroll 4
-    for (int k = 0; k < parts; ++k, at += nq * np) v[u] += *reinterpret_cast<const float4_t*>(at);
-  }
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int r = 16 * u + threadIdx.x / 16, c = 4 * (threadIdx.x % 16);
-    const int64_t q = q0 + r, p = p0 + c;
-    if (q >= nq || p >= np) continue;
-    const float4_t y = out.join(q, p, v[u]);
+#pragma unroll 8
+    for (int k = 0; k < parts; ++k, at += nq * np) v += *reinterpret_cast<const float4_t*>(at);
+    const float4_t y = out.join(q, p, v);
     if (mirror) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) tile[c + e][r] = y[e];
@@ -165,11 +159,7 @@ __global__ __launch_bounds__(kBlock) void sums_join_kernel(const float* part, in
   }
   if (!mirror) return;
   __syncthreads();
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int r = 16 * u + threadIdx.x / 16, c = 4 * (threadIdx.x % 16);
-    if (p0 + r < np && q0 + c < nq) out.to.put(p0 + r, q0 + c, *reinterpret_cast<const float4_t*>(&tile[r][c]), false);
-  }
+  if (p0 + r < np && q0 + c < nq) out.to.put(p0 + r, q0 + c, *reinterpret_cast<const float4_t*>(&tile[r][c]), false);
 }
 
 // ---- the way in: the norm, X = G / |G|
@@ -562,7 +552,7 @@ static hgnn_status orth_product(const char* who, const Pairs& Q, const Pairs& P,
   if (split.parts == 1) return go(out);
   const hgnn_status st = go(SumsPart{part, nq, np});
   if (st != HGNN_OK) return st;
-  sums_join_kernel<<<dim3(unsigned(ceil_div(nq, 64)), unsigned(ceil_div(np, 64))), kBlock, 0, s>>>(part, split.parts, nq, np, lower, out);
+  sums_join_kernel<<<dim3(unsigned(ceil_div(nq, kJoinTile)), unsigned(ceil_div(np, kJoinTile))), kBlock, 0, s>>>(part, split.parts, nq, np, lower, out);
   HGNN_LAUNCH_CHECK("sums_join_kernel");
   return HGNN_OK;
 }
