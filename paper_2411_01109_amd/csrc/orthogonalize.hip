@@ -3,7 +3,7 @@
 //
 // The polynomial multiplies small singular values by a at each step, so an error of the first products comes out a^steps times as large: half precision products
 // leave a result that is off by percents.  Every value is therefore kept as two fp16 numbers, v = hi + lo with hi = fp16(v) and lo = fp16(v - hi), some 22 bits, and
-// a product is hi hi + hi lo + lo hi in fp32 sums (lo lo is below the last bit): three products on the matrix cores, a fifth of what fp32's own rate would take.
+// a product is hi hi + hi lo + lo hi in fp32 sums (lo lo is below the last bit; narrow matrices, whose few sums do not hide it, add it): three products on the matrix cores, a fifth of what fp32's own rate would take.
 // Powers of two bring the values into fp16's range: X at 2^11 (values up to 8 x 2^11 fit, what is lost at the small end is 2^-36), A and B at 2^9 (up to 64).
 // A and B are symmetric: tiles on and below the diagonal alone, each written to its mirror place, too (a tile on the diagonal only once: its two triangles are
 // summed in different orders, and two writers would make the result a race).
@@ -381,16 +381,33 @@ __device__ __forceinline__ float4_t narrow_get(const unsigned char* at, int q, i
   const int piece = (p & 31) >> 3, turn = (q & 15) >> 1;
   return Pairs::Four{*reinterpret_cast<const half4_t*>(line + (piece ^ turn) * 16), *reinterpret_cast<const half4_t*>(line + ((piece + 4) ^ turn) * 16)}.value();
 }
-// 32 x 16 U sums, 32 steps
+// Sums of products of two parts each.  The matrix cores cut what they add off where a lane's addition rounds it, so the high parts of 32 steps are summed by
+// themselves and added to the rest by the lane, and what the low parts add has a sum of its own: 9 x 809, eight steps, is off by 1.1e-6 of its norm (median of eight), in
+// one sum for all by 1.7e-6, and products in fp32 by 1.1e-6.
 template <int U>
-__device__ __forceinline__ void narrow_multiply(float4_t (&acc)[2][U], const half8_t (&a)[2][2], const half8_t (&b)[2][U]) {  // [part][16 items]
-#pragma unroll
-  for (int k = 3; k >= 0; --k)  // low low, then low high, high low, high high
+struct NarrowSums {
+  float4_t high[2][U], low[2][U];  // [16 lines][16 items]
+  __device__ __forceinline__ NarrowSums() {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int u = 0; u < U; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k >> 1][u], a[k & 1][t], acc[t][u], 0, 0, 0);
-}
+      for (int u = 0; u < U; ++u) high[t][u] = low[t][u] = float4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void add(const half8_t (&a)[2][2], const half8_t (&b)[2][U]) {  // [part][16 items]
+    const float4_t none = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int u = 0; u < U; ++u) high[t][u] += __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0][u], a[0][t], none, 0, 0, 0);
+#pragma unroll
+    for (int k = 3; k >= 1; --k)  // low low, then low high, high low
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int u = 0; u < U; ++u) low[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[k >> 1][u], a[k & 1][t], low[t][u], 0, 0, 0);
+  }
+  __device__ __forceinline__ float4_t sum(int t, int u) const { return high[t][u] + low[t][u]; }
+};
 __global__ __launch_bounds__(kNarrowWaves* kWave) void narrow_step_kernel(NarrowArgs a) {
   extern __shared__ __align__(1024) unsigned char lds[];
   constexpr int kStage = 2 * kNarrowTile;  // 64 steps
@@ -417,13 +434,12 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void narrow_step_kernel(Narrow
     to += kStage;
     if (to >= lds0 + kNarrowRing * kStage) to -= kNarrowRing * kStage;
   };
-  const float4_t none = {0.f, 0.f, 0.f, 0.f};
   int asked = 0;
   for (; asked < kNarrowRing - 1 && asked < steps; ++asked) ask();
   {
     const int team = wave >> 2, wq = (wave >> 1) & 1, wp = wave & 1;
     const ProductReads<false, true, 2> read_q(2 * wq, lane), read_p(2 * wp, lane);
-    float4_t A[2][2] = {{none, none}, {none, none}};
+    NarrowSums<2> A;
     const unsigned char* stage = lds + team * kNarrowTile;
     for (int s = 0; s < steps; ++s) {
       const int behind = asked - 1 - s;
@@ -437,7 +453,7 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void narrow_step_kernel(Narrow
       for (int o = 0; o < 2; ++o)
 #pragma unroll
         for (int t = 0; t < 2; ++t) u[o][t] = read_q.get(stage, t, o), v[o][t] = read_p.get(stage, t, o);
-      narrow_multiply<2>(A, u, v);
+      A.add(u, v);
       stage += kStage;
       if (stage >= columns) stage -= kNarrowRing * kStage;
     }
@@ -445,13 +461,13 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void narrow_step_kernel(Narrow
     float4_t* const over = reinterpret_cast<float4_t*>(poly) + (wave & 3) * 4 * kWave + lane;
     if (team == 1) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) over[t * kWave] = A[t >> 1][t & 1];
+      for (int t = 0; t < 4; ++t) over[t * kWave] = A.sum(t >> 1, t & 1);
     }
     __syncthreads();
     if (team == 0) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
-        narrow_put(gram, 16 * (2 * wq + (t >> 1)) + i, 16 * (2 * wp + (t & 1)) + 4 * qq, (A[t >> 1][t & 1] + over[t * kWave]) * (kA / (kX * kX)));
+        narrow_put(gram, 16 * (2 * wq + (t >> 1)) + i, 16 * (2 * wp + (t & 1)) + 4 * qq, (A.sum(t >> 1, t & 1) + over[t * kWave]) * (kA / (kX * kX)));
     }
     __syncthreads();
   }
@@ -459,7 +475,7 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void narrow_step_kernel(Narrow
   const ProductReads<false, true, 2> read_q(2 * wq, lane);
   const ProductReads<false, true, 1> read_p(wp, lane);
   const auto q_of = [&](int t) { return 16 * (2 * wq + t) + i; };
-  float4_t B[2][1] = {{none}, {none}}, Y[2][1] = {{none}, {none}};
+  NarrowSums<1> B, Y;
   const auto lines_of = [&](const unsigned char* at, half8_t (&u)[2][2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int o = 0; o < 2; ++o)
@@ -473,11 +489,11 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void narrow_step_kernel(Narrow
       lines_of(gram + s * kNarrowTile, u);
 #pragma unroll
       for (int o = 0; o < 2; ++o) v[o][0] = read_p.get(gram + s * kNarrowTile, 0, o);
-      narrow_multiply<1>(B, u, v);
+      B.add(u, v);
     }
   }
 #pragma unroll
-  for (int t = 0; t < 2; ++t) narrow_put(poly, q_of(t), p, narrow_get(gram, q_of(t), p) * a.b + B[t][0] * (a.c / kA));
+  for (int t = 0; t < 2; ++t) narrow_put(poly, q_of(t), p, narrow_get(gram, q_of(t), p) * a.b + B.sum(t, 0) * (a.c / kA));
   __syncthreads();
   const ProductReads<true, true, 2> read_columns(wp & ~1, lane);
 #pragma unroll
@@ -489,17 +505,17 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void narrow_step_kernel(Narrow
       if (wp & 1) v[o][0] = read_columns.get(columns + s * kNarrowTile, 1, o);  // uniform
       else v[o][0] = read_columns.get(columns + s * kNarrowTile, 0, o);
     }
-    narrow_multiply<1>(Y, u, v);
+    Y.add(u, v);
   }
   const Pairs X{n.X, ld};
   if (a.last) {
     const LastOut out{X, X, a.a, n.scale / kX, n.m.out, n.m.ldo, n.flip ? n.m.cols : n.m.rows, n.flip ? n.m.rows : n.m.cols, n.m.out_type, n.flip};
 #pragma unroll
-    for (int t = 0; t < 2; ++t) out.put<false>(0, q_of(t), p0 + p, out.read(q_of(t), p0 + p), Y[t][0]);
+    for (int t = 0; t < 2; ++t) out.put<false>(0, q_of(t), p0 + p, out.read(q_of(t), p0 + p), Y.sum(t, 0));
   } else {
     const StepOut out{Pairs{n.next, ld}, X, a.a};
 #pragma unroll
-    for (int t = 0; t < 2; ++t) out.put<false>(0, q_of(t), p0 + p, out.read(q_of(t), p0 + p), Y[t][0]);
+    for (int t = 0; t < 2; ++t) out.put<false>(0, q_of(t), p0 + p, out.read(q_of(t), p0 + p), Y.sum(t, 0));
   }
 }
 static bool is_narrow(int64_t rows, int64_t cols) { return std::min(rows, cols) <= kNarrowM && std::max(rows, cols) <= kNarrowK; }
