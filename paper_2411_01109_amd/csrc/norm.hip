@@ -67,13 +67,14 @@ __device__ __forceinline__ float lanes_sum(float v, int L) {
   return v;
 }
 
-// Rows of L lanes (W = 1), or of W waves; P pieces of eight elements a lane.
-template <int L, int P, int W>
+// Rows of L lanes (W = 1), or of W waves, eight elements a lane.
+template <int L_, int W_>
 struct RowShape {
+  static constexpr int L = L_, W = W_;
   static constexpr int kRows = W > 1 ? 1 : kBlock / L;       // rows of a workgroup at a time
   static constexpr int kThreads = W > 1 ? W * kWave : kBlock;
   static constexpr int kLanes = W > 1 ? W * kWave : L;       // of a row
-  static constexpr bool kKeep = P == 1 && W <= 4;            // weights stay in registers over the rows of a workgroup
+  static constexpr bool kKeep = W <= 4;                      // weights stay in registers over the rows of a workgroup
   __device__ static int lane() { return threadIdx.x % kLanes; }
   __device__ static int row() { return W > 1 ? 0 : threadIdx.x / L; }
   // of both at once: where the row is several waves', one turn through LDS
@@ -100,9 +101,9 @@ struct Eight {
   float v[8];
 };
 
-// columns of piece p of the lane: [col, col + 8), `left` of them in the row
-template <class S, int P>
-__device__ __forceinline__ int col_of(int p) { return 8 * (S::lane() + p * S::kLanes); }
+// columns of the lane: [col, col + 8), `left` of them in the row
+template <class S>
+__device__ __forceinline__ int col_of() { return 8 * S::lane(); }
 
 // Eight elements of a row as they are in memory, `left` of them the row's; zeros behind the row and for rows that do not exist, which then stay zeros through all that
 // follows and add nothing anywhere.  after(): the elements from here to the tensor's end, behind which nothing is read.
@@ -174,97 +175,77 @@ __device__ __forceinline__ Eight weights_at(const float* w, int col, int F, floa
 }
 
 // (x - mean) r in the place of x, zeros behind the row; returns r
-template <class S, int P>
-__device__ __forceinline__ float normed(Eight (&x)[P], int kind, int F, float eps, float* lds) {
+template <class S>
+__device__ __forceinline__ float normed(Eight& x, int kind, int F, float eps, float* lds) {
   const float inv = 1.f / float(F);
   if (kind == HGNN_NORM_LAYER) {
     float s = 0.f;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s += x[p].v[i];
-    const float mean = S::sum(s, lds) * inv;
-#pragma unroll
-    for (int p = 0; p < P; ++p) less(x[p], mean, F - col_of<S, P>(p));
+    for (int i = 0; i < 8; ++i) s += x.v[i];
+    less(x, S::sum(s, lds) * inv, F - col_of<S>());
   }
   float q = 0.f;
 #pragma unroll
-  for (int p = 0; p < P; ++p)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q = fmaf(x[p].v[i], x[p].v[i], q);
+  for (int i = 0; i < 8; ++i) q = fmaf(x.v[i], x.v[i], q);
   const float r = __builtin_amdgcn_rsqf(S::sum(q, lds) * inv + eps);
 #pragma unroll
-  for (int p = 0; p < P; ++p)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[p].v[i] *= r;
+  for (int i = 0; i < 8; ++i) x.v[i] *= r;
   return r;
 }
 
 // to + N^T(d) in the place of `to`: what comes back through a norm whose output was xh w + c
-template <class S, int P, class Weight>
-__device__ __forceinline__ void through(Eight (&to)[P], Eight (&d)[P], const Eight (&xh)[P], Weight&& weight, float r, int kind, int F, float* lds) {
+template <class S>
+__device__ __forceinline__ void through(Eight& to, Eight& d, const Eight& xh, const Eight& w, float r, int kind, int F, float* lds) {
   float su = 0.f, sx = 0.f;
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const Eight w = weight(p);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      d[p].v[i] *= w.v[i];
-      su += d[p].v[i];
-      sx = fmaf(d[p].v[i], xh[p].v[i], sx);
-    }
+  for (int i = 0; i < 8; ++i) {
+    d.v[i] *= w.v[i];
+    su += d.v[i];
+    sx = fmaf(d.v[i], xh.v[i], sx);
   }
   if (kind == HGNN_NORM_LAYER) S::sum(su, sx, lds);
   else sx = S::sum(sx, lds);
   sx *= r / float(F), su *= r / float(F);
+  if (kind == HGNN_NORM_LAYER) less(to, su, F - col_of<S>());
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    if (kind == HGNN_NORM_LAYER) less(to[p], su, F - col_of<S, P>(p));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) to[p].v[i] = fmaf(d[p].v[i], r, fmaf(-xh[p].v[i], sx, to[p].v[i]));
-  }
+  for (int i = 0; i < 8; ++i) to.v[i] = fmaf(d.v[i], r, fmaf(-xh.v[i], sx, to.v[i]));
 }
 
-template <class T, int L, int P, int W>
+template <class T, int L, int W>
 __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_kernel(BlockArgs a) {
-  typedef RowShape<L, P, W> S;
+  typedef RowShape<L, W> S;
   __shared__ float lds[2 * W];
-  Eight post_w[P], post_b[P], gate[P], pre_w[P], pre_b[P];
+  Eight post_w, post_b, gate, pre_w, pre_b;
+  const int col = col_of<S>(), left = a.F - col;
   const auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int c = col_of<S, P>(p);
-      post_w[p] = weights_at(a.post_w, c, a.F, 1.f), post_b[p] = weights_at(a.post_b, c, a.F, 0.f), gate[p] = weights_at(a.gate, c, a.F, 1.f);
-      pre_w[p] = weights_at(a.pre_w, c, a.F, 1.f), pre_b[p] = weights_at(a.pre_b, c, a.F, 0.f);
-    }
+    post_w = weights_at(a.post_w, col, a.F, 1.f), post_b = weights_at(a.post_b, col, a.F, 0.f), gate = weights_at(a.gate, col, a.F, 1.f);
+    pre_w = weights_at(a.pre_w, col, a.F, 1.f), pre_b = weights_at(a.pre_b, col, a.F, 0.f);
   };
   if (S::kKeep) weights();
   // (asking for the next rows ahead, as the gradients do, costs registers and with them waves: 2.4 M x 128 512 -> 567 us)
-  static_assert(P == 1, "pieces");
   const int64_t first = int64_t(blockIdx.x) * S::kRows + S::row(), stride = int64_t(gridDim.x) * S::kRows;
-  const int col = col_of<S, P>(0), left = a.F - col;
   Place<half_t> Y(a.Y, a.ldy, first, stride, col), G(a.gate_rows, a.ld_gate, first, stride, col), Z(a.Z, a.ldz, first, stride, col);
   Place<T> R(a.R, a.ldr, first, stride, col), H(a.H, a.ldh, first, stride, col);
   for (int64_t row = first; row - S::row() < a.n; row += stride) {  // all waves alike: the sums meet
     if (!S::kKeep) weights();
     const int mine = row < a.n ? left : 0;
-    Eight b[1], h[1];
-    b[0] = a.Y ? eight_of(Y.fetch(row, a.n, left), left) : Eight{};
-    h[0] = a.R ? eight_of(R.fetch(row, a.n, left), left) : Eight{};
-    if (a.gate_rows) gate[0] = eight_of(G.fetch(row, a.n, left), left);
+    Eight b = {}, h = {};
+    if (a.Y) b = eight_of(Y.fetch(row, a.n, left), left);
+    if (a.R) h = eight_of(R.fetch(row, a.n, left), left);
+    if (a.gate_rows) gate = eight_of(G.fetch(row, a.n, left), left);
     if (a.post != HGNN_NORM_NONE) {
-      normed<S, P>(b, a.post, a.F, a.eps, lds);
+      normed<S>(b, a.post, a.F, a.eps, lds);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) b[0].v[i] = fmaf(b[0].v[i], post_w[0].v[i], post_b[0].v[i]);
+      for (int i = 0; i < 8; ++i) b.v[i] = fmaf(b.v[i], post_w.v[i], post_b.v[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[0].v[i] = float(T(fmaf(gate[0].v[i], b[0].v[i], a.alpha * h[0].v[i])));  // as it is stored
-    if (a.H) store_eight(H.at, mine, h[0], a.past & 1);
+    for (int i = 0; i < 8; ++i) h.v[i] = float(T(fmaf(gate.v[i], b.v[i], a.alpha * h.v[i])));  // as it is stored
+    if (a.H) store_eight(H.at, mine, h, a.past & 1);
     if (a.pre != HGNN_NORM_NONE) {
-      normed<S, P>(h, a.pre, a.F, a.eps, lds);
+      normed<S>(h, a.pre, a.F, a.eps, lds);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[0].v[i] = fmaf(h[0].v[i], pre_w[0].v[i], pre_b[0].v[i]);
-      store_eight(Z.at, mine, h[0], a.past & 2);
+      for (int i = 0; i < 8; ++i) h.v[i] = fmaf(h.v[i], pre_w.v[i], pre_b.v[i]);
+      store_eight(Z.at, mine, h, a.past & 2);
     }
     Y.move(), R.move(), G.move(), H.move(), Z.move();
   }
@@ -272,34 +253,29 @@ __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_kernel(
 
 // Sums over rows: a lane keeps those of its columns over all rows of its workgroup, the row groups of the workgroup are added in LDS in order, and the
 // workgroup leaves one partial result, which block_sums_kernel adds in order: no atomics, the same bits on every run.
-template <class T, int L, int P, int W>
+template <class T, int L, int W>
 __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_grad_kernel(BlockGradArgs a) {
-  typedef RowShape<L, P, W> S;
+  typedef RowShape<L, W> S;
   __shared__ float lds[2 * W];
   __shared__ float sums[S::kRows > 1 ? S::kThreads * 9 : 1];
-  Eight gate[P], total[kVectors][P] = {};
+  Eight gate, total[kVectors] = {};
+  const int col = col_of<S>(), left = a.F - col;
   // Weights stand in LDS: as registers of every lane they would cost a wave of three (153 registers, 2.4 M x 128 911 us).
   enum { kAtPreW, kAtPostW, kAtPostB, kAtGate, kWeights };
-  __shared__ __align__(16) float s_weights[kWeights][P * S::kLanes * 8];
+  __shared__ __align__(16) float s_weights[kWeights][S::kLanes * 8];
   if (S::row() == 0) {
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int c = col_of<S, P>(p);
-      *reinterpret_cast<Eight*>(&s_weights[kAtPreW][c]) = weights_at(a.pre_w, c, a.F, 1.f);
-      *reinterpret_cast<Eight*>(&s_weights[kAtPostW][c]) = weights_at(a.post_w, c, a.F, 1.f);
-      *reinterpret_cast<Eight*>(&s_weights[kAtPostB][c]) = weights_at(a.post_b, c, a.F, 0.f);
-      *reinterpret_cast<Eight*>(&s_weights[kAtGate][c]) = weights_at(a.gate, c, a.F, 1.f);
-    }
+    *reinterpret_cast<Eight*>(&s_weights[kAtPreW][col]) = weights_at(a.pre_w, col, a.F, 1.f);
+    *reinterpret_cast<Eight*>(&s_weights[kAtPostW][col]) = weights_at(a.post_w, col, a.F, 1.f);
+    *reinterpret_cast<Eight*>(&s_weights[kAtPostB][col]) = weights_at(a.post_b, col, a.F, 0.f);
+    *reinterpret_cast<Eight*>(&s_weights[kAtGate][col]) = weights_at(a.gate, col, a.F, 1.f);
   }
   __syncthreads();
-  const auto weight = [&](int k, int p) __attribute__((always_inline)) {
-    const float4_t* const at = reinterpret_cast<const float4_t*>(&s_weights[k][col_of<S, P>(p)]);
+  const auto weight = [&](int k) __attribute__((always_inline)) {
+    const float4_t* const at = reinterpret_cast<const float4_t*>(&s_weights[k][col]);
     const float4_t lo = at[0], hi = at[1];
     return Eight{{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
   };
-  static_assert(P == 1, "pieces");
   const int64_t first = int64_t(blockIdx.x) * S::kRows + S::row(), stride = int64_t(gridDim.x) * S::kRows;
-  const int col = col_of<S, P>(0), left = a.F - col;
   const bool pre = a.pre != HGNN_NORM_NONE, post = a.post != HGNN_NORM_NONE;
   struct {
     RawPiece<half_t> dZ, Y, gate;
@@ -321,78 +297,72 @@ __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_grad_ke
     asm volatile("" ::: "memory");  // weights are read again, not kept
     if (!kAhead) fetch(row);
     const int mine = row < a.n ? left : 0;
-    Eight e[1] = {eight_of(next.dH, left)}, h[1] = {eight_of(next.H, left)}, d[1] = {eight_of(next.dZ, left)}, b[1] = {eight_of(next.Y, left)};
-    if (a.gate_rows) gate[0] = eight_of(next.gate, left);
+    Eight e = eight_of(next.dH, left), h = eight_of(next.H, left), d = eight_of(next.dZ, left), b = eight_of(next.Y, left);
+    if (a.gate_rows) gate = eight_of(next.gate, left);
     if (kAhead && row - S::row() + stride < a.n) fetch(row + stride);
     if (pre) {
-      const float r = normed<S, P>(h, a.pre, a.F, a.eps, lds);
+      const float r = normed<S>(h, a.pre, a.F, a.eps, lds);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        total[kPreW][0].v[i] = fmaf(d[0].v[i], h[0].v[i], total[kPreW][0].v[i]);
-        total[kPreB][0].v[i] += d[0].v[i];
+        total[kPreW].v[i] = fmaf(d.v[i], h.v[i], total[kPreW].v[i]);
+        total[kPreB].v[i] += d.v[i];
       }
-      through<S, P>(e, d, h, [&](int p) { return weight(kAtPreW, p); }, r, a.pre, a.F, lds);
+      through<S>(e, d, h, weight(kAtPreW), r, a.pre, a.F, lds);
     }
     if (a.dR) {
       if (a.alpha == 1.f) {
-        store_eight(out_R.at, mine, e[0], a.past & 1);
+        store_eight(out_R.at, mine, e, a.past & 1);
       } else {
         Eight out;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out.v[i] = a.alpha * e[0].v[i];
+        for (int i = 0; i < 8; ++i) out.v[i] = a.alpha * e.v[i];
         store_eight(out_R.at, mine, out, a.past & 1);
       }
       out_R.move();
     }
     if (!a.dY && !a.dgate_rows && !(a.vectors & (1 << kGate | 1 << kPostW | 1 << kPostB))) continue;
     float r = 1.f;
-    if (post) r = normed<S, P>(b, a.post, a.F, a.eps, lds);  // b: xh
+    if (post) r = normed<S>(b, a.post, a.F, a.eps, lds);  // b: xh
     if (a.gate || a.gate_rows) {
-      const Eight w = weight(kAtPostW, 0), c = weight(kAtPostB, 0);
-      if (!a.gate_rows) gate[0] = weight(kAtGate, 0);
+      const Eight w = weight(kAtPostW), c = weight(kAtPostB);
+      if (!a.gate_rows) gate = weight(kAtGate);
       Eight g;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        g.v[i] = e[0].v[i] * (post ? fmaf(b[0].v[i], w.v[i], c.v[i]) : b[0].v[i]);
-        total[kGate][0].v[i] += g.v[i];
-        e[0].v[i] *= gate[0].v[i];
+        g.v[i] = e.v[i] * (post ? fmaf(b.v[i], w.v[i], c.v[i]) : b.v[i]);
+        total[kGate].v[i] += g.v[i];
+        e.v[i] *= gate.v[i];
       }
       if (a.dgate_rows) store_eight(out_gate.at, mine, g), out_gate.move();
     }
     if (post) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        total[kPostW][0].v[i] = fmaf(e[0].v[i], b[0].v[i], total[kPostW][0].v[i]);
-        total[kPostB][0].v[i] += e[0].v[i];
+        total[kPostW].v[i] = fmaf(e.v[i], b.v[i], total[kPostW].v[i]);
+        total[kPostB].v[i] += e.v[i];
       }
-      Eight y[1] = {};
-      through<S, P>(y, e, b, [&](int p) { return weight(kAtPostW, p); }, r, a.post, a.F, lds);
-      e[0] = y[0];
+      Eight y = {};
+      through<S>(y, e, b, weight(kAtPostW), r, a.post, a.F, lds);
+      e = y;
     }
-    if (a.dY) store_eight(out_Y.at, mine, e[0], a.past & 2), out_Y.move();
+    if (a.dY) store_eight(out_Y.at, mine, e, a.past & 2), out_Y.move();
   }
   const auto part = [&](int k) { return gridDim.x == 1 ? a.out[k] : a.part + (int64_t(blockIdx.x) * kVectors + k) * a.pitch; };
 #pragma unroll
   for (int k = 0; k < kVectors; ++k) {
     if (!(a.vectors & (1 << k))) continue;  // uniform
-    if constexpr (S::kRows > 1) {  // P = 1: lanes of a row, groups of rows
-      static_assert(P <= 2, "pieces");
+    if constexpr (S::kRows > 1) {  // lanes of a row, groups of rows
+      __syncthreads();
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sums[threadIdx.x * 9 + i] = total[k][p].v[i];
-        __syncthreads();
-        for (int c = threadIdx.x; c < 8 * L; c += S::kThreads) {
-          float s = 0.f;
-          for (int g = 0; g < S::kRows; ++g) s += sums[(g * L + c / 8) * 9 + c % 8];
-          const int col = 8 * p * L + c;
-          if (col < a.F) part(k)[col] = s;
-        }
+      for (int i = 0; i < 8; ++i) sums[threadIdx.x * 9 + i] = total[k].v[i];
+      __syncthreads();
+      for (int c = threadIdx.x; c < 8 * L; c += S::kThreads) {
+        float s = 0.f;
+        for (int g = 0; g < S::kRows; ++g) s += sums[(g * L + c / 8) * 9 + c % 8];
+        if (c < a.F) part(k)[c] = s;
       }
     } else {
-#pragma unroll
-      for (int p = 0; p < P; ++p) store_eight(part(k) + col_of<S, P>(p), a.F - col_of<S, P>(p), total[k][p]);
+      store_eight(part(k) + col, left, total[k]);
     }
   }
 }
@@ -440,25 +410,19 @@ template <class Call>
 static hgnn_status with_shape(int F, Call&& call) {
   const int lanes = pow2_at_least((F + 7) / 8);
   switch (lanes) {
-    case 1: return call(RowShape<1, 1, 1>());
-    case 2: return call(RowShape<2, 1, 1>());
-    case 4: return call(RowShape<4, 1, 1>());
-    case 8: return call(RowShape<8, 1, 1>());
-    case 16: return call(RowShape<16, 1, 1>());
-    case 32: return call(RowShape<32, 1, 1>());
-    case 64: return call(RowShape<64, 1, 1>());
-    case 128: return call(RowShape<64, 1, 2>());
-    case 256: return call(RowShape<64, 1, 4>());
-    case 512: return call(RowShape<64, 1, 8>());
-    default: return call(RowShape<64, 1, 16>());
+    case 1: return call(RowShape<1, 1>());
+    case 2: return call(RowShape<2, 1>());
+    case 4: return call(RowShape<4, 1>());
+    case 8: return call(RowShape<8, 1>());
+    case 16: return call(RowShape<16, 1>());
+    case 32: return call(RowShape<32, 1>());
+    case 64: return call(RowShape<64, 1>());
+    case 128: return call(RowShape<64, 2>());
+    case 256: return call(RowShape<64, 4>());
+    case 512: return call(RowShape<64, 8>());
+    default: return call(RowShape<64, 16>());
   }
 }
-template <class S>
-struct ShapeOf;
-template <int l, int p, int w>
-struct ShapeOf<RowShape<l, p, w>> {
-  static constexpr int L = l, P = p, W = w;
-};
 
 // Workgroups that are resident at once where a SIMD holds so many waves of a kernel: with more, the last ones run by themselves (the gradients of 2.4 M x 128 by
 // 1024 workgroups, 768 of them at once, 910 us).
@@ -529,10 +493,9 @@ hgnn_status hgnn_residual_norm(int64_t n, int32_t F, const hgnn_block* block, hg
   hipStream_t s = static_cast<hipStream_t>(stream);
   return with_shape(F, [&](auto shape) -> hgnn_status {
     typedef decltype(shape) S;
-    typedef ShapeOf<S> D;
     const unsigned blocks = unsigned(std::min<int64_t>(ceil_div(n, S::kRows), resident<S>(S::kThreads > 512 ? 4 : 5)));
-    if (type == HGNN_F16) block_norm_kernel<half_t, D::L, D::P, D::W><<<blocks, S::kThreads, 0, s>>>(a);
-    else block_norm_kernel<float, D::L, D::P, D::W><<<blocks, S::kThreads, 0, s>>>(a);
+    if (type == HGNN_F16) block_norm_kernel<half_t, S::L, S::W><<<blocks, S::kThreads, 0, s>>>(a);
+    else block_norm_kernel<float, S::L, S::W><<<blocks, S::kThreads, 0, s>>>(a);
     HGNN_LAUNCH_CHECK("block_norm_kernel");
     return HGNN_OK;
   });
@@ -595,10 +558,9 @@ hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* bloc
   if (n > 0) {
     st = with_shape(F, [&](auto shape) -> hgnn_status {
       typedef decltype(shape) S;
-      typedef ShapeOf<S> D;
       blocks = grad_blocks<S>(n, type);
-      if (type == HGNN_F16) block_norm_grad_kernel<half_t, D::L, D::P, D::W><<<unsigned(blocks), S::kThreads, 0, s>>>(a);
-      else block_norm_grad_kernel<float, D::L, D::P, D::W><<<unsigned(blocks), S::kThreads, 0, s>>>(a);
+      if (type == HGNN_F16) block_norm_grad_kernel<half_t, S::L, S::W><<<unsigned(blocks), S::kThreads, 0, s>>>(a);
+      else block_norm_grad_kernel<float, S::L, S::W><<<unsigned(blocks), S::kThreads, 0, s>>>(a);
       HGNN_LAUNCH_CHECK("block_norm_grad_kernel");
       return HGNN_OK;
     });
