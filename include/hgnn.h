@@ -640,7 +640,8 @@ typedef struct {
  * [n][ld].  R or Y may be NULL and count as 0 (without Y no post and no gate); H may be NULL where it is not wanted, and may
  * be R itself (with the same pitch); Z is there if and only if there is a norm `pre`, which takes H as it is stored, rounded
  * to its type.  Statistics and all arithmetic are fp32.  Rows have any width up to 8192 (HGNN_EUNSUPPORTED beyond) and any
- * pitch, arrays are aligned to their elements, nothing between or behind rows is written, nothing behind the last one read. */
+ * pitch, arrays are aligned to their elements, nothing between or behind rows is written, nothing behind the last one read.
+ * But for H in the place of R no output may overlap an input or the other output. */
 hgnn_status hgnn_residual_norm(int64_t n, int32_t F, const hgnn_block* block, hgnn_type type, const void* R, int64_t ldr, const hgnn_half* Y,
                                int64_t ldy, void* H, int64_t ldh, hgnn_half* Z, int64_t ldz, void* stream);
 
@@ -661,7 +662,8 @@ typedef struct {
  * with `pre`), from H as hgnn_residual_norm stored it (where there is a norm `pre`) and Y (where there is a norm `post` or a
  * gate).  The statistics of the rows are formed again.  Sums over rows are fp32, in a fixed order: no atomics, the same bits
  * on every run.  workspace is device memory of at least hgnn_residual_norm_grad_workspace(n, F) bytes (16-byte aligned),
- * owned by the caller and overwritten; it may be NULL where no sum over rows is wanted. */
+ * owned by the caller and overwritten; it may be NULL where no sum over rows is wanted.  But for dR in the place of dH no
+ * output may overlap an input or another output. */
 size_t hgnn_residual_norm_grad_workspace(int64_t n, int32_t F);
 hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* block, hgnn_type type, const void* H, int64_t ldh, const hgnn_half* Y,
                                     int64_t ldy, const void* dH, int64_t lddh, const hgnn_half* dZ, int64_t lddz, const hgnn_block_grad* grads,
@@ -685,7 +687,8 @@ hgnn_status hgnn_gated(int64_t n, int32_t K, int32_t F, hgnn_activation act, con
  * dWg = X^T dG, dWu = X^T dU (fp16, laid out as the weights, pitch lddw; HGNN_RELU has the derivative 0 at 0).  dX, or dWg and
  * dWu together, may be NULL: not wanted.  G and U are formed again; dG and dU pass through the workspace in fp16 as all
  * vertex-level gradients here do (scale the loss as for those), and sums are fp32 in a fixed order.  Tensors as for
- * hgnn_gated; workspace at least hgnn_gated_grad_workspace(n, K, F) bytes (16-byte aligned). */
+ * hgnn_gated, no output may overlap an input or another output; workspace at least hgnn_gated_grad_workspace(n, K, F) bytes
+ * (16-byte aligned). */
 size_t hgnn_gated_grad_workspace(int64_t n, int32_t K, int32_t F);
 hgnn_status hgnn_gated_grad(int64_t n, int32_t K, int32_t F, hgnn_activation act, const hgnn_half* X, int64_t ldx, const hgnn_half* Wg,
                             const hgnn_half* Wu, int64_t ldw, int32_t trans_w, const hgnn_half* dY, int64_t lddy, hgnn_half* dX, int64_t lddx,

@@ -203,7 +203,7 @@ static Split split_of(int64_t nq, int64_t np, int64_t K, bool two, int segments)
 }
 
 // ---- many rows through a narrow weight (K up to 256): bound by the rows of X and Y, which the product kernel's workgroups, a tile and two steps each, do not stream
-// (233 000 x 128 -> 256 96 us, of it 35 by the bytes at a copy's rate).  Eight waves keep their features of both weights in registers for all rows of the
+// (233 000 x 128 -> 256 96 us, here 45, of it 35 by the bytes at a copy's rate).  Eight waves keep their features of both weights in registers for all rows of the
 // workgroup, 32 features for K <= 128, 16 beyond; a ninth brings X into a ring in LDS, 64 rows at a time, and is the only one that waits for loads to LDS, so that
 // the other waves' stores are never waited for.  A barrier a tile hands it over and takes back the one before.  (Two
 // workgroups of four waves and one do not fit a compute unit's registers: 65 -> 100 us.)  Features are dealt out such that a lane's 2 x 4 sums are eight consecutive ones.
@@ -375,7 +375,8 @@ static hgnn_status gated_rows(const char* who, GatedRowsArgs& a, const Out& out,
 
 // ---- few rows (up to 64), a served model's: bound by reading the two weights once.  A workgroup owns 32 features of both, its sixteen waves share the contraction, 32
 // steps at a time, and take the weights straight into the registers that the products read, a stage ahead for up to 16 rows; their sums meet in LDS.  One launch: by the
-// product kernel the contraction is cut over workgroups, and joining the parts is a launch of 3.5 us (1 row of 1024 -> 4096 9.3 us, 13 of 2048 -> 5461 16).
+// product kernel the contraction is cut over workgroups, and joining the parts is a launch of 3.5 us (1 row of 1024 -> 4096 9.3 us, here 6.7; 13 of 2048 -> 5461 16,
+// here 14: 45 MB at 3.2 TB/s).
 // Fragment e, item i is feature 2 i + e of the 32: of [K][F] a lane takes two neighbouring features of eight steps, 64 bytes of a line a load, and a lane's sums are
 // eight consecutive features.
 constexpr int kFewWaves = 16, kFewRows = 64, kFewFeatures = 32;

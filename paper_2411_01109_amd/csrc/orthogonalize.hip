@@ -306,7 +306,7 @@ static OrthSplit orth_split(int64_t nq, int64_t np, int64_t K, bool lower) {
   };
   OrthSplit s;
   // Tiles of 64 read LDS twice as often for their products: where a side is short, or where a compute unit has at most one of them and a short contraction (1024 x
-  // 1024, K = 1024, us: 136 of them 15, 36 of 128 in four parts 14 and the join 8; K = 4096: 136 in four parts 22.5 + 11, 36 of 128 in seven 20.5 + 10.5).  Parts until
+  // 1024, K = 1024, us: 136 of them 15, 36 of 128 in four parts 14 and a join of 5; K = 4096: 136 in four parts 22.5, 36 of 128 in seven 20.5, and the join).  Parts until
   // every compute unit has a workgroup, of 256 steps at least (a join costs about as much as those).
   s.tile = std::min(nq, np) < 192 || (tiles(64) <= kOrthFull && K <= 1024) ? 64 : 128;
   const int64_t t = tiles(s.tile), parts = t > kOrthFull / 2 || K <= 1024 ? 1 : std::min(kOrthFull / t, std::max<int64_t>(1, K / 256));
@@ -335,7 +335,8 @@ static OrthSizes orth_sizes(int64_t rows, int64_t cols) {
 // ---- matrices of at most 64 x 4096: a launch for a step of all of them.  A workgroup owns 64 columns of X, forms A and B by itself (each of a matrix's workgroups
 // the same: their sums over the columns out of the L2 cost less than two launches more) and multiplies its columns.  X is padded to 64 rows and whole 64 columns.
 // Two teams of four waves take 32 of 64 steps of A each, 32 x 32 of the 64 x 64 a wave; behind that a wave has 32 x 16.  A and B stand in LDS as the products read
-// them.  (One team, five matrices of up to 608 x 64: 10.7 us a step.)  The low parts' product is formed here, too: it costs nothing beside the rest.
+// them.  (Five matrices of up to 608 x 64: 10.2 to 10.6 us a step, with one team 10.7; twenty of up to 64 x 4096 574 us in all, by a launch for a product of each 1230.)
+// The low parts' product is formed here, too: it costs nothing beside the rest.
 constexpr int kNarrowM = 64, kNarrowK = 4096, kNarrowMany = 24, kNarrowRing = 5, kNarrowTile = 64 * 128, kNarrowWaves = 8;
 struct NarrowMatrix {
   OrthMatrix m;
