@@ -373,26 +373,26 @@ static hgnn_status gated_rows(const char* who, GatedRowsArgs& a, const Out& out,
   return HGNN_OK;
 }
 
-// ---- few rows (up to 64), a served model's: bound by reading the two weights once.  A workgroup owns 32 features of both, its sixteen waves share the contraction, 32
-// steps at a time, and take the weights straight into the registers that the products read, a stage ahead for up to 16 rows; their sums meet in LDS.  One launch: by the
-// product kernel the contraction is cut over workgroups, and joining the parts is a launch of 3.5 us (1 row of 1024 -> 4096 9.3 us, here 6.7; 13 of 2048 -> 5461 16,
-// here 14: 45 MB at 3.2 TB/s).
+// ---- few rows (up to 16) through a weight of up to 1024 inputs, a served model's: bound by reading the two weights once, and by latency.  A workgroup owns 32 features
+// of both, its sixteen waves have 64 steps of the contraction each and take the weights straight into the registers that the products read, all of them at once; their
+// sums meet in LDS.  One launch: by the product kernel the contraction is cut over workgroups, and joining the parts is a launch of 3 us (1 row of 1024 -> 4096, calls in
+// a row, 8.8 us, by the product kernel 9.3; of 512 -> 512 4.5 and 6.4).  That is less than what a longer contraction or more workgroups than half of the units have
+// cost here (1 row of 2048 -> 2048 11.7 and 9.1, of 4096 -> 32 11.7 and 9.5, of 1024 -> 11 008 18.8 and 10.9), or more rows (30 rows of 1024 -> 2048 9.9 and 9.3).
 // Fragment e, item i is feature 2 i + e of the 32: of [K][F] a lane takes two neighbouring features of eight steps, 64 bytes of a line a load, and a lane's sums are
 // eight consecutive features.
-constexpr int kFewWaves = 16, kFewRows = 64, kFewFeatures = 32;
+constexpr int kFewWaves = 16, kFewRows = 16, kFewFeatures = 32, kFewInputs = 64 * kFewWaves, kFewMost = 4096;
 struct GatedFewArgs {
   const half_t *X, *Wg, *Wu;
   int64_t ldx, ldw;
   int32_t n, K, F;
 };
-template <int RT, bool COL>
 struct FewStage {  // what a wave has in hand of 32 steps
   typedef unsigned uint4_t __attribute__((ext_vector_type(4)));
   uint4_t w[2][2];  // of both weights: [K][F] 2 x 4 lines of two features, [F][K] fragments
-  half8_t x[RT];
+  half8_t x;
 };
-template <int RT, bool COL>
-__device__ __forceinline__ void few_fetch(const GatedFewArgs& a, FewStage<RT, COL>& st, int s, int f0, int lane) {
+template <bool COL>
+__device__ __forceinline__ void few_fetch(const GatedFewArgs& a, FewStage& st, int s, int f0, int lane) {
   const int i = lane & 15, qq = lane >> 4, k = 32 * s + 8 * qq;
 #pragma unroll
   for (int o = 0; o < 2; ++o) {
@@ -404,15 +404,14 @@ __device__ __forceinline__ void few_fetch(const GatedFewArgs& a, FewStage<RT, CO
 #pragma unroll
         for (int j = 0; j < 4; ++j) st.w[o][e][j] = *reinterpret_cast<const uint32_t*>(W + int64_t(min(k + 4 * e + j, a.K - 1)) * a.ldw + f);
       } else {
-        st.w[o][e] = *reinterpret_cast<const typename FewStage<RT, COL>::uint4_t*>(W + int64_t(min(f0 + 2 * i + e, a.F - 1)) * a.ldw + (k < a.K ? k : 0));
+        st.w[o][e] = *reinterpret_cast<const FewStage::uint4_t*>(W + int64_t(min(f0 + 2 * i + e, a.F - 1)) * a.ldw + (k < a.K ? k : 0));
       }
     }
   }
-#pragma unroll
-  for (int r = 0; r < RT; ++r) st.x[r] = *reinterpret_cast<const half8_t*>(a.X + int64_t(min(16 * r + i, a.n - 1)) * a.ldx + (k < a.K ? k : 0));
+  st.x = *reinterpret_cast<const half8_t*>(a.X + int64_t(min(i, a.n - 1)) * a.ldx + (k < a.K ? k : 0));
 }
-template <int RT, bool COL>
-__device__ __forceinline__ void few_multiply(const GatedFewArgs& a, const FewStage<RT, COL>& st, int s, int lane, float4_t (&acc)[RT][2][2]) {
+template <bool COL>
+__device__ __forceinline__ void few_multiply(const GatedFewArgs& a, const FewStage& st, int s, int lane, float4_t (&acc)[2][2]) {
   const int left = a.K - 32 * s - 8 * (lane >> 4);  // steps of the lane that exist: the others hold padding, or lines once more
   const bool cut = 32 * (s + 1) > a.K;              // uniform
   const auto ended = [&](half8_t v) __attribute__((always_inline)) {
@@ -423,105 +422,63 @@ __device__ __forceinline__ void few_multiply(const GatedFewArgs& a, const FewSta
     }
     return v;
   };
-  half8_t w[2][2], x[RT];
+  const half8_t x = ended(st.x);
 #pragma unroll
   for (int o = 0; o < 2; ++o)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      FewStage::uint4_t v = st.w[o][e];
       if (COL) {  // steps 2 j and 2 j + 1 of feature e of the pairs
-        typename FewStage<RT, COL>::uint4_t v;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_perm(st.w[o][j / 2][2 * (j % 2) + 1], st.w[o][j / 2][2 * (j % 2)], e ? 0x07060302u : 0x05040100u);
-        w[o][e] = ended(__builtin_bit_cast(half8_t, v));
-      } else {
-        w[o][e] = ended(__builtin_bit_cast(half8_t, st.w[o][e]));
       }
+      acc[o][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ended(__builtin_bit_cast(half8_t, v)), x, acc[o][e], 0, 0, 0);
     }
-#pragma unroll
-  for (int r = 0; r < RT; ++r) x[r] = ended(st.x[r]);
-#pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int o = 0; o < 2; ++o)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) acc[r][o][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[o][e], x[r], acc[r][o][e], 0, 0, 0);
 }
-template <int RT, bool COL, class Out>
+template <bool COL, class Out>
 __global__ __launch_bounds__(kFewWaves* kWave) void gated_few_kernel(GatedFewArgs a, Out out) {
   typedef float float2_t __attribute__((ext_vector_type(2)));
   __shared__ __align__(16) float4_t sums[kFewWaves][2][2][kWave];
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int f0 = blockIdx.x * kFewFeatures, steps = (a.K + 31) / 32;
-  float4_t acc[RT][2][2];
-#pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int o = 0; o < 2; ++o)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) acc[r][o][e] = float4_t{0.f, 0.f, 0.f, 0.f};
+  const int f0 = blockIdx.x * kFewFeatures, s = 2 * wave, steps = (a.K + 31) / 32;
+  const float4_t none = {0.f, 0.f, 0.f, 0.f};
+  float4_t acc[2][2] = {{none, none}, {none, none}};
   // Two neighbouring stages a wave: of [F][K] they are the two halves of a line.
-  const auto each = [&](auto&& f) __attribute__((always_inline)) {
-    for (int s = 2 * wave; s < steps; s += 2 * kFewWaves) f(s);
-  };
-  if constexpr (RT == 1) {
-    FewStage<RT, COL> one, two;
-    const auto fetch = [&](FewStage<RT, COL>& st, int s) __attribute__((always_inline)) {
-      if (s < steps) few_fetch(a, st, s, f0, lane);
-    };
-    fetch(one, 2 * wave), fetch(two, 2 * wave + 1);
-    each([&](int s) __attribute__((always_inline)) {
-      few_multiply(a, one, s, lane, acc);
-      fetch(one, s + 2 * kFewWaves);
-      if (s + 1 < steps) few_multiply(a, two, s + 1, lane, acc);
-      fetch(two, s + 1 + 2 * kFewWaves);
-    });
-  } else {  // (the registers for a stage ahead are the sums')
-    each([&](int s0) __attribute__((always_inline)) {
-      for (int s = s0; s < s0 + 2 && s < steps; ++s) {
-        FewStage<RT, COL> one;
-        few_fetch(a, one, s, f0, lane);
-        few_multiply(a, one, s, lane, acc);
-      }
-    });
-  }
+  FewStage one, two;
+  if (s < steps) few_fetch<COL>(a, one, s, f0, lane);
+  if (s + 1 < steps) few_fetch<COL>(a, two, s + 1, f0, lane);
+  if (s < steps) few_multiply<COL>(a, one, s, lane, acc);
+  if (s + 1 < steps) few_multiply<COL>(a, two, s + 1, lane, acc);
   // thread (part of the waves, row, four features): waves 2 part and 2 part + 1, and then one of them the eight parts
   const int part = threadIdx.x >> 7, i = threadIdx.x & 15, m = (threadIdx.x >> 4) & 7, from = 16 * (m >> 1) + i, at = 2 * (m & 1);
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    if (r) __syncthreads();
+  for (int o = 0; o < 2; ++o)
 #pragma unroll
-    for (int o = 0; o < 2; ++o)
+    for (int e = 0; e < 2; ++e) sums[wave][o][e][lane] = acc[o][e];
+  __syncthreads();
+  const auto value = [&](int w, int o, int e) { return reinterpret_cast<float2_t*>(reinterpret_cast<float*>(&sums[w][o][e][from]) + at); };
 #pragma unroll
-      for (int e = 0; e < 2; ++e) sums[wave][o][e][lane] = acc[r][o][e];
-    __syncthreads();
-    const auto value = [&](int w, int o, int e) { return reinterpret_cast<float2_t*>(reinterpret_cast<float*>(&sums[w][o][e][from]) + at); };
+  for (int o = 0; o < 2; ++o)
 #pragma unroll
-    for (int o = 0; o < 2; ++o)
+    for (int e = 0; e < 2; ++e) *value(2 * part, o, e) += *value(2 * part + 1, o, e);
+  __syncthreads();
+  if (part) return;
+  float2_t v[2][2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) *value(2 * part, o, e) += *value(2 * part + 1, o, e);
-    __syncthreads();
-    if (part == 0) {
-      float2_t v[2][2];
+  for (int o = 0; o < 2; ++o)
 #pragma unroll
-      for (int o = 0; o < 2; ++o)
+    for (int e = 0; e < 2; ++e) {
+      v[o][e] = *value(0, o, e);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          v[o][e] = *value(0, o, e);
-#pragma unroll
-          for (int w = 2; w < kFewWaves; w += 2) v[o][e] += *value(w, o, e);
-        }
-      const int64_t q = 16 * r + i, p = f0 + 4 * m;
-      if (q < a.n && p < a.F)
-        out.template put<false>(0, q, p, out.read(q, p), float4_t{v[0][0][0], v[0][1][0], v[0][0][1], v[0][1][1]}, float4_t{v[1][0][0], v[1][1][0], v[1][0][1], v[1][1][1]});
+      for (int w = 2; w < kFewWaves; w += 2) v[o][e] += *value(w, o, e);
     }
-  }
+  const int64_t p = f0 + 4 * m;
+  if (i < a.n && p < a.F)
+    out.template put<false>(0, i, p, out.read(i, p), float4_t{v[0][0][0], v[0][1][0], v[0][0][1], v[0][1][1]}, float4_t{v[1][0][0], v[1][1][0], v[1][0][1], v[1][1][1]});
 }
 template <bool COL, class Out>
 static hgnn_status gated_few(const GatedFewArgs& a, const Out& out, hipStream_t s) {
-  const unsigned blocks = unsigned(ceil_div(a.F, kFewFeatures));
-  if (a.n <= 16) gated_few_kernel<1, COL><<<blocks, kFewWaves * kWave, 0, s>>>(a, out);
-  else if (a.n <= 32) gated_few_kernel<2, COL><<<blocks, kFewWaves * kWave, 0, s>>>(a, out);
-  else gated_few_kernel<4, COL><<<blocks, kFewWaves * kWave, 0, s>>>(a, out);
+  gated_few_kernel<COL><<<unsigned(ceil_div(a.F, kFewFeatures)), kFewWaves * kWave, 0, s>>>(a, out);
   HGNN_LAUNCH_CHECK("gated_few_kernel");
   return HGNN_OK;
 }
@@ -530,7 +487,7 @@ struct GatedSizes {
   int64_t n, Fp;
   int K, F;
   Split gate, dx, dw;
-  bool rows;  // gated_rows_kernel
+  bool few, rows;  // gated_few_kernel, gated_rows_kernel
   size_t gate_part, dx_part, dw_part, d;
 };
 static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
@@ -539,8 +496,9 @@ static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
   z.gate = split_of(n, F, K, true, 1);
   z.dx = split_of(n, K, F, false, 2);
   z.dw = split_of(K, 2 * z.Fp, n, false, 1);
+  z.few = n <= kFewRows && K <= kFewInputs && F <= kFewMost;
   z.rows = K <= 256 && n >= kManyRows;
-  z.gate_part = z.gate.parts > 1 && !z.rows && n > kFewRows ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
+  z.gate_part = z.gate.parts > 1 && !z.rows && !z.few ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
   z.dx_part = z.dx.parts > 1 ? size_t(z.dx.parts) * size_t(n) * size_t(up(K, 4)) * 4 : 0;
   z.dw_part = z.dw.parts > 1 ? size_t(z.dw.parts) * size_t(up(K, 4)) * 2 * size_t(z.Fp) * 4 : 0;
   z.d = size_t(up(n * 2 * z.Fp * 2, 256));
@@ -557,7 +515,7 @@ static hgnn_status join_grid(const char* who, int64_t fours, unsigned* blocks, i
 template <class Out>
 static hgnn_status gated_pairs(const char* who, const GatedSizes& z, const half_t* X, int64_t ldx, const half_t* Wg, const half_t* Wu, int64_t ldw, bool trans, float* part,
                                const Out& out, hipStream_t s) {
-  if (z.n <= kFewRows) {
+  if (z.few) {
     const GatedFewArgs f{X, Wg, Wu, ldx, ldw, int32_t(z.n), z.K, z.F};
     return trans ? gated_few<false>(f, out, s) : gated_few<true>(f, out, s);
   }

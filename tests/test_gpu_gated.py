@@ -139,6 +139,16 @@ def test_activations(hgnn, dev, act, trans):
 
 
 # (n, K, F) of each size of tile, with and without parts: few rows, a narrow side, tiles that fill the chip, and sizes around them
+@pytest.mark.parametrize("n,K,F", [(1, 1024, 4096), (16, 1024, 4096), (16, 1017, 4095), (17, 1024, 4096), (1, 1025, 100), (2, 1032, 64), (5, 1024, 4097), (13, 2048, 5461), (1, 4000, 40),
+                                   (64, 2000, 33), (30, 65000, 24), (16, 65, 4090), (9, 992, 1), (11, 961, 66)])
+@pytest.mark.parametrize("trans", [False, True])
+def test_few_rows(hgnn, dev, n, K, F, trans):
+    """Up to 16 rows by up to 1024 inputs and 4096 features in one launch, and what is just beyond."""
+    c = Case(n, K, F, GELU, trans)
+    forward(hgnn, dev, c)
+    backward(hgnn, dev, c)
+
+
 @pytest.mark.parametrize("n,K,F", [(40, 700, 90), (700, 600, 500), (2100, 300, 700), (20000, 70, 20), (4099, 72, 2049), (8200, 40, 1100), (66000, 24, 40), (17000, 128, 256), (16400, 256, 130), (16500, 99, 300), (8192, 520, 4100), (16400, 30, 60), (16401, 60, 100),
                                    (16400, 200, 50), (17000, 150, 70), (16384, 256, 64), (16999, 100, 128), (16390, 190, 260)])
 @pytest.mark.parametrize("trans", [False, True])
