@@ -175,7 +175,6 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 enum Size { kFew, kMid, kWide };
 constexpr int kFull = 256;  // compute units
 constexpr int kLong = 512;
-constexpr int64_t kManyRows = 16384;
 template <ProductKind KIND, bool QCOL, bool PCOL, class Call>
 static hgnn_status with_product(Size size, Call&& call) {
   constexpr int two = KIND == kTwo ? 2 : 1;  // two results: half as many items of P
@@ -208,6 +207,9 @@ static Split split_of(int64_t nq, int64_t np, int64_t K, bool two, int segments)
 // the other waves' stores are never waited for.  A barrier a tile hands it over and takes back the one before.  (Two
 // workgroups of four waves and one do not fit a compute unit's registers: 65 -> 100 us.)  Features are dealt out such that a lane's 2 x 4 sums are eight consecutive ones.
 constexpr int kRowsWaves = 8, kRowsTile = 64;
+// From 16 384 rows on, and from 2048 on where the features are one workgroup's or C is large (the product kernel behind, us: 16 384 x 128 -> 512 11.5 and 12.4, -> 2048 29.0 and
+// 39.5; 6000 x 128 -> 40 4.3 and 5.8, -> 512 7.5 and 7.3, -> 2048 14.7 and 17.7, -> 5461 30 and 43; 2000 x 256 -> 5461 25.3 and 24.6).
+static bool is_rows(int64_t n, int64_t K, int64_t F) { return K <= 256 && (n >= 16384 || (n >= 2048 && (F <= 64 || n * F >= int64_t(1) << 23))); }
 struct GatedRowsArgs {
   const half_t *X, *Wg, *Wu;
   int64_t ldx, ldw, n;
@@ -497,7 +499,7 @@ static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
   z.dx = split_of(n, K, F, false, 2);
   z.dw = split_of(K, 2 * z.Fp, n, false, 1);
   z.few = n <= kFewRows && K <= kFewInputs && F <= kFewMost;
-  z.rows = K <= 256 && n >= kManyRows;
+  z.rows = is_rows(n, K, F);
   z.gate_part = z.gate.parts > 1 && !z.rows && !z.few ? size_t(z.gate.parts) * size_t(n) * 2 * size_t(z.Fp) * 4 : 0;
   z.dx_part = z.dx.parts > 1 ? size_t(z.dx.parts) * size_t(n) * size_t(up(K, 4)) * 4 : 0;
   z.dw_part = z.dw.parts > 1 ? size_t(z.dw.parts) * size_t(up(K, 4)) * 2 * size_t(z.Fp) * 4 : 0;

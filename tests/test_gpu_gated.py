@@ -150,7 +150,7 @@ def test_few_rows(hgnn, dev, n, K, F, trans):
 
 
 @pytest.mark.parametrize("n,K,F", [(40, 700, 90), (700, 600, 500), (2100, 300, 700), (20000, 70, 20), (4099, 72, 2049), (8200, 40, 1100), (66000, 24, 40), (17000, 128, 256), (16400, 256, 130), (16500, 99, 300), (8192, 520, 4100), (16400, 30, 60), (16401, 60, 100),
-                                   (16400, 200, 50), (17000, 150, 70), (16384, 256, 64), (16999, 100, 128), (16390, 190, 260)])
+                                   (16400, 200, 50), (17000, 150, 70), (16384, 256, 64), (16999, 100, 128), (16390, 190, 260), (2048, 100, 4096), (2047, 100, 4100), (2050, 250, 40), (3001, 33, 64)])
 @pytest.mark.parametrize("trans", [False, True])
 def test_tiles(hgnn, dev, n, K, F, trans):
     c = Case(n, K, F, SILU, trans)
