@@ -124,33 +124,34 @@ struct LastOut {  // the same into the caller's matrix
     return v;
   }
 };
-struct SumsPart {  // [parts][nq][np]
+struct SumsPart {  // [parts][nq - q0][np]
   float* part;
-  int64_t nq, np;
+  int64_t q0, nq, np;
   typedef ProductNothing Read;
   __device__ Read read(int64_t, int64_t) const { return {}; }
   template <bool WHOLE>
-  __device__ void put(int64_t k, int64_t q, int64_t p, const Read&, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * nq + q) * np + p) = v; }
+  __device__ void put(int64_t k, int64_t q, int64_t p, const Read&, const float4_t& v) const { *reinterpret_cast<float4_t*>(part + (k * (nq - q0) + q - q0) * np + p) = v; }
 };
-// The parts of 32 x 32 sums in order (blockIdx.x and y, of the tiles on and below the diagonal with `lower`), four sums a lane, and what becomes of them; the mirror
+// The parts of 32 x 32 sums in order (blockIdx.x and y, from line `from` on, of the tiles on and below the diagonal with `lower`, and of those the ones in tiles of
+// 128 x 128 from number `first` on), four sums a lane, and what becomes of them; the mirror
 // places get theirs through LDS, in whole pieces (by twos the join of 1024 x 1024 took 11 us; tiles of 64 x 64, sixteen sums a lane, took 10.4 us for 7 parts of
 // 1024 x 1024, bound by their chains of loads, these 5.4).
 constexpr int kJoinTile = 32;
 template <class Out>
-__global__ __launch_bounds__(kBlock) void sums_join_kernel(const float* part, int parts, int64_t nq, int64_t np, int lower, Out out) {
+__global__ __launch_bounds__(kBlock) void sums_join_kernel(const float* part, int parts, int64_t from, int64_t nq, int64_t np, int lower, int first, Out out) {
   __shared__ __align__(16) float tile[kJoinTile][kJoinTile + 4];
   static_assert(kJoinTile * kJoinTile == 4 * kBlock, "four sums a lane");
-  const int64_t tq = blockIdx.x, tp = blockIdx.y;
-  if (lower && tp > tq) return;  // uniform
+  const int64_t tq = from / kJoinTile + blockIdx.x, tp = blockIdx.y, line = tq * kJoinTile / 128;
+  if (lower && (tp > tq || line * (line + 1) / 2 + tp * kJoinTile / 128 < first)) return;  // uniform
   const int64_t q0 = tq * kJoinTile, p0 = tp * kJoinTile;
   const bool mirror = lower && tp < tq;
   const int r = threadIdx.x / (kJoinTile / 4), c = 4 * (threadIdx.x % (kJoinTile / 4));
   const int64_t q = q0 + r, p = p0 + c;
   if (q < nq && p < np) {
     float4_t v = {0.f, 0.f, 0.f, 0.f};
-    const float* at = part + q * np + p;
+    const float* at = part + (q - from) * np + p;
 #pragma unroll 8
-    for (int k = 0; k < parts; ++k, at += nq * np) v += *reinterpret_cast<const float4_t*>(at);
+    for (int k = 0; k < parts; ++k, at += (nq - from) * np) v += *reinterpret_cast<const float4_t*>(at);
     const float4_t y = out.join(q, p, v);
     if (mirror) {
 #pragma unroll
@@ -298,13 +299,18 @@ constexpr int kOrthFull = 256;
 struct OrthSplit {
   int tile, parts;
   int64_t part;
+  int first, rest, rest_parts;  // the tiles from `first` on by themselves, their contraction cut; rest = 0: none
+  int64_t rest_part, from;      // lines from `from` on
 };
+// 128 x 128 tiles that run at a time, two a compute unit.  A few more than a multiple of that would take as long as half of all: they are a launch of their own, their
+// contraction cut for as many workgroups (4096 x 4096, five steps, ten such products of 528 tiles: 4.00 ms in one launch each, 3.85 so: 198 us, 15 and 6 for the join).
+constexpr int kOrthAtOnce = 512;
 static OrthSplit orth_split(int64_t nq, int64_t np, int64_t K, bool lower) {
   const auto tiles = [&](int64_t b) {
     const int64_t l = ceil_div(nq, b);
     return lower ? l * (l + 1) / 2 : l * ceil_div(np, b);
   };
-  OrthSplit s;
+  OrthSplit s{};
   // Tiles of 64 read LDS twice as often for their products: where a side is short, or where a compute unit has at most one of them and a short contraction (1024 x
   // 1024, K = 1024, us: 136 of them 15, 36 of 128 in four parts 14 and a join of 5; K = 4096: 136 in four parts 22.5, 36 of 128 in seven 20.5, and the join).  Parts until
   // every compute unit has a workgroup, of 256 steps at least (a join costs about as much as those).
@@ -312,6 +318,15 @@ static OrthSplit orth_split(int64_t nq, int64_t np, int64_t K, bool lower) {
   const int64_t t = tiles(s.tile), parts = t > kOrthFull / 2 || K <= 1024 ? 1 : std::min(kOrthFull / t, std::max<int64_t>(1, K / 256));
   s.part = std::max<int64_t>(32, up32(ceil_div(K, std::max<int64_t>(parts, 1))));
   s.parts = int(std::max<int64_t>(1, ceil_div(K, s.part)));
+  const int64_t rest = t % kOrthAtOnce;
+  if (lower && s.tile == 128 && t > kOrthAtOnce && t <= 4 * kOrthAtOnce && rest > 0 && rest <= kOrthAtOnce / 4 && K >= 1024) {
+    s.first = int(t - rest), s.rest = int(rest);
+    s.rest_part = up32(ceil_div(K, std::min(kOrthAtOnce / rest, K / 256)));
+    s.rest_parts = int(ceil_div(K, s.rest_part));
+    int64_t line = 0;
+    while ((line + 1) * (line + 2) / 2 <= s.first) ++line;
+    s.from = line * 128;
+  }
   return s;
 }
 struct OrthSizes {
@@ -325,7 +340,9 @@ static OrthSizes orth_sizes(int64_t rows, int64_t cols) {
   z.flip = rows > cols;
   z.m = up32(std::min(rows, cols)), z.k = up32(std::max(rows, cols));
   z.gram = orth_split(z.m, z.m, z.k, true), z.square = orth_split(z.m, z.m, z.m, true), z.step = orth_split(z.m, z.k, z.m, false);
-  const auto part = [](const OrthSplit& s, int64_t q, int64_t p) { return s.parts > 1 ? size_t(s.parts) * size_t(q) * size_t(p) * 4 : 0; };
+  const auto part = [](const OrthSplit& s, int64_t q, int64_t p) {
+    return s.parts > 1 ? size_t(s.parts) * size_t(q) * size_t(p) * 4 : s.rest ? size_t(s.rest_parts) * size_t(q - s.from) * size_t(p) * 4 : 0;
+  };
   z.x = size_t(z.m) * size_t(z.k) * 2, z.a = size_t(z.m) * size_t(z.m) * 2;
   z.part = std::max({part(z.gram, z.m, z.m), part(z.square, z.m, z.m), part(z.step, z.m, z.k)});
   z.bytes = kNormParts * sizeof(double) + 4 * z.x + 4 * z.a + z.part;
@@ -566,12 +583,21 @@ static hgnn_status orth_product(const char* who, const Pairs& Q, const Pairs& P,
     product_tiles<SplitMid<PCOL>>(a);
     return int64_t(a.tiles) * a.parts <= kOrthFull ? product<SplitDeep<PCOL>>(who, a, to, s) : product<SplitMid<PCOL>>(who, a, to, s);
   };
-  if (split.parts == 1) return go(out);
-  const hgnn_status st = go(SumsPart{part, nq, np});
-  if (st != HGNN_OK) return st;
-  sums_join_kernel<<<dim3(unsigned(ceil_div(nq, kJoinTile)), unsigned(ceil_div(np, kJoinTile))), kBlock, 0, s>>>(part, split.parts, nq, np, lower, out);
-  HGNN_LAUNCH_CHECK("sums_join_kernel");
-  return HGNN_OK;
+  const auto join = [&](int parts, int64_t from, int first) -> hgnn_status {
+    sums_join_kernel<<<dim3(unsigned(ceil_div(nq - from, kJoinTile)), unsigned(ceil_div(np, kJoinTile))), kBlock, 0, s>>>(part, parts, from, nq, np, lower, first, out);
+    HGNN_LAUNCH_CHECK("sums_join_kernel");
+    return HGNN_OK;
+  };
+  if (split.parts == 1) {
+    a.some = split.first;
+    hgnn_status st = go(out);
+    if (st != HGNN_OK || !split.rest) return st;
+    a.first = split.first, a.some = split.rest, a.part = split.rest_part, a.parts = split.rest_parts;
+    st = go(SumsPart{part, split.from, nq, np});
+    return st == HGNN_OK ? join(split.rest_parts, split.from, split.first) : st;
+  }
+  const hgnn_status st = go(SumsPart{part, 0, nq, np});
+  return st == HGNN_OK ? join(split.parts, 0, 0) : st;
 }
 
 static hgnn_status orth_matrix(const char* who, const hgnn_grad& g, int32_t steps, const float* coef, float scale, char* ws, hipStream_t s) {

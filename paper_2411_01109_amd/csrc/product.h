@@ -46,6 +46,7 @@ struct ProductArgs {
   int32_t lines, tiles_p;
   int32_t parts;
   int32_t lower;    // square C of square tiles: those on and below the diagonal alone
+  int32_t first, some;  // the first tile of this launch, and how many (0: all)
 };
 
 static __device__ const uint4 g_product_zero = {0, 0, 0, 0};
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs a, 
   const uint32_t work = x * (all >> 3) + min(x, more) + (id >> 3);
   const int64_t part = __builtin_amdgcn_readfirstlane(int(a.parts == 1 ? 0 : work / uint32_t(a.tiles)));
   uint32_t tq, tp;
-  product_tile(a, work - uint32_t(part) * uint32_t(a.tiles), tq, tp);
+  product_tile(a, uint32_t(a.first) + work - uint32_t(part) * uint32_t(a.tiles), tq, tp);
   // (the divisions go through vector registers: back to scalar ones, which the loads to LDS take their places from)
   const int64_t q0 = int64_t(__builtin_amdgcn_readfirstlane(int(tq))) * S::BQ, p0 = int64_t(__builtin_amdgcn_readfirstlane(int(tp))) * S::BP;
   const int64_t k_begin = part * a.part, k_end = min(a.K, k_begin + a.part), count = k_end - k_begin;  // of a segment
@@ -361,7 +362,7 @@ inline void product_tiles(ProductArgs& a) {
   const int64_t lines = ceil_div(a.nq, S::BQ), tiles_p = ceil_div(a.np, S::BP);
   const int64_t tiles = a.lower ? lines * (lines + 1) / 2 : lines * tiles_p;
   a.lines = int32_t(lines), a.tiles_p = int32_t(tiles_p);
-  a.tiles = int32_t(std::min<int64_t>(tiles, 0x7fffffff));
+  a.tiles = a.some ? a.some : int32_t(std::min<int64_t>(tiles, 0x7fffffff));
 }
 // beyond 64 KB of dynamic LDS the runtime wants to be told, once for a kernel and a device (told: a bit a device; two threads write the same at worst)
 inline hgnn_status product_lds(const void* kernel, int bytes, uint64_t* told) {

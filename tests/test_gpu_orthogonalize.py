@@ -83,6 +83,12 @@ def test_shapes(hgnn, dev, rows, cols):
     check(hgnn, dev, [matrix(rows, cols, F16)], [CUBIC] * 7, F16, scales=[0.2 * max(1, rows / cols) ** 0.5], pitch=3, offset=1)
 
 
+@pytest.mark.parametrize("rows,cols", [(4096, 4096), (4130, 4101)])
+def test_tiles_left_over(hgnn, dev, rows, cols):
+    """Sides whose tiles are a few more than run at once: those have their contraction cut and their sums joined."""
+    check(hgnn, dev, [matrix(rows, cols)], [QUINTIC])
+
+
 @pytest.mark.parametrize("rows,cols", [(1024, 1500), (1300, 1200), (100, 5000), (5000, 70), (2100, 300), (60, 4096), (4096, 33), (10, 4097), (2500, 2), (64, 4500)])
 def test_large(hgnn, dev, rows, cols):
     check(hgnn, dev, [matrix(rows, cols)], [QUINTIC] * 5)
