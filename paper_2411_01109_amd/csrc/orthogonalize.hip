@@ -374,11 +374,23 @@ __device__ __forceinline__ const NarrowMatrix& narrow_matrix(const NarrowArgs& a
   while (i + 1 < a.count && a.m[i + 1].first <= block) ++i;  // uniform
   return a.m[i];
 }
-// the norm (each of a matrix's workgroups the same) and X = G / |G|; without steps the result
+// the norm (each of a matrix's workgroups the same, from all of the gradient, which this launch therefore only reads) and X = G / |G|
 __global__ __launch_bounds__(1024) void narrow_begin_kernel(NarrowArgs a) {
   const NarrowMatrix& n = narrow_matrix(a, blockIdx.x);
   const double inv = inverse_root(block_sum<1024>(squares_of(n.m, 0, 1)));
-  orth_turn<1024>(n.m, n.flip, inv, 0, 64 * int64_t(int(blockIdx.x) - n.first), Pairs{n.X, 2 * int64_t(n.k)}, kNarrowM, n.k, a.last, n.scale);
+  orth_turn<1024>(n.m, n.flip, inv, 0, 64 * int64_t(int(blockIdx.x) - n.first), Pairs{n.X, 2 * int64_t(n.k)}, kNarrowM, n.k, 0, n.scale);
+}
+// Without steps the result is the scaled gradient, in place over the gradient itself: the norms, a workgroup a matrix, are a launch before it, since no workgroup may
+// write its columns while another still sums the squares of all of them.
+__global__ __launch_bounds__(1024) void narrow_norms_kernel(NarrowArgs a) {
+  const NarrowMatrix& n = a.m[blockIdx.x];
+  const double inv = inverse_root(block_sum<1024>(squares_of(n.m, 0, 1)));
+  if (threadIdx.x == 0) *reinterpret_cast<double*>(n.X) = inv;
+}
+__global__ __launch_bounds__(1024) void narrow_scale_kernel(NarrowArgs a) {
+  const NarrowMatrix& n = narrow_matrix(a, blockIdx.x);
+  const double inv = *reinterpret_cast<const double*>(n.X);
+  orth_turn<1024>(n.m, n.flip, inv, 0, 64 * int64_t(int(blockIdx.x) - n.first), Pairs{n.X, 2 * int64_t(n.k)}, kNarrowM, n.k, 1, n.scale);
 }
 // four values (q, p .. p + 3) of a 64 x 64 matrix to where ProductReads<false, true> finds them
 __device__ __forceinline__ void narrow_put(unsigned char* at, int q, int p, const float4_t& v) {
@@ -558,9 +570,15 @@ static hgnn_status orth_narrow(const char* who, int32_t count, const hgnn_grad* 
       ws += narrow_bytes(g.rows, g.cols);
     }
     if (a.count == 0) break;
+    if (steps == 0) {
+      narrow_norms_kernel<<<unsigned(a.count), 1024, 0, s>>>(a);
+      HGNN_LAUNCH_CHECK("narrow_norms_kernel");
+      narrow_scale_kernel<<<unsigned(blocks), 1024, 0, s>>>(a);
+      HGNN_LAUNCH_CHECK("narrow_scale_kernel");
+      continue;
+    }
     const hgnn_status st = product_lds(reinterpret_cast<const void*>(&narrow_step_kernel), kBytes, &told);
     if (st != HGNN_OK) return st;
-    a.last = steps == 0;
     narrow_begin_kernel<<<unsigned(blocks), 1024, 0, s>>>(a);
     HGNN_LAUNCH_CHECK("narrow_begin_kernel");
     for (int k = 0; k < steps; ++k) {

@@ -1,0 +1,65 @@
+"""What the calls between two aggregations, and between the clipped gradient and the weight, launch and refuse, on the host: libhgnn.so on a runtime that executes
+nothing and writes launches down (fake_hip.cpp)."""
+import ctypes
+import os
+import re
+import subprocess
+import sys
+
+import pytest
+
+from test_host_memory import A, LIB, Host, fake, i64, vp  # noqa: F401
+
+F16, F32 = 0, 1
+f32, size_t = ctypes.c_float, ctypes.c_size_t
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("grad", vp), ("out", vp), ("rows", i64), ("cols", i64), ("ld", i64), ("ld_out", i64), ("type", ctypes.c_int), ("out_type", ctypes.c_int)]
+
+
+def launches(h, call):
+    h.fake.fake_reset(h.path)
+    st = call()
+    return st, [re.match(r"_ZN4hgnn(\d+)(.*)", n) for n in h.fake.fake_launched().decode().split()]
+
+
+def names_of(found):
+    return [m.group(2)[:int(m.group(1))] for m in found]
+
+
+def orthogonalize(h, sides, steps, in_place):
+    mats = (Grad * len(sides))()
+    for i, (r, c) in enumerate(sides):
+        at = h.data + (i + 1) * (1 << 21)
+        mats[i] = Grad(at, None if in_place else at + (1 << 20), r, c, c, c, F32, F32)
+    h.lib.hgnn_orthogonalize_workspace.restype = size_t
+    need = h.lib.hgnn_orthogonalize_workspace(len(sides), mats)
+    coef = (f32 * max(1, 3 * steps))(*([1.5, -0.5, 0.0] * steps))
+    st, found = launches(h, lambda: h.lib.hgnn_orthogonalize(len(sides), mats, steps, coef, None, vp(h.data), size_t(need), vp(A)))
+    assert st == 0
+    return names_of(found)
+
+
+def norms_before_results(h):
+    """No launch reads all of a gradient and writes the result, which in place is that gradient: without steps the norms are a launch of their own."""
+    for in_place in (True, False):
+        assert orthogonalize(h, [(64, 608)], 0, in_place) == ["narrow_norms_kernel", "narrow_scale_kernel"]
+        assert orthogonalize(h, [(64, 4096)] * 30, 0, in_place) == ["narrow_norms_kernel", "narrow_scale_kernel"] * 2
+        assert orthogonalize(h, [(65, 100)], 0, in_place) == ["orth_squares_kernel", "orth_begin_kernel"]
+        assert orthogonalize(h, [(64, 608), (64, 64)], 2, in_place) == ["narrow_begin_kernel"] + ["narrow_step_kernel"] * 2
+
+
+SCENARIOS = [norms_before_results]
+
+
+@pytest.mark.parametrize("name", [s.__name__ for s in SCENARIOS])
+def test_launches(hgnn, fake, name):  # noqa: F811
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), fake, LIB, name], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
+if __name__ == "__main__":
+    host = Host(sys.argv[1], sys.argv[2])
+    {s.__name__: s for s in SCENARIOS}[sys.argv[3]](host)
+    print("ok")
