@@ -42,7 +42,9 @@ __device__ __forceinline__ void gate_both(int act, const float4_t& x, float4_t& 
     case HGNN_SILU: HGNN_EACH(const float p = gate_sigmoid(x[e]); value[e] = x[e] * p; slope[e] = p * (1.f + x[e] * (1.f - p)))
     case HGNN_GELU:
       HGNN_EACH(float d; const float phi = gate_normal(x[e], d); value[e] = x[e] * phi; slope[e] = fmaf(x[e] * 0.39894228f, d, phi))
-    case HGNN_SIGMOID: HGNN_EACH(value[e] = gate_sigmoid(x[e]); slope[e] = value[e] * (1.f - value[e]))
+    case HGNN_SIGMOID:  // exp(-|x|) / (1 + exp(-|x|))^2: p (1 - p) would lose its digits where p is near 1 (all of them from x = 17 on)
+      HGNN_EACH(const float d = __builtin_amdgcn_exp2f(__builtin_fabsf(x[e]) * -1.44269504f), r = __builtin_amdgcn_rcpf(1.f + d); value[e] = x[e] < 0.f ? d * r : r;
+                slope[e] = d * r * r)
     default: HGNN_EACH(value[e] = x[e] > 0.f ? x[e] : x[e] == x[e] ? 0.f : x[e]; slope[e] = x[e] > 0.f ? 1.f : 0.f)
   }
 #undef HGNN_EACH
