@@ -661,8 +661,8 @@ typedef struct {
 /* The gradients of a block given those of H (dH, of the stream's type, or NULL: 0; required without `pre`) and of Z (dZ,
  * with `pre`), from H as hgnn_residual_norm stored it (where there is a norm `pre`) and Y (where there is a norm `post` or a
  * gate).  The statistics of the rows are formed again.  Sums over rows are fp32, in a fixed order: no atomics, the same bits
- * on every run.  workspace is device memory of at least hgnn_residual_norm_grad_workspace(n, F) bytes (16-byte aligned),
- * owned by the caller and overwritten; it may be NULL where no sum over rows is wanted.  But for dR in the place of dH no
+ * on every run.  workspace is device memory of at least hgnn_residual_norm_grad_workspace(n, F) bytes (16-byte aligned; enough
+ * for any fewer rows of that F, too), owned by the caller and overwritten; it may be NULL where no sum over rows is wanted.  But for dR in the place of dH no
  * output may overlap an input or another output. */
 size_t hgnn_residual_norm_grad_workspace(int64_t n, int32_t F);
 hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* block, hgnn_type type, const void* H, int64_t ldh, const hgnn_half* Y,
@@ -678,7 +678,8 @@ typedef enum { HGNN_SILU = 0, HGNN_GELU = 1, HGNN_SIGMOID = 2, HGNN_RELU = 3 } h
  * (HGNN_EUNSUPPORTED beyond).  All tensors need 16-byte aligned addresses and pitches that are multiples of 8, up
  * to 2^22 (HGNN_EUNSUPPORTED otherwise); rows are read in 16-byte pieces up to the pitch, whatever the padding columns hold never
  * reaches a result, and padding columns of outputs are not written.  Y may overlap no input.  workspace is device memory of
- * at least hgnn_gated_workspace(n, K, F) bytes (16-byte aligned; 0: none is needed), owned by the caller and overwritten. */
+ * at least hgnn_gated_workspace(n, K, F) bytes (16-byte aligned; 0: none is needed; enough for any fewer rows of that K and F,
+ * too), owned by the caller and overwritten. */
 size_t hgnn_gated_workspace(int64_t n, int32_t K, int32_t F);
 hgnn_status hgnn_gated(int64_t n, int32_t K, int32_t F, hgnn_activation act, const hgnn_half* X, int64_t ldx, const hgnn_half* Wg, const hgnn_half* Wu,
                        int64_t ldw, int32_t trans_w, hgnn_half* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
@@ -688,7 +689,7 @@ hgnn_status hgnn_gated(int64_t n, int32_t K, int32_t F, hgnn_activation act, con
  * dWu together, may be NULL: not wanted.  G and U are formed again; dG and dU pass through the workspace in fp16 as all
  * vertex-level gradients here do (scale the loss as for those), and sums are fp32 in a fixed order.  Tensors as for
  * hgnn_gated, no output may overlap an input or another output; workspace at least hgnn_gated_grad_workspace(n, K, F) bytes
- * (16-byte aligned). */
+ * (16-byte aligned; enough for any fewer rows, too). */
 size_t hgnn_gated_grad_workspace(int64_t n, int32_t K, int32_t F);
 hgnn_status hgnn_gated_grad(int64_t n, int32_t K, int32_t F, hgnn_activation act, const hgnn_half* X, int64_t ldx, const hgnn_half* Wg,
                             const hgnn_half* Wu, int64_t ldw, int32_t trans_w, const hgnn_half* dY, int64_t lddy, hgnn_half* dX, int64_t lddx,

@@ -188,6 +188,7 @@ struct Split {
   Size size;
   int parts;
   int64_t part;  // contraction steps of a part
+  int most;      // parts that were asked for: no fewer, and no fewer for a longer contraction
 };
 // nq x np sums (`two`: a pair of each) over segments of K steps, which are cut alike.
 static Split split_of(int64_t nq, int64_t np, int64_t K, bool two, int segments) {
@@ -198,6 +199,7 @@ static Split split_of(int64_t nq, int64_t np, int64_t K, bool two, int segments)
   // A launch of these takes 6 us and 0.6 for 64 steps, a join 4 to 6: parts of 512 steps at least, and none where half of the units have a tile (370 x 565 -> 1173, us:
   // the pairs by 57 tiles in five parts 14.6 and 6.1 for the join, X^T D in three 13.0 and 6.0; 9611 x 1402 -> 91, 152 tiles in two 18.5 and 5.4).
   const int64_t parts = 2 * t > kFull ? 1 : std::min(ceil_div(kFull, t), std::max<int64_t>(1, segments * K / 512));
+  s.most = int(parts);
   s.part = std::max<int64_t>(64, up(ceil_div(K, std::max<int64_t>(parts, 1)), 64));
   s.parts = int(std::max<int64_t>(1, ceil_div(K, s.part)));
   return s;
@@ -508,6 +510,22 @@ static GatedSizes gated_sizes(int64_t n, int32_t K, int32_t F) {
   z.d = size_t(up(n * 2 * z.Fp * 2, 256));
   return z;
 }
+// What the queries answer: enough for every number of rows up to n, since a program keeps one workspace for batches of all sizes, and fewer rows have fewer tiles
+// and then more parts.  For the same number of tiles the most rows need most; from 128 rows on parts only become fewer, until there is one.  (The gradients' contraction
+// over the rows has the parts of n, asked for.)
+static size_t gated_most(int64_t n, int32_t K, int32_t F, bool grad) {
+  size_t most = 0;
+  const auto look = [&](int64_t rows) {
+    const GatedSizes z = gated_sizes(rows, K, F);
+    most = std::max(most, grad ? std::max(z.gate_part, z.dx_part) : z.gate_part);
+    return rows < 128 || z.gate.parts > 1 || (grad && z.dx.parts > 1);
+  };
+  look(n);
+  for (int64_t rows = 64; rows < n && look(rows); rows += 64) {}
+  if (!grad) return most;
+  const GatedSizes z = gated_sizes(n, K, F);
+  return z.d + std::max(most, z.dw.most > 1 ? size_t(z.dw.most) * size_t(up(K, 4)) * 2 * size_t(z.Fp) * 4 : 0);
+}
 
 static hgnn_status join_grid(const char* who, int64_t fours, unsigned* blocks, int per = kJoinFours) {
   HGNN_REQUIRE(ceil_div(fours, per) <= 0xffffff, HGNN_EUNSUPPORTED, "%s: grid too large", who);
@@ -586,7 +604,7 @@ extern "C" {
 
 size_t hgnn_gated_workspace(int64_t n, int32_t K, int32_t F) {
   if (n <= 0 || n > 0x7fffffff || K <= 0 || F <= 0 || K > 65536 || F > 65536) return 0;
-  return gated_sizes(n, K, F).gate_part;
+  return gated_most(n, K, F, false);
 }
 
 hgnn_status hgnn_gated(int64_t n, int32_t K, int32_t F, hgnn_activation act, const hgnn_half* X, int64_t ldx, const hgnn_half* Wg, const hgnn_half* Wu, int64_t ldw,
@@ -608,8 +626,7 @@ hgnn_status hgnn_gated(int64_t n, int32_t K, int32_t F, hgnn_activation act, con
 
 size_t hgnn_gated_grad_workspace(int64_t n, int32_t K, int32_t F) {
   if (n <= 0 || n > 0x7fffffff || K <= 0 || F <= 0 || K > 65536 || F > 65536) return 0;
-  const GatedSizes z = gated_sizes(n, K, F);
-  return z.d + std::max({z.gate_part, z.dx_part, z.dw_part});
+  return gated_most(n, K, F, true);
 }
 
 hgnn_status hgnn_gated_grad(int64_t n, int32_t K, int32_t F, hgnn_activation act, const hgnn_half* X, int64_t ldx, const hgnn_half* Wg, const hgnn_half* Wu, int64_t ldw,
@@ -644,7 +661,7 @@ hgnn_status hgnn_gated_grad(int64_t n, int32_t K, int32_t F, hgnn_activation act
   HGNN_REQUIRE(fits(X, ldx) && fits(Wg, ldw) && fits(Wu, ldw) && fits(dY, lddy), HGNN_EUNSUPPORTED,
                "%s: needs 16-byte aligned tensors and pitches that are multiples of 8, up to 2^22", who);
   const GatedSizes z = gated_sizes(n, K, F);
-  const size_t need = hgnn_gated_grad_workspace(n, K, F);
+  const size_t need = z.d + std::max({z.gate_part, z.dx_part, z.dw_part});
   HGNN_REQUIRE(workspace && workspace_bytes >= need && aligned16(workspace), HGNN_EINVAL, "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_gated_grad_workspace)", who,
                workspace_bytes, need);
   if (!dX && !dWg) return HGNN_OK;

@@ -441,6 +441,17 @@ static int64_t grad_blocks(int64_t n, hgnn_type type) {
   return std::max<int64_t>(1, std::min(resident<S>(type == HGNN_F16 ? 3 : 2), ceil_div(n, per)));
 }
 
+// the partial sums of a call, by the type with more workgroups
+static size_t grad_bytes(int64_t n, int32_t F) {
+  if (n == 0) return 0;
+  int64_t blocks = 0;
+  with_shape(F, [&](auto shape) -> hgnn_status {
+    blocks = grad_blocks<decltype(shape)>(n, HGNN_F16);
+    return HGNN_OK;
+  });
+  return size_t(blocks) * kVectors * size_t((F + 7) / 8 * 8) * sizeof(float);
+}
+
 static hgnn_status check_block(const char* who, int64_t n, int32_t F, const hgnn_block* b, hgnn_type type, bool branch) {
   HGNN_REQUIRE(n >= 0 && F > 0, HGNN_EINVAL, "%s: n = %lld, F = %d", who, static_cast<long long>(n), F);
   HGNN_REQUIRE(b != nullptr, HGNN_EINVAL, "%s: block is NULL", who);
@@ -505,12 +516,9 @@ hgnn_status hgnn_residual_norm(int64_t n, int32_t F, const hgnn_block* block, hg
 
 size_t hgnn_residual_norm_grad_workspace(int64_t n, int32_t F) {
   if (n <= 0 || F <= 0 || F > kMostNormed) return 0;
-  int64_t blocks = 0;
-  with_shape(F, [&](auto shape) -> hgnn_status {
-    blocks = grad_blocks<decltype(shape)>(n, HGNN_F16);  // the more of the two
-    return HGNN_OK;
-  });
-  return size_t(blocks) * kVectors * size_t((F + 7) / 8 * 8) * sizeof(float);
+  size_t most = grad_bytes(n, F);
+  for (int64_t rows = kUnits; rows < n && rows <= 8 * kUnits; rows += kUnits) most = std::max(most, grad_bytes(rows, F));  // fewer rows may be dealt out to more workgroups
+  return most;
 }
 
 hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* block, hgnn_type type, const void* H, int64_t ldh, const hgnn_half* Y, int64_t ldy,
@@ -544,7 +552,7 @@ hgnn_status hgnn_residual_norm_grad(int64_t n, int32_t F, const hgnn_block* bloc
   block_args(a, n, F, block);
   float* const out[kVectors] = {g.dpre_w, g.dpre_b, g.dgate, g.dpost_w, g.dpost_b};
   for (int k = 0; k < kVectors; ++k) a.vectors |= out[k] ? 1 << k : 0, a.out[k] = out[k];
-  const size_t need = hgnn_residual_norm_grad_workspace(n, F);
+  const size_t need = grad_bytes(n, F);
   HGNN_REQUIRE(a.vectors == 0 || need == 0 || (workspace && workspace_bytes >= need && aligned16(workspace)), HGNN_EINVAL,
                "%s: workspace of %zu bytes, needs %zu aligned to 16 (hgnn_residual_norm_grad_workspace)", who, workspace_bytes, need);
   if (n == 0 && a.vectors == 0) return HGNN_OK;

@@ -50,7 +50,44 @@ def norms_before_results(h):
         assert orthogonalize(h, [(64, 608), (64, 64)], 2, in_place) == ["narrow_begin_kernel"] + ["narrow_step_kernel"] * 2
 
 
-SCENARIOS = [norms_before_results]
+def sizes(h):
+    """The queries, with 64-bit results."""
+    for f in (h.lib.hgnn_gated_workspace, h.lib.hgnn_gated_grad_workspace, h.lib.hgnn_residual_norm_grad_workspace):
+        f.restype = size_t
+    return (lambda n, K, F: h.lib.hgnn_gated_workspace(i64(n), K, F), lambda n, K, F: h.lib.hgnn_gated_grad_workspace(i64(n), K, F),
+            lambda n, F: h.lib.hgnn_residual_norm_grad_workspace(i64(n), F))
+
+
+NUMBERS = sorted({*range(1, 2400, 7), *(64 * k + d for k in range(1, 40) for d in (-1, 0, 1)), *(1 << k for k in range(8, 21)), 3000, 4099, 70001, 99991, 233000})
+
+
+def workspaces_for_fewer_rows(h):
+    """What holds a call of n rows holds any of fewer: a program keeps one workspace for batches of all sizes."""
+    gated, grad, norm = sizes(h)
+    x = vp(h.data)
+    for F in (8, 100, 333, 512, 513, 1024, 2048, 4096, 8192):
+        need = [norm(n, F) for n in NUMBERS]
+        assert need == sorted(need) and need[0] > 0, F
+    for K, F in ((16, 8), (100, 200), (128, 256), (1024, 4096), (2048, 2048), (2048, 8192), (4096, 64), (4096, 20), (20, 4096), (8192, 333), (65536, 65536)):
+        for f in (gated, grad):
+            need = [f(n, K, F) for n in NUMBERS]
+            assert need == sorted(need), (K, F, f is grad)
+        up = lambda n: (n + 7) // 8 * 8  # noqa: E731
+        most = NUMBERS[-1]
+        for n in NUMBERS[::9]:
+            st, _ = launches(h, lambda: h.lib.hgnn_gated(i64(n), K, F, 0, x, i64(up(K)), x, x, i64(up(F)), 0, x, i64(up(F)), x, size_t(gated(most, K, F)), vp(A)))
+            assert st == 0, (n, K, F)
+            st, _ = launches(h, lambda: h.lib.hgnn_gated_grad(i64(n), K, F, 0, x, i64(up(K)), x, x, i64(up(F)), 0, x, i64(up(F)), x, i64(up(K)), x, vp(h.data + 64), i64(up(F)), x,
+                                                              size_t(grad(most, K, F)), vp(A)))
+            assert st == 0, (n, K, F)
+    # and the queries do not ask for much more than a call needs: sums of at most 256 tiles of 128 x 128, twice for pairs, and for the gradients D
+    for K, F in ((2048, 2048), (4096, 64), (1024, 4096), (65536, 65536)):
+        for n in (1, 100, 1000, 10000):
+            tiles = 256 * 2 * 2 * 128 * 128 * 4
+            assert gated(n, K, F) <= tiles and grad(n, K, F) <= tiles + n * 2 * (F + 31) * 2 + 256, (n, K, F)
+
+
+SCENARIOS = [norms_before_results, workspaces_for_fewer_rows]
 
 
 @pytest.mark.parametrize("name", [s.__name__ for s in SCENARIOS])
