@@ -674,8 +674,8 @@ typedef enum { HGNN_SILU = 0, HGNN_GELU = 1, HGNN_SIGMOID = 2, HGNN_RELU = 3 } h
 
 /* Y[i, f] = fp16( act(G[i, f]) * U[i, f] ),  G = X Wg,  U = X Wu:  both projections of a gated block, the activation and
  * their product in one kernel; G and U stay in fp32 registers.  X is [n][ldx] with K columns, Y [n][ldy] with F; Wg and Wu
- * are [K][ldw >= F] (trans_w = 0) or [F][ldw >= K] (trans_w != 0), all fp16.  K and F are any numbers up to 65536
- * (HGNN_EUNSUPPORTED beyond).  All tensors need 16-byte aligned addresses and pitches that are multiples of 8, up
+ * are [K][ldw >= F] (trans_w = 0) or [F][ldw >= K] (trans_w != 0), all fp16.  K and F are any numbers up to 65536, n is
+ * below 2^31 (HGNN_EUNSUPPORTED beyond).  All tensors need 16-byte aligned addresses and pitches that are multiples of 8, up
  * to 2^22 (HGNN_EUNSUPPORTED otherwise); rows are read in 16-byte pieces up to the pitch, whatever the padding columns hold never
  * reaches a result, and padding columns of outputs are not written.  Y may overlap no input.  workspace is device memory of
  * at least hgnn_gated_workspace(n, K, F) bytes (16-byte aligned; 0: none is needed; enough for any fewer rows of that K and F,

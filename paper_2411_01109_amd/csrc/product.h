@@ -356,13 +356,14 @@ __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs a, 
 
 struct ProductNothing {};
 
-// tiles and workgroups of a product, and its launch
+// tiles of a product: all there are, and in a.tiles those of a launch
 template <class S>
-inline void product_tiles(ProductArgs& a) {
+inline int64_t product_tiles(ProductArgs& a) {
   const int64_t lines = ceil_div(a.nq, S::BQ), tiles_p = ceil_div(a.np, S::BP);
   const int64_t tiles = a.lower ? lines * (lines + 1) / 2 : lines * tiles_p;
   a.lines = int32_t(lines), a.tiles_p = int32_t(tiles_p);
   a.tiles = a.some ? a.some : int32_t(std::min<int64_t>(tiles, 0x7fffffff));
+  return a.some ? a.some : tiles;
 }
 // beyond 64 KB of dynamic LDS the runtime wants to be told, once for a kernel and a device (told: a bit a device; two threads write the same at worst)
 inline hgnn_status product_lds(const void* kernel, int bytes, uint64_t* told) {
@@ -376,13 +377,18 @@ inline hgnn_status product_lds(const void* kernel, int bytes, uint64_t* told) {
 }
 template <class S, class Epilogue>
 inline hgnn_status product(const char* who, ProductArgs& a, const Epilogue& e, hipStream_t s) {
-  product_tiles<S>(a);
-  HGNN_REQUIRE(int64_t(a.tiles) * a.parts <= 0x7ffffe, HGNN_EUNSUPPORTED, "%s: grid too large", who);
+  constexpr int64_t kMost = 0x7ffffe;  // workgroups of a launch: a grid's lanes fit 32 bits
+  const int64_t tiles = product_tiles<S>(a);
+  HGNN_REQUIRE(tiles <= 0x7fffffff && (a.parts == 1 || tiles * a.parts <= kMost), HGNN_EUNSUPPORTED, "%s: grid too large", who);
   static uint64_t told = 0;
   const hgnn_status st = product_lds(reinterpret_cast<const void*>(&product_kernel<S, Epilogue>), S::kLds, &told);
   if (st != HGNN_OK) return st;
-  product_kernel<S, Epilogue><<<dim3(unsigned(a.tiles) * unsigned(a.parts)), S::kThreads, S::kLds, s>>>(a, e);
-  HGNN_LAUNCH_CHECK("product_kernel");
+  ProductArgs b = a;
+  for (int64_t done = 0; done < tiles; done += b.tiles) {
+    b.first = a.first + int32_t(done), b.tiles = int32_t(a.parts == 1 ? std::min(tiles - done, kMost) : tiles);
+    product_kernel<S, Epilogue><<<dim3(unsigned(b.tiles) * unsigned(b.parts)), S::kThreads, S::kLds, s>>>(b, e);
+    HGNN_LAUNCH_CHECK("product_kernel");
+  }
   return HGNN_OK;
 }
 

@@ -87,7 +87,22 @@ def workspaces_for_fewer_rows(h):
             assert gated(n, K, F) <= tiles and grad(n, K, F) <= tiles + n * 2 * (F + 31) * 2 + 256, (n, K, F)
 
 
-SCENARIOS = [norms_before_results, workspaces_for_fewer_rows]
+def more_tiles_than_a_grid(h):
+    """A result of more tiles than a grid has room for takes several launches; the grid's lanes fit 32 bits in each."""
+    x, far = vp(h.data), vp(h.data + 64)
+    room = size_t(1 << 50)
+    for n, K, F, most in ((500000000, 300, 8, 1), (600000000, 300, 8, 2), (1100000, 300, 65536, 2), (1000000, 300, 65536, 1), (2000000000, 300, 32, 4)):
+        st, found = launches(h, lambda: h.lib.hgnn_gated(i64(n), K, F, 0, x, i64(304), x, x, i64(65536), 0, x, i64(65536), None, size_t(0), vp(A)))
+        names = names_of(found)
+        assert st == 0 and len(names) == most and set(names) == {"product_kernel"}, (n, K, F, st, names)
+        assert 0 < h.fake.fake_last_grid() * h.fake.fake_last_block() < 1 << 32
+    for n, K, F, most in ((500000000, 8, 8, 1), (600000000, 8, 8, 2), (1100000000, 64, 16, 3)):
+        st, found = launches(h, lambda: h.lib.hgnn_gated_grad(i64(n), K, F, 0, x, i64(64), x, x, i64(64), 0, x, i64(64), x, i64(64), None, None, i64(0), far, room, vp(A)))
+        names = names_of(found)
+        assert st == 0 and names == ["gated_rows_kernel"] + ["product_kernel"] * most, (n, K, F, st, names)
+
+
+SCENARIOS = [norms_before_results, workspaces_for_fewer_rows, more_tiles_than_a_grid]
 
 
 @pytest.mark.parametrize("name", [s.__name__ for s in SCENARIOS])
