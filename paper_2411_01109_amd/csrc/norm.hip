@@ -31,7 +31,6 @@ struct BlockArgs {
   int64_t ldh;
   half_t* Z;
   int64_t ldz;
-  int past;  // 1: H (dR), 2: Z (dY)
 };
 enum { kPreW = 0, kPreB, kGate, kPostW, kPostB, kVectors };
 struct BlockGradArgs : BlockArgs {
@@ -45,6 +44,7 @@ struct BlockGradArgs : BlockArgs {
   int64_t lddy;
   half_t* dgate_rows;
   int64_t ldd_gate;
+  int past;     // 1: dR, 2: dY go past the caches
   int vectors;  // kPreW | ...: which sums over rows are wanted
   float* part;  // [gridDim.x][kVectors][pitch]
   int pitch;
@@ -242,12 +242,12 @@ __global__ __launch_bounds__(W > 1 ? W * kWave : kBlock) void block_norm_kernel(
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) h.v[i] = float(T(fmaf(gate.v[i], b.v[i], a.alpha * h.v[i])));  // as it is stored
-    if (a.H) store_eight(H.at, mine, h, a.past & 1);
+    if (a.H) store_eight(H.at, mine, h);
     if (a.pre != HGNN_NORM_NONE) {
       normed<S>(h, a.pre, a.F, a.eps, lds);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h.v[i] = fmaf(h.v[i], pre_w.v[i], pre_b.v[i]);
-      store_eight(Z.at, mine, h, a.past & 2);
+      store_eight(Z.at, mine, h);
     }
     Y.move(), R.move(), G.move(), H.move(), Z.move();
   }
