@@ -2,7 +2,9 @@
 //   dG = dY U act'(G),  dU = dY act(G),  dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU
 // on the product kernel of product.h.  The forward forms both sums of an element in the same lane, so the activation and the product cost no pass of their own.
 // The gradients form G and U once more (two of their six products) and leave dG and dU beside each other in the workspace, [n][2 Fp] in fp16: a rounding of
-// 2^-11 of each value, as every vertex-level gradient of this library takes it; then dX is one product over both halves and (dWg, dWu) is one, too.
+// 2^-11 of each value (2^-25 below fp16's normal numbers; beyond 65 504 infinite, and then no output is finite that it is a part of), as every vertex-level gradient of this
+// library takes it; then dX is one product over both halves and (dWg, dWu) is one, too.  What is stored is off by 2.9e-4 of its norm, where dG and dU in more bits
+// would leave the 2.1e-4 of its own rounding: two parts of each would be four products of the six twice.
 // Where C has too few tiles for the chip the contraction is cut; the parts' fp32 sums go through the workspace and are added in their order.
 #include <algorithm>
 #include <cmath>
@@ -206,7 +208,7 @@ static Split split_of(int64_t nq, int64_t np, int64_t K, bool two, int segments)
 }
 
 // ---- many rows through a narrow weight (K up to 256): bound by the rows of X and Y, which the product kernel's workgroups, a tile and two steps each, do not stream
-// (233 000 x 128 -> 256 96 us, here 45, of it 35 by the bytes at a copy's rate).  Eight waves keep their features of both weights in registers for all rows of the
+// (233 000 x 128 -> 256 96 us, here 45 with X and Y in the last-level cache and 60 from memory, 35 by the bytes at a copy's rate).  Eight waves keep their features of both weights in registers for all rows of the
 // workgroup, 32 features for K <= 128, 16 beyond; a ninth brings X into a ring in LDS, 64 rows at a time, and is the only one that waits for loads to LDS, so that
 // the other waves' stores are never waited for.  A barrier a tile hands it over and takes back the one before.  (Two
 // workgroups of four waves and one do not fit a compute unit's registers: 65 -> 100 us.)  Features are dealt out such that a lane's 2 x 4 sums are eight consecutive ones.

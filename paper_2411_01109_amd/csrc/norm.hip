@@ -5,8 +5,8 @@
 // A row stays in registers from its load to its stores, so every tensor crosses the memory once, which is what bounds both kernels; sums over a row and all
 // that is formed from them are fp32, the variance is formed from the differences to the mean.  The gradients recompute the statistics from the rows that they
 // read in any case: two more reductions over lanes, no array of statistics that a caller could hand over stale.
-// 2.4 M x 128 in fp16 with both norms and a gate, one MI355X: forward 2.46 GB in 472 us (5.2 TB/s, a large copy's rate), gradients 3.69 GB in 758 (4.9);
-// 99 991 x 333 of an fp32 stream with a gate of every element 742 MB in 184 (4.0).
+// 2.4 M x 128 in fp16 with both norms and a gate, one MI355X, calls in a row: forward 2.46 GB in 468 us (5.2 TB/s, a large copy's rate), gradients 3.69 GB in 737 (5.0);
+// of an fp32 stream 718 (3.69 GB, 5.1) and 1219 (5.53 GB, 4.5); 99 991 x 333 of an fp32 stream with a gate of every element, gradients, 742 MB in 183 (4.1).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

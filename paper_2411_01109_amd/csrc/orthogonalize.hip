@@ -303,7 +303,9 @@ struct OrthSplit {
   int64_t rest_part, from;      // lines from `from` on
 };
 // 128 x 128 tiles that run at a time, two a compute unit.  A few more than a multiple of that would take as long as half of all: they are a launch of their own, their
-// contraction cut for as many workgroups (4096 x 4096, five steps, ten such products of 528 tiles: 4.00 ms in one launch each, 3.85 so: 198 us, 15 and 6 for the join).
+// contraction cut for as many workgroups.  Five steps, ten such products, ms in one launch each and so: 4096 x 4096 (528 tiles) 3.94 and 3.67, 4224 (561) 4.47 and 4.27, 4352 (595)
+// 4.66 and 4.52, 4480 (630) 4.91 and 4.84, 5760 (1035) 10.43 and 9.95, 6016 (1128) 11.71 and 11.51, 7040 (1540) 18.96 and 18.45, 7296 (1653) 20.93 and 20.58; 4096 x 5120 4.67 and
+// 4.31, 4480 x 5504 5.81 and 5.59.
 constexpr int kOrthAtOnce = 512;
 static OrthSplit orth_split(int64_t nq, int64_t np, int64_t K, bool lower) {
   const auto tiles = [&](int64_t b) {

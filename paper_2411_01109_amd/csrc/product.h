@@ -10,13 +10,14 @@
 // Values that are two fp16 numbers each lie as 32 high parts and 32 low parts in turn, so that the same 128 bytes are 32 steps (items) of both.
 // (With 64 bytes of 16 rows an instruction, at pitches that are multiples of 4 KB, requests met on the L2's channels: 8192 x 16384 x 2048 592 us.)
 // What is behind the contraction's end is asked for at a place that holds zeros; where the end lies inside a piece, the rest of the piece is cleared in LDS
-// (the bytes there are the caller's padding and may be NaN).  Items that do not exist are asked for at the last one that does: they meet only results that
-// are not stored.
+// (the bytes there are the caller's padding and may be NaN).  Items that do not exist are asked for at one that does, in rows at the last, in columns at the tile's first
+// eight: they meet only results that are not stored.
 //
 // v_mfma_f32_16x16x32_f16 with P as its first operand: a lane has four consecutive p of one q.  A wave's block of sums decides how often an operand is read
 // from LDS, and that is what bounds the large shape (256 x 256: 8 waves of 128 x 64, (128 + 64) 64 bytes a step for 32 products of 16 cycles).
-// Of 8192 rows, 2048 and 2 x 8192 features, 550 Gflop each, us at their fastest and in the middle: pairs 579 / 651 (950 / 845 Tflop/s), the sum of two segments 443 / 535
-// (1240 / 1030), X^T D 464 / 559 (1185 / 985); two parts, 4096 x 4096 x 4096 at three products each, 332 / 350 (1240 / 1180).  A library's product reaches 1170 to 1510
+// Of 8192 rows, 2048 and 2 x 8192 features, 550 Gflop each, us at their fastest and in the middle: pairs with dY read and D written 554 / 599 (990 / 920 Tflop/s; the
+// forward, which writes a fourth of that, 462), the sum of two segments 441 / 483 (1250 / 1140), X^T D 474 / 516 (1160 / 1070); two parts, 4096 x 4096 x 4096 at three
+// products each, 343 / 358 (1200 / 1150).  A library's product reaches 1170 to 1510
 // at such sizes.  The matrix units are busy for 46 to 61 % of the cycles, and the clock falls to 1.83 GHz under them.
 #pragma once
 
